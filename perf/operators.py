@@ -202,8 +202,8 @@ def _own_product(s):
     from paper_2607_07388_amd import tfe
     x, out = s["x"], s["out"]
     rows, dim = x.shape
-    space = _space(s, tfe.tfe_fp8_workspace(rows, dim))
-    tfe.tfe_fp8_linear(x, _number(x.dtype), dim, s["w"], s["scales"], rows, out.shape[1], dim, out, _number(out.dtype),
+    space = _space(s, tfe.tfe_quantized_workspace(rows, dim))
+    tfe.tfe_quantized_linear(x, _number(x.dtype), dim, s["w"], s["scales"], rows, out.shape[1], dim, out, _number(out.dtype),
                        out.shape[1], *space, s["stream"])
     return out
 
