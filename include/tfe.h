@@ -37,11 +37,12 @@
  *   - A table handle is not thread-safe: calls on one handle must be issued
  *     from one host thread at a time.
  *   - HIP graph capture: lookups on resident tables (tfe_lookup_inject,
- *     tfe_lookup_inject_multi) and tfe_head_topk enqueue kernels only and may
- *     be captured.  Lookups on tiered tables, tfe_prefetch,
- *     tfe_prefetch_scored and tfe_ngram_top keep per-call host state or
- *     synchronise; on a capturing stream they return TFE_ERR_UNSUPPORTED
- *     without enqueuing anything.
+ *     tfe_lookup_inject_multi), tfe_head_topk and the calls on logits
+ *     (tfe_quantize, tfe_quantized_..., tfe_sample, tfe_distill_...) enqueue
+ *     kernels only and may be captured.  Lookups on tiered tables,
+ *     tfe_prefetch, tfe_prefetch_scored and tfe_ngram_top keep per-call host
+ *     state or synchronise; on a capturing stream they return
+ *     TFE_ERR_UNSUPPORTED without enqueuing anything.
  */
 #ifndef TFE_H_
 #define TFE_H_
@@ -338,6 +339,120 @@ tfe_status tfe_head_free(tfe_head *head);
 tfe_status tfe_head_topk_noalloc(const void *w_pref, int32_t vocab, int32_t dim,
                                  const void *hidden, int32_t B, int32_t K, int32_t *top_ids,
                                  float *top_prob, void *stream);
+
+/* ---- The head's logits: 8-bit product, sampling, distillation --------------
+ * What a program does around the early-exit head (Eq. 13): its projection in
+ * 8 bits, a token drawn from its logits, and its learning from a teacher's
+ * top logits (the approximation of the next-token distribution that the head
+ * is for).  These calls keep no state and allocate nothing: scratch is the
+ * caller's `workspace` (DEVICE, 16-byte aligned, at least as many bytes as the
+ * call's ..._workspace function says; nothing need be in it, and nothing in it
+ * outlives the call).  They enqueue kernels only, may be captured in HIP
+ * graphs, and may be made from any host thread; calls that share a workspace
+ * must be ordered by the caller.  Matrices are row-major with a row pitch in
+ * elements (ldx, ldo, ld, ldg >= the row's length); pointers need the
+ * alignment of their element unless said otherwise.  Zero rows: nothing is
+ * enqueued. */
+
+/* 8-bit layout.  A matrix [rows x dim] becomes
+ *   codes   DEVICE uint8 [rows x P], P = dim rounded up to 128: OCP e4m3
+ *           values, zero from column dim on; 16-byte aligned;
+ *   scales  DEVICE uint8 [ceil(rows / block_rows) x Q], Q = ceil(P / 128)
+ *           rounded up to 4: one byte per block of block_rows rows x 128
+ *           columns, the exponent e of its scale 2^e plus 127 (127 behind the
+ *           last block); 4-byte aligned;
+ * value = code * 2^e.  The scale is a power of two so that scaling rounds
+ * nothing and the matrix instruction can apply it. */
+
+/* Lays `x` (DEVICE, dtype TFE_F32 or TFE_BF16, [rows x dim], pitch ldx) out.
+ * e is the least exponent (>= -127) with |x| <= 448 * 2^e for all finite x of
+ * the block; codes are nearest, ties to even.  Infinities become +-448, NaN
+ * stays NaN; neither takes part in the scale.  block_rows is 1 (hidden states)
+ * or 128 (weights); dim <= 65536, rows <= 2^20. */
+tfe_status tfe_quantize(const void *x, int32_t dtype, int64_t ldx, int64_t rows, int32_t dim,
+                        int32_t block_rows, uint8_t *codes, uint8_t *scales, void *stream);
+
+/* out[r, n] = sum over k of A[r, k] W[n, k], for A laid out with block_rows 1
+ * and W with block_rows 128 (scales w_scales); out DEVICE [rows x out_dim] of
+ * out_dtype.  Products are exact; float32 results are accumulated in float32,
+ * bfloat16 results may be accumulated by the 8-bit matrix instruction, whose
+ * sums carry about 17 bits (far below the rounding of the result).
+ * rows <= 2^20, 1 <= out_dim <= 2^20, dim <= 65536. */
+tfe_status tfe_quantized_matmul(const uint8_t *a, const uint8_t *a_scales, const uint8_t *w,
+                                const uint8_t *w_scales, int64_t rows, int32_t out_dim,
+                                int32_t dim, void *out, int32_t out_dtype, int64_t ldo,
+                                void *stream);
+
+/* tfe_quantize (block_rows 1) of x and tfe_quantized_matmul in one call: the
+ * logits of hidden states x [rows x dim] under a projection laid out once. */
+tfe_status tfe_quantized_linear(const void *x, int32_t dtype, int64_t ldx, const uint8_t *w,
+                                const uint8_t *w_scales, int64_t rows, int32_t out_dim,
+                                int32_t dim, void *out, int32_t out_dtype, int64_t ldo,
+                                void *workspace, int64_t workspace_bytes, void *stream);
+int64_t tfe_quantized_workspace(int64_t rows, int32_t dim); /* -1: bad size */
+
+/* Draws one token per row of logits (DEVICE, dtype, [rows x vocab], pitch ld).
+ * Per row, with l the logits (NaN counts as -infinity) and M their maximum:
+ *   weights  w_i = 2^31 exp((l_i - M) / T) rounded to an integer; l_i = M gives
+ *            2^31, l_i = -infinity gives 0;
+ *   order    larger weight first, equal weights by lower token id;
+ *   top-k    the first top_k are kept;
+ *   top-p    of those, the shortest prefix whose sum reaches
+ *            max(1, floor(top_p * their sum));
+ *   min-p    of those, the ones with w_i >= 2^31 min_p rounded;
+ *   token    of those (sum Z), the first whose running sum exceeds
+ *            floor(u * Z); prob = its w / Z.
+ * Sums are integers, so a token does not depend on how the work was split.
+ *   temperature, top_k, top_p, min_p  DEVICE [rows] (float, int32, float,
+ *            float), each may be NULL: 1, off, off, off.  T <= 0 or NaN: the
+ *            most likely token.  top_k <= 0, top_p >= 1 or NaN, min_p <= 0 or
+ *            NaN: off; top_p < 0 counts as 0, min_p > 1 as 1.
+ *   u        DEVICE float [rows], uniform in [0, 1) (clamped to it; NaN is 0).
+ *   token    DEVICE int32 [rows]; -1 for a row without a finite or +infinite logit.
+ *   prob     DEVICE float [rows] or NULL; 0 for such a row.
+ * 1 <= vocab <= 2^18; rows <= 2^20. */
+tfe_status tfe_sample(const void *logits, int32_t dtype, int64_t ld, int64_t rows, int32_t vocab,
+                      const float *temperature, const int32_t *top_k, const float *top_p,
+                      const float *min_p, const float *u, int32_t *token, float *prob,
+                      void *workspace, int64_t workspace_bytes, void *stream);
+int64_t tfe_sample_workspace(int64_t rows, int32_t vocab); /* -1: bad size */
+
+/* Distillation from a teacher's top logits.  Per row, with s the student's
+ * logits (DEVICE, dtype, [rows x vocab], pitch ld), t the teacher's K top
+ * logits (DEVICE, teacher_dtype, [rows x K]) of the tokens teacher_ids
+ * (DEVICE int32 [rows x K]) and tau the temperature (> 0, finite):
+ *   q = softmax(t / tau) over the row's K entries,  lse = log sum exp(s / tau),
+ *   loss = tau^2 sum_k q_k (log q_k - (s[id_k] / tau - lse)),
+ *   d loss / d s_v = tau (exp(s_v / tau - lse) - sum of q_k with id_k = v).
+ * Entries whose id lies outside [0, vocab) are padding: their logits may hold
+ * anything.  A row without an entry of finite logit has loss 0 and gradient 0.
+ * A student logit of -infinity has probability 0 (the loss is +infinity where
+ * the teacher gives that token weight).  1 <= K <= 256, 1 <= vocab <= 2^18,
+ * rows <= 2^20.  Softmax sums are float32.
+ *   loss, lse   DEVICE float [rows] (lse of the student's row, also where the
+ *               loss is 0).
+ *   grad_loss   DEVICE float [rows] or NULL (1): the gradient with respect to
+ *               loss; the row's gradient is multiplied by it.  Where it is 0 the
+ *               gradient is 0 whatever the logits hold.
+ *   grad        DEVICE of the student's dtype, [rows x vocab], pitch ldg; may be
+ *               `logits` itself when ldg = ld.
+ * tfe_distill_grad takes lse as tfe_distill_loss wrote it. */
+tfe_status tfe_distill_loss(const void *logits, int32_t dtype, int64_t ld, int64_t rows,
+                            int32_t vocab, const int32_t *teacher_ids, const void *teacher_logits,
+                            int32_t teacher_dtype, int32_t K, float temperature, float *loss,
+                            float *lse, void *workspace, int64_t workspace_bytes, void *stream);
+tfe_status tfe_distill_grad(const void *logits, int32_t dtype, int64_t ld, int64_t rows,
+                            int32_t vocab, const int32_t *teacher_ids, const void *teacher_logits,
+                            int32_t teacher_dtype, int32_t K, float temperature, const float *lse,
+                            const float *grad_loss, void *grad, int64_t ldg, void *stream);
+/* Both in one call. */
+tfe_status tfe_distill_loss_grad(const void *logits, int32_t dtype, int64_t ld, int64_t rows,
+                                 int32_t vocab, const int32_t *teacher_ids,
+                                 const void *teacher_logits, int32_t teacher_dtype, int32_t K,
+                                 float temperature, const float *grad_loss, float *loss,
+                                 float *lse, void *grad, int64_t ldg, void *workspace,
+                                 int64_t workspace_bytes, void *stream);
+int64_t tfe_distill_workspace(int64_t rows, int32_t vocab); /* -1: bad size */
 
 /* ---- Offline phrase-table construction -----------------------------------
  * Paper: Sec. 4.2 (candidate phrases mined from a corpus and selected by

@@ -6,7 +6,8 @@ arithmetic lives in ``oracle.cpp`` (std::map on token tuples, scalar double
 loops); this file only marshals numpy arrays.  ``head.cpp`` is the
 early-exit prefetch head, ``ngram.cpp`` the frequency-ranked phrase-table
 construction; ``lru.py`` is the reference model of the HBM cache
-tier's replacement policy.
+tier's replacement policy; ``logits.py`` is the 8-bit product, sampling and
+distillation of the head's logits in numpy.
 """
 import ctypes
 import os

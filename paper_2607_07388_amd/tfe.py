@@ -108,6 +108,21 @@ def _load():
         "tfe_head_free": ([vp], ctypes.c_int),
         "tfe_head_last_fault": ([vp, ctypes.POINTER(i64)], ctypes.c_int),
         "tfe_head_topk_noalloc": ([vp, i32, i32, vp, i32, i32, vp, vp, vp], ctypes.c_int),
+        "tfe_quantize": ([vp, i32, i64, i64, i32, i32, vp, vp, vp], ctypes.c_int),
+        "tfe_quantized_matmul": ([vp, vp, vp, vp, i64, i32, i32, vp, i32, i64, vp], ctypes.c_int),
+        "tfe_quantized_linear": ([vp, i32, i64, vp, vp, i64, i32, i32, vp, i32, i64, vp, i64, vp],
+                           ctypes.c_int),
+        "tfe_quantized_workspace": ([i64, i32], i64),
+        "tfe_sample": ([vp, i32, i64, i64, i32, vp, vp, vp, vp, vp, vp, vp, vp, i64, vp],
+                       ctypes.c_int),
+        "tfe_sample_workspace": ([i64, i32], i64),
+        "tfe_distill_loss": ([vp, i32, i64, i64, i32, vp, vp, i32, i32, ctypes.c_float, vp, vp,
+                              vp, i64, vp], ctypes.c_int),
+        "tfe_distill_grad": ([vp, i32, i64, i64, i32, vp, vp, i32, i32, ctypes.c_float, vp, vp,
+                              vp, i64, vp], ctypes.c_int),
+        "tfe_distill_loss_grad": ([vp, i32, i64, i64, i32, vp, vp, i32, i32, ctypes.c_float, vp,
+                                   vp, vp, vp, i64, vp, i64, vp], ctypes.c_int),
+        "tfe_distill_workspace": ([i64, i32], i64),
         "tfe_ngram_release": ([], ctypes.c_int),
         "tfe_ngram_top": ([vp, i64, i32, i32, i64, i64, vp, vp, ctypes.POINTER(i64), vp],
                           ctypes.c_int),
@@ -134,6 +149,9 @@ EXPORTED = ("tfe_table_load", "tfe_table_free", "tfe_lookup_inject", "tfe_lookup
             "tfe_prefetch",
             "tfe_prefetch_scored", "tfe_head_create", "tfe_head_topk", "tfe_head_free",
             "tfe_head_last_fault", "tfe_head_topk_noalloc",
+            "tfe_quantize", "tfe_quantized_matmul", "tfe_quantized_linear", "tfe_quantized_workspace",
+            "tfe_sample", "tfe_sample_workspace", "tfe_distill_loss", "tfe_distill_grad",
+            "tfe_distill_loss_grad", "tfe_distill_workspace",
             "tfe_ngram_top", "tfe_ngram_release",
             "tfe_get_stats", "tfe_reset_stats", "tfe_residency", "tfe_last_error",
             "tfe_memory_held", "tfe_index_capacity",
@@ -239,6 +257,76 @@ def tfe_head_last_fault(head):
     n = ctypes.c_int64()
     _check(lib.tfe_head_last_fault(head, ctypes.byref(n)))
     return n.value
+
+
+def tfe_quantize(x, dtype, ldx, rows, dim, block_rows, codes, scales, stream=None):
+    return _check(lib.tfe_quantize(addr(x), dtype, ldx, rows, dim, block_rows, addr(codes),
+                                   addr(scales), stream_handle(stream)))
+
+
+def tfe_quantized_matmul(a, a_scales, w, w_scales, rows, out_dim, dim, out, out_dtype, ldo,
+                         stream=None):
+    return _check(lib.tfe_quantized_matmul(addr(a), addr(a_scales), addr(w), addr(w_scales), rows,
+                                           out_dim, dim, addr(out), out_dtype, ldo,
+                                           stream_handle(stream)))
+
+
+def tfe_quantized_linear(x, dtype, ldx, w, w_scales, rows, out_dim, dim, out, out_dtype, ldo,
+                         workspace, workspace_bytes, stream=None):
+    return _check(lib.tfe_quantized_linear(addr(x), dtype, ldx, addr(w), addr(w_scales), rows,
+                                           out_dim, dim, addr(out), out_dtype, ldo,
+                                           addr(workspace), workspace_bytes,
+                                           stream_handle(stream)))
+
+
+def tfe_quantized_workspace(rows, dim):
+    """Bytes of workspace a tfe_quantized_linear call of this size needs."""
+    return _check(lib.tfe_quantized_workspace(rows, dim))
+
+
+def tfe_sample(logits, dtype, ld, rows, vocab, temperature, top_k, top_p, min_p, u, token, prob,
+               workspace, workspace_bytes, stream=None):
+    return _check(lib.tfe_sample(addr(logits), dtype, ld, rows, vocab, addr(temperature),
+                                 addr(top_k), addr(top_p), addr(min_p), addr(u), addr(token),
+                                 addr(prob), addr(workspace), workspace_bytes,
+                                 stream_handle(stream)))
+
+
+def tfe_sample_workspace(rows, vocab):
+    """Bytes of workspace a tfe_sample call of this size needs."""
+    return _check(lib.tfe_sample_workspace(rows, vocab))
+
+
+def tfe_distill_loss(logits, dtype, ld, rows, vocab, teacher_ids, teacher_logits, teacher_dtype,
+                     K, temperature, loss, lse, workspace, workspace_bytes, stream=None):
+    return _check(lib.tfe_distill_loss(addr(logits), dtype, ld, rows, vocab, addr(teacher_ids),
+                                       addr(teacher_logits), teacher_dtype, K, temperature,
+                                       addr(loss), addr(lse), addr(workspace), workspace_bytes,
+                                       stream_handle(stream)))
+
+
+def tfe_distill_grad(logits, dtype, ld, rows, vocab, teacher_ids, teacher_logits, teacher_dtype,
+                     K, temperature, lse, grad_loss, grad, ldg, stream=None):
+    return _check(lib.tfe_distill_grad(addr(logits), dtype, ld, rows, vocab, addr(teacher_ids),
+                                       addr(teacher_logits), teacher_dtype, K, temperature,
+                                       addr(lse), addr(grad_loss), addr(grad), ldg,
+                                       stream_handle(stream)))
+
+
+def tfe_distill_loss_grad(logits, dtype, ld, rows, vocab, teacher_ids, teacher_logits,
+                          teacher_dtype, K, temperature, grad_loss, loss, lse, grad, ldg,
+                          workspace, workspace_bytes, stream=None):
+    return _check(lib.tfe_distill_loss_grad(addr(logits), dtype, ld, rows, vocab,
+                                            addr(teacher_ids), addr(teacher_logits),
+                                            teacher_dtype, K, temperature, addr(grad_loss),
+                                            addr(loss), addr(lse), addr(grad), ldg,
+                                            addr(workspace), workspace_bytes,
+                                            stream_handle(stream)))
+
+
+def tfe_distill_workspace(rows, vocab):
+    """Bytes of workspace a tfe_distill_loss(_grad) call of this size needs."""
+    return _check(lib.tfe_distill_workspace(rows, vocab))
 
 
 def tfe_ngram_top(tokens, n_tokens, vocab, n, skip, top, out_tuples, out_counts, stream=None):
