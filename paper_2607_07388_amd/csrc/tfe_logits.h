@@ -37,6 +37,9 @@ struct MatmulArgs {
   uint32_t rows, n, pitch, spitch;
 };
 hipError_t launch_fp8_matmul(const MatmulArgs& a, int out_dtype, hipStream_t s);
+// Both: x's codes and scales are a.a and a.as.
+hipError_t launch_fp8_linear(const QuantizeArgs& x, const MatmulArgs& a, int dtype, int out_dtype,
+                             hipStream_t s);
 
 struct SampleArgs {
   const void* logits;

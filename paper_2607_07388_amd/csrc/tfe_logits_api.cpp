@@ -56,14 +56,8 @@ tfe_status fp8_sizes(int64_t rows, int32_t dim) {
   return TFE_OK;
 }
 
-tfe_status quantize(const void* x, int32_t dtype, int64_t ldx, int64_t rows, int32_t dim,
-                    int32_t block_rows, uint8_t* codes, uint8_t* scales, hipStream_t s) {
-  TRY(fp8_sizes(rows, dim));
-  NEED(block_rows == 1 || block_rows == kFp8Block, "block_rows is 1 or 128");
-  TRY(matrix(x, dtype, ldx, rows, dim, "x"));
-  if (rows == 0) return TFE_OK;
-  NEED(codes && aligned(codes, 16), "codes: null or not 16-byte aligned");
-  NEED(scales && aligned(scales, 4), "scales: null or not 4-byte aligned");
+QuantizeArgs quantize_args(const void* x, int64_t ldx, int64_t rows, int32_t dim, uint8_t* codes,
+                           uint8_t* scales) {
   QuantizeArgs a{};
   a.x = x;
   a.ldx = ldx;
@@ -73,18 +67,11 @@ tfe_status quantize(const void* x, int32_t dtype, int64_t ldx, int64_t rows, int
   a.spitch = fp8_scale_pitch(dim);
   a.codes = codes;
   a.scales = scales;
-  return launched(launch_fp8_quantize(a, dtype, block_rows, s), "quantize launch");
+  return a;
 }
 
-tfe_status matmul(const uint8_t* x, const uint8_t* xs, const uint8_t* w, const uint8_t* ws,
-                  int64_t rows, int32_t n, int32_t dim, void* out, int32_t out_dtype, int64_t ldo,
-                  hipStream_t s) {
-  TRY(fp8_sizes(rows, dim));
-  NEED(n >= 1 && n <= kFp8MaxOut, "out_dim outside [1, 2^20]");
-  TRY(matrix(out, out_dtype, ldo, rows, n, "out"));
-  if (rows == 0) return TFE_OK;
-  NEED(x && aligned(x, 16) && w && aligned(w, 16), "codes: null or not 16-byte aligned");
-  NEED(xs && aligned(xs, 4) && ws && aligned(ws, 4), "scales: null or not 4-byte aligned");
+MatmulArgs matmul_args(const uint8_t* x, const uint8_t* xs, const uint8_t* w, const uint8_t* ws,
+                       int64_t rows, int32_t n, int32_t dim, void* out, int64_t ldo) {
   MatmulArgs a{};
   a.a = x;
   a.as = xs;
@@ -96,7 +83,33 @@ tfe_status matmul(const uint8_t* x, const uint8_t* xs, const uint8_t* w, const u
   a.n = (uint32_t)n;
   a.pitch = fp8_pitch(dim);
   a.spitch = fp8_scale_pitch(dim);
-  return launched(launch_fp8_matmul(a, out_dtype, s), "8-bit product launch");
+  return a;
+}
+
+tfe_status quantize(const void* x, int32_t dtype, int64_t ldx, int64_t rows, int32_t dim,
+                    int32_t block_rows, uint8_t* codes, uint8_t* scales, hipStream_t s) {
+  TRY(fp8_sizes(rows, dim));
+  NEED(block_rows == 1 || block_rows == kFp8Block, "block_rows is 1 or 128");
+  TRY(matrix(x, dtype, ldx, rows, dim, "x"));
+  if (rows == 0) return TFE_OK;
+  NEED(codes && aligned(codes, 16), "codes: null or not 16-byte aligned");
+  NEED(scales && aligned(scales, 4), "scales: null or not 4-byte aligned");
+  return launched(launch_fp8_quantize(quantize_args(x, ldx, rows, dim, codes, scales), dtype,
+                                      block_rows, s),
+                  "quantize launch");
+}
+
+tfe_status matmul(const uint8_t* x, const uint8_t* xs, const uint8_t* w, const uint8_t* ws,
+                  int64_t rows, int32_t n, int32_t dim, void* out, int32_t out_dtype, int64_t ldo,
+                  hipStream_t s) {
+  TRY(fp8_sizes(rows, dim));
+  NEED(n >= 1 && n <= kFp8MaxOut, "out_dim outside [1, 2^20]");
+  TRY(matrix(out, out_dtype, ldo, rows, n, "out"));
+  if (rows == 0) return TFE_OK;
+  NEED(x && aligned(x, 16) && w && aligned(w, 16), "codes: null or not 16-byte aligned");
+  NEED(xs && aligned(xs, 4) && ws && aligned(ws, 4), "scales: null or not 4-byte aligned");
+  return launched(launch_fp8_matmul(matmul_args(x, xs, w, ws, rows, n, dim, out, ldo), out_dtype, s),
+                  "8-bit product launch");
 }
 
 // Codes of the rows, then their scales.
@@ -118,8 +131,10 @@ tfe_status linear(const void* x, int32_t dtype, int64_t ldx, const uint8_t* w, c
   TRY(space(workspace, bytes, linear_space(rows, dim)));
   uint8_t* codes = (uint8_t*)workspace;
   uint8_t* scales = codes + linear_codes(rows, dim);
-  TRY(quantize(x, dtype, ldx, rows, dim, 1, codes, scales, s));
-  return matmul(codes, scales, w, ws, rows, n, dim, out, out_dtype, ldo, s);
+  return launched(launch_fp8_linear(quantize_args(x, ldx, rows, dim, codes, scales),
+                                    matmul_args(codes, scales, w, ws, rows, n, dim, out, ldo), dtype,
+                                    out_dtype, s),
+                  "8-bit product launch");
 }
 
 tfe_status vocab_ok(int32_t vocab) {

@@ -4,6 +4,8 @@
 #include <stdint.h>
 
 #include <algorithm>
+#include <atomic>
+#include <type_traits>
 
 #include "tfe_logits.h"
 #include "tfe_rows.h"
@@ -64,6 +66,21 @@ __device__ __forceinline__ void store8(const QuantizeArgs& a, int64_t row, uint3
   *(u32x2*)(a.codes + (size_t)row * a.pitch + c) = u32x2{codes4(f), codes4(f + 4)};
 }
 
+// Eight columns of a block that 16 lanes hold: their codes (f is scaled in
+// place) and the block's exponent.
+__device__ __forceinline__ u32x2 encode8(float* f, uint32_t* biased) {
+  float amax = 0.f;
+#pragma unroll
+  for (int j = 0; j < 8; ++j) amax = fmaxf(amax, finite_abs(f[j]));
+#pragma unroll
+  for (int o = 8; o; o >>= 1) amax = fmaxf(amax, __shfl_xor(amax, o));
+  *biased = block_exponent(amax);
+  const float inv = unscale(*biased);
+#pragma unroll
+  for (int j = 0; j < 8; ++j) f[j] *= inv;
+  return u32x2{codes4(f), codes4(f + 4)};
+}
+
 // Blocks of one row: 16 lanes hold a block of 128.  One thread per 8 columns;
 // the threads behind a row's columns write its padding of the scales.
 template <int DT> __global__ __launch_bounds__(256) void k_quantize_rows(QuantizeArgs a) {
@@ -77,13 +94,7 @@ template <int DT> __global__ __launch_bounds__(256) void k_quantize_rows(Quantiz
     uint32_t biased = 127;
     if (c < a.pitch) {
       load8<DT>(a, row, c, f);
-      float amax = 0.f;
-#pragma unroll
-      for (int j = 0; j < 8; ++j) amax = fmaxf(amax, finite_abs(f[j]));
-#pragma unroll
-      for (int o = 8; o; o >>= 1) amax = fmaxf(amax, __shfl_xor(amax, o));
-      biased = block_exponent(amax);
-      store8(a, row, c, f, biased);
+      *(u32x2*)(a.codes + (size_t)row * a.pitch + c) = encode8(f, &biased);
     }
     if ((threadIdx.x & 15) == 0)
       a.scales[(size_t)row * a.spitch + c / kFp8Block] = (uint8_t)biased;
@@ -133,41 +144,380 @@ __device__ __forceinline__ float scale_of(uint32_t biased) {
   return __uint_as_float(biased ? biased << 23 : 0x400000u);  // 2^-127 is subnormal
 }
 
-// One wave per 16 x 16 outputs.  The lane (g, i) of an operand holds columns
-// 32 g .. 32 g + 31 of row i of a block of 128; the matrix instruction takes 8
-// of them at a time, the same ones of both operands.
-template <int DT> __global__ __launch_bounds__(256) void k_product(MatmulArgs a) {
-  const uint32_t wave = threadIdx.x >> 6, lane = threadIdx.x & 63, i = lane & 15, g = lane >> 4;
-  const uint32_t n0 = (blockIdx.x * 4 + wave) * 16;
-  if (n0 >= a.n) return;
-  const uint32_t n = min(n0 + i, a.n - 1);
-  const uint8_t* wp = a.w + (size_t)n * a.pitch + g * 32;
-  for (uint32_t r0 = blockIdx.y * 16; r0 < a.rows; r0 += gridDim.y * 16) {
-    const uint32_t r = min(r0 + i, a.rows - 1);
-    const uint8_t* xp = a.a + (size_t)r * a.pitch + g * 32;
-    f32x4 acc{0.f, 0.f, 0.f, 0.f};
-    for (uint32_t b = 0; b < a.pitch / kFp8Block; ++b) {
-      const float sw = scale_of(a.ws[(size_t)(n0 / kFp8Block) * a.spitch + b]);
-      const float sx = scale_of(a.as[(size_t)r * a.spitch + b]);
-      u32x4 w[2], x[2];
-#pragma unroll
-      for (int j = 0; j < 2; ++j) {
-        w[j] = *(const u32x4*)(wp + b * kFp8Block + 16 * j);
-        x[j] = *(const u32x4*)(xp + b * kFp8Block + 16 * j);
-      }
-#pragma unroll
-      for (int j = 0; j < 4; ++j)
-        acc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(
-            widen(w[j >> 1][2 * (j & 1)], w[j >> 1][2 * (j & 1) + 1], sw),
-            widen(x[j >> 1][2 * (j & 1)], x[j >> 1][2 * (j & 1) + 1], sx), acc, 0, 0, 0);
-    }
-    if (r0 + i >= a.rows) continue;
-    char* out = (char*)a.out + (size_t)(r0 + i) * a.ldo * sizeof(typename Elem<DT>::T);
+__device__ __forceinline__ uint32_t byte_of(uint32_t w, int i) { return (w >> (8 * i)) & 255u; }
+
+// Where lane (g, i) of a 16-row operand finds its bytes of a block of 128
+// columns: two 16-byte pieces, 4 p + g for p = 0, 1, so that a load
+// instruction takes 64 consecutive bytes of each row.  Both operands of a
+// product use the same pieces, so the matrix instruction multiplies matching
+// columns, whatever their order.
+
+// Four results of a lane (columns n .. n + 3 of one row), stored together
+// where the row has them.
+template <int DT>
+__device__ __forceinline__ void store4(const MatmulArgs& a, uint32_t r, uint32_t n, f32x4 v) {
+  typedef uint32_t u2 __attribute__((ext_vector_type(2), aligned(2)));
+  typedef f32x4 f4 __attribute__((aligned(4)));
+  char* out = (char*)a.out + ((size_t)r * a.ldo + n) * sizeof(typename Elem<DT>::T);
+  if (n + 4 <= a.n) {
+    if (DT == TFE_F32)
+      *(f4*)out = v;
+    else
+      *(u2*)out = u2{pack2(v[0], v[1]), pack2(v[2], v[3])};
+  } else {
 #pragma unroll
     for (int j = 0; j < 4; ++j)
-      if (n0 + g * 4 + j < a.n) store1<DT>(out, n0 + g * 4 + j, acc[j]);
+      if (n + j < a.n) store1<DT>(out, j, v[j]);
   }
 }
+
+// Few rows (at most 16 MT): bound by W's bytes, read once.  One block a
+// compute unit (MT = 1: two); the rows lie in LDS as bfloat16, laid out there
+// by the block itself when they come as hidden states (XDT a float type; one
+// launch less), 16 bytes behind each row so that the 16 rows of an operand read
+// fall on different banks.  A wave takes TPW 16-row tiles of W at a time and
+// keeps PC blocks of 128 columns of each in flight ahead of those it
+// multiplies.  Results of either type: the exact bfloat16 instruction, which
+// has time enough here.
+constexpr int kCodes = 2;  // XDT of rows that are laid out already
+constexpr int kSkinnyWaves = 8;
+constexpr uint32_t kSkinnyLds = 135168;
+
+template <int XDT>
+__device__ void stage_rows(const MatmulArgs& a, const QuantizeArgs& x, uint32_t rows, char* xs,
+                           uint32_t xp) {
+  const uint32_t per_row = a.pitch / 8;  // threads; 16 of them a block
+  for (uint32_t t = threadIdx.x; t < rows * per_row; t += kSkinnyWaves * 64) {
+    const uint32_t r = t / per_row, c = (t - r * per_row) * 8;
+    u32x4 v{0, 0, 0, 0};
+    if (r < a.rows) {
+      u32x2 codes;
+      uint32_t biased;
+      if constexpr (XDT == kCodes) {
+        codes = *(const u32x2*)(a.a + (size_t)r * a.pitch + c);
+        biased = a.as[(size_t)r * a.spitch + c / kFp8Block];
+      } else {
+        float f[8];
+        load8<XDT>(x, r, c, f);
+        codes = encode8(f, &biased);
+      }
+      v = __builtin_bit_cast(u32x4, widen(codes[0], codes[1], scale_of(biased)));
+    }
+    *(u32x4*)(xs + r * xp + c * 2) = v;
+  }
+}
+
+template <int MT, int TPW, int PC, int XDT, int DT>
+__global__ __launch_bounds__(kSkinnyWaves * 64) void k_skinny(MatmulArgs a, QuantizeArgs x) {
+  extern __shared__ __attribute__((aligned(16))) char xs[];
+  const uint32_t wave = threadIdx.x >> 6, lane = threadIdx.x & 63, i = lane & 15, g = lane >> 4;
+  const uint32_t xp = a.pitch * 2 + 16, kb = a.pitch / kFp8Block, chunks = (kb + PC - 1) / PC;
+  const uint32_t groups = (a.n + 16 * TPW - 1) / (16 * TPW);
+  const uint32_t lo = (uint32_t)((uint64_t)groups * blockIdx.x / gridDim.x);
+  const uint32_t hi = (uint32_t)((uint64_t)groups * (blockIdx.x + 1) / gridDim.x);
+  u32x4 buf[2][TPW][PC][2];
+  // Loads of one chunk (columns past the last block read the last again).
+  auto load = [&](u32x4 (&v)[TPW][PC][2], uint32_t grp, uint32_t ch) {
+#pragma unroll
+    for (int t = 0; t < TPW; ++t) {
+      const uint8_t* p = a.w + (size_t)min((grp * TPW + t) * 16 + i, a.n - 1) * a.pitch + g * 16;
+#pragma unroll
+      for (int c = 0; c < PC; ++c) {
+        const uint32_t b = min(ch * PC + c, kb - 1);
+#pragma unroll
+        for (int q = 0; q < 2; ++q)
+          v[t][c][q] = __builtin_nontemporal_load((const u32x4*)(p + b * kFp8Block + q * 64));
+      }
+    }
+  };
+  uint32_t grp = lo + wave;
+  if (grp < hi) load(buf[0], grp, 0);
+  stage_rows<XDT>(a, x, MT * 16, xs, xp);
+  __syncthreads();
+  f32x4 acc[TPW][MT];
+  auto multiply = [&](const u32x4 (&v)[TPW][PC][2], uint32_t grp, uint32_t ch) {
+    if (ch == 0) {
+#pragma unroll
+      for (int t = 0; t < TPW; ++t)
+#pragma unroll
+        for (int m = 0; m < MT; ++m) acc[t][m] = f32x4{0.f, 0.f, 0.f, 0.f};
+    }
+#pragma unroll
+    for (int c = 0; c < PC; ++c) {
+      const uint32_t b = ch * PC + c;
+      if (b >= kb) break;
+#pragma unroll
+      for (int q = 0; q < 2; ++q) {
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+          bf16x8 xv[MT];
+#pragma unroll
+          for (int m = 0; m < MT; ++m)
+            xv[m] = *(const bf16x8*)(xs + (m * 16 + i) * xp +
+                                     (b * kFp8Block + q * 64 + g * 16 + h * 8) * 2);
+#pragma unroll
+          for (int t = 0; t < TPW; ++t) {
+            // A group of tiles may span two blocks of 128 rows of W.
+            const uint32_t nb = min((grp * TPW + t) * 16, a.n - 1) / kFp8Block;
+            const float sw = scale_of(a.ws[(size_t)nb * a.spitch + b]);
+            const bf16x8 wv = widen(v[t][c][q][2 * h], v[t][c][q][2 * h + 1], sw);
+#pragma unroll
+            for (int m = 0; m < MT; ++m)
+              acc[t][m] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(wv, xv[m], acc[t][m], 0, 0, 0);
+          }
+        }
+      }
+    }
+    if (ch + 1 == chunks) {
+#pragma unroll
+      for (int t = 0; t < TPW; ++t)
+#pragma unroll
+        for (int m = 0; m < MT; ++m) {
+          const uint32_t r = m * 16 + i, n = (grp * TPW + t) * 16 + g * 4;
+          if (r < a.rows && n < a.n) store4<DT>(a, r, n, acc[t][m]);
+        }
+    }
+  };
+  uint32_t ch = 0;
+  // Two chunks a turn: the buffers stay in registers by name.
+  while (grp < hi) {
+    uint32_t ng = grp, nc = ch + 1;
+    if (nc == chunks) nc = 0, ng += kSkinnyWaves;
+    if (ng < hi) load(buf[1], ng, nc);
+    multiply(buf[0], grp, ch);
+    grp = ng, ch = nc;
+    if (grp >= hi) break;
+    nc = ch + 1;
+    if (nc == chunks) nc = 0, ng += kSkinnyWaves;
+    if (ng < hi) load(buf[0], ng, nc);
+    multiply(buf[1], grp, ch);
+    grp = ng, ch = nc;
+  }
+}
+
+// Many rows: bound by the matrix instructions and the write of the results.
+// A block computes TN columns (rows of W) x TM rows in accumulators of WN x WM
+// waves; blocks of 128 columns of both operands go from memory straight into
+// LDS, one ahead of the one that is multiplied, and a block takes one tile
+// after another so that a tile's first loads are under way while the last
+// one's results are written.
+// In LDS a row's eight 16-byte pieces are exchanged by its number mod 8, so that
+// the 8 lanes that an LDS cycle serves read different banks.
+// float32 results: the exact bfloat16 instruction, codes widened in registers.
+// bfloat16 results: the scaled 8-bit instruction, twice its rate; its sums are
+// off by about 1.4e-5 of the result's size, their rounding by 2e-3.
+template <int TN, int TM, int WN, int WM, int DT>
+__global__ __launch_bounds__(WN* WM * 64) void k_tiles(MatmulArgs a, uint32_t tiles_n,
+                                                        uint32_t tiles_m) {
+  constexpr int WAVES = WN * WM, NT = TN / WN / 16, MT = TM / WM / 16;
+  constexpr int LOADS = (TN + TM) / 8 / WAVES, STAGE = (TN + TM) * kFp8Block;
+  __shared__ __attribute__((aligned(1024))) uint8_t lds[2][STAGE];
+  const uint32_t wave = threadIdx.x >> 6, lane = threadIdx.x & 63, i = lane & 15, g = lane >> 4;
+  const uint32_t wn = (wave % WN) * (TN / WN), wm = (wave / WN) * (TM / WM);
+  const uint32_t kb = a.pitch / kFp8Block;
+  // Tile t: all row tiles of a column tile one after another on one XCD (blocks
+  // go to the 8 XCDs in turn), so that its part of W is read into one L2.
+  auto place = [&](uint32_t t, uint32_t* n0, uint32_t* m0) {
+    const uint32_t x = t & 7, l = t >> 3;
+    *m0 = (l % tiles_m) * TM;
+    *n0 = ((l / tiles_m) * 8 + x) * TN;
+  };
+  // This lane's places in a stage: LOADS rows, as offsets from the tile's first row of W (of
+  // A, from `splits` on) with the exchanged piece; rows past the last read the last again.
+  constexpr int SPLIT = TN / 8 / WAVES;
+  static_assert(TN % (8 * WAVES) == 0 && TM % (8 * WAVES) == 0, "whole loads of either operand");
+  uint32_t off[LOADS];
+  auto offsets = [&](uint32_t n0, uint32_t m0) {
+    const uint32_t p = ((lane & 7) ^ (lane >> 3)) * 16;
+#pragma unroll
+    for (int c = 0; c < LOADS; ++c) {
+      const uint32_t r = (c * WAVES + wave) * 8 + (lane >> 3);
+      off[c] = (c < SPLIT ? min(r, a.n - 1 - n0) : min(r - TN, a.rows - 1 - m0)) * a.pitch + p;
+    }
+  };
+  auto stage = [&](int to, uint32_t n0, uint32_t m0, uint32_t b) {
+    const uint8_t* w = a.w + (size_t)n0 * a.pitch + b * kFp8Block;
+    const uint8_t* x = a.a + (size_t)m0 * a.pitch + b * kFp8Block;
+#pragma unroll
+    for (int c = 0; c < LOADS; ++c)
+      __builtin_amdgcn_global_load_lds(
+          (const __attribute__((address_space(1))) void*)((c < SPLIT ? w : x) + off[c]),
+          (__attribute__((address_space(3))) void*)(lds[to] + (c * WAVES + wave) * 8 * kFp8Block),
+          16, 0, 0);
+  };
+  uint32_t t = blockIdx.x, n0, m0;
+  const uint32_t padded = (tiles_n + 7) / 8 * 8 * tiles_m;
+  auto next = [&](uint32_t t) {  // the next tile of this block that exists
+    for (t += gridDim.x; t < padded; t += gridDim.x) {
+      uint32_t n, m;
+      place(t, &n, &m);
+      if (n < a.n) break;
+    }
+    return t;
+  };
+  place(t, &n0, &m0);
+  if (t < padded && n0 >= a.n) t = next(t);
+  if (t >= padded) return;
+  place(t, &n0, &m0);
+  int at = 0;
+  const uint32_t slot = (g ^ (i & 7)) * 16;
+  const uint32_t own_w = (wn + i) * kFp8Block, own_x = (TN + wm + i) * kFp8Block;
+  offsets(n0, m0);
+  stage(at, n0, m0, 0);
+  while (true) {
+    f32x4 acc[NT][MT];
+#pragma unroll
+    for (int n = 0; n < NT; ++n)
+#pragma unroll
+      for (int m = 0; m < MT; ++m) acc[n][m] = f32x4{0.f, 0.f, 0.f, 0.f};
+    const uint32_t after = next(t);
+    uint32_t n1 = 0, m1 = 0;
+    if (after < padded) place(after, &n1, &m1);
+    const uint32_t* wsp =
+        (const uint32_t*)(a.ws + (size_t)(min(n0 + wn, a.n - 1) / kFp8Block) * a.spitch);
+    uint32_t soff[MT];  // the rows' scales, from the tile's first row's
+#pragma unroll
+    for (int m = 0; m < MT; ++m)
+      soff[m] = min(wm + m * 16 + i, a.rows - 1 - m0) * a.spitch;
+    const uint8_t* asp = a.as + (size_t)m0 * a.spitch;
+    for (uint32_t b4 = 0; b4 < kb; b4 += 4) {
+      const uint32_t sw = __builtin_amdgcn_readfirstlane(wsp[b4 / 4]);
+      uint32_t sx[MT];
+#pragma unroll
+      for (int m = 0; m < MT; ++m) sx[m] = *(const uint32_t*)(asp + soff[m] + b4);
+      auto step = [&](auto J) {
+        constexpr int j = decltype(J)::value;
+        const uint32_t b = b4 + j;
+        if (b >= kb) return;
+        // The stage has arrived, and everybody is done with the other one.
+        asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+        __syncthreads();
+        if (b + 1 < kb) {
+          stage(at ^ 1, n0, m0, b + 1);
+        } else if (after < padded) {
+          offsets(n1, m1);
+          stage(at ^ 1, n1, m1, 0);
+        }
+        // Piece p of row 16 k + i lies at slot p ^ (i & 7); p = g and g + 4 differ in one bit.
+        const uint8_t* lw = lds[at] + own_w;
+        const uint8_t* lx = lds[at] + own_x;
+        at ^= 1;
+        if constexpr (DT == TFE_BF16) {
+          typedef int v8i __attribute__((ext_vector_type(8)));
+          auto operand = [&](const uint8_t* from, int k) {
+            const u32x4 lo = *(const u32x4*)(from + slot + k * 16 * kFp8Block);
+            const u32x4 hi = *(const u32x4*)(from + (slot ^ 64) + k * 16 * kFp8Block);
+            return v8i{(int)lo[0], (int)lo[1], (int)lo[2], (int)lo[3],
+                       (int)hi[0], (int)hi[1], (int)hi[2], (int)hi[3]};
+          };
+          v8i wv[NT];
+#pragma unroll
+          for (int n = 0; n < NT; ++n) wv[n] = operand(lw, n);
+#pragma unroll
+          for (int m = 0; m < MT; ++m) {
+            const v8i xv = operand(lx, m);
+#pragma unroll
+            for (int n = 0; n < NT; ++n)
+              acc[n][m] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(
+                  wv[n], xv, acc[n][m], 0, 0, j, (int)sw, j, (int)sx[m]);
+          }
+        } else {
+          const float fw = scale_of(byte_of(sw, j));
+#pragma unroll
+          for (int q = 0; q < 4; ++q) {
+            auto operand = [&](const uint8_t* from, int k, float f) {
+              const u32x2 v = *(const u32x2*)(from + (q < 2 ? slot : slot ^ 64) + (q & 1) * 8 +
+                                              k * 16 * kFp8Block);
+              return widen(v[0], v[1], f);
+            };
+            bf16x8 wv[NT];
+#pragma unroll
+            for (int n = 0; n < NT; ++n) wv[n] = operand(lw, n, fw);
+#pragma unroll
+            for (int m = 0; m < MT; ++m) {
+              const bf16x8 xv = operand(lx, m, scale_of(byte_of(sx[m], j)));
+#pragma unroll
+              for (int n = 0; n < NT; ++n)
+                acc[n][m] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(wv[n], xv, acc[n][m], 0, 0, 0);
+            }
+          }
+        }
+      };
+      step(std::integral_constant<int, 0>{});
+      step(std::integral_constant<int, 1>{});
+      step(std::integral_constant<int, 2>{});
+      step(std::integral_constant<int, 3>{});
+    }
+#pragma unroll
+    for (int m = 0; m < MT; ++m) {
+      const uint32_t r = m0 + wm + m * 16 + i;
+      if (r >= a.rows) continue;
+#pragma unroll
+      for (int n = 0; n < NT; ++n) {
+        const uint32_t c = n0 + wn + n * 16 + g * 4;
+        if (c < a.n) store4<DT>(a, r, c, acc[n][m]);
+      }
+    }
+    if (after >= padded) break;
+    t = after, n0 = n1, m0 = m1;
+  }
+}
+
+// ---- launches ------------------------------------------------------------------
+
+int compute_units() {
+  constexpr int kDevices = 64;
+  static std::atomic<int> known[kDevices];
+  int dev = 0, cus = 0;
+  if (hipGetDevice(&dev) != hipSuccess) return 256;
+  if (dev >= 0 && dev < kDevices && (cus = known[dev].load(std::memory_order_relaxed)) > 0) return cus;
+  if (hipDeviceGetAttribute(&cus, hipDeviceAttributeMultiprocessorCount, dev) != hipSuccess || cus < 1)
+    return 256;
+  if (dev >= 0 && dev < kDevices) known[dev].store(cus, std::memory_order_relaxed);
+  return cus;
+}
+
+uint32_t skinny_lds(const MatmulArgs& a) {
+  const uint32_t mt = (a.rows + 15) / 16;
+  return mt * 16 * (a.pitch * 2 + 16);
+}
+
+template <int MT, int TPW, int PC, int XDT, int DT>
+hipError_t skinny(const MatmulArgs& a, const QuantizeArgs& x, hipStream_t s) {
+  const uint32_t lds = skinny_lds(a), groups = (a.n + 16 * TPW - 1) / (16 * TPW);
+  auto* k = k_skinny<MT, TPW, PC, XDT, DT>;
+  const hipError_t e = hipFuncSetAttribute((const void*)k, hipFuncAttributeMaxDynamicSharedMemorySize,
+                                           (int)kSkinnyLds);
+  if (e != hipSuccess) return e;
+  const uint32_t most = (uint32_t)compute_units() * (lds <= 65536 ? 2 : 1);
+  const uint32_t want = (groups + kSkinnyWaves - 1) / kSkinnyWaves;
+  k<<<dim3(std::min(most, want)), dim3(kSkinnyWaves * 64), lds, s>>>(a, x);
+  return hipGetLastError();
+}
+template <int XDT, int DT>
+hipError_t skinny_rows(const MatmulArgs& a, const QuantizeArgs& x, hipStream_t s) {
+  switch ((a.rows + 15) / 16) {
+    case 1: return skinny<1, 1, 8, XDT, DT>(a, x, s);
+    case 2: return skinny<2, 2, 4, XDT, DT>(a, x, s);
+    case 3: return skinny<3, 2, 4, XDT, DT>(a, x, s);
+    default: return skinny<4, 2, 4, XDT, DT>(a, x, s);
+  }
+}
+
+template <int TN, int TM, int WN, int WM>
+hipError_t tiles(const MatmulArgs& a, int dt, int blocks_per_cu, hipStream_t s) {
+  const uint32_t tn = (a.n + TN - 1) / TN, tm = (a.rows + TM - 1) / TM;
+  const uint32_t padded = (tn + 7) / 8 * 8 * tm;
+  const uint32_t most = (uint32_t)(compute_units() * blocks_per_cu + 7) / 8 * 8;
+  const dim3 grid(std::min(padded, most)), block(WN * WM * 64);
+  if (dt == TFE_F32)
+    k_tiles<TN, TM, WN, WM, TFE_F32><<<grid, block, 0, s>>>(a, tn, tm);
+  else
+    k_tiles<TN, TM, WN, WM, TFE_BF16><<<grid, block, 0, s>>>(a, tn, tm);
+  return hipGetLastError();
+}
+
+bool is_skinny(const MatmulArgs& a) { return a.rows <= 64 && skinny_lds(a) <= kSkinnyLds; }
 
 }  // namespace
 
@@ -189,12 +539,25 @@ hipError_t launch_fp8_quantize(const QuantizeArgs& a, int dtype, int block_rows,
 }
 
 hipError_t launch_fp8_matmul(const MatmulArgs& a, int out_dtype, hipStream_t s) {
-  const dim3 grid((a.n + 63) / 64, std::min((a.rows + 15) / 16, 32768u));
-  if (out_dtype == TFE_F32)
-    k_product<TFE_F32><<<grid, dim3(256), 0, s>>>(a);
-  else
-    k_product<TFE_BF16><<<grid, dim3(256), 0, s>>>(a);
-  return hipGetLastError();
+  if (is_skinny(a))
+    return out_dtype == TFE_F32 ? skinny_rows<kCodes, TFE_F32>(a, QuantizeArgs{}, s)
+                                : skinny_rows<kCodes, TFE_BF16>(a, QuantizeArgs{}, s);
+  const uint64_t large = (uint64_t)((a.n + 255) / 256) * ((a.rows + 255) / 256);
+  if (large >= (uint64_t)compute_units() * 2) return tiles<256, 256, 4, 2>(a, out_dtype, 1, s);
+  return tiles<128, 128, 2, 2>(a, out_dtype, 2, s);
+}
+
+hipError_t launch_fp8_linear(const QuantizeArgs& x, const MatmulArgs& a, int dtype, int out_dtype,
+                             hipStream_t s) {
+  if (is_skinny(a)) {
+    if (dtype == TFE_F32)
+      return out_dtype == TFE_F32 ? skinny_rows<TFE_F32, TFE_F32>(a, x, s)
+                                  : skinny_rows<TFE_F32, TFE_BF16>(a, x, s);
+    return out_dtype == TFE_F32 ? skinny_rows<TFE_BF16, TFE_F32>(a, x, s)
+                                : skinny_rows<TFE_BF16, TFE_BF16>(a, x, s);
+  }
+  const hipError_t e = launch_fp8_quantize(x, dtype, 1, s);
+  return e == hipSuccess ? launch_fp8_matmul(a, out_dtype, s) : e;
 }
 
 }  // namespace tfe
