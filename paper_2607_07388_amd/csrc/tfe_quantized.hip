@@ -154,16 +154,19 @@ __device__ __forceinline__ uint32_t byte_of(uint32_t w, int i) { return (w >> (8
 
 // Four results of a lane (columns n .. n + 3 of one row), stored together
 // where the row has them.
-template <int DT>
-__device__ __forceinline__ void store4(const MatmulArgs& a, uint32_t r, uint32_t n, f32x4 v) {
+template <int DT> __device__ __forceinline__ void store4_at(char* out, f32x4 v) {
   typedef uint32_t u2 __attribute__((ext_vector_type(2), aligned(2)));
   typedef f32x4 f4 __attribute__((aligned(4)));
+  if (DT == TFE_F32)
+    *(f4*)out = v;
+  else
+    *(u2*)out = u2{pack2(v[0], v[1]), pack2(v[2], v[3])};
+}
+template <int DT>
+__device__ __forceinline__ void store4(const MatmulArgs& a, uint32_t r, uint32_t n, f32x4 v) {
   char* out = (char*)a.out + ((size_t)r * a.ldo + n) * sizeof(typename Elem<DT>::T);
   if (n + 4 <= a.n) {
-    if (DT == TFE_F32)
-      *(f4*)out = v;
-    else
-      *(u2*)out = u2{pack2(v[0], v[1]), pack2(v[2], v[3])};
+    store4_at<DT>(out, v);
   } else {
 #pragma unroll
     for (int j = 0; j < 4; ++j)
@@ -306,85 +309,92 @@ __global__ __launch_bounds__(kSkinnyWaves * 64) void k_skinny(MatmulArgs a, Quan
 // float32 results: the exact bfloat16 instruction, codes widened in registers.
 // bfloat16 results: the scaled 8-bit instruction, twice its rate; its sums are
 // off by about 1.4e-5 of the result's size, their rounding by 2e-3.
+#if defined(__HIP_DEVICE_COMPILE__)  // the host compiler has no buffer descriptors
+// Loads go through buffer descriptors: 32-bit offsets, and rows past a matrix'
+// last read as zeros (the whole offset is in the vector register, so that the
+// descriptor's range covers it).
+__device__ __forceinline__ __amdgpu_buffer_rsrc_t rows_of(const uint8_t* p, uint32_t row, uint32_t rows,
+                                                          uint32_t most, uint32_t pitch) {
+  const uint32_t left = min(rows - row, most) * pitch;  // most * pitch < 2^25
+  return __builtin_amdgcn_make_buffer_rsrc((void*)(p + (size_t)row * pitch), 0, (int)left, 0x00020000);
+}
+#endif
+
 template <int TN, int TM, int WN, int WM, int DT>
-__global__ __launch_bounds__(WN* WM * 64) void k_tiles(MatmulArgs a, uint32_t tiles_n,
-                                                        uint32_t tiles_m) {
+__global__ __launch_bounds__(WN* WM * 64) void k_tiles(MatmulArgs a, uint32_t tiles_m,
+                                                        uint32_t places) {
+#if defined(__HIP_DEVICE_COMPILE__)
   constexpr int WAVES = WN * WM, NT = TN / WN / 16, MT = TM / WM / 16;
-  constexpr int LOADS = (TN + TM) / 8 / WAVES, STAGE = (TN + TM) * kFp8Block;
-  __shared__ __attribute__((aligned(1024))) uint8_t lds[2][STAGE];
-  const uint32_t wave = threadIdx.x >> 6, lane = threadIdx.x & 63, i = lane & 15, g = lane >> 4;
+  constexpr int LW = TN / 8 / WAVES, LX = TM / 8 / WAVES, STAGE = (TN + TM) * kFp8Block;
+  static_assert(TN % (8 * WAVES) == 0 && TM % (8 * WAVES) == 0, "whole loads of either operand");
+  static_assert(kFp8Block % (TN / WN) == 0 || (TN / WN) % kFp8Block == 0, "one scale of W a wave");
+  __shared__ __attribute__((aligned(1024))) uint8_t lds[2 * STAGE];
+  const uint32_t wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const uint32_t lane = threadIdx.x & 63, i = lane & 15, g = lane >> 4;
   const uint32_t wn = (wave % WN) * (TN / WN), wm = (wave / WN) * (TM / WM);
   const uint32_t kb = a.pitch / kFp8Block;
-  // Tile t: all row tiles of a column tile one after another on one XCD (blocks
-  // go to the 8 XCDs in turn), so that its part of W is read into one L2.
-  auto place = [&](uint32_t t, uint32_t* n0, uint32_t* m0) {
-    const uint32_t x = t & 7, l = t >> 3;
-    *m0 = (l % tiles_m) * TM;
-    *n0 = ((l / tiles_m) * 8 + x) * TN;
+
+  // Place t: all row tiles of a column tile one after another on one XCD
+  // (blocks go to the 8 XCDs in turn), so that its part of W is read into one
+  // L2.  Places beyond the last column are empty.
+  struct Tile {
+    uint32_t t, n, m;
   };
-  // This lane's places in a stage: LOADS rows, as offsets from the tile's first row of W (of
-  // A, from `splits` on) with the exchanged piece; rows past the last read the last again.
-  constexpr int SPLIT = TN / 8 / WAVES;
-  static_assert(TN % (8 * WAVES) == 0 && TM % (8 * WAVES) == 0, "whole loads of either operand");
-  uint32_t off[LOADS];
-  auto offsets = [&](uint32_t n0, uint32_t m0) {
-    const uint32_t p = ((lane & 7) ^ (lane >> 3)) * 16;
+  auto find = [&](uint32_t t) {
+    Tile r{t, 0, 0};
+    for (; r.t < places; r.t += gridDim.x) {
+      const uint32_t l = r.t >> 3, q = l / tiles_m;
+      r.n = (q * 8 + (r.t & 7)) * TN;
+      r.m = (l - q * tiles_m) * TM;
+      if (r.n < a.n) break;
+    }
+    r.t = __builtin_amdgcn_readfirstlane(r.t);
+    r.n = __builtin_amdgcn_readfirstlane(r.n);
+    r.m = __builtin_amdgcn_readfirstlane(r.m);
+    return r;
+  };
+  // A load instruction fills 8 rows of a stage: lane l piece l % 8 ^ l / 8 of row l / 8.
+  const uint32_t from = (lane >> 3) * a.pitch + ((lane & 7) ^ (lane >> 3)) * 16;
+  auto stage = [&](uint32_t to, const Tile& t, uint32_t b) {
+    const auto w = rows_of(a.w, t.n, a.n, TN, a.pitch), x = rows_of(a.a, t.m, a.rows, TM, a.pitch);
 #pragma unroll
-    for (int c = 0; c < LOADS; ++c) {
-      const uint32_t r = (c * WAVES + wave) * 8 + (lane >> 3);
-      off[c] = (c < SPLIT ? min(r, a.n - 1 - n0) : min(r - TN, a.rows - 1 - m0)) * a.pitch + p;
+    for (int c = 0; c < LW + LX; ++c) {
+      const uint32_t row = ((c < LW ? c : c - LW) * WAVES + wave) * 8;
+      __builtin_amdgcn_raw_ptr_buffer_load_lds(
+          c < LW ? w : x,
+          (__attribute__((address_space(3))) void*)(lds + to + ((c < LW ? 0 : TN) + row) * kFp8Block), 16,
+          (int)(from + row * a.pitch + b * kFp8Block), 0, 0, 0);
     }
   };
-  auto stage = [&](int to, uint32_t n0, uint32_t m0, uint32_t b) {
-    const uint8_t* w = a.w + (size_t)n0 * a.pitch + b * kFp8Block;
-    const uint8_t* x = a.a + (size_t)m0 * a.pitch + b * kFp8Block;
+  // Scales of four blocks from b: the wave's part of W lies in one block of 128 rows.
+  auto scales = [&](const Tile& t, uint32_t b, uint32_t& sw, uint32_t (&sx)[MT]) {
+    const uint32_t row = min(t.n + wn, a.n - 1) / kFp8Block;
+    sw = *(const uint32_t*)(a.ws + (size_t)row * a.spitch + b);
+    const auto x = rows_of(a.as, t.m, a.rows, TM, a.spitch);
 #pragma unroll
-    for (int c = 0; c < LOADS; ++c)
-      __builtin_amdgcn_global_load_lds(
-          (const __attribute__((address_space(1))) void*)((c < SPLIT ? w : x) + off[c]),
-          (__attribute__((address_space(3))) void*)(lds[to] + (c * WAVES + wave) * 8 * kFp8Block),
-          16, 0, 0);
+    for (int m = 0; m < MT; ++m)
+      sx[m] = __builtin_amdgcn_raw_buffer_load_b32(x, (int)((wm + m * 16 + i) * a.spitch + b), 0, 0);
   };
-  uint32_t t = blockIdx.x, n0, m0;
-  const uint32_t padded = (tiles_n + 7) / 8 * 8 * tiles_m;
-  auto next = [&](uint32_t t) {  // the next tile of this block that exists
-    for (t += gridDim.x; t < padded; t += gridDim.x) {
-      uint32_t n, m;
-      place(t, &n, &m);
-      if (n < a.n) break;
-    }
-    return t;
-  };
-  place(t, &n0, &m0);
-  if (t < padded && n0 >= a.n) t = next(t);
-  if (t >= padded) return;
-  place(t, &n0, &m0);
-  int at = 0;
+
+  Tile cur = find(blockIdx.x);
+  if (cur.t >= places) return;
+  uint32_t at = 0, sw, sx[MT], sw_next, sx_next[MT];
+  // Piece p of row 16 k + i lies at slot p ^ (i & 7); p = g and g + 4 differ in one bit.
   const uint32_t slot = (g ^ (i & 7)) * 16;
-  const uint32_t own_w = (wn + i) * kFp8Block, own_x = (TN + wm + i) * kFp8Block;
-  offsets(n0, m0);
-  stage(at, n0, m0, 0);
+  const uint32_t own_w = (wn + i) * kFp8Block + slot, own_x = (TN + wm + i) * kFp8Block + slot;
+  stage(at, cur, 0);
+  scales(cur, 0, sw_next, sx_next);
   while (true) {
     f32x4 acc[NT][MT];
 #pragma unroll
     for (int n = 0; n < NT; ++n)
 #pragma unroll
       for (int m = 0; m < MT; ++m) acc[n][m] = f32x4{0.f, 0.f, 0.f, 0.f};
-    const uint32_t after = next(t);
-    uint32_t n1 = 0, m1 = 0;
-    if (after < padded) place(after, &n1, &m1);
-    const uint32_t* wsp =
-        (const uint32_t*)(a.ws + (size_t)(min(n0 + wn, a.n - 1) / kFp8Block) * a.spitch);
-    uint32_t soff[MT];  // the rows' scales, from the tile's first row's
-#pragma unroll
-    for (int m = 0; m < MT; ++m)
-      soff[m] = min(wm + m * 16 + i, a.rows - 1 - m0) * a.spitch;
-    const uint8_t* asp = a.as + (size_t)m0 * a.spitch;
+    const Tile next = find(cur.t + gridDim.x);
     for (uint32_t b4 = 0; b4 < kb; b4 += 4) {
-      const uint32_t sw = __builtin_amdgcn_readfirstlane(wsp[b4 / 4]);
-      uint32_t sx[MT];
+      sw = sw_next;
 #pragma unroll
-      for (int m = 0; m < MT; ++m) sx[m] = *(const uint32_t*)(asp + soff[m] + b4);
+      for (int m = 0; m < MT; ++m) sx[m] = sx_next[m];
       auto step = [&](auto J) {
         constexpr int j = decltype(J)::value;
         const uint32_t b = b4 + j;
@@ -392,53 +402,55 @@ __global__ __launch_bounds__(WN* WM * 64) void k_tiles(MatmulArgs a, uint32_t ti
         // The stage has arrived, and everybody is done with the other one.
         asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
         __syncthreads();
+        const uint32_t to = STAGE - at;
         if (b + 1 < kb) {
-          stage(at ^ 1, n0, m0, b + 1);
-        } else if (after < padded) {
-          offsets(n1, m1);
-          stage(at ^ 1, n1, m1, 0);
+          stage(to, cur, b + 1);
+          if (j == 3) scales(cur, b + 1, sw_next, sx_next);
+        } else if (next.t < places) {
+          stage(to, next, 0);
+          scales(next, 0, sw_next, sx_next);
         }
-        // Piece p of row 16 k + i lies at slot p ^ (i & 7); p = g and g + 4 differ in one bit.
-        const uint8_t* lw = lds[at] + own_w;
-        const uint8_t* lx = lds[at] + own_x;
-        at ^= 1;
+        const uint8_t* lw = lds + at + own_w;
+        const uint8_t* lx = lds + at + own_x;
+        const uint8_t* lw2 = lds + at + (own_w ^ 64);
+        const uint8_t* lx2 = lds + at + (own_x ^ 64);
+        at = to;
         if constexpr (DT == TFE_BF16) {
           typedef int v8i __attribute__((ext_vector_type(8)));
-          auto operand = [&](const uint8_t* from, int k) {
-            const u32x4 lo = *(const u32x4*)(from + slot + k * 16 * kFp8Block);
-            const u32x4 hi = *(const u32x4*)(from + (slot ^ 64) + k * 16 * kFp8Block);
+          auto operand = [&](const uint8_t* p, const uint8_t* p2, int k) {
+            const u32x4 lo = *(const u32x4*)(p + k * 16 * kFp8Block);
+            const u32x4 hi = *(const u32x4*)(p2 + k * 16 * kFp8Block);
             return v8i{(int)lo[0], (int)lo[1], (int)lo[2], (int)lo[3],
                        (int)hi[0], (int)hi[1], (int)hi[2], (int)hi[3]};
           };
-          v8i wv[NT];
+          v8i xv[MT];
 #pragma unroll
-          for (int n = 0; n < NT; ++n) wv[n] = operand(lw, n);
+          for (int m = 0; m < MT; ++m) xv[m] = operand(lx, lx2, m);
 #pragma unroll
-          for (int m = 0; m < MT; ++m) {
-            const v8i xv = operand(lx, m);
+          for (int n = 0; n < NT; ++n) {
+            const v8i wv = operand(lw, lw2, n);
 #pragma unroll
-            for (int n = 0; n < NT; ++n)
+            for (int m = 0; m < MT; ++m)
               acc[n][m] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(
-                  wv[n], xv, acc[n][m], 0, 0, j, (int)sw, j, (int)sx[m]);
+                  wv, xv[m], acc[n][m], 0, 0, j, (int)sw, j, (int)sx[m]);
           }
         } else {
           const float fw = scale_of(byte_of(sw, j));
 #pragma unroll
           for (int q = 0; q < 4; ++q) {
-            auto operand = [&](const uint8_t* from, int k, float f) {
-              const u32x2 v = *(const u32x2*)(from + (q < 2 ? slot : slot ^ 64) + (q & 1) * 8 +
-                                              k * 16 * kFp8Block);
+            auto operand = [&](const uint8_t* p, const uint8_t* p2, int k, float f) {
+              const u32x2 v = *(const u32x2*)((q < 2 ? p : p2) + (q & 1) * 8 + k * 16 * kFp8Block);
               return widen(v[0], v[1], f);
             };
-            bf16x8 wv[NT];
+            bf16x8 xv[MT];
 #pragma unroll
-            for (int n = 0; n < NT; ++n) wv[n] = operand(lw, n, fw);
+            for (int m = 0; m < MT; ++m) xv[m] = operand(lx, lx2, m, scale_of(byte_of(sx[m], j)));
 #pragma unroll
-            for (int m = 0; m < MT; ++m) {
-              const bf16x8 xv = operand(lx, m, scale_of(byte_of(sx[m], j)));
+            for (int n = 0; n < NT; ++n) {
+              const bf16x8 wv = operand(lw, lw2, n, fw);
 #pragma unroll
-              for (int n = 0; n < NT; ++n)
-                acc[n][m] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(wv[n], xv, acc[n][m], 0, 0, 0);
+              for (int m = 0; m < MT; ++m)
+                acc[n][m] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(wv, xv[m], acc[n][m], 0, 0, 0);
             }
           }
         }
@@ -448,19 +460,28 @@ __global__ __launch_bounds__(WN* WM * 64) void k_tiles(MatmulArgs a, uint32_t ti
       step(std::integral_constant<int, 2>{});
       step(std::integral_constant<int, 3>{});
     }
+    const uint32_t r0 = cur.m + wm + i, c0 = cur.n + wn + g * 4;
+    if (cur.n + TN <= a.n && cur.m + TM <= a.rows) {
+      constexpr int ES = sizeof(typename Elem<DT>::T);
+      char* out = (char*)a.out + ((size_t)r0 * a.ldo + c0) * ES;
 #pragma unroll
-    for (int m = 0; m < MT; ++m) {
-      const uint32_t r = m0 + wm + m * 16 + i;
-      if (r >= a.rows) continue;
+      for (int m = 0; m < MT; ++m) {
 #pragma unroll
-      for (int n = 0; n < NT; ++n) {
-        const uint32_t c = n0 + wn + n * 16 + g * 4;
-        if (c < a.n) store4<DT>(a, r, c, acc[n][m]);
+        for (int n = 0; n < NT; ++n) store4_at<DT>(out + n * 16 * ES, acc[n][m]);
+        out += (size_t)a.ldo * 16 * ES;
       }
+    } else {
+#pragma unroll
+      for (int m = 0; m < MT; ++m)
+#pragma unroll
+        for (int n = 0; n < NT; ++n)
+          if (r0 + m * 16 < a.rows && c0 + n * 16 < a.n)
+            store4<DT>(a, r0 + m * 16, c0 + n * 16, acc[n][m]);
     }
-    if (after >= padded) break;
-    t = after, n0 = n1, m0 = m1;
+    if (next.t >= places) break;
+    cur = next;
   }
+#endif
 }
 
 // ---- launches ------------------------------------------------------------------
@@ -507,13 +528,13 @@ hipError_t skinny_rows(const MatmulArgs& a, const QuantizeArgs& x, hipStream_t s
 template <int TN, int TM, int WN, int WM>
 hipError_t tiles(const MatmulArgs& a, int dt, int blocks_per_cu, hipStream_t s) {
   const uint32_t tn = (a.n + TN - 1) / TN, tm = (a.rows + TM - 1) / TM;
-  const uint32_t padded = (tn + 7) / 8 * 8 * tm;
+  const uint32_t places = (tn + 7) / 8 * 8 * tm;
   const uint32_t most = (uint32_t)(compute_units() * blocks_per_cu + 7) / 8 * 8;
-  const dim3 grid(std::min(padded, most)), block(WN * WM * 64);
+  const dim3 grid(std::min(places, most)), block(WN * WM * 64);
   if (dt == TFE_F32)
-    k_tiles<TN, TM, WN, WM, TFE_F32><<<grid, block, 0, s>>>(a, tn, tm);
+    k_tiles<TN, TM, WN, WM, TFE_F32><<<grid, block, 0, s>>>(a, tm, places);
   else
-    k_tiles<TN, TM, WN, WM, TFE_BF16><<<grid, block, 0, s>>>(a, tn, tm);
+    k_tiles<TN, TM, WN, WM, TFE_BF16><<<grid, block, 0, s>>>(a, tm, places);
   return hipGetLastError();
 }
 
@@ -543,7 +564,7 @@ hipError_t launch_fp8_matmul(const MatmulArgs& a, int out_dtype, hipStream_t s) 
     return out_dtype == TFE_F32 ? skinny_rows<kCodes, TFE_F32>(a, QuantizeArgs{}, s)
                                 : skinny_rows<kCodes, TFE_BF16>(a, QuantizeArgs{}, s);
   const uint64_t large = (uint64_t)((a.n + 255) / 256) * ((a.rows + 255) / 256);
-  if (large >= (uint64_t)compute_units() * 2) return tiles<256, 256, 4, 2>(a, out_dtype, 1, s);
+  if (large >= (uint64_t)compute_units() * 2) return tiles<256, 256, 2, 4>(a, out_dtype, 1, s);
   return tiles<128, 128, 2, 2>(a, out_dtype, 2, s);
 }
 
