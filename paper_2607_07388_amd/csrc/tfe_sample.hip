@@ -7,9 +7,20 @@
 // weights of at most 2^31: exact, and exact as doubles too), so the answer
 // does not depend on the order of the additions.  2^-31 of the most likely
 // token's weight is the resolution: finer than that of a float32 u.
-// Bound by the logits' bytes.
+//
+// Nothing is sorted but a few hundred elements.  A histogram of the weights by
+// their leading bits gives the running count and sum at every bin's edge; from
+// those, and the settings, follows in which bins the answers to the four
+// questions can lie (later ones depend on earlier ones, so a question can have
+// a short range of bins).  Only those bins' elements are collected and sorted,
+// and the questions answered in turn.  Three passes over the logits: their
+// maximum, the histogram, the collection.
+// Bound by the logits' bytes for the first pass, then by the weights' arithmetic
+// (about 27 instruction slots a logit) and the LDS additions of the second.
 #include <hip/hip_runtime.h>
 #include <stdint.h>
+
+#include <algorithm>
 
 #include "tfe_logits.h"
 #include "tfe_rows.h"
@@ -19,7 +30,6 @@ namespace {
 
 using namespace rows;
 
-constexpr int kThreads = 1024;
 // A weight w >= 1 is a float32 without error (it is one, or an integer below
 // 2^24), and its bits order as it does.  The order's key: 28 bits of the
 // weight's float bits above those of 1, then 18 bits of the token, lower
@@ -38,72 +48,134 @@ __device__ __forceinline__ uint32_t key_id(uint64_t k) {
   return (1u << kIdBits) - 1 - (uint32_t)(k & ((1u << kIdBits) - 1));
 }
 
-// A row's settings.
-struct Row {
-  float top, inv_t;  // largest logit, 1 / T
-  bool greedy;
+// A row's largest logit and 1 / T.  The most likely token alone (T <= 0 or NaN)
+// is 1 / T = infinity: every smaller logit has weight 0.
+struct Scale {
+  float top, inv_t;
 };
-// The weight of logit l, an integer in float32; 0 for NaN and -infinity.
-__device__ __forceinline__ float weight(const Row& r, float l) {
-  if (l == r.top) return kUnit;
-  if (r.greedy || !(l > -INFINITY)) return 0.f;
-  const float e = rintf(expf((l - r.top) * r.inv_t) * kUnit);
-  return e >= 1.f ? e : 0.f;  // NaN (0 x infinity) is no weight either
+__device__ __forceinline__ float inverse_temperature(const SampleArgs& a, uint32_t row) {
+  const float T = a.temperature ? a.temperature[row] : 1.f;
+  return T > 0.f ? 1.f / T : INFINITY;
 }
 
-constexpr int kBins = 4096;
-struct Shared {
-  uint32_t cnt[kBins];
-  unsigned long long sum[kBins];
-  unsigned long long red[kThreads / 64];
-  uint32_t redc[kThreads / 64];
-  // What a scan of the bins found.
-  uint32_t bin;
-  uint64_t before_c, before_w, in_c, in_w;
-};
+// The weight of logit l, an integer in float32; 0 for NaN and -infinity.
+// exp(d) is 2^(d log2 e) with the product in two parts (its rounding would be
+// as much as |d| 2^-24 of the result) and the hardware's exponential: about an
+// ulp in all.  The maximum with -30, where weights are 0, also takes the NaN
+// of infinity - infinity and 0 x infinity.
+__device__ __forceinline__ float weight(const Scale& r, float l) {
+  const float d = fmaxf((l - r.top) * r.inv_t, -30.f);
+  const float p = d * 1.44269504f;
+  const float e = fmaf(d, 1.92596303e-8f, fmaf(d, 1.44269504f, -p));
+  const float x = __builtin_amdgcn_exp2f(p);
+  const float w = rintf(fmaf(x, e * 0.693147181f, x) * kUnit);
+  return l == r.top ? kUnit : w;
+}
 
-// Calls f(l, id) for every logit of the row.
-template <int DT, class F> __device__ __forceinline__ void each(const SampleArgs& a, const char* x, F f) {
-  constexpr int N = Elem<DT>::N;
-  const uint32_t nv = a.vocab / N;
-  for (uint32_t v = threadIdx.x; v < nv; v += kThreads) {
+// The histogram: 4096 bins of 1/128 of an octave, the leading 12 bits of the
+// key.  An entry holds the number of its elements (from bit 43 on) and the sum
+// of what their weights have above the bin's lowest (below 2^24 each, 2^42 in
+// all): one 64-bit addition an element.
+constexpr int kBins = 4096, kBinShift = 16, kCountShift = 43;
+__device__ __forceinline__ uint32_t bin_of(float w) {
+  return (__float_as_uint(w) - kOneBits) >> kBinShift;
+}
+__device__ __forceinline__ uint32_t bin_low(uint32_t bin) {
+  return (uint32_t)__uint_as_float((bin << kBinShift) + kOneBits);
+}
+__device__ __forceinline__ uint64_t bin_entry(float w) {
+  const uint32_t low = (uint32_t)__uint_as_float(__float_as_uint(w) & ~((1u << kBinShift) - 1));
+  return ((uint64_t)1 << kCountShift) | ((uint32_t)w - low);
+}
+__device__ __forceinline__ uint32_t entry_count(uint64_t e) { return (uint32_t)(e >> kCountShift); }
+__device__ __forceinline__ uint64_t entry_sum(uint64_t e, uint32_t bin) {
+  return (e & (((uint64_t)1 << kCountShift) - 1)) + (uint64_t)entry_count(e) * bin_low(bin);
+}
+
+// Calls f(logit, token) for the logits that thread `from` of `threads` of a row
+// takes, four 16-byte loads in flight.
+template <int DT, class F>
+__device__ __forceinline__ void each(const char* x, uint32_t vocab, uint32_t from, uint32_t threads,
+                                     F f) {
+  constexpr int N = Elem<DT>::N, U = 4;
+  const uint32_t nv = vocab / N;
+  uint32_t v = from;
+  for (; v + (U - 1) * threads < nv; v += U * threads) {
+    u32x4 q[U];
+#pragma unroll
+    for (int u = 0; u < U; ++u) q[u] = load_vec<DT>(x, v + u * threads);
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      float l[N];
+      unpack<DT>(q[u], l);
+#pragma unroll
+      for (int i = 0; i < N; ++i) f(l[i], (v + u * threads) * N + i);
+    }
+  }
+  for (; v < nv; v += threads) {
     float l[N];
     unpack<DT>(load_vec<DT>(x, v), l);
 #pragma unroll
     for (int i = 0; i < N; ++i) f(l[i], v * N + i);
   }
-  for (uint32_t i = nv * N + threadIdx.x; i < a.vocab; i += kThreads) f(load1<DT>(x, i), i);
+  for (uint32_t i = nv * N + from; i < vocab; i += threads) f(load1<DT>(x, i), i);
+}
+template <int DT> __device__ __forceinline__ const char* row_of(const SampleArgs& a, uint32_t row) {
+  return (const char*)a.logits + (size_t)row * a.ld * sizeof(typename Elem<DT>::T);
 }
 
-// The bin, from the highest down, in which the running count (by_count) or sum
-// reaches `target`, what lies before it and in it.  target is at most the total.
-__device__ void find_bin(Shared& sh, uint64_t target, bool by_count) {
-  constexpr int PER = kBins / kThreads;
+constexpr int kThreads = 1024;  // of the kernels with one block a row
+constexpr uint32_t kList = 2048;  // collected elements that are sorted in LDS
+
+// Running counts and sums before each bin, bins in the order's direction
+// (q = 4095 - bin), and in all at q = 4096.
+struct Edges {
+  uint64_t sum[kBins + 1];
+  uint32_t cnt[kBins + 1];
+};
+struct Shared {
+  Edges e;
+  uint64_t list[kList];
+  uint64_t red[kThreads / 64];
+  uint32_t redc[kThreads / 64];
+  uint32_t n;
+  // Answers of a search.
+  uint32_t q[2];
+  uint64_t key, sum;
+};
+
+// Edges from the histogram in sh.e.sum (in place) or in memory.
+template <int THREADS> __device__ void make_edges(Shared& sh, const unsigned long long* hist) {
+  constexpr int PER = kBins / THREADS;
   const int t = threadIdx.x, lane = t & 63, wave = t >> 6;
   uint32_t c[PER];
-  uint64_t w[PER], cs = 0, ws = 0;
+  uint64_t w[PER], ws = 0;
+  uint32_t cs = 0;
 #pragma unroll
   for (int i = 0; i < PER; ++i) {
-    const int b = kBins - 1 - (t * PER + i);
-    c[i] = sh.cnt[b];
-    w[i] = sh.sum[b];
+    const uint32_t b = kBins - 1 - (t * PER + i);
+    const uint64_t x = hist ? hist[b] : sh.e.sum[b];
+    c[i] = entry_count(x);
+    w[i] = entry_sum(x, b);
     cs += c[i];
     ws += w[i];
   }
-  uint64_t pc = cs, pw = ws;  // inclusive over the wave
+  uint32_t pc = cs;
+  uint64_t pw = ws;
 #pragma unroll
   for (int o = 1; o < 64; o <<= 1) {
-    const uint64_t xc = __shfl_up(pc, o), xw = __shfl_up(pw, o);
+    const uint32_t xc = __shfl_up(pc, o);
+    const uint64_t xw = __shfl_up(pw, o);
     if (lane >= o) {
       pc += xc;
       pw += xw;
     }
   }
   if (lane == 63) {
-    sh.redc[wave] = (uint32_t)pc;
+    sh.redc[wave] = pc;
     sh.red[wave] = pw;
   }
-  __syncthreads();
+  __syncthreads();  // also: the histogram has been read
   for (int i = 0; i < wave; ++i) {
     pc += sh.redc[i];
     pw += sh.red[i];
@@ -112,123 +184,516 @@ __device__ void find_bin(Shared& sh, uint64_t target, bool by_count) {
   pw -= ws;
 #pragma unroll
   for (int i = 0; i < PER; ++i) {
-    const uint64_t have = by_count ? pc : pw, get = by_count ? c[i] : w[i];
-    if (have < target && target <= have + get) {
-      sh.bin = (uint32_t)(kBins - 1 - (t * PER + i));
-      sh.before_c = pc;
-      sh.before_w = pw;
-      sh.in_c = c[i];
-      sh.in_w = w[i];
-    }
+    sh.e.cnt[t * PER + i] = pc;
+    sh.e.sum[t * PER + i] = pw;
     pc += c[i];
     pw += w[i];
+  }
+  if (t == THREADS - 1) {
+    sh.e.cnt[kBins] = pc;
+    sh.e.sum[kBins] = pw;
   }
   __syncthreads();
 }
 
-// The element of the order at which the running count or sum reaches `target`
-// (at least 1, at most the row's): its key, and the sum through it.  Twelve
-// bits of the key at a time, over the elements that share the bits so far.
+// The bins in which the running sum reaches a and b (at least 1, at most the
+// total; a <= b).
+template <int THREADS>
+__device__ void bins_of_sums(Shared& sh, uint64_t a, uint64_t b, uint32_t* qa, uint32_t* qb) {
+  for (int q = threadIdx.x; q < kBins; q += THREADS) {
+    const uint64_t lo = sh.e.sum[q], hi = sh.e.sum[q + 1];
+    if (lo < a && a <= hi) sh.q[0] = q;
+    if (lo < b && b <= hi) sh.q[1] = q;
+  }
+  __syncthreads();
+  *qa = sh.q[0];
+  *qb = sh.q[1];
+  __syncthreads();
+}
+template <int THREADS> __device__ uint32_t bin_of_count(Shared& sh, uint32_t k) {
+  for (int q = threadIdx.x; q < kBins; q += THREADS)
+    if (sh.e.cnt[q] < k && k <= sh.e.cnt[q + 1]) sh.q[0] = q;
+  __syncthreads();
+  const uint32_t q = sh.q[0];
+  __syncthreads();
+  return q;
+}
+
+// A row's settings, the inactive ones at k = 0, p = 1, least = 0.
+struct Settings {
+  uint32_t k;
+  float p, least, u;  // least: min-p's smallest weight
+};
+__device__ Settings settings_of(const SampleArgs& a, uint32_t row) {
+  Settings s;
+  const int32_t k = a.top_k ? a.top_k[row] : 0;
+  s.k = k > 0 ? (uint32_t)k : 0;
+  // The most likely token alone: of equal ones the first.
+  if (a.temperature && !(a.temperature[row] > 0.f)) s.k = 1;
+  const float p = a.top_p ? a.top_p[row] : 1.f;
+  s.p = p < 1.f ? fmaxf(p, 0.f) : 1.f;
+  const float m = a.min_p ? a.min_p[row] : 0.f;
+  const float least = m > 0.f ? rintf(fminf(m, 1.f) * kUnit) : 0.f;
+  s.least = least > 1.f ? least : 0.f;
+  const float u = a.u[row];
+  s.u = u > 0.f ? fminf(u, 1.f) : 0.f;
+  return s;
+}
+__device__ __forceinline__ bool cuts(const Settings& s, const Shared& sh) {
+  return s.k && s.k < sh.e.cnt[kBins];
+}
+__device__ __forceinline__ uint64_t part_of(uint64_t sum, float p) {
+  const uint64_t x = (uint64_t)((double)sum * (double)p);
+  return x > 1 ? x : 1;
+}
+__device__ __forceinline__ uint64_t target_of(uint64_t sum, float u) {
+  const uint64_t x = (uint64_t)((double)sum * (double)u);
+  return (x < sum ? x : sum - 1) + 1;
+}
+
+// The bins that may hold an answer.
+struct Ranges {
+  uint32_t lo[4], n[4];  // q from lo on, n bins
+  __device__ bool holds(uint32_t q) const {
+    return q - lo[0] < n[0] || q - lo[1] < n[1] || q - lo[2] < n[2] || q - lo[3] < n[3];
+  }
+};
+template <int THREADS> __device__ Ranges ranges_of(Shared& sh, const Settings& s) {
+  Ranges r{{0, 0, 0, 0}, {0, 0, 0, 0}};
+  uint64_t lo = sh.e.sum[kBins], hi = lo;  // what is kept so far sums to something in lo .. hi
+  if (cuts(s, sh)) {
+    const uint32_t q = bin_of_count<THREADS>(sh, s.k);
+    lo = sh.e.sum[q] + 1;
+    hi = sh.e.sum[q + 1];
+    r.lo[0] = q;
+    r.n[0] = 1;
+  }
+  if (s.p < 1.f) {
+    uint32_t qa, qb;
+    lo = part_of(lo, s.p);
+    bins_of_sums<THREADS>(sh, lo, part_of(hi, s.p), &qa, &qb);
+    hi = min(hi, sh.e.sum[qb + 1]);
+    r.lo[1] = qa;
+    r.n[1] = qb - qa + 1;
+  }
+  if (s.least != 0.f) {
+    const uint32_t q = kBins - 1 - bin_of(s.least);
+    if (sh.e.sum[q] < hi) {
+      r.lo[2] = q;
+      r.n[2] = 1;
+      hi = min(hi, sh.e.sum[q + 1]);
+      lo = max((uint64_t)1, min(lo, sh.e.sum[q]));
+    }
+  }
+  uint32_t qa, qb;
+  bins_of_sums<THREADS>(sh, target_of(lo, s.u), target_of(hi, s.u), &qa, &qb);
+  r.lo[3] = qa;
+  r.n[3] = qb - qa + 1;
+  return r;
+}
+
+// Sorts sh.list[0 .. n), larger keys first; n <= kList.
+__device__ void sort_list(Shared& sh, uint32_t n) {
+  uint32_t size = 64;
+  while (size < n) size <<= 1;
+  for (uint32_t i = n + threadIdx.x; i < size; i += kThreads) sh.list[i] = 0;
+  __syncthreads();
+  for (uint32_t k = 2; k <= size; k <<= 1)
+    for (uint32_t j = k >> 1; j; j >>= 1) {
+      for (uint32_t p = threadIdx.x; p < size / 2; p += kThreads) {
+        const uint32_t i = 2 * p - (p & (j - 1)), o = i + j;  // i without bit j
+        const uint64_t x = sh.list[i], y = sh.list[o];
+        if ((x < y) == ((i & k) == 0)) {
+          sh.list[i] = y;
+          sh.list[o] = x;
+        }
+      }
+      __syncthreads();
+    }
+}
+
+__device__ __forceinline__ uint32_t order_bin(uint64_t key) {
+  return kBins - 1 - (uint32_t)(key >> (kKeyBits - 12));
+}
+__device__ void answer(const SampleArgs& a, uint32_t row, uint64_t key, uint64_t kept) {
+  a.token[row] = (int32_t)key_id(key);
+  if (a.prob) a.prob[row] = (float)((double)(uint64_t)key_weight(key) / (double)kept);
+}
+
+// Answers the four questions from the edges and the collected bins' n elements,
+// sorted in sh.list.
+__device__ void resolve(const SampleArgs& a, uint32_t row, Shared& sh, const Settings& s, uint32_t n) {
+  constexpr int PER = kList / kThreads;
+  const int t = threadIdx.x, lane = t & 63, wave = t >> 6;
+  const uint32_t qm = s.least != 0.f ? kBins - 1 - bin_of(s.least) : 0;
+  const uint64_t total = sh.e.sum[kBins], edge_m = sh.e.sum[qm];
+  const bool k_cuts = cuts(s, sh);
+  // Running sums of the list.
+  uint64_t key[PER], w[PER], cum[PER], run = 0;
+  uint32_t cnt[PER];
+#pragma unroll
+  for (int i = 0; i < PER; ++i) {
+    const uint32_t at = t * PER + i;
+    key[i] = at < n ? sh.list[at] : 0;
+    w[i] = at < n ? (uint64_t)key_weight(key[i]) : 0;
+    run += w[i];
+    cum[i] = run;
+  }
+  uint64_t pre = run;
+#pragma unroll
+  for (int o = 1; o < 64; o <<= 1) {
+    const uint64_t x = __shfl_up(pre, o);
+    if (lane >= o) pre += x;
+  }
+  if (lane == 63) sh.red[wave] = pre;
+  __syncthreads();
+  pre -= run;
+  for (int i = 0; i < wave; ++i) pre += sh.red[i];
+  // Of the order: an element's bin's edge, plus what the list has of its bin up
+  // to it.  The first element of each bin makes the bin's edge relative to the list.
+#pragma unroll
+  for (int i = 0; i < PER; ++i) {
+    const uint32_t at = t * PER + i;
+    cum[i] += pre;
+    if (at < n) {
+      const uint32_t q = order_bin(key[i]);
+      if (at == 0 || q != order_bin(sh.list[at - 1])) {
+        sh.e.sum[q] -= cum[i] - w[i];
+        sh.e.cnt[q] -= at;
+      }
+    }
+  }
+  __syncthreads();
+#pragma unroll
+  for (int i = 0; i < PER; ++i) {
+    const uint32_t at = t * PER + i, q = order_bin(key[i]);
+    if (at < n) {
+      cum[i] += sh.e.sum[q];
+      cnt[i] = at + 1 + sh.e.cnt[q];
+    }
+  }
+  uint64_t kept = total, cut = 0;
+  // The element that `is` holds for: its key and running sum.
+  auto find = [&](auto is) {
+#pragma unroll
+    for (int i = 0; i < PER; ++i)
+      if ((uint32_t)(t * PER + i) < n && is(i)) {
+        sh.key = key[i];
+        sh.sum = cum[i];
+      }
+    __syncthreads();
+    cut = sh.key;
+    const uint64_t sum = sh.sum;
+    __syncthreads();
+    return sum;
+  };
+  if (k_cuts) kept = find([&](int i) { return cnt[i] == s.k; });
+  if (s.p < 1.f) {
+    const uint64_t part = part_of(kept, s.p);
+    kept = find([&](int i) { return cum[i] >= part && cum[i] - w[i] < part; });
+  }
+  const uint64_t key_m = s.least != 0.f ? (uint64_t)(__float_as_uint(s.least) - kOneBits) << kIdBits : 0;
+  if (key_m > cut) {  // through the last element of at least that weight
+    if (t == 0) sh.sum = edge_m;
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < PER; ++i)
+      if ((uint32_t)(t * PER + i) < n && order_bin(key[i]) == qm && key[i] >= key_m)
+        atomicMax((unsigned long long*)&sh.sum, (unsigned long long)cum[i]);
+    __syncthreads();
+    kept = sh.sum;
+    __syncthreads();
+  }
+  const uint64_t at = target_of(kept, s.u);
+  find([&](int i) { return cum[i] >= at && cum[i] - w[i] < at; });
+  if (t == 0) answer(a, row, cut, kept);
+}
+
+// Rows whose answers' bins hold more than kList elements (many equal or nearly
+// equal logits): the element at which the running count or sum reaches
+// `target`, twelve bits of the key at a time over the elements that share the
+// bits so far, each time over the whole row.  *sum: the sum through it.
 template <int DT>
-__device__ uint64_t reach(const SampleArgs& a, const char* x, const Row& r, Shared& sh,
+__device__ uint64_t reach(const char* x, uint32_t vocab, const Scale& r, Shared& sh,
                           uint64_t target, bool by_count, uint64_t* sum) {
-  uint64_t prefix = 0, base_w = 0;
-  int left = kKeyBits;
-  while (left > 0) {
+  uint64_t prefix = 0, base = 0;
+  for (int left = kKeyBits; left > 0;) {
     const int digit = left > 12 ? 12 : left, shift = left - digit;
+    __syncthreads();
     for (int b = threadIdx.x; b < kBins; b += kThreads) {
-      sh.cnt[b] = 0;
-      sh.sum[b] = 0;
+      sh.e.cnt[b] = 0;
+      sh.e.sum[b] = 0;
     }
     __syncthreads();
-    each<DT>(a, x, [&](float l, uint32_t id) {
+    each<DT>(x, vocab, threadIdx.x, kThreads, [&](float l, uint32_t id) {
       const float w = weight(r, l);
       if (w == 0.f) return;
       const uint64_t k = key_of(w, id);
       if (k >> left != prefix) return;
-      const uint32_t b = (uint32_t)(k >> shift) & ((1u << digit) - 1);
-      atomicAdd(&sh.cnt[b], 1u);
-      atomicAdd(&sh.sum[b], (unsigned long long)w);
+      const uint32_t q = kBins - 1 - ((uint32_t)(k >> shift) & ((1u << digit) - 1));
+      atomicAdd(&sh.e.cnt[q], 1u);
+      atomicAdd((unsigned long long*)&sh.e.sum[q], (unsigned long long)w);
     });
     __syncthreads();
-    find_bin(sh, target, by_count);
-    prefix = (prefix << digit) | sh.bin;
-    target -= by_count ? sh.before_c : sh.before_w;
-    base_w += sh.before_w;
-    left = shift;
-    if (left == 0) base_w += sh.in_w;
+    // Edges of these bins (a thread's four in turn), and the one that holds the target.
+    constexpr int PER = kBins / kThreads;
+    const int t = threadIdx.x, lane = t & 63, wave = t >> 6;
+    uint64_t w[PER], ws = 0;
+    uint32_t c[PER], cs = 0;
+#pragma unroll
+    for (int i = 0; i < PER; ++i) {
+      c[i] = sh.e.cnt[t * PER + i];
+      w[i] = sh.e.sum[t * PER + i];
+      cs += c[i];
+      ws += w[i];
+    }
+    uint64_t pc = cs, pw = ws;
+#pragma unroll
+    for (int o = 1; o < 64; o <<= 1) {
+      const uint64_t xc = __shfl_up(pc, o), xw = __shfl_up(pw, o);
+      if (lane >= o) {
+        pc += xc;
+        pw += xw;
+      }
+    }
+    if (lane == 63) {
+      sh.redc[wave] = (uint32_t)pc;
+      sh.red[wave] = pw;
+    }
     __syncthreads();
+    for (int i = 0; i < wave; ++i) {
+      pc += sh.redc[i];
+      pw += sh.red[i];
+    }
+    pc -= cs;
+    pw -= ws;
+#pragma unroll
+    for (int i = 0; i < PER; ++i) {
+      const uint64_t have = by_count ? pc : pw, get = by_count ? c[i] : w[i];
+      if (have < target && target <= have + get) {
+        sh.q[0] = t * PER + i;
+        sh.key = have;
+        sh.sum = base + pw + (shift == 0 ? w[i] : 0);
+      }
+      pc += c[i];
+      pw += w[i];
+    }
+    __syncthreads();
+    prefix = (prefix << digit) | ((kBins - 1 - sh.q[0]) & ((1u << digit) - 1));
+    target -= sh.key;
+    base = sh.sum;
+    left = shift;
   }
-  *sum = base_w;
+  *sum = base;
+  __syncthreads();
   return prefix;
 }
 
-template <int DT> __global__ __launch_bounds__(kThreads) void k_sample(SampleArgs a) {
+template <int DT>
+__device__ void resolve_long(const SampleArgs& a, uint32_t row, const Scale& r, Shared& sh,
+                             const Settings& s) {
+  const char* x = row_of<DT>(a, row);
+  uint64_t kept = sh.e.sum[kBins], cut = 0;
+  const bool k_cuts = cuts(s, sh);
+  if (k_cuts) cut = reach<DT>(x, a.vocab, r, sh, s.k, true, &kept);
+  if (s.p < 1.f) cut = reach<DT>(x, a.vocab, r, sh, part_of(kept, s.p), false, &kept);
+  if (s.least != 0.f && (uint64_t)(__float_as_uint(s.least) - kOneBits) << kIdBits > cut) {
+    uint64_t sum = 0;
+    each<DT>(x, a.vocab, threadIdx.x, kThreads, [&](float l, uint32_t) {
+      const float w = weight(r, l);
+      sum += w >= s.least ? (uint64_t)w : 0;
+    });
+    kept = block_add<uint64_t, kThreads>(sum, sh.red);
+  }
+  uint64_t through;
+  const uint64_t key = reach<DT>(x, a.vocab, r, sh, target_of(kept, s.u), false, &through);
+  if (threadIdx.x == 0) answer(a, row, key, kept);
+}
+
+// Collects the elements of the ranges' bins that this thread's logits hold:
+// f(key).  Logits surely below the last bin are passed over by a comparison
+// (a thousandth of slack; the bins of the others are exact).
+template <int DT, class F>
+__device__ __forceinline__ void collect(const char* x, uint32_t vocab, uint32_t from,
+                                        uint32_t threads, const Scale& r, const Ranges& g, F f) {
+  uint32_t last = 0;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) last = g.n[i] ? max(last, g.lo[i] + g.n[i] - 1) : last;
+  const float low = fmaxf((float)bin_low(kBins - 1 - last) - 1.f, 0.25f);
+  const float below = (__logf(low * (1.f / kUnit)) - 1e-3f) / r.inv_t;
+  const float least = r.top == INFINITY ? r.top : r.top + below * (1.f + 1e-3f) - fabsf(r.top) * 1e-6f;
+  each<DT>(x, vocab, from, threads, [&](float l, uint32_t id) {
+    if (!(l >= least)) return;
+    const float w = weight(r, l);
+    if (w != 0.f && g.holds(kBins - 1 - bin_of(w))) f(key_of(w, id));
+  });
+}
+
+__device__ void no_token(const SampleArgs& a, uint32_t row) {
+  a.token[row] = -1;
+  if (a.prob) a.prob[row] = 0.f;
+}
+
+// One block a row.
+template <int DT> __global__ __launch_bounds__(kThreads) void k_row(SampleArgs a) {
   __shared__ Shared sh;
   const uint32_t row = blockIdx.x;
-  const char* x = (const char*)a.logits + (size_t)row * a.ld * sizeof(typename Elem<DT>::T);
-  const float T = a.temperature ? a.temperature[row] : 1.f;
-  Row r;
-  r.greedy = !(T > 0.f);
-  r.inv_t = 1.f / T;
+  const char* x = row_of<DT>(a, row);
+  Scale r{-INFINITY, inverse_temperature(a, row)};
+  for (int b = threadIdx.x; b < kBins; b += kThreads) sh.e.sum[b] = 0;
+  if (threadIdx.x == 0) sh.n = 0;
   float top = -INFINITY;
-  each<DT>(a, x, [&](float l, uint32_t) { top = fmaxf(top, l); });
+  each<DT>(x, a.vocab, threadIdx.x, kThreads, [&](float l, uint32_t) { top = fmaxf(top, l); });
   r.top = block_max<float, kThreads>(top, (float*)sh.red);
   if (r.top == -INFINITY) {
-    if (threadIdx.x == 0) {
-      a.token[row] = -1;
-      if (a.prob) a.prob[row] = 0.f;
-    }
+    if (threadIdx.x == 0) no_token(a, row);
     return;
   }
-  uint64_t sum = 0, cnt = 0;
-  each<DT>(a, x, [&](float l, uint32_t) {
+  each<DT>(x, a.vocab, threadIdx.x, kThreads, [&](float l, uint32_t) {
     const float w = weight(r, l);
-    sum += (uint64_t)w;
-    cnt += w != 0.f;
+    if (w != 0.f) atomicAdd((unsigned long long*)&sh.e.sum[bin_of(w)], (unsigned long long)bin_entry(w));
   });
-  sum = block_add<unsigned long long, kThreads>(sum, sh.red);
-  cnt = block_add<unsigned long long, kThreads>(cnt, sh.red);
-  uint64_t cut = 0;  // the last key kept so far
-  const int32_t k = r.greedy ? 1 : a.top_k ? a.top_k[row] : 0;
-  if (k > 0 && (uint64_t)k < cnt) cut = reach<DT>(a, x, r, sh, (uint64_t)k, true, &sum);
-  const float p = a.top_p ? a.top_p[row] : 1.f;
-  if (p < 1.f) {
-    const uint64_t part = (uint64_t)((double)sum * (double)fmaxf(p, 0.f));
-    cut = reach<DT>(a, x, r, sh, part > 1 ? part : 1, false, &sum);
+  __syncthreads();
+  make_edges<kThreads>(sh, nullptr);
+  const Settings s = settings_of(a, row);
+  const Ranges g = ranges_of<kThreads>(sh, s);
+  collect<DT>(x, a.vocab, threadIdx.x, kThreads, r, g, [&](uint64_t key) {
+    const uint32_t at = atomicAdd(&sh.n, 1u);
+    if (at < kList) sh.list[at] = key;
+  });
+  __syncthreads();
+  const uint32_t n = sh.n;
+  if (n <= kList) {
+    sort_list(sh, n);
+    resolve(a, row, sh, s, n);
+  } else {
+    resolve_long<DT>(a, row, r, sh, s);
   }
-  const float mp = a.min_p ? a.min_p[row] : 0.f;
-  const float least = mp > 0.f ? rintf(fminf(mp, 1.f) * kUnit) : 0.f;
-  if (least > 1.f && (((uint64_t)(__float_as_uint(least) - kOneBits)) << kIdBits) > cut) {
-    cut = (uint64_t)(__float_as_uint(least) - kOneBits) << kIdBits;
-    uint64_t s = 0;
-    each<DT>(a, x, [&](float l, uint32_t) {
-      const float w = weight(r, l);
-      s += w >= least ? (uint64_t)w : 0;
-    });
-    sum = block_add<unsigned long long, kThreads>(s, sh.red);
-  }
-  const float u = a.u[row];
-  uint64_t at = (uint64_t)((double)sum * (double)(u > 0.f ? fminf(u, 1.f) : 0.f));
-  at = at < sum ? at : sum - 1;
-  uint64_t through;
-  const uint64_t got = reach<DT>(a, x, r, sh, at + 1, false, &through);
+}
+
+// Few rows: a row's passes are split over `parts` blocks each (a launch a pass:
+// the kernel's end is the barrier), and a block a row finishes.
+constexpr int kPartThreads = 256;
+constexpr uint32_t kMaxParts = 64;
+struct Part {  // a row's workspace
+  unsigned long long hist[kBins];
+  unsigned long long list[kList];
+  float top[kMaxParts];
+  uint32_t n, pad[3];
+};
+
+template <int DT> __global__ __launch_bounds__(kPartThreads) void k_part_max(SampleArgs a, uint32_t parts) {
+  __shared__ float red[kPartThreads / 64];
+  const uint32_t row = blockIdx.y, part = blockIdx.x;
+  Part& p = ((Part*)a.space)[row];
+  for (uint32_t b = part * kPartThreads + threadIdx.x; b < kBins; b += parts * kPartThreads) p.hist[b] = 0;
+  float top = -INFINITY;
+  each<DT>(row_of<DT>(a, row), a.vocab, part * kPartThreads + threadIdx.x, parts * kPartThreads,
+           [&](float l, uint32_t) { top = fmaxf(top, l); });
+  top = block_max<float, kPartThreads>(top, red);
   if (threadIdx.x == 0) {
-    a.token[row] = (int32_t)key_id(got);
-    if (a.prob) a.prob[row] = (float)((double)key_weight(got) / (double)sum);
+    p.top[part] = top;
+    if (part == 0) p.n = 0;
   }
+}
+__device__ __forceinline__ float top_of(const Part& p, uint32_t parts) {
+  const uint32_t lane = threadIdx.x & 63;
+  return wave_max(lane < parts ? p.top[lane] : -INFINITY);
+}
+
+template <int DT> __global__ __launch_bounds__(kPartThreads) void k_part_hist(SampleArgs a, uint32_t parts) {
+  __shared__ unsigned long long hist[kBins];
+  const uint32_t row = blockIdx.y, part = blockIdx.x;
+  Part& p = ((Part*)a.space)[row];
+  const Scale r{top_of(p, parts), inverse_temperature(a, row)};
+  if (r.top == -INFINITY) return;
+  for (int b = threadIdx.x; b < kBins; b += kPartThreads) hist[b] = 0;
+  __syncthreads();
+  each<DT>(row_of<DT>(a, row), a.vocab, part * kPartThreads + threadIdx.x, parts * kPartThreads,
+           [&](float l, uint32_t) {
+             const float w = weight(r, l);
+             if (w != 0.f) atomicAdd(&hist[bin_of(w)], (unsigned long long)bin_entry(w));
+           });
+  __syncthreads();
+  for (int b = threadIdx.x; b < kBins; b += kPartThreads)
+    if (hist[b]) atomicAdd(&p.hist[b], hist[b]);
+}
+
+template <int DT> __global__ __launch_bounds__(kPartThreads) void k_part_collect(SampleArgs a, uint32_t parts) {
+  __shared__ Shared sh;
+  __shared__ uint32_t base;
+  const uint32_t row = blockIdx.y, part = blockIdx.x;
+  Part& p = ((Part*)a.space)[row];
+  const Scale r{top_of(p, parts), inverse_temperature(a, row)};
+  if (r.top == -INFINITY) return;
+  if (threadIdx.x == 0) sh.n = 0;
+  make_edges<kPartThreads>(sh, p.hist);
+  const Ranges g = ranges_of<kPartThreads>(sh, settings_of(a, row));
+  collect<DT>(row_of<DT>(a, row), a.vocab, part * kPartThreads + threadIdx.x, parts * kPartThreads, r, g,
+              [&](uint64_t key) {
+                const uint32_t at = atomicAdd(&sh.n, 1u);
+                if (at < kList) sh.list[at] = key;
+              });
+  __syncthreads();
+  const uint32_t n = sh.n;
+  if (n == 0) return;
+  // Their number counts even where the list is full: it then exceeds kList.
+  if (threadIdx.x == 0) base = atomicAdd(&p.n, n);
+  __syncthreads();
+  for (uint32_t i = threadIdx.x; i < min(n, kList) && base + i < kList; i += kPartThreads)
+    p.list[base + i] = sh.list[i];
+}
+
+template <int DT> __global__ __launch_bounds__(kThreads) void k_part_finish(SampleArgs a, uint32_t parts) {
+  __shared__ Shared sh;
+  const uint32_t row = blockIdx.x;
+  const Part& p = ((const Part*)a.space)[row];
+  const Scale r{top_of(p, parts), inverse_temperature(a, row)};
+  if (r.top == -INFINITY) {
+    if (threadIdx.x == 0) no_token(a, row);
+    return;
+  }
+  const uint32_t n = p.n;
+  make_edges<kThreads>(sh, p.hist);
+  const Settings s = settings_of(a, row);
+  if (n <= kList) {
+    for (uint32_t i = threadIdx.x; i < n; i += kThreads) sh.list[i] = p.list[i];
+    sort_list(sh, n);
+    resolve(a, row, sh, s, n);
+  } else {
+    resolve_long<DT>(a, row, r, sh, s);
+  }
+}
+
+// Blocks a row: about 512 in all, of at least 2048 logits each.
+uint32_t parts_of(int64_t rows, int32_t vocab) {
+  if (rows >= 128) return 1;
+  const uint32_t most = std::min<uint32_t>(kMaxParts, ((uint32_t)vocab + 2047) / 2048);
+  return std::max(1u, std::min(most, (512 + (uint32_t)rows - 1) / (uint32_t)rows));
+}
+
+template <int DT> hipError_t launch(const SampleArgs& a, hipStream_t s) {
+  const uint32_t parts = parts_of(a.rows, (int32_t)a.vocab);
+  if (parts == 1) {
+    k_row<DT><<<dim3(a.rows), dim3(kThreads), 0, s>>>(a);
+    return hipGetLastError();
+  }
+  const dim3 grid(parts, a.rows), block(kPartThreads);
+  k_part_max<DT><<<grid, block, 0, s>>>(a, parts);
+  k_part_hist<DT><<<grid, block, 0, s>>>(a, parts);
+  k_part_collect<DT><<<grid, block, 0, s>>>(a, parts);
+  k_part_finish<DT><<<dim3(a.rows), dim3(kThreads), 0, s>>>(a, parts);
+  return hipGetLastError();
 }
 
 }  // namespace
 
-int64_t sample_space(int64_t, int32_t) { return 0; }
+int64_t sample_space(int64_t rows, int32_t vocab) {
+  return rows == 0 || parts_of(rows, vocab) == 1 ? 0 : rows * (int64_t)sizeof(Part);
+}
 
 hipError_t launch_sample(const SampleArgs& a, int dtype, hipStream_t s) {
-  if (dtype == TFE_F32)
-    k_sample<TFE_F32><<<dim3(a.rows), dim3(kThreads), 0, s>>>(a);
-  else
-    k_sample<TFE_BF16><<<dim3(a.rows), dim3(kThreads), 0, s>>>(a);
-  return hipGetLastError();
+  return dtype == TFE_F32 ? launch<TFE_F32>(a, s) : launch<TFE_BF16>(a, s);
 }
 
 }  // namespace tfe
