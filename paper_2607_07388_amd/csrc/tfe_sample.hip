@@ -124,20 +124,19 @@ template <int DT> __device__ __forceinline__ const char* row_of(const SampleArgs
   return (const char*)a.logits + (size_t)row * a.ld * sizeof(typename Elem<DT>::T);
 }
 
-constexpr int kThreads = 1024;  // of the kernels with one block a row
-constexpr uint32_t kList = 2048;  // collected elements that are sorted in LDS
-
 // Running counts and sums before each bin, bins in the order's direction
 // (q = 4095 - bin), and in all at q = 4096.
 struct Edges {
   uint64_t sum[kBins + 1];
   uint32_t cnt[kBins + 1];
 };
-struct Shared {
+template <int THREADS_, uint32_t LIST_> struct Shared {
+  static constexpr int THREADS = THREADS_;
+  static constexpr uint32_t LIST = LIST_;  // collected elements that are sorted in LDS
   Edges e;
-  uint64_t list[kList];
-  uint64_t red[kThreads / 64];
-  uint32_t redc[kThreads / 64];
+  uint64_t list[LIST];
+  uint64_t red[THREADS / 64];
+  uint32_t redc[THREADS / 64];
   uint32_t n;
   // Answers of a search.
   uint32_t q[2];
@@ -145,8 +144,8 @@ struct Shared {
 };
 
 // Edges from the histogram in sh.e.sum (in place) or in memory.
-template <int THREADS> __device__ void make_edges(Shared& sh, const unsigned long long* hist) {
-  constexpr int PER = kBins / THREADS;
+template <class S> __device__ void make_edges(S& sh, unsigned long long* hist) {
+  constexpr int THREADS = S::THREADS, PER = kBins / THREADS;
   const int t = threadIdx.x, lane = t & 63, wave = t >> 6;
   uint32_t c[PER];
   uint64_t w[PER], ws = 0;
@@ -154,7 +153,9 @@ template <int THREADS> __device__ void make_edges(Shared& sh, const unsigned lon
 #pragma unroll
   for (int i = 0; i < PER; ++i) {
     const uint32_t b = kBins - 1 - (t * PER + i);
-    const uint64_t x = hist ? hist[b] : sh.e.sum[b];
+    // Other blocks of the launch may have added to it: device scope.
+    const uint64_t x = hist ? __hip_atomic_load(hist + b, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT)
+                            : sh.e.sum[b];
     c[i] = entry_count(x);
     w[i] = entry_sum(x, b);
     cs += c[i];
@@ -198,9 +199,9 @@ template <int THREADS> __device__ void make_edges(Shared& sh, const unsigned lon
 
 // The bins in which the running sum reaches a and b (at least 1, at most the
 // total; a <= b).
-template <int THREADS>
-__device__ void bins_of_sums(Shared& sh, uint64_t a, uint64_t b, uint32_t* qa, uint32_t* qb) {
-  for (int q = threadIdx.x; q < kBins; q += THREADS) {
+template <class S>
+__device__ void bins_of_sums(S& sh, uint64_t a, uint64_t b, uint32_t* qa, uint32_t* qb) {
+  for (int q = threadIdx.x; q < kBins; q += S::THREADS) {
     const uint64_t lo = sh.e.sum[q], hi = sh.e.sum[q + 1];
     if (lo < a && a <= hi) sh.q[0] = q;
     if (lo < b && b <= hi) sh.q[1] = q;
@@ -210,8 +211,8 @@ __device__ void bins_of_sums(Shared& sh, uint64_t a, uint64_t b, uint32_t* qa, u
   *qb = sh.q[1];
   __syncthreads();
 }
-template <int THREADS> __device__ uint32_t bin_of_count(Shared& sh, uint32_t k) {
-  for (int q = threadIdx.x; q < kBins; q += THREADS)
+template <class S> __device__ uint32_t bin_of_count(S& sh, uint32_t k) {
+  for (int q = threadIdx.x; q < kBins; q += S::THREADS)
     if (sh.e.cnt[q] < k && k <= sh.e.cnt[q + 1]) sh.q[0] = q;
   __syncthreads();
   const uint32_t q = sh.q[0];
@@ -239,7 +240,7 @@ __device__ Settings settings_of(const SampleArgs& a, uint32_t row) {
   s.u = u > 0.f ? fminf(u, 1.f) : 0.f;
   return s;
 }
-__device__ __forceinline__ bool cuts(const Settings& s, const Shared& sh) {
+template <class S> __device__ __forceinline__ bool cuts(const Settings& s, const S& sh) {
   return s.k && s.k < sh.e.cnt[kBins];
 }
 __device__ __forceinline__ uint64_t part_of(uint64_t sum, float p) {
@@ -258,11 +259,11 @@ struct Ranges {
     return q - lo[0] < n[0] || q - lo[1] < n[1] || q - lo[2] < n[2] || q - lo[3] < n[3];
   }
 };
-template <int THREADS> __device__ Ranges ranges_of(Shared& sh, const Settings& s) {
+template <class S> __device__ Ranges ranges_of(S& sh, const Settings& s) {
   Ranges r{{0, 0, 0, 0}, {0, 0, 0, 0}};
   uint64_t lo = sh.e.sum[kBins], hi = lo;  // what is kept so far sums to something in lo .. hi
   if (cuts(s, sh)) {
-    const uint32_t q = bin_of_count<THREADS>(sh, s.k);
+    const uint32_t q = bin_of_count(sh, s.k);
     lo = sh.e.sum[q] + 1;
     hi = sh.e.sum[q + 1];
     r.lo[0] = q;
@@ -271,7 +272,7 @@ template <int THREADS> __device__ Ranges ranges_of(Shared& sh, const Settings& s
   if (s.p < 1.f) {
     uint32_t qa, qb;
     lo = part_of(lo, s.p);
-    bins_of_sums<THREADS>(sh, lo, part_of(hi, s.p), &qa, &qb);
+    bins_of_sums(sh, lo, part_of(hi, s.p), &qa, &qb);
     hi = min(hi, sh.e.sum[qb + 1]);
     r.lo[1] = qa;
     r.n[1] = qb - qa + 1;
@@ -286,14 +287,15 @@ template <int THREADS> __device__ Ranges ranges_of(Shared& sh, const Settings& s
     }
   }
   uint32_t qa, qb;
-  bins_of_sums<THREADS>(sh, target_of(lo, s.u), target_of(hi, s.u), &qa, &qb);
+  bins_of_sums(sh, target_of(lo, s.u), target_of(hi, s.u), &qa, &qb);
   r.lo[3] = qa;
   r.n[3] = qb - qa + 1;
   return r;
 }
 
-// Sorts sh.list[0 .. n), larger keys first; n <= kList.
-__device__ void sort_list(Shared& sh, uint32_t n) {
+// Sorts sh.list[0 .. n), larger keys first; n <= LIST.
+template <class S> __device__ void sort_list(S& sh, uint32_t n) {
+  constexpr int kThreads = S::THREADS;
   uint32_t size = 64;
   while (size < n) size <<= 1;
   for (uint32_t i = n + threadIdx.x; i < size; i += kThreads) sh.list[i] = 0;
@@ -322,8 +324,9 @@ __device__ void answer(const SampleArgs& a, uint32_t row, uint64_t key, uint64_t
 
 // Answers the four questions from the edges and the collected bins' n elements,
 // sorted in sh.list.
-__device__ void resolve(const SampleArgs& a, uint32_t row, Shared& sh, const Settings& s, uint32_t n) {
-  constexpr int PER = kList / kThreads;
+template <class S>
+__device__ void resolve(const SampleArgs& a, uint32_t row, S& sh, const Settings& s, uint32_t n) {
+  constexpr int PER = S::LIST / S::THREADS;
   const int t = threadIdx.x, lane = t & 63, wave = t >> 6;
   const uint32_t qm = s.least != 0.f ? kBins - 1 - bin_of(s.least) : 0;
   const uint64_t total = sh.e.sum[kBins], edge_m = sh.e.sum[qm];
@@ -409,13 +412,14 @@ __device__ void resolve(const SampleArgs& a, uint32_t row, Shared& sh, const Set
   if (t == 0) answer(a, row, cut, kept);
 }
 
-// Rows whose answers' bins hold more than kList elements (many equal or nearly
+// Rows whose answers' bins hold more than LIST elements (many equal or nearly
 // equal logits): the element at which the running count or sum reaches
 // `target`, twelve bits of the key at a time over the elements that share the
 // bits so far, each time over the whole row.  *sum: the sum through it.
-template <int DT>
-__device__ uint64_t reach(const char* x, uint32_t vocab, const Scale& r, Shared& sh,
+template <int DT, class S>
+__device__ uint64_t reach(const char* x, uint32_t vocab, const Scale& r, S& sh,
                           uint64_t target, bool by_count, uint64_t* sum) {
+  constexpr int kThreads = S::THREADS;
   uint64_t prefix = 0, base = 0;
   for (int left = kKeyBits; left > 0;) {
     const int digit = left > 12 ? 12 : left, shift = left - digit;
@@ -489,9 +493,10 @@ __device__ uint64_t reach(const char* x, uint32_t vocab, const Scale& r, Shared&
   return prefix;
 }
 
-template <int DT>
-__device__ void resolve_long(const SampleArgs& a, uint32_t row, const Scale& r, Shared& sh,
+template <int DT, class S>
+__device__ void resolve_long(const SampleArgs& a, uint32_t row, const Scale& r, S& sh,
                              const Settings& s) {
+  constexpr int kThreads = S::THREADS;
   const char* x = row_of<DT>(a, row);
   uint64_t kept = sh.e.sum[kBins], cut = 0;
   const bool k_cuts = cuts(s, sh);
@@ -535,8 +540,9 @@ __device__ void no_token(const SampleArgs& a, uint32_t row) {
 }
 
 // One block a row.
-template <int DT> __global__ __launch_bounds__(kThreads) void k_row(SampleArgs a) {
-  __shared__ Shared sh;
+template <int DT, int kThreads, uint32_t LIST>
+__global__ __launch_bounds__(kThreads, 4) void k_row(SampleArgs a) {
+  __shared__ Shared<kThreads, LIST> sh;
   const uint32_t row = blockIdx.x;
   const char* x = row_of<DT>(a, row);
   Scale r{-INFINITY, inverse_temperature(a, row)};
@@ -554,16 +560,16 @@ template <int DT> __global__ __launch_bounds__(kThreads) void k_row(SampleArgs a
     if (w != 0.f) atomicAdd((unsigned long long*)&sh.e.sum[bin_of(w)], (unsigned long long)bin_entry(w));
   });
   __syncthreads();
-  make_edges<kThreads>(sh, nullptr);
+  make_edges(sh, nullptr);
   const Settings s = settings_of(a, row);
-  const Ranges g = ranges_of<kThreads>(sh, s);
+  const Ranges g = ranges_of(sh, s);
   collect<DT>(x, a.vocab, threadIdx.x, kThreads, r, g, [&](uint64_t key) {
     const uint32_t at = atomicAdd(&sh.n, 1u);
-    if (at < kList) sh.list[at] = key;
+    if (at < LIST) sh.list[at] = key;
   });
   __syncthreads();
   const uint32_t n = sh.n;
-  if (n <= kList) {
+  if (n <= LIST) {
     sort_list(sh, n);
     resolve(a, row, sh, s, n);
   } else {
@@ -573,27 +579,30 @@ template <int DT> __global__ __launch_bounds__(kThreads) void k_row(SampleArgs a
 
 // Few rows: a row's passes are split over `parts` blocks each (a launch a pass:
 // the kernel's end is the barrier), and a block a row finishes.
-constexpr int kPartThreads = 256;
 constexpr uint32_t kMaxParts = 64;
+constexpr uint32_t kList = 8192, kPartList = 2048;
+constexpr int kMaxThreads = 256, kHistThreads = 512, kCollectThreads = 256, kFinishThreads = 1024;
 struct Part {  // a row's workspace
   unsigned long long hist[kBins];
   unsigned long long list[kList];
   float top[kMaxParts];
-  uint32_t n, pad[3];
+  Ranges ranges;
+  uint32_t n, done, pad[2];
 };
 
-template <int DT> __global__ __launch_bounds__(kPartThreads) void k_part_max(SampleArgs a, uint32_t parts) {
-  __shared__ float red[kPartThreads / 64];
+template <int DT>
+__global__ __launch_bounds__(kMaxThreads) void k_part_max(SampleArgs a, uint32_t parts) {
+  __shared__ float red[kMaxThreads / 64];
   const uint32_t row = blockIdx.y, part = blockIdx.x;
   Part& p = ((Part*)a.space)[row];
-  for (uint32_t b = part * kPartThreads + threadIdx.x; b < kBins; b += parts * kPartThreads) p.hist[b] = 0;
+  for (uint32_t b = part * kMaxThreads + threadIdx.x; b < kBins; b += parts * kMaxThreads) p.hist[b] = 0;
   float top = -INFINITY;
-  each<DT>(row_of<DT>(a, row), a.vocab, part * kPartThreads + threadIdx.x, parts * kPartThreads,
+  each<DT>(row_of<DT>(a, row), a.vocab, part * kMaxThreads + threadIdx.x, parts * kMaxThreads,
            [&](float l, uint32_t) { top = fmaxf(top, l); });
-  top = block_max<float, kPartThreads>(top, red);
+  top = block_max<float, kMaxThreads>(top, red);
   if (threadIdx.x == 0) {
     p.top[part] = top;
-    if (part == 0) p.n = 0;
+    if (part == 0) p.n = p.done = 0;
   }
 }
 __device__ __forceinline__ float top_of(const Part& p, uint32_t parts) {
@@ -601,66 +610,85 @@ __device__ __forceinline__ float top_of(const Part& p, uint32_t parts) {
   return wave_max(lane < parts ? p.top[lane] : -INFINITY);
 }
 
-template <int DT> __global__ __launch_bounds__(kPartThreads) void k_part_hist(SampleArgs a, uint32_t parts) {
-  __shared__ unsigned long long hist[kBins];
+template <int DT>
+__global__ __launch_bounds__(kHistThreads) void k_part_hist(SampleArgs a, uint32_t parts) {
+  __shared__ Shared<kHistThreads, 1> sh;
   const uint32_t row = blockIdx.y, part = blockIdx.x;
   Part& p = ((Part*)a.space)[row];
   const Scale r{top_of(p, parts), inverse_temperature(a, row)};
   if (r.top == -INFINITY) return;
-  for (int b = threadIdx.x; b < kBins; b += kPartThreads) hist[b] = 0;
+  for (int b = threadIdx.x; b < kBins; b += kHistThreads) sh.e.sum[b] = 0;
   __syncthreads();
-  each<DT>(row_of<DT>(a, row), a.vocab, part * kPartThreads + threadIdx.x, parts * kPartThreads,
+  each<DT>(row_of<DT>(a, row), a.vocab, part * kHistThreads + threadIdx.x, parts * kHistThreads,
            [&](float l, uint32_t) {
              const float w = weight(r, l);
-             if (w != 0.f) atomicAdd(&hist[bin_of(w)], (unsigned long long)bin_entry(w));
+             if (w != 0.f)
+               atomicAdd((unsigned long long*)&sh.e.sum[bin_of(w)], (unsigned long long)bin_entry(w));
            });
   __syncthreads();
-  for (int b = threadIdx.x; b < kBins; b += kPartThreads)
-    if (hist[b]) atomicAdd(&p.hist[b], hist[b]);
+  for (int b = threadIdx.x; b < kBins; b += kHistThreads)
+    if (sh.e.sum[b])
+      __hip_atomic_fetch_add(&p.hist[b], sh.e.sum[b], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+  // The last block to get here has the row's whole histogram: it finds the bins.
+  // What blocks tell each other goes through device-scope atomics alone, and a
+  // block counts itself in once its own are done: no fence (writing the L2s
+  // back for one took 100 us at 64 rows).
+  asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+  __syncthreads();
+  if (threadIdx.x == 0)
+    sh.n = __hip_atomic_fetch_add(&p.done, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+  __syncthreads();
+  if (sh.n != parts - 1) return;
+  make_edges(sh, p.hist);
+  const Ranges g = ranges_of(sh, settings_of(a, row));
+  if (threadIdx.x == 0) p.ranges = g;
 }
 
-template <int DT> __global__ __launch_bounds__(kPartThreads) void k_part_collect(SampleArgs a, uint32_t parts) {
-  __shared__ Shared sh;
-  __shared__ uint32_t base;
+template <int DT>
+__global__ __launch_bounds__(kCollectThreads) void k_part_collect(SampleArgs a, uint32_t parts) {
+  __shared__ uint64_t list[kPartList];
+  __shared__ uint32_t count, base;
   const uint32_t row = blockIdx.y, part = blockIdx.x;
   Part& p = ((Part*)a.space)[row];
   const Scale r{top_of(p, parts), inverse_temperature(a, row)};
   if (r.top == -INFINITY) return;
-  if (threadIdx.x == 0) sh.n = 0;
-  make_edges<kPartThreads>(sh, p.hist);
-  const Ranges g = ranges_of<kPartThreads>(sh, settings_of(a, row));
-  collect<DT>(row_of<DT>(a, row), a.vocab, part * kPartThreads + threadIdx.x, parts * kPartThreads, r, g,
-              [&](uint64_t key) {
-                const uint32_t at = atomicAdd(&sh.n, 1u);
-                if (at < kList) sh.list[at] = key;
+  if (threadIdx.x == 0) count = 0;
+  __syncthreads();
+  const Ranges g = p.ranges;
+  collect<DT>(row_of<DT>(a, row), a.vocab, part * kCollectThreads + threadIdx.x,
+              parts * kCollectThreads, r, g, [&](uint64_t key) {
+                const uint32_t at = atomicAdd(&count, 1u);
+                if (at < kPartList) list[at] = key;
               });
   __syncthreads();
-  const uint32_t n = sh.n;
+  const uint32_t n = count;
   if (n == 0) return;
-  // Their number counts even where the list is full: it then exceeds kList.
-  if (threadIdx.x == 0) base = atomicAdd(&p.n, n);
+  // More than a list holds: the row's number is to exceed kList.
+  if (threadIdx.x == 0) base = atomicAdd(&p.n, n <= kPartList ? n : kList + 1);
   __syncthreads();
-  for (uint32_t i = threadIdx.x; i < min(n, kList) && base + i < kList; i += kPartThreads)
-    p.list[base + i] = sh.list[i];
+  for (uint32_t i = threadIdx.x; i < min(n, kPartList) && base + i < kList; i += kCollectThreads)
+    p.list[base + i] = list[i];
 }
 
-template <int DT> __global__ __launch_bounds__(kThreads) void k_part_finish(SampleArgs a, uint32_t parts) {
-  __shared__ Shared sh;
+template <int DT>
+__global__ __launch_bounds__(kFinishThreads) void k_part_finish(SampleArgs a, uint32_t parts) {
+  __shared__ Shared<kFinishThreads, kList> sh;
   const uint32_t row = blockIdx.x;
-  const Part& p = ((const Part*)a.space)[row];
+  Part& p = ((Part*)a.space)[row];
   const Scale r{top_of(p, parts), inverse_temperature(a, row)};
   if (r.top == -INFINITY) {
     if (threadIdx.x == 0) no_token(a, row);
     return;
   }
   const uint32_t n = p.n;
-  make_edges<kThreads>(sh, p.hist);
   const Settings s = settings_of(a, row);
   if (n <= kList) {
-    for (uint32_t i = threadIdx.x; i < n; i += kThreads) sh.list[i] = p.list[i];
+    for (uint32_t i = threadIdx.x; i < n; i += kFinishThreads) sh.list[i] = p.list[i];
+    make_edges(sh, p.hist);
     sort_list(sh, n);
     resolve(a, row, sh, s, n);
   } else {
+    make_edges(sh, p.hist);
     resolve_long<DT>(a, row, r, sh, s);
   }
 }
@@ -675,14 +703,18 @@ uint32_t parts_of(int64_t rows, int32_t vocab) {
 template <int DT> hipError_t launch(const SampleArgs& a, hipStream_t s) {
   const uint32_t parts = parts_of(a.rows, (int32_t)a.vocab);
   if (parts == 1) {
-    k_row<DT><<<dim3(a.rows), dim3(kThreads), 0, s>>>(a);
+    // A short row's block leaves room for another on its compute unit.
+    if (a.vocab <= 65536)
+      k_row<DT, 512, 2048><<<dim3(a.rows), dim3(512), 0, s>>>(a);
+    else
+      k_row<DT, 1024, 8192><<<dim3(a.rows), dim3(1024), 0, s>>>(a);
     return hipGetLastError();
   }
-  const dim3 grid(parts, a.rows), block(kPartThreads);
-  k_part_max<DT><<<grid, block, 0, s>>>(a, parts);
-  k_part_hist<DT><<<grid, block, 0, s>>>(a, parts);
-  k_part_collect<DT><<<grid, block, 0, s>>>(a, parts);
-  k_part_finish<DT><<<dim3(a.rows), dim3(kThreads), 0, s>>>(a, parts);
+  const dim3 grid(parts, a.rows);
+  k_part_max<DT><<<grid, dim3(kMaxThreads), 0, s>>>(a, parts);
+  k_part_hist<DT><<<grid, dim3(kHistThreads), 0, s>>>(a, parts);
+  k_part_collect<DT><<<grid, dim3(kCollectThreads), 0, s>>>(a, parts);
+  k_part_finish<DT><<<dim3(a.rows), dim3(kFinishThreads), 0, s>>>(a, parts);
   return hipGetLastError();
 }
 
