@@ -5,9 +5,17 @@
 //   loss = tau^2 sum_k q_k (log q_k - s_k / tau + lse)
 //   d loss / d s_v = tau (p_v - q_v),    p_v = exp(s_v / tau - lse)
 // Bound by the logits' bytes: the loss reads them, the gradient reads and
-// writes them.
+// writes them, and both together read and write them once.
+//
+// A row is split into parts of up to 2048 16-byte vectors, each a block of 256
+// threads with eight vectors a thread in registers: many small blocks keep more
+// of memory's latency hidden than few large ones (512 rows of 151936 bfloat16,
+// loss alone: 33 us; one block of 1024 threads a row, the next row loaded while
+// one is worked on: 41).
 #include <hip/hip_runtime.h>
 #include <stdint.h>
+
+#include <algorithm>
 
 #include "tfe_logits.h"
 #include "tfe_rows.h"
@@ -17,14 +25,14 @@ namespace {
 
 using namespace rows;
 
-constexpr int kThreads = 1024;
 constexpr float kLog2e = 1.44269504088896340736f;
 constexpr float kLn2 = 0.69314718055994530942f;
 
 __device__ __forceinline__ float exp2_hw(float x) { return __builtin_amdgcn_exp2f(x); }
+__device__ __forceinline__ float log2_hw(float x) { return __builtin_amdgcn_logf(x); }
 
-// Running maximum m and sum s of exp((x - m) c / log2 e).  While every element
-// was -infinity, m stays -infinity and s 0.
+// Maximum m and sum s of exp((x - m) / tau) of some logits.  While every one of
+// them was -infinity, m is -infinity and s 0.  c = log2(e) / tau.
 struct Running {
   float m, s;
 };
@@ -36,174 +44,417 @@ __device__ __forceinline__ Running join(Running a, Running b, float c) {
   r.s = a.s * exp2_hw((a.m - ref) * c) + b.s * exp2_hw((b.m - ref) * c);
   return r;
 }
+__device__ __forceinline__ float lse_of(const DistillArgs& a, Running r) {
+  return fmaf(r.m, a.inv_tau, log2_hw(r.s) * kLn2);
+}
+// One vector's logits into r.
+template <int DT> __device__ __forceinline__ void add(Running& r, u32x4 q, float c) {
+  constexpr int N = Elem<DT>::N;
+  float x[N];
+  unpack<DT>(q, x);
+  float m = r.m;
+#pragma unroll
+  for (int i = 0; i < N; ++i) m = fmaxf(m, x[i]);
+  const float ref = finite_max(m);
+  float s = r.s * exp2_hw((r.m - ref) * c);
+#pragma unroll
+  for (int i = 0; i < N; ++i) s += exp2_hw((x[i] - ref) * c);
+  r = Running{m, s};
+}
+__device__ __forceinline__ void add1(Running& r, float x, float c) {
+  r = join(r, Running{x, x == -INFINITY ? 0.f : (x == x ? 1.f : x)}, c);
+}
 
-struct Shared {
-  float q[kDistillMaxK];
-  int32_t id[kDistillMaxK];
-  float red[kThreads / 64], red2[kThreads / 64];
-};
+// The gradient's main part f p for one vector (f = upstream gradient x tau).
+template <int DT>
+__device__ __forceinline__ u32x4 scaled_softmax(const DistillArgs& a, u32x4 q, float lse, float f) {
+  constexpr int N = Elem<DT>::N;
+  float x[N];
+  unpack<DT>(q, x);
+#pragma unroll
+  for (int i = 0; i < N; ++i) x[i] = f * exp2_hw(fmaf(x[i], a.inv_tau, -lse) * kLog2e);
+  return pack<DT>(x);
+}
+__device__ __forceinline__ float scaled_softmax1(const DistillArgs& a, float x, float lse, float f) {
+  return f * exp2_hw(fmaf(x, a.inv_tau, -lse) * kLog2e);
+}
 
-// The teacher's row: thread k < K gets its entry's log q and q, all of them
-// in sh.  Padding has q = 0 and id -1; so has every entry of an empty row.
+// Entry k < K of a row is thread k's: its token (-1: padding), the teacher's and
+// the student's logit over tau (-infinity for padding).
 struct Entry {
   int32_t id;
-  float q, logq;
+  float t, s;
 };
-template <int TDT> __device__ Entry teacher_row(const DistillArgs& a, uint32_t row, Shared& sh) {
-  const uint32_t k = threadIdx.x;
-  const size_t at = (size_t)row * a.K + k;
-  Entry e{-1, 0.f, 0.f};
-  float t = -INFINITY;
-  if (k < a.K) {
-    e.id = a.ids[at];
-    if (e.id < 0 || (uint32_t)e.id >= a.vocab) e.id = -1;
-    if (e.id >= 0) t = load1<TDT>(a.teacher, at) * a.inv_tau;
+template <int DT, int TDT>
+__device__ __forceinline__ Entry entry_of(const DistillArgs& a, uint32_t row, const char* x) {
+  Entry e{-1, -INFINITY, 0.f};
+  if (threadIdx.x >= a.K) return e;
+  const size_t at = (size_t)row * a.K + threadIdx.x;
+  e.id = a.ids[at];
+  if (e.id < 0 || (uint32_t)e.id >= a.vocab) {
+    e.id = -1;
+    return e;
   }
-  const float top = block_max<float, kThreads>(t, sh.red);
-  const float some = block_max<float, kThreads>(t == -INFINITY ? 0.f : 1.f, sh.red);
-  float x = t == -INFINITY ? 0.f : expf(t - top);
-  const float sum = block_add<float, kThreads>(x, sh.red);
-  if (some != 0.f) {
-    e.q = x / sum;
-    e.logq = (t - top) - logf(sum);
-  }
-  if (k < kDistillMaxK) {
-    sh.q[k] = e.q;
-    sh.id[k] = some != 0.f ? e.id : -1;
-  }
-  if (some == 0.f) e.id = -1;
-  __syncthreads();
+  e.t = load1<TDT>(a.teacher, at) * a.inv_tau;
+  if (x) e.s = load1<DT>(x, (uint32_t)e.id) * a.inv_tau;
   return e;
 }
 
-// Maximum and sum of one row.
-template <int DT> __device__ Running row_sum(const DistillArgs& a, const char* row, Shared& sh) {
-  constexpr int N = Elem<DT>::N;
-  const float c = a.inv_tau * kLog2e;
-  Running r{-INFINITY, 0.f};
-  const uint32_t nv = a.vocab / N;
-  for (uint32_t v = threadIdx.x; v < nv; v += kThreads) {
-    float x[N];
-    unpack<DT>(load_vec<DT>(row, v), x);
-    float top = x[0];
-#pragma unroll
-    for (int i = 1; i < N; ++i) top = fmaxf(top, x[i]);
-    const float m = fmaxf(r.m, top), ref = finite_max(m);
-    float s = r.s * exp2_hw((r.m - ref) * c);
-#pragma unroll
-    for (int i = 0; i < N; ++i) s += exp2_hw((x[i] - ref) * c);
-    r = Running{m, s};
-  }
-  for (uint32_t i = nv * N + threadIdx.x; i < a.vocab; i += kThreads) {
-    const float x = load1<DT>(row, i);
-    r = join(r, Running{x, x == -INFINITY ? 0.f : (x == x ? 1.f : x)}, c);
-  }
-#pragma unroll
-  for (int o = 32; o; o >>= 1)
-    r = join(r, Running{__shfl_xor(r.m, o), __shfl_xor(r.s, o)}, c);
-  if ((threadIdx.x & 63) == 0) {
-    sh.red[threadIdx.x >> 6] = r.m;
-    sh.red2[threadIdx.x >> 6] = r.s;
-  }
-  __syncthreads();
-  r = Running{sh.red[0], sh.red2[0]};
-  for (int w = 1; w < kThreads / 64; ++w) r = join(r, Running{sh.red[w], sh.red2[w]}, c);
-  __syncthreads();
-  return r;
-}
+constexpr int kThreads = 256, kWaves = kThreads / 64;
+static_assert(kDistillMaxK <= kThreads, "an entry a thread");
+struct Shared {
+  float q[kDistillMaxK];
+  int32_t id[kDistillMaxK];
+  float m[kWaves], s[kWaves], t[kWaves], some[kWaves], x[kWaves], y[kWaves];
+  uint32_t ticket;
+};
+// What a row's entries come to.
+struct Teacher {
+  bool any;         // an entry has weight
+  float q;          // this thread's entry's
+  float gap;        // sum_k q_k (log q_k - s_k / tau)
+};
 
-__device__ __forceinline__ float lse_of(const DistillArgs& a, Running r) {
-  return fmaf(r.m, a.inv_tau, __builtin_amdgcn_logf(r.s) * kLn2);
-}
-
-template <int DT>
-__device__ void row_grad(const DistillArgs& a, const char* row, char* out, float lse, float g,
-                         const Entry& e, float student, const Shared& sh) {
-  constexpr int N = Elem<DT>::N;
-  const uint32_t nv = a.vocab / N;
-  // An empty teacher's row, or one that the loss' gradient leaves out.
-  bool any = false;
-  for (uint32_t k = 0; k < a.K; ++k) any |= sh.id[k] >= 0;
-  const bool zero = !any || g == 0.f;
-  const float f = g * a.tau;
-  for (uint32_t v = threadIdx.x; v < nv; v += kThreads) {
-    float x[N];
-    if (zero) {
+// Joins the block's running sums and evaluates the entries; two barriers.  Every
+// thread gets the row's sum (if `r` is given) and its entry's q; sh.q and sh.id
+// hold the entries' after the caller's next barrier.
+__device__ __forceinline__ Teacher join_block(const DistillArgs& a, const Entry& e, Shared& sh,
+                                              Running* r, float c) {
+  const uint32_t wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
+  // NaN is weight, and stays NaN in the sums; fmaxf passes over it.
+  const float top = wave_max(e.t == e.t ? e.t : -INFINITY);
+  const bool some = __builtin_amdgcn_ballot_w64(!(e.t == -INFINITY)) != 0;
+  if (r) {
 #pragma unroll
-      for (int i = 0; i < N; ++i) x[i] = 0.f;
-    } else {
-      unpack<DT>(load_vec<DT>(row, v), x);
-#pragma unroll
-      for (int i = 0; i < N; ++i) x[i] = f * exp2_hw(fmaf(x[i], a.inv_tau, -lse) * kLog2e);
+    for (int o = 32; o; o >>= 1) *r = join(*r, Running{__shfl_xor(r->m, o), __shfl_xor(r->s, o)}, c);
+  }
+  if (lane == 0) {
+    if (r) {
+      sh.m[wave] = r->m;
+      sh.s[wave] = r->s;
     }
-    store_vec<DT>(out, v, pack<DT>(x));
+    sh.t[wave] = top;
+    sh.some[wave] = some ? 1.f : 0.f;
   }
-  for (uint32_t i = nv * N + threadIdx.x; i < a.vocab; i += kThreads)
-    store1<DT>(out, i,
-               zero ? 0.f : f * exp2_hw(fmaf(load1<DT>(row, i), a.inv_tau, -lse) * kLog2e));
   __syncthreads();
-  // The listed tokens again, with their q (an id listed twice: each writer
-  // adds the same entries in the same order).
-  if (!zero && e.id >= 0) {
-    float q = 0.f;
-    for (uint32_t k = 0; k < a.K; ++k) q += sh.id[k] == e.id ? sh.q[k] : 0.f;
-    store1<DT>(out, (uint32_t)e.id,
-               f * (exp2_hw(fmaf(student, a.inv_tau, -lse) * kLog2e) - q));
+  if (r) {
+    *r = Running{sh.m[0], sh.s[0]};
+    for (int w = 1; w < kWaves; ++w) *r = join(*r, Running{sh.m[w], sh.s[w]}, c);
   }
+  Teacher t;
+  float tm = sh.t[0], any = sh.some[0];
+#pragma unroll
+  for (int w = 1; w < kWaves; ++w) {
+    tm = fmaxf(tm, sh.t[w]);
+    any = fmaxf(any, sh.some[w]);
+  }
+  t.any = any != 0.f;
+  // exp(t - max), their sum and that of exp(t - max) (t - max - s).
+  float x = e.t == -INFINITY ? 0.f : expf(e.t - tm);
+  const float xs = wave_add(x), ys = wave_add(x == 0.f ? 0.f : x * ((e.t - tm) - e.s));
+  if (lane == 0) {
+    sh.x[wave] = xs;
+    sh.y[wave] = ys;
+  }
+  __syncthreads();
+  float sum = sh.x[0], gap = sh.y[0];
+#pragma unroll
+  for (int w = 1; w < kWaves; ++w) {
+    sum += sh.x[w];
+    gap += sh.y[w];
+  }
+  t.q = t.any ? x / sum : 0.f;
+  t.gap = t.any ? gap / sum - logf(sum) : 0.f;
+  if (threadIdx.x < kDistillMaxK) {
+    sh.q[threadIdx.x] = t.q;
+    sh.id[threadIdx.x] = t.any ? e.id : -1;
+  }
+  return t;
+}
+// The listed tokens again, with their q (an id listed twice: each writer adds
+// the same entries in the same order).
+template <int DT>
+__device__ __forceinline__ void write_entry(const DistillArgs& a, const Entry& e, const Shared& sh,
+                                            char* out, float lse, float f) {
+  float q = 0.f;
+  for (uint32_t k = 0; k < a.K; ++k) q += sh.id[k] == e.id ? sh.q[k] : 0.f;
+  store1<DT>(out, (uint32_t)e.id, f * (exp2_hw((e.s - lse) * kLog2e) - q));
 }
 
-template <int DT, int TDT, bool LOSS, bool GRAD>
-__global__ __launch_bounds__(kThreads) void k_distill(DistillArgs a) {
+template <int DT> __device__ __forceinline__ const char* logits_of(const DistillArgs& a, uint32_t row) {
+  return (const char*)a.logits + (size_t)row * a.ld * sizeof(typename Elem<DT>::T);
+}
+template <int DT> __device__ __forceinline__ char* grad_of(const DistillArgs& a, uint32_t row) {
+  return (char*)a.grad + (size_t)row * a.ldg * sizeof(typename Elem<DT>::T);
+}
+
+// ---- parts of a row ------------------------------------------------------------
+
+constexpr int kVectors = 8;  // of a thread
+constexpr uint32_t kPart = kThreads * kVectors;
+constexpr uint32_t kMaxParts = kLogitsMaxVocab / 4 / kPart;
+static_assert(kMaxParts <= kThreads, "a part's sum a thread");
+
+// Workspace: eight counters, then a record for each row of a launch: its parts' running
+// sums (m in the low word, s in the high one).
+struct Record {
+  unsigned long long r[kMaxParts];
+};
+constexpr uint32_t kQueues = 8;
+constexpr size_t kLine = 128, kRecords = kQueues * kLine;
+__device__ __forceinline__ uint32_t* counter_of(const DistillArgs& a, uint32_t queue) {
+  return (uint32_t*)(a.space + queue * kLine);
+}
+__device__ __forceinline__ Record& record_of(const DistillArgs& a, uint32_t row) {
+  return ((Record*)(a.space + kRecords))[row];
+}
+// No sum looks like this: NaN is published as 0x7FC00000.
+constexpr unsigned long long kUnset = ~0ull;
+__device__ __forceinline__ unsigned long long packed(Running r) {
+  const uint32_t s = r.s == r.s ? __float_as_uint(r.s) : 0x7FC00000u;
+  return (unsigned long long)s << 32 | __float_as_uint(r.m);
+}
+__device__ __forceinline__ Running unpacked(unsigned long long x) {
+  return Running{__uint_as_float((uint32_t)x), __uint_as_float((uint32_t)(x >> 32))};
+}
+
+// This thread's share of a part.
+template <int DT> struct Share {
+  int first, nv;  // its first vector; the row's
+  u32x4 v[kVectors];
+  __device__ __forceinline__ Share(const DistillArgs& a, uint32_t part)
+      : first((int)(part * kPart + threadIdx.x)), nv((int)(a.vocab / Elem<DT>::N)) {}
+  __device__ __forceinline__ bool has(int k) const { return first + k * kThreads < nv; }
+  __device__ __forceinline__ void load(const char* x) {
+#pragma unroll
+    for (int k = 0; k < kVectors; ++k)
+      if (has(k)) v[k] = load_stream<DT>(x, first + k * kThreads);
+  }
+  // The block's running sum, in thread 0.
+  __device__ __forceinline__ Running sum(const DistillArgs& a, const char* x, bool last, float c,
+                                         Shared& sh) const {
+    Running r{-INFINITY, 0.f};
+#pragma unroll
+    for (int k = 0; k < kVectors; ++k)
+      if (has(k)) add<DT>(r, v[k], c);
+    if (last)
+      for (uint32_t i = nv * Elem<DT>::N + threadIdx.x; i < a.vocab; i += kThreads)
+        add1(r, load1<DT>(x, i), c);
+#pragma unroll
+    for (int o = 32; o; o >>= 1) r = join(r, Running{__shfl_xor(r.m, o), __shfl_xor(r.s, o)}, c);
+    if ((threadIdx.x & 63) == 0) {
+      sh.m[threadIdx.x >> 6] = r.m;
+      sh.s[threadIdx.x >> 6] = r.s;
+    }
+    __syncthreads();
+    r = Running{sh.m[0], sh.s[0]};
+    for (int w = 1; w < kWaves; ++w) r = join(r, Running{sh.m[w], sh.s[w]}, c);
+    return r;
+  }
+  // The part's gradient; the listed tokens among its logits last.
+  template <class Own>
+  __device__ __forceinline__ void grad(const DistillArgs& a, const char* x, char* out, bool last,
+                                       bool zero, float lse, float f, const Entry& e, Own own,
+                                       const Shared& sh) const {
+#pragma unroll
+    for (int k = 0; k < kVectors; ++k)
+      if (has(k))
+        store_stream<DT>(out, first + k * kThreads,
+                         zero ? u32x4{0, 0, 0, 0} : scaled_softmax<DT>(a, v[k], lse, f));
+    if (last)
+      for (uint32_t i = nv * Elem<DT>::N + threadIdx.x; i < a.vocab; i += kThreads)
+        store1<DT>(out, i, zero ? 0.f : scaled_softmax1(a, load1<DT>(x, i), lse, f));
+    __syncthreads();
+    if (!zero && own) write_entry<DT>(a, e, sh, out, lse, f);
+  }
+};
+template <int DT>
+__device__ __forceinline__ bool owns(const DistillArgs& a, const Entry& e, uint32_t part, uint32_t parts) {
+  const uint32_t from = part * kPart * Elem<DT>::N;
+  return e.id >= 0 && (uint32_t)e.id >= from && (part == parts - 1 || (uint32_t)e.id < from + kPart * Elem<DT>::N);
+}
+__device__ __forceinline__ void write_loss(const DistillArgs& a, uint32_t row, const Teacher& q, float lse) {
+  a.loss[row] = q.any ? a.tau * a.tau * (q.gap + lse) : 0.f;
+  a.lse[row] = lse;
+}
+
+// The loss of rows in several parts: the parts' sums, then a block a row.
+template <int DT, int TDT>
+__global__ __launch_bounds__(kThreads, 8) void k_sum(DistillArgs a) {
+  __shared__ Shared sh;
+  const uint32_t row = blockIdx.y, part = blockIdx.x;
+  const char* x = logits_of<DT>(a, row);
+  Share<DT> v(a, part);
+  v.load(x);
+  const Running r = v.sum(a, x, part == gridDim.x - 1, a.inv_tau * kLog2e, sh);
+  if (threadIdx.x == 0) record_of(a, row).r[part] = packed(r);
+}
+template <int DT, int TDT>
+__global__ __launch_bounds__(kThreads, 8) void k_loss(DistillArgs a, uint32_t parts) {
   __shared__ Shared sh;
   const uint32_t row = blockIdx.x;
-  const char* x = (const char*)a.logits + (size_t)row * a.ld * sizeof(typename Elem<DT>::T);
-  const Entry e = teacher_row<TDT>(a, row, sh);
-  const float student = e.id >= 0 ? load1<DT>(x, (uint32_t)e.id) : 0.f;
-  float lse;
-  if (LOSS) {
-    lse = lse_of(a, row_sum<DT>(a, x, sh));
-    const float part =
-        e.id < 0 || e.q == 0.f ? 0.f : e.q * (e.logq - fmaf(student, a.inv_tau, -lse));
-    const float sum = block_add<float, kThreads>(part, sh.red);
-    if (threadIdx.x == 0) {
-      a.loss[row] = a.tau * a.tau * sum;
-      a.lse[row] = lse;
-    }
-  } else {
-    lse = a.lse[row];
+  const Entry e = entry_of<DT, TDT>(a, row, logits_of<DT>(a, row));
+  Running r{-INFINITY, 0.f};
+  if (threadIdx.x < parts) r = unpacked(record_of(a, row).r[threadIdx.x]);
+  const Teacher q = join_block(a, e, sh, &r, a.inv_tau * kLog2e);
+  if (threadIdx.x == 0) write_loss(a, row, q, lse_of(a, r));
+}
+
+// The gradient from a known log-sum-exp.
+template <int DT, int TDT>
+__global__ __launch_bounds__(kThreads, 8) void k_grad(DistillArgs a) {
+  __shared__ Shared sh;
+  const uint32_t row = blockIdx.y, part = blockIdx.x, parts = gridDim.x;
+  const char* x = logits_of<DT>(a, row);
+  Share<DT> v(a, part);
+  v.load(x);
+  Entry e = entry_of<DT, TDT>(a, row, nullptr);
+  const bool own = owns<DT>(a, e, part, parts);
+  if (own) e.s = load1<DT>(x, (uint32_t)e.id) * a.inv_tau;
+  const Teacher q = join_block(a, e, sh, nullptr, 0.f);
+  const float g = a.weight ? a.weight[row] : 1.f;
+  v.grad(a, x, grad_of<DT>(a, row), part == parts - 1, !q.any || g == 0.f, a.lse[row], g * a.tau, e, own, sh);
+}
+
+// Both at once, the logits read once.  The parts of a row exchange their sums
+// while each keeps its logits in registers: a part publishes its sum and waits
+// for the others'.
+//   Every wait ends: rows are dealt to eight queues, and a block takes the next
+// part of its queue from a counter when it starts.  A queue's blocks that wait
+// are therefore all of its newest row (at most 31 of 32; those of its earlier
+// rows have all their parts running and need nobody else), eight queues' at
+// most 248, and the device has room for 1536 blocks: another one starts, until
+// the rows are whole.  The wait is bounded all the same; running out would
+// leave NaN.  (One counter alone is the limit at about 100 parts a us.)
+//   In place: a part writes its logits' gradient only after every part, part 0
+// with all the listed tokens' logits among them, has published.
+constexpr uint32_t kPolls = 1u << 18;
+__global__ __launch_bounds__(256) void k_unset(DistillArgs a, uint32_t parts) {
+  const uint32_t i = blockIdx.x * 256 + threadIdx.x, row = i / parts;
+  if (i < kQueues) *counter_of(a, i) = 0;
+  if (row < a.rows) record_of(a, row).r[i - row * parts] = kUnset;
+}
+template <int DT, int TDT, bool GRAD>
+__global__ __launch_bounds__(kThreads, 6) void k_joined(DistillArgs a, uint32_t parts) {
+  __shared__ Shared sh;
+  const uint32_t t = threadIdx.x;
+  const float c = a.inv_tau * kLog2e;
+  uint32_t row = blockIdx.x, part = 0;
+  if (parts > 1) {
+    const uint32_t queue = blockIdx.x / kQueues % kQueues;
+    if (t == 0)
+      sh.ticket = __hip_atomic_fetch_add(counter_of(a, queue), 1u, __ATOMIC_RELAXED,
+                                         __HIP_MEMORY_SCOPE_AGENT);
+    __syncthreads();
+    const uint32_t ticket = __builtin_amdgcn_readfirstlane(sh.ticket);
+    row = ticket / parts;
+    part = ticket - row * parts;
+    row = row * kQueues + queue;
+    if (row >= a.rows) return;
   }
+  const char* x = logits_of<DT>(a, row);
+  const bool last = part == parts - 1;
+  Share<DT> v(a, part);
+  v.load(x);
+  Entry e = entry_of<DT, TDT>(a, row, part == 0 ? x : nullptr);
+  const bool own = owns<DT>(a, e, part, parts);
+  if (part != 0 && own) e.s = load1<DT>(x, (uint32_t)e.id) * a.inv_tau;
+  Running r = v.sum(a, x, last, c, sh);
+  if (parts > 1) {
+    unsigned long long* slot = record_of(a, row).r;
+    // Every thread's loads are done before the sum is out.
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+    __syncthreads();
+    if (t == 0) __hip_atomic_store(slot + part, packed(r), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    unsigned long long got = packed(Running{-INFINITY, 0.f});
+    if (t < parts) {
+      got = kUnset;
+      for (uint32_t n = 0; n < kPolls && got == kUnset; ++n) {
+        got = __hip_atomic_load(slot + t, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+        if (got == kUnset) __builtin_amdgcn_s_sleep(16);
+      }
+    }
+    r = unpacked(got);  // unset: NaN
+  } else if (t != 0) {
+    r = Running{-INFINITY, 0.f};
+  }
+  const Teacher q = join_block(a, e, sh, &r, c);
+  const float lse = lse_of(a, r);
+  if (part == 0 && t == 0) write_loss(a, row, q, lse);
   if (GRAD) {
     const float g = a.weight ? a.weight[row] : 1.f;
-    char* out = (char*)a.grad + (size_t)row * a.ldg * sizeof(typename Elem<DT>::T);
-    row_grad<DT>(a, x, out, lse, g, e, student, sh);
+    v.grad(a, x, grad_of<DT>(a, row), last, !q.any || g == 0.f, lse, g * a.tau, e, own, sh);
   }
 }
 
-template <bool LOSS, bool GRAD>
-hipError_t launch(const DistillArgs& a, int dtype, int tdtype, hipStream_t s) {
-  const dim3 grid(a.rows), block(kThreads);
-  if (dtype == TFE_F32 && tdtype == TFE_F32)
-    k_distill<TFE_F32, TFE_F32, LOSS, GRAD><<<grid, block, 0, s>>>(a);
-  else if (dtype == TFE_F32)
-    k_distill<TFE_F32, TFE_BF16, LOSS, GRAD><<<grid, block, 0, s>>>(a);
-  else if (tdtype == TFE_F32)
-    k_distill<TFE_BF16, TFE_F32, LOSS, GRAD><<<grid, block, 0, s>>>(a);
-  else
-    k_distill<TFE_BF16, TFE_BF16, LOSS, GRAD><<<grid, block, 0, s>>>(a);
+// ---- launches ------------------------------------------------------------------
+
+uint32_t parts_of(int dtype, int32_t vocab) {
+  const uint32_t nv = (uint32_t)vocab / (dtype == TFE_F32 ? 4 : 8);
+  return std::max(1u, (nv + kPart - 1) / kPart);
+}
+
+// The call for n rows from r0 on.
+DistillArgs rows_from(DistillArgs a, uint32_t r0, uint32_t n, int dtype, int tdtype) {
+  const size_t es = dtype == TFE_F32 ? 4 : 2, ts = tdtype == TFE_F32 ? 4 : 2;
+  a.logits = (const char*)a.logits + (size_t)r0 * a.ld * es;
+  if (a.grad) a.grad = (char*)a.grad + (size_t)r0 * a.ldg * es;
+  a.ids += (size_t)r0 * a.K;
+  a.teacher = (const char*)a.teacher + (size_t)r0 * a.K * ts;
+  if (a.weight) a.weight += r0;
+  if (a.loss) a.loss += r0;
+  a.lse += r0;
+  a.rows = n;
+  return a;
+}
+
+// Rows of a launch: the grid's second axis, and 2^20 parts.
+uint32_t launch_rows(uint32_t parts) { return std::min(32768u, (1u << 20) / parts); }
+
+template <int DT, int TDT, bool LOSS, bool GRAD> hipError_t launch(const DistillArgs& a, hipStream_t s) {
+  const uint32_t parts = parts_of(DT, (int32_t)a.vocab), most = launch_rows(parts);
+  const dim3 block(kThreads);
+  for (uint32_t r0 = 0; r0 < a.rows; r0 += most) {
+    const uint32_t n = std::min(most, a.rows - r0);
+    const DistillArgs b = rows_from(a, r0, n, DT, TDT);
+    if (LOSS && (GRAD || parts == 1)) {
+      if (parts > 1) k_unset<<<dim3((n * parts + 255) / 256), dim3(256), 0, s>>>(b, parts);
+      // As many blocks for each queue, and enough for the longest.
+      const uint32_t rounds = ((n + kQueues - 1) / kQueues * parts + kQueues - 1) / kQueues;
+      k_joined<DT, TDT, GRAD><<<dim3(parts > 1 ? rounds * kQueues * kQueues : n), block, 0, s>>>(b, parts);
+    } else if (GRAD) {
+      k_grad<DT, TDT><<<dim3(parts, n), block, 0, s>>>(b);
+    } else {
+      k_sum<DT, TDT><<<dim3(parts, n), block, 0, s>>>(b);
+      k_loss<DT, TDT><<<dim3(n), block, 0, s>>>(b, parts);
+    }
+  }
   return hipGetLastError();
+}
+template <bool LOSS, bool GRAD>
+hipError_t launch_types(const DistillArgs& a, int dtype, int tdtype, hipStream_t s) {
+  if (dtype == TFE_F32)
+    return tdtype == TFE_F32 ? launch<TFE_F32, TFE_F32, LOSS, GRAD>(a, s)
+                             : launch<TFE_F32, TFE_BF16, LOSS, GRAD>(a, s);
+  return tdtype == TFE_F32 ? launch<TFE_BF16, TFE_F32, LOSS, GRAD>(a, s)
+                           : launch<TFE_BF16, TFE_BF16, LOSS, GRAD>(a, s);
 }
 
 }  // namespace
 
-int64_t distill_space(int64_t, int32_t) { return 0; }
+int64_t distill_space(int64_t rows, int32_t vocab) {
+  const uint32_t parts = parts_of(TFE_F32, vocab);  // bfloat16 rows have fewer
+  if (rows == 0 || parts == 1) return 0;
+  return (int64_t)kRecords + std::min<int64_t>(rows, 32768) * (int64_t)sizeof(Record);
+}
 hipError_t launch_distill_loss(const DistillArgs& a, int dtype, int tdtype, hipStream_t s) {
-  return launch<true, false>(a, dtype, tdtype, s);
+  return launch_types<true, false>(a, dtype, tdtype, s);
 }
 hipError_t launch_distill_grad(const DistillArgs& a, int dtype, int tdtype, hipStream_t s) {
-  return launch<false, true>(a, dtype, tdtype, s);
+  return launch_types<false, true>(a, dtype, tdtype, s);
 }
 hipError_t launch_distill_loss_grad(const DistillArgs& a, int dtype, int tdtype, hipStream_t s) {
-  return launch<true, true>(a, dtype, tdtype, s);
+  return launch_types<true, true>(a, dtype, tdtype, s);
 }
 
 }  // namespace tfe

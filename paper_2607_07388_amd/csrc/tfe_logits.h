@@ -7,6 +7,9 @@
 
 namespace tfe {
 
+// Compute units of the current device.
+int compute_units();
+
 constexpr int kFp8Block = 128;
 constexpr int kFp8MaxDim = 65536;
 constexpr int kDistillMaxK = 256;

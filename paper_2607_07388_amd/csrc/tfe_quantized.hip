@@ -4,7 +4,6 @@
 #include <stdint.h>
 
 #include <algorithm>
-#include <atomic>
 #include <type_traits>
 
 #include "tfe_logits.h"
@@ -485,18 +484,6 @@ __global__ __launch_bounds__(WN* WM * 64) void k_tiles(MatmulArgs a, uint32_t ti
 }
 
 // ---- launches ------------------------------------------------------------------
-
-int compute_units() {
-  constexpr int kDevices = 64;
-  static std::atomic<int> known[kDevices];
-  int dev = 0, cus = 0;
-  if (hipGetDevice(&dev) != hipSuccess) return 256;
-  if (dev >= 0 && dev < kDevices && (cus = known[dev].load(std::memory_order_relaxed)) > 0) return cus;
-  if (hipDeviceGetAttribute(&cus, hipDeviceAttributeMultiprocessorCount, dev) != hipSuccess || cus < 1)
-    return 256;
-  if (dev >= 0 && dev < kDevices) known[dev].store(cus, std::memory_order_relaxed);
-  return cus;
-}
 
 uint32_t skinny_lds(const MatmulArgs& a) {
   const uint32_t mt = (a.rows + 15) / 16;

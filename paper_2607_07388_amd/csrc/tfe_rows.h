@@ -44,11 +44,19 @@ template <int DT> __device__ __forceinline__ void store1(void* row, size_t i, fl
   else
     ((uint16_t*)row)[i] = (uint16_t)pack2(v, v);
 }
+// Vector v of a row (of less than 2^32 bytes: a scalar base and a 32-bit offset).
 template <int DT> __device__ __forceinline__ u32x4 load_vec(const void* row, uint32_t v) {
-  return *(const typename Elem<DT>::V*)((const char*)row + (size_t)v * 16);
+  return *(const typename Elem<DT>::V*)((const char*)row + v * 16u);
 }
 template <int DT> __device__ __forceinline__ void store_vec(void* row, uint32_t v, u32x4 x) {
-  *(typename Elem<DT>::V*)((char*)row + (size_t)v * 16) = x;
+  *(typename Elem<DT>::V*)((char*)row + v * 16u) = x;
+}
+// The same for logits and results that pass by once.
+template <int DT> __device__ __forceinline__ u32x4 load_stream(const void* row, uint32_t v) {
+  return __builtin_nontemporal_load((const typename Elem<DT>::V*)((const char*)row + v * 16u));
+}
+template <int DT> __device__ __forceinline__ void store_stream(void* row, uint32_t v, u32x4 x) {
+  __builtin_nontemporal_store(x, (typename Elem<DT>::V*)((char*)row + v * 16u));
 }
 template <int DT> __device__ __forceinline__ void unpack(u32x4 v, float* f) {
   if (DT == TFE_F32) {
