@@ -145,11 +145,9 @@ __device__ __forceinline__ float scale_of(uint32_t biased) {
 
 __device__ __forceinline__ uint32_t byte_of(uint32_t w, int i) { return (w >> (8 * i)) & 255u; }
 
-// Where lane (g, i) of a 16-row operand finds its bytes of a block of 128
-// columns: two 16-byte pieces, 4 p + g for p = 0, 1, so that a load
-// instruction takes 64 consecutive bytes of each row.  Both operands of a
-// product use the same pieces, so the matrix instruction multiplies matching
-// columns, whatever their order.
+// Lane (g, i) of a 16-row operand holds of row i's block of 128 columns two
+// 16-byte pieces: g and 4 + g.  Both operands of a product use the same pieces,
+// so the matrix instruction multiplies matching columns, whatever their order.
 
 // Four results of a lane (columns n .. n + 3 of one row), stored together
 // where the row has them.
@@ -183,61 +181,95 @@ __device__ __forceinline__ void store4(const MatmulArgs& a, uint32_t r, uint32_t
 // has time enough here.
 constexpr int kCodes = 2;  // XDT of rows that are laid out already
 constexpr int kSkinnyWaves = 8;
-constexpr uint32_t kSkinnyLds = 135168;
+constexpr uint32_t kTurn = 2048;  // bytes of LDS a wave turns W's tiles in
+constexpr uint32_t kSkinnyLds = 135168 + kSkinnyWaves * kTurn;
 
 template <int XDT>
-__device__ void stage_rows(const MatmulArgs& a, const QuantizeArgs& x, uint32_t rows, char* xs,
-                           uint32_t xp) {
-  const uint32_t per_row = a.pitch / 8;  // threads; 16 of them a block
-  for (uint32_t t = threadIdx.x; t < rows * per_row; t += kSkinnyWaves * 64) {
-    const uint32_t r = t / per_row, c = (t - r * per_row) * 8;
-    u32x4 v{0, 0, 0, 0};
-    if (r < a.rows) {
-      u32x2 codes;
-      uint32_t biased;
+__device__ __forceinline__ void stage_rows(const MatmulArgs& a, const QuantizeArgs& x, uint32_t rows,
+                                           char* xs, uint32_t xp) {
+  constexpr int U = 4;  // pieces of 8 columns in flight a thread
+  const uint32_t per_row = a.pitch / 8, n = rows * per_row;  // 16 of them a block
+  for (uint32_t t0 = threadIdx.x; t0 < n; t0 += U * kSkinnyWaves * 64) {
+    float f[U][8];
+    u32x2 codes[U];
+    uint32_t biased[U];
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      const uint32_t t = t0 + u * kSkinnyWaves * 64, r = t / per_row, c = (t - r * per_row) * 8;
+      codes[u] = u32x2{0, 0};
+      biased[u] = 127;
+#pragma unroll
+      for (int j = 0; j < 8; ++j) f[u][j] = 0.f;
+      if (t >= n || r >= a.rows) continue;
       if constexpr (XDT == kCodes) {
-        codes = *(const u32x2*)(a.a + (size_t)r * a.pitch + c);
-        biased = a.as[(size_t)r * a.spitch + c / kFp8Block];
+        codes[u] = *(const u32x2*)(a.a + (size_t)r * a.pitch + c);
+        biased[u] = a.as[(size_t)r * a.spitch + c / kFp8Block];
       } else {
-        float f[8];
-        load8<XDT>(x, r, c, f);
-        codes = encode8(f, &biased);
+        load8<XDT>(x, r, c, f[u]);
       }
-      v = __builtin_bit_cast(u32x4, widen(codes[0], codes[1], scale_of(biased)));
     }
-    *(u32x4*)(xs + r * xp + c * 2) = v;
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      const uint32_t t = t0 + u * kSkinnyWaves * 64, r = t / per_row, c = (t - r * per_row) * 8;
+      if constexpr (XDT != kCodes) codes[u] = encode8(f[u], &biased[u]);
+      if (t < n)
+        *(u32x4*)(xs + r * xp + c * 2) =
+            __builtin_bit_cast(u32x4, widen(codes[u][0], codes[u][1], scale_of(biased[u])));
+    }
   }
 }
 
 template <int MT, int TPW, int PC, int XDT, int DT>
 __global__ __launch_bounds__(kSkinnyWaves * 64) void k_skinny(MatmulArgs a, QuantizeArgs x) {
-  extern __shared__ __attribute__((aligned(16))) char xs[];
-  const uint32_t wave = threadIdx.x >> 6, lane = threadIdx.x & 63, i = lane & 15, g = lane >> 4;
+  static_assert(PC == 4, "a chunk's scales are one word");
+  extern __shared__ __attribute__((aligned(16))) char lds[];
+  const uint32_t wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const uint32_t lane = threadIdx.x & 63, i = lane & 15, g = lane >> 4;
   const uint32_t xp = a.pitch * 2 + 16, kb = a.pitch / kFp8Block, chunks = (kb + PC - 1) / PC;
   const uint32_t groups = (a.n + 16 * TPW - 1) / (16 * TPW);
   const uint32_t lo = (uint32_t)((uint64_t)groups * blockIdx.x / gridDim.x);
   const uint32_t hi = (uint32_t)((uint64_t)groups * (blockIdx.x + 1) / gridDim.x);
+  char* turn = lds + wave * kTurn;
+  char* xs = lds + kSkinnyWaves * kTurn;
   u32x4 buf[2][TPW][PC][2];
-  // Loads of one chunk (columns past the last block read the last again).
-  auto load = [&](u32x4 (&v)[TPW][PC][2], uint32_t grp, uint32_t ch) {
+  uint32_t sbuf[2][TPW];
+  // Loads of one chunk (columns past the last block read the last again): 8 rows
+  // of 128 bytes an instruction.  Lane l has piece l % 8 of rows l / 8 and
+  // 8 + l / 8 of a tile.
+  auto load = [&](u32x4 (&v)[TPW][PC][2], uint32_t (&sw)[TPW], uint32_t grp, uint32_t ch) {
 #pragma unroll
     for (int t = 0; t < TPW; ++t) {
-      const uint8_t* p = a.w + (size_t)min((grp * TPW + t) * 16 + i, a.n - 1) * a.pitch + g * 16;
 #pragma unroll
-      for (int c = 0; c < PC; ++c) {
-        const uint32_t b = min(ch * PC + c, kb - 1);
+      for (int q = 0; q < 2; ++q) {
+        const uint32_t row = (grp * TPW + t) * 16 + q * 8 + (lane >> 3);
+        const uint8_t* p = a.w + (size_t)min(row, a.n - 1) * a.pitch + (lane & 7) * 16;
 #pragma unroll
-        for (int q = 0; q < 2; ++q)
-          v[t][c][q] = __builtin_nontemporal_load((const u32x4*)(p + b * kFp8Block + q * 64));
+        for (int c = 0; c < PC; ++c)
+          v[t][c][q] = __builtin_nontemporal_load(
+              (const u32x4*)(p + min(ch * PC + c, kb - 1) * kFp8Block));
       }
+      // A group of tiles may span two blocks of 128 rows of W.
+      const uint32_t nb = min((grp * TPW + t) * 16, a.n - 1) / kFp8Block;
+      sw[t] = *(const uint32_t*)(a.ws + (size_t)nb * a.spitch + ch * PC);
     }
   };
+  // A block of a tile in the operand's layout, by way of the wave's own 2 KB of
+  // LDS (pieces exchanged by row, so that neither side's lanes share banks).
+  const uint32_t put = (lane >> 3) * 128 + ((lane & 7) ^ (lane >> 3)) * 16;
+  const uint32_t get = i * 128 + (g ^ (i & 7)) * 16;
+  auto operand = [&](const u32x4 (&v)[2], u32x4 (&w)[2]) {
+    *(u32x4*)(turn + put) = v[0];
+    *(u32x4*)(turn + 1024 + put) = v[1];
+    w[0] = *(const u32x4*)(turn + get);
+    w[1] = *(const u32x4*)(turn + (get ^ 64));
+  };
   uint32_t grp = lo + wave;
-  if (grp < hi) load(buf[0], grp, 0);
+  if (grp < hi) load(buf[0], sbuf[0], grp, 0);
   stage_rows<XDT>(a, x, MT * 16, xs, xp);
   __syncthreads();
   f32x4 acc[TPW][MT];
-  auto multiply = [&](const u32x4 (&v)[TPW][PC][2], uint32_t grp, uint32_t ch) {
+  auto multiply = [&](const u32x4 (&v)[TPW][PC][2], const uint32_t (&sw)[TPW], uint32_t grp,
+                      uint32_t ch) {
     if (ch == 0) {
 #pragma unroll
       for (int t = 0; t < TPW; ++t)
@@ -248,6 +280,9 @@ __global__ __launch_bounds__(kSkinnyWaves * 64) void k_skinny(MatmulArgs a, Quan
     for (int c = 0; c < PC; ++c) {
       const uint32_t b = ch * PC + c;
       if (b >= kb) break;
+      u32x4 w[TPW][2];
+#pragma unroll
+      for (int t = 0; t < TPW; ++t) operand(v[t][c], w[t]);
 #pragma unroll
       for (int q = 0; q < 2; ++q) {
 #pragma unroll
@@ -259,10 +294,7 @@ __global__ __launch_bounds__(kSkinnyWaves * 64) void k_skinny(MatmulArgs a, Quan
                                      (b * kFp8Block + q * 64 + g * 16 + h * 8) * 2);
 #pragma unroll
           for (int t = 0; t < TPW; ++t) {
-            // A group of tiles may span two blocks of 128 rows of W.
-            const uint32_t nb = min((grp * TPW + t) * 16, a.n - 1) / kFp8Block;
-            const float sw = scale_of(a.ws[(size_t)nb * a.spitch + b]);
-            const bf16x8 wv = widen(v[t][c][q][2 * h], v[t][c][q][2 * h + 1], sw);
+            const bf16x8 wv = widen(w[t][q][2 * h], w[t][q][2 * h + 1], scale_of(byte_of(sw[t], c)));
 #pragma unroll
             for (int m = 0; m < MT; ++m)
               acc[t][m] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(wv, xv[m], acc[t][m], 0, 0, 0);
@@ -285,14 +317,14 @@ __global__ __launch_bounds__(kSkinnyWaves * 64) void k_skinny(MatmulArgs a, Quan
   while (grp < hi) {
     uint32_t ng = grp, nc = ch + 1;
     if (nc == chunks) nc = 0, ng += kSkinnyWaves;
-    if (ng < hi) load(buf[1], ng, nc);
-    multiply(buf[0], grp, ch);
+    if (ng < hi) load(buf[1], sbuf[1], ng, nc);
+    multiply(buf[0], sbuf[0], grp, ch);
     grp = ng, ch = nc;
     if (grp >= hi) break;
     nc = ch + 1;
     if (nc == chunks) nc = 0, ng += kSkinnyWaves;
-    if (ng < hi) load(buf[0], ng, nc);
-    multiply(buf[1], grp, ch);
+    if (ng < hi) load(buf[0], sbuf[0], ng, nc);
+    multiply(buf[1], sbuf[1], grp, ch);
     grp = ng, ch = nc;
   }
 }
@@ -487,7 +519,7 @@ __global__ __launch_bounds__(WN* WM * 64) void k_tiles(MatmulArgs a, uint32_t ti
 
 uint32_t skinny_lds(const MatmulArgs& a) {
   const uint32_t mt = (a.rows + 15) / 16;
-  return mt * 16 * (a.pitch * 2 + 16);
+  return mt * 16 * (a.pitch * 2 + 16) + kSkinnyWaves * kTurn;
 }
 
 template <int MT, int TPW, int PC, int XDT, int DT>
@@ -497,7 +529,7 @@ hipError_t skinny(const MatmulArgs& a, const QuantizeArgs& x, hipStream_t s) {
   const hipError_t e = hipFuncSetAttribute((const void*)k, hipFuncAttributeMaxDynamicSharedMemorySize,
                                            (int)kSkinnyLds);
   if (e != hipSuccess) return e;
-  const uint32_t most = (uint32_t)compute_units() * (lds <= 65536 ? 2 : 1);
+  const uint32_t most = (uint32_t)compute_units() * (lds <= 81920 ? 2 : 1);
   const uint32_t want = (groups + kSkinnyWaves - 1) / kSkinnyWaves;
   k<<<dim3(std::min(most, want)), dim3(kSkinnyWaves * 64), lds, s>>>(a, x);
   return hipGetLastError();
@@ -505,7 +537,7 @@ hipError_t skinny(const MatmulArgs& a, const QuantizeArgs& x, hipStream_t s) {
 template <int XDT, int DT>
 hipError_t skinny_rows(const MatmulArgs& a, const QuantizeArgs& x, hipStream_t s) {
   switch ((a.rows + 15) / 16) {
-    case 1: return skinny<1, 1, 8, XDT, DT>(a, x, s);
+    case 1: return skinny<1, 1, 4, XDT, DT>(a, x, s);
     case 2: return skinny<2, 2, 4, XDT, DT>(a, x, s);
     case 3: return skinny<3, 2, 4, XDT, DT>(a, x, s);
     default: return skinny<4, 2, 4, XDT, DT>(a, x, s);
