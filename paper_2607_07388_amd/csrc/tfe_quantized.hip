@@ -65,19 +65,41 @@ __device__ __forceinline__ void store8(const QuantizeArgs& a, int64_t row, uint3
   *(u32x2*)(a.codes + (size_t)row * a.pitch + c) = u32x2{codes4(f), codes4(f + 4)};
 }
 
+__device__ __forceinline__ uint32_t pack4(const float* x) {
+  const uint32_t r = (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(x[0], x[1], 0, false);
+  return (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(x[2], x[3], (int)r, true);
+}
+// Maximum over the 16 lanes of a row of the wave.
+template <int CTRL> __device__ __forceinline__ float dpp_max(float x) {
+  return fmaxf(x, __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(x), CTRL, 0xF, 0xF, false)));
+}
+__device__ __forceinline__ float max16(float x) {
+  x = dpp_max<0xB1>(x);   // quad_perm [1,0,3,2]
+  x = dpp_max<0x4E>(x);   // quad_perm [2,3,0,1]
+  x = dpp_max<0x141>(x);  // row_half_mirror
+  return dpp_max<0x140>(x);  // row_mirror
+}
 // Eight columns of a block that 16 lanes hold: their codes (f is scaled in
-// place) and the block's exponent.
+// place) and the block's exponent.  Infinities and NaN, which the scale passes
+// over and the codes must not, are looked for by one fma a number.
 __device__ __forceinline__ u32x2 encode8(float* f, uint32_t* biased) {
-  float amax = 0.f;
+  float amax = 0.f, odd = 0.f;
 #pragma unroll
-  for (int j = 0; j < 8; ++j) amax = fmaxf(amax, finite_abs(f[j]));
+  for (int j = 0; j < 8; ++j) {
+    amax = fmaxf(amax, fabsf(f[j]));
+    odd = fmaf(f[j], 0.f, odd);
+  }
+  const bool some = __builtin_amdgcn_ballot_w64(odd != 0.f) != 0;  // NaN compares unequal
+  if (some) {
+    amax = 0.f;
 #pragma unroll
-  for (int o = 8; o; o >>= 1) amax = fmaxf(amax, __shfl_xor(amax, o));
-  *biased = block_exponent(amax);
+    for (int j = 0; j < 8; ++j) amax = fmaxf(amax, finite_abs(f[j]));
+  }
+  *biased = block_exponent(max16(amax));
   const float inv = unscale(*biased);
 #pragma unroll
   for (int j = 0; j < 8; ++j) f[j] *= inv;
-  return u32x2{codes4(f), codes4(f + 4)};
+  return some ? u32x2{codes4(f), codes4(f + 4)} : u32x2{pack4(f), pack4(f + 4)};
 }
 
 // Blocks of one row: 16 lanes hold a block of 128.  One thread per 8 columns;
