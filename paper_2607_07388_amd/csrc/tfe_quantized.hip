@@ -422,7 +422,7 @@ __global__ __launch_bounds__(WN* WM * 64) void k_tiles(MatmulArgs a, uint32_t ti
   // Scales of four blocks from b: the wave's part of W lies in one block of 128 rows.
   auto scales = [&](const Tile& t, uint32_t b, uint32_t& sw, uint32_t (&sx)[MT]) {
     const uint32_t row = min(t.n + wn, a.n - 1) / kFp8Block;
-    sw = *(const uint32_t*)(a.ws + (size_t)row * a.spitch + b);
+    sw = *(const __attribute__((address_space(4))) uint32_t*)(a.ws + (size_t)row * a.spitch + b);
     const auto x = rows_of(a.as, t.m, a.rows, TM, a.spitch);
 #pragma unroll
     for (int m = 0; m < MT; ++m)
@@ -431,7 +431,8 @@ __global__ __launch_bounds__(WN* WM * 64) void k_tiles(MatmulArgs a, uint32_t ti
 
   Tile cur = find(blockIdx.x);
   if (cur.t >= places) return;
-  uint32_t at = 0, sw, sx[MT], sw_next, sx_next[MT];
+  uint32_t at = 0, sw = 0, sx[MT], sw_next, sx_next[MT];
+  bool stored = false;
   // Piece p of row 16 k + i lies at slot p ^ (i & 7); p = g and g + 4 differ in one bit.
   const uint32_t slot = (g ^ (i & 7)) * 16;
   const uint32_t own_w = (wn + i) * kFp8Block + slot, own_x = (TN + wm + i) * kFp8Block + slot;
@@ -444,86 +445,121 @@ __global__ __launch_bounds__(WN* WM * 64) void k_tiles(MatmulArgs a, uint32_t ti
 #pragma unroll
       for (int m = 0; m < MT; ++m) acc[n][m] = f32x4{0.f, 0.f, 0.f, 0.f};
     const Tile next = find(cur.t + gridDim.x);
-    for (uint32_t b4 = 0; b4 < kb; b4 += 4) {
-      sw = sw_next;
-#pragma unroll
-      for (int m = 0; m < MT; ++m) sx[m] = sx_next[m];
-      auto step = [&](auto J) {
-        constexpr int j = decltype(J)::value;
-        const uint32_t b = b4 + j;
-        if (b >= kb) return;
-        // The stage has arrived, and everybody is done with the other one.
+    for (uint32_t b = 0; b < kb; ++b) {
+      // The stage has arrived, and everybody is done with the other one.  A tile's
+      // first stage was asked for before the last tile's results were stored
+      // (more than eight stores a lane, and memory operations complete in
+      // order): those need not have landed.
+      if (stored)
+        asm volatile("s_waitcnt vmcnt(8)" ::: "memory");
+      else
         asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
-        __syncthreads();
-        const uint32_t to = STAGE - at;
-        if (b + 1 < kb) {
-          stage(to, cur, b + 1);
-          if (j == 3) scales(cur, b + 1, sw_next, sx_next);
-        } else if (next.t < places) {
-          stage(to, next, 0);
-          scales(next, 0, sw_next, sx_next);
-        }
-        const uint8_t* lw = lds + at + own_w;
-        const uint8_t* lx = lds + at + own_x;
-        const uint8_t* lw2 = lds + at + (own_w ^ 64);
-        const uint8_t* lx2 = lds + at + (own_x ^ 64);
-        at = to;
-        if constexpr (DT == TFE_BF16) {
-          typedef int v8i __attribute__((ext_vector_type(8)));
-          auto operand = [&](const uint8_t* p, const uint8_t* p2, int k) {
-            const u32x4 lo = *(const u32x4*)(p + k * 16 * kFp8Block);
-            const u32x4 hi = *(const u32x4*)(p2 + k * 16 * kFp8Block);
-            return v8i{(int)lo[0], (int)lo[1], (int)lo[2], (int)lo[3],
-                       (int)hi[0], (int)hi[1], (int)hi[2], (int)hi[3]};
-          };
-          v8i xv[MT];
+      stored = false;
+      __builtin_amdgcn_s_barrier();
+      // The scales have come too; told here, or the compiler waits for them, and so
+      // for the next stage, where they are used.
 #pragma unroll
-          for (int m = 0; m < MT; ++m) xv[m] = operand(lx, lx2, m);
+      for (int m = 0; m < MT; ++m) asm volatile("" : "+v"(sx_next[m]));
+      asm volatile("" : "+s"(sw_next));
+      __builtin_amdgcn_sched_barrier(0);
+      const uint32_t to = STAGE - at;
+      const uint8_t* lw = lds + at + own_w;
+      const uint8_t* lx = lds + at + own_x;
+      const uint8_t* lw2 = lds + at + (own_w ^ 64);
+      const uint8_t* lx2 = lds + at + (own_x ^ 64);
+      at = to;
+      if ((b & 3) == 0) {
+        sw = sw_next;
+#pragma unroll
+        for (int m = 0; m < MT; ++m) sx[m] = sx_next[m];
+      }
+      if (b + 1 < kb) {
+        stage(to, cur, b + 1);
+        if ((b & 3) == 3) scales(cur, b + 1, sw_next, sx_next);
+      } else if (next.t < places) {
+        stage(to, next, 0);
+        scales(next, 0, sw_next, sx_next);
+      }
+      __builtin_amdgcn_sched_barrier(0);
+      if constexpr (DT == TFE_BF16) {
+        typedef int v8i __attribute__((ext_vector_type(8)));
+        auto operand = [&](const uint8_t* p, const uint8_t* p2, int k) {
+          const u32x4 lo = *(const u32x4*)(p + k * 16 * kFp8Block);
+          const u32x4 hi = *(const u32x4*)(p2 + k * 16 * kFp8Block);
+          return v8i{(int)lo[0], (int)lo[1], (int)lo[2], (int)lo[3],
+                     (int)hi[0], (int)hi[1], (int)hi[2], (int)hi[3]};
+        };
+        v8i xv[MT], wv = operand(lw, lw2, 0);
+#pragma unroll
+        for (int m = 0; m < MT; ++m) xv[m] = operand(lx, lx2, m);
+#pragma unroll
+        for (int n = 0; n < NT; ++n) {
+          v8i ahead;
+          if (n + 1 < NT) ahead = operand(lw, lw2, n + 1);
+#pragma unroll
+          for (int m = 0; m < MT; ++m)
+            acc[n][m] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(
+                wv, xv[m], acc[n][m], 0, 0, 0, (int)sw, 0, (int)sx[m]);
+          if (n + 1 < NT) wv = ahead;
+        }
+        // The next tile's operand is read while this one's is multiplied.
+        __builtin_amdgcn_sched_group_barrier(0x100, 2 * MT + 4, 0);
+#pragma unroll
+        for (int n = 0; n < NT; ++n) {
+          __builtin_amdgcn_sched_group_barrier(0x008, MT, 0);
+          if (n + 2 < NT) __builtin_amdgcn_sched_group_barrier(0x100, 2, 0);
+        }
+      } else {
+        const float fw = scale_of(sw & 255u);
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {
+          auto operand = [&](const uint8_t* p, const uint8_t* p2, int k, float f) {
+            const u32x2 v = *(const u32x2*)((q < 2 ? p : p2) + (q & 1) * 8 + k * 16 * kFp8Block);
+            return widen(v[0], v[1], f);
+          };
+          bf16x8 xv[MT];
+#pragma unroll
+          for (int m = 0; m < MT; ++m) xv[m] = operand(lx, lx2, m, scale_of(sx[m] & 255u));
 #pragma unroll
           for (int n = 0; n < NT; ++n) {
-            const v8i wv = operand(lw, lw2, n);
+            const bf16x8 wv = operand(lw, lw2, n, fw);
 #pragma unroll
             for (int m = 0; m < MT; ++m)
-              acc[n][m] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(
-                  wv, xv[m], acc[n][m], 0, 0, j, (int)sw, j, (int)sx[m]);
-          }
-        } else {
-          const float fw = scale_of(byte_of(sw, j));
-#pragma unroll
-          for (int q = 0; q < 4; ++q) {
-            auto operand = [&](const uint8_t* p, const uint8_t* p2, int k, float f) {
-              const u32x2 v = *(const u32x2*)((q < 2 ? p : p2) + (q & 1) * 8 + k * 16 * kFp8Block);
-              return widen(v[0], v[1], f);
-            };
-            bf16x8 xv[MT];
-#pragma unroll
-            for (int m = 0; m < MT; ++m) xv[m] = operand(lx, lx2, m, scale_of(byte_of(sx[m], j)));
-#pragma unroll
-            for (int n = 0; n < NT; ++n) {
-              const bf16x8 wv = operand(lw, lw2, n, fw);
-#pragma unroll
-              for (int m = 0; m < MT; ++m)
-                acc[n][m] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(wv, xv[m], acc[n][m], 0, 0, 0);
-            }
+              acc[n][m] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(wv, xv[m], acc[n][m], 0, 0, 0);
           }
         }
-      };
-      step(std::integral_constant<int, 0>{});
-      step(std::integral_constant<int, 1>{});
-      step(std::integral_constant<int, 2>{});
-      step(std::integral_constant<int, 3>{});
+      }
+      sw >>= 8;
+#pragma unroll
+      for (int m = 0; m < MT; ++m) sx[m] >>= 8;
     }
     const uint32_t r0 = cur.m + wm + i, c0 = cur.n + wn + g * 4;
     if (cur.n + TN <= a.n && cur.m + TM <= a.rows) {
+      // bfloat16: neighbouring lane rows exchange halves of two column tiles, so that
+      // a lane stores 16 bytes and an instruction 64 of each row.
+      static_assert(DT == TFE_F32 || NT % 2 == 0, "column tiles in pairs");
       constexpr int ES = sizeof(typename Elem<DT>::T);
-      char* out = (char*)a.out + ((size_t)r0 * a.ldo + c0) * ES;
+      const uint32_t cx = DT == TFE_F32 ? c0 : cur.n + wn + (g & 1) * 16 + (g >> 1) * 8;
+      char* out = (char*)a.out + ((size_t)r0 * a.ldo + cx) * ES;
 #pragma unroll
       for (int m = 0; m < MT; ++m) {
+        if constexpr (DT == TFE_F32) {
 #pragma unroll
-        for (int n = 0; n < NT; ++n) store4_at<DT>(out + n * 16 * ES, acc[n][m]);
+          for (int n = 0; n < NT; ++n) store4_at<DT>(out + n * 16 * ES, acc[n][m]);
+        } else {
+#pragma unroll
+          for (int n = 0; n < NT; n += 2) {
+            const f32x4 p = acc[n][m], q = acc[n + 1][m];
+            const auto lo = __builtin_amdgcn_permlane16_swap(pack2(p[0], p[1]), pack2(q[0], q[1]), false, false);
+            const auto hi = __builtin_amdgcn_permlane16_swap(pack2(p[2], p[3]), pack2(q[2], q[3]), false, false);
+            *(u32x4_a2*)(out + n * 16 * ES) = u32x4{lo[0], hi[0], lo[1], hi[1]};
+          }
+        }
         out += (size_t)a.ldo * 16 * ES;
       }
+      stored = true;
     } else {
+      stored = false;
 #pragma unroll
       for (int m = 0; m < MT; ++m)
 #pragma unroll

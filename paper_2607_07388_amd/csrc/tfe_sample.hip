@@ -539,6 +539,296 @@ __device__ void no_token(const SampleArgs& a, uint32_t row) {
   if (a.prob) a.prob[row] = 0.f;
 }
 
+// ---- bfloat16 rows -------------------------------------------------------------
+// A bfloat16 logit has few values, so the values themselves are counted: a bin a
+// value, for magnitudes from 2^-8 up to 2^8 (2048 of either sign), in one pass
+// that needs neither the maximum nor a weight for each logit.  All elements of a
+// bin have one weight, so the counts give the running sums exactly, and an
+// answer is a bin and a number in it; bins whose weights are equal once rounded
+// are one group.  A second pass finds the token, the group's j-th.
+// Logits below 2^-8 in magnitude ("small") are kept one by one for their sum; a
+// row whose answer they touch, or that has a logit of 2^8 or more, or one of
+// -2^8 or less with a weight, takes the way of float32 rows.
+constexpr uint32_t kFirst = 119u << 7, kHalf = 2048, kSmall = kHalf;  // the bits of 2^-8
+static_assert(2 * kHalf == kBins, "the values' counts lie where the edges do");
+__device__ __forceinline__ float value_of(uint32_t q) {  // of a bin other than kSmall
+  return __uint_as_float((q < kSmall ? kFirst + (kHalf - 1 - q) : 0x8000u | (kFirst + (q - kSmall - 1))) << 16);
+}
+
+template <class S>
+__device__ bool row_of_values(const SampleArgs& a, uint32_t row, const char* x, float inv_t, S& sh) {
+  constexpr int THREADS = S::THREADS, WAVES = THREADS / 64, PER = (kBins + THREADS) / THREADS;
+  constexpr uint32_t MOST = S::LIST;
+  const int t = threadIdx.x, lane = t & 63;
+  const uint32_t wave = __builtin_amdgcn_readfirstlane(t >> 6);
+  uint32_t* cnt = sh.e.cnt;
+  float* small = (float*)sh.list;
+  for (int q = t; q <= kBins; q += THREADS) cnt[q] = 0;
+  if (t == 0) {
+    sh.n = 0;         // small logits
+    sh.q[0] = 0;      // a logit of 2^8 or more
+    sh.q[1] = 0xFFFFu;  // bits of the largest logit of -2^8 or less
+  }
+  __syncthreads();
+  auto count = [&](uint32_t u) {
+    const uint32_t m = (u & 0x7FFFu) - kFirst;
+    if (m < kHalf) {
+      atomicAdd(&cnt[(u & 0x8000u) ? kSmall + 1 + m : kHalf - 1 - m], 1u);
+    } else if ((u & 0x7FFFu) < kFirst) {
+      const uint32_t at = atomicAdd(&sh.n, 1u);
+      if (at < MOST) small[at] = __uint_as_float(u << 16);
+    } else if ((u & 0x7FFFu) <= 0x7F80u) {  // no NaN
+      if (u & 0x8000u)
+        atomicMin(&sh.q[1], u);
+      else
+        sh.q[0] = 1;
+    }
+  };
+  const uint32_t nv = a.vocab / 8;
+  {
+    auto eight = [&](u32x4 q) {
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        count(q[i] & 0xFFFFu);
+        count(q[i] >> 16);
+      }
+    };
+    constexpr int U = 4;
+    uint32_t i = t;
+    for (; i + (U - 1) * THREADS < nv; i += U * THREADS) {
+      u32x4 q[U];
+#pragma unroll
+      for (int u = 0; u < U; ++u) q[u] = load_vec<TFE_BF16>(x, i + u * THREADS);
+#pragma unroll
+      for (int u = 0; u < U; ++u) eight(q[u]);
+    }
+    for (; i < nv; i += THREADS) eight(load_vec<TFE_BF16>(x, i));
+    for (uint32_t k = nv * 8 + t; k < a.vocab; k += THREADS) count(((const uint16_t*)x)[k]);
+  }
+  __syncthreads();
+  // The largest logit.
+  const uint32_t smalls = sh.n, far = sh.q[1];
+  if (sh.q[0] || smalls > MOST) return false;
+  uint32_t c[PER];
+  float top = -INFINITY;
+#pragma unroll
+  for (int i = 0; i < PER; ++i) {
+    const uint32_t q = t * PER + i;
+    c[i] = q <= kBins && q != kSmall ? cnt[q] : 0;
+    if (c[i]) top = fmaxf(top, value_of(q));
+  }
+  for (uint32_t i = t; i < smalls; i += THREADS) top = fmaxf(top, small[i]);
+  const Scale r{block_max<float, THREADS>(top, (float*)sh.red), inv_t};
+  if (r.top == -INFINITY) return false;
+  if (far != 0xFFFFu && weight(r, __uint_as_float(far << 16)) != 0.f) return false;
+  // The small logits' sum, and their least and largest weight.
+  uint64_t small_sum = 0;
+  uint32_t small_cnt = 0;
+  float small_most = 0.f, small_least = kUnit;
+  if (smalls) {
+    for (uint32_t i = t; i < smalls; i += THREADS) {
+      const float w = weight(r, small[i]);
+      small_sum += (uint64_t)w;
+      small_cnt += w != 0.f;
+      small_most = fmaxf(small_most, w);
+      small_least = fminf(small_least, w);
+    }
+    small_sum = block_add<uint64_t, THREADS>(small_sum, sh.red);
+    small_cnt = block_add<uint32_t, THREADS>(small_cnt, sh.redc);
+    small_most = block_max<float, THREADS>(small_most, (float*)sh.red);
+    small_least = -block_max<float, THREADS>(-small_least, (float*)sh.red);
+  }
+  // Whether the small logits' order matters to an answer of weight w.
+  auto touched = [&](float w) { return smalls && w >= small_least && w <= small_most; };
+  // Edges: this thread's bins' counts and sums, and those before them.
+  float w[PER];
+  uint64_t sum[PER], ws = 0, pw[PER];
+  uint32_t cs = 0, pc[PER];
+#pragma unroll
+  for (int i = 0; i < PER; ++i) {
+    const uint32_t q = t * PER + i;
+    w[i] = c[i] ? weight(r, value_of(q)) : 0.f;
+    if (w[i] == 0.f) c[i] = 0;
+    sum[i] = (uint64_t)c[i] * (uint32_t)w[i];
+    if (q == kSmall && smalls) {
+      c[i] = small_cnt;
+      sum[i] = small_sum;
+    }
+    cs += c[i];
+    ws += sum[i];
+  }
+  uint32_t ic = cs;
+  uint64_t iw = ws;
+#pragma unroll
+  for (int o = 1; o < 64; o <<= 1) {
+    const uint32_t xc = __shfl_up(ic, o);
+    const uint64_t xw = __shfl_up(iw, o);
+    if (lane >= o) {
+      ic += xc;
+      iw += xw;
+    }
+  }
+  if (lane == 63) {
+    sh.redc[wave] = ic;
+    sh.red[wave] = iw;
+  }
+  __syncthreads();
+  uint32_t all_c = 0;
+  uint64_t kept = 0;
+  ic -= cs;
+  iw -= ws;
+  for (uint32_t i = 0; i < (uint32_t)WAVES; ++i) {
+    if (i < wave) {
+      ic += sh.redc[i];
+      iw += sh.red[i];
+    }
+    all_c += sh.redc[i];
+    kept += sh.red[i];
+  }
+#pragma unroll
+  for (int i = 0; i < PER; ++i) {
+    pc[i] = ic;
+    pw[i] = iw;
+    ic += c[i];
+    iw += sum[i];
+  }
+  // The group in which the running count or sum reaches `target`: its weight
+  // (0: the small logits), and the count and sum before it.
+  struct Group {
+    float w;
+    uint32_t cnt;
+    uint64_t sum;
+  };
+  auto find = [&](uint64_t target, bool by_count) {
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < PER; ++i) {
+      const uint64_t have = by_count ? pc[i] : pw[i], get = by_count ? c[i] : sum[i];
+      if (have < target && target <= have + get) sh.n = __float_as_uint(w[i]);
+    }
+    if (t == 0) {
+      sh.sum = ~(uint64_t)0;
+      sh.q[0] = ~0u;
+    }
+    __syncthreads();
+    Group g;
+    g.w = __uint_as_float(sh.n);
+#pragma unroll
+    for (int i = 0; i < PER; ++i)
+      if (c[i] && w[i] == g.w) {
+        atomicMin((unsigned long long*)&sh.sum, (unsigned long long)pw[i]);
+        atomicMin(&sh.q[0], pc[i]);
+      }
+    __syncthreads();
+    g.cnt = sh.q[0];
+    g.sum = sh.sum;
+    return g;
+  };
+  const Settings s = settings_of(a, row);
+  if (s.k && s.k < all_c) {
+    const Group g = find(s.k, true);
+    if (g.w == 0.f || touched(g.w)) return false;
+    kept = g.sum + (uint64_t)(s.k - g.cnt) * (uint32_t)g.w;
+  }
+  if (s.p < 1.f) {
+    const uint64_t part = part_of(kept, s.p);
+    const Group g = find(part, false);
+    if (g.w == 0.f || touched(g.w)) return false;
+    const uint32_t u = (uint32_t)g.w;
+    kept = g.sum + (part - g.sum + u - 1) / u * u;
+  }
+  if (s.least != 0.f) {
+    if (smalls && s.least > small_least && s.least <= small_most) return false;
+    __syncthreads();
+    if (t == 0) sh.sum = 0;
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < PER; ++i)
+      if (c[i] && (t * PER + i == (int)kSmall ? small_least : w[i]) >= s.least)
+        atomicMax((unsigned long long*)&sh.sum, (unsigned long long)(pw[i] + sum[i]));
+    __syncthreads();
+    kept = min(kept, sh.sum);
+  }
+  const uint64_t at = target_of(kept, s.u);
+  const Group g = find(at, false);
+  if (g.w == 0.f || touched(g.w)) return false;
+  const uint32_t nth = (uint32_t)((at - 1 - g.sum) / (uint32_t)g.w);
+  // The group's values, and its nth element by token: a wave has consecutive logits.
+  __syncthreads();
+  if (t == 0) {
+    sh.q[0] = ~0u;
+    sh.q[1] = 0;
+  }
+  __syncthreads();
+#pragma unroll
+  for (int i = 0; i < PER; ++i)
+    if (c[i] && w[i] == g.w) {
+      atomicMin(&sh.q[0], (uint32_t)(t * PER + i));
+      atomicMax(&sh.q[1], (uint32_t)(t * PER + i));
+    }
+  __syncthreads();
+  const float most = value_of(sh.q[0]), least = value_of(sh.q[1]);
+  const uint32_t lo = (uint32_t)((uint64_t)nv * wave / WAVES), hi = (uint32_t)((uint64_t)nv * (wave + 1) / WAVES);
+  const uint32_t tail = wave == WAVES - 1 && nv * 8 + lane < a.vocab ? nv * 8 + lane : ~0u;
+  auto in = [&](float l) { return l >= least && l <= most; };
+  auto matches = [&](u32x4 q) {
+    float l[8];
+    unpack<TFE_BF16>(q, l);
+    uint32_t n = 0;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) n += in(l[i]);
+    return n;
+  };
+  uint32_t n = 0;
+  {
+    constexpr int U = 4;
+    uint32_t i = lo + lane;
+    for (; i + (U - 1) * 64 < hi; i += U * 64) {
+      u32x4 q[U];
+#pragma unroll
+      for (int u = 0; u < U; ++u) q[u] = load_vec<TFE_BF16>(x, i + u * 64);
+#pragma unroll
+      for (int u = 0; u < U; ++u) n += matches(q[u]);
+    }
+    for (; i < hi; i += 64) n += matches(load_vec<TFE_BF16>(x, i));
+    if (tail != ~0u) n += in(load1<TFE_BF16>(x, tail));
+  }
+  n = wave_add(n);
+  if (lane == 0) sh.redc[wave] = n;
+  __syncthreads();
+  uint32_t before = 0;
+  for (uint32_t i = 0; i < wave; ++i) before += sh.redc[i];
+  if (nth >= before && nth < before + n) {
+    for (uint32_t i = lo; i < hi; i += 64) {
+      const u32x4 q = i + lane < hi ? load_vec<TFE_BF16>(x, i + lane) : u32x4{0x7FC07FC0u, 0x7FC07FC0u, 0x7FC07FC0u, 0x7FC07FC0u};
+      const uint32_t m = matches(q);
+      uint32_t up = m;
+#pragma unroll
+      for (int o = 1; o < 64; o <<= 1) {
+        const uint32_t y = __shfl_up(up, o);
+        if (lane >= o) up += y;
+      }
+      const uint32_t first = before + up - m;
+      before += __shfl(up, 63);
+      if (nth >= first && nth < first + m) {
+        float l[8];
+        unpack<TFE_BF16>(q, l);
+        uint32_t k = first;
+#pragma unroll
+        for (int j = 0; j < 8; ++j)
+          if (in(l[j]) && k++ == nth) a.token[row] = (int32_t)((i + lane) * 8 + j);
+      }
+      if (before > nth) break;
+    }
+    const uint64_t last = __builtin_amdgcn_ballot_w64(tail != ~0u && in(load1<TFE_BF16>(x, tail != ~0u ? tail : 0)));
+    if (before <= nth && tail != ~0u && ((last >> lane) & 1) &&
+        before + (uint32_t)__builtin_popcountll(last & ((1ull << lane) - 1)) == nth)
+      a.token[row] = (int32_t)tail;
+  }
+  if (t == 0 && a.prob) a.prob[row] = (float)((double)(uint64_t)g.w / (double)kept);
+  return true;
+}
+
 // One block a row.
 template <int DT, int kThreads, uint32_t LIST>
 __global__ __launch_bounds__(kThreads, 4) void k_row(SampleArgs a) {
@@ -546,6 +836,8 @@ __global__ __launch_bounds__(kThreads, 4) void k_row(SampleArgs a) {
   const uint32_t row = blockIdx.x;
   const char* x = row_of<DT>(a, row);
   Scale r{-INFINITY, inverse_temperature(a, row)};
+  if (DT == TFE_BF16 && row_of_values(a, row, x, r.inv_t, sh)) return;
+  __syncthreads();
   for (int b = threadIdx.x; b < kBins; b += kThreads) sh.e.sum[b] = 0;
   if (threadIdx.x == 0) sh.n = 0;
   float top = -INFINITY;
