@@ -799,29 +799,40 @@ __device__ bool row_of_values(const SampleArgs& a, uint32_t row, const char* x, 
   uint32_t before = 0;
   for (uint32_t i = 0; i < wave; ++i) before += sh.redc[i];
   if (nth >= before && nth < before + n) {
-    for (uint32_t i = lo; i < hi; i += 64) {
-      const u32x4 q = i + lane < hi ? load_vec<TFE_BF16>(x, i + lane) : u32x4{0x7FC07FC0u, 0x7FC07FC0u, 0x7FC07FC0u, 0x7FC07FC0u};
-      const uint32_t m = matches(q);
-      uint32_t up = m;
+    // 64 vectors at a time, eight such loads in flight; their matches are counted
+    // by ballots until the one that holds the element.
+    constexpr int U = 8;
+    bool found = false;
+    for (uint32_t i = lo; i < hi && !found; i += U * 64) {
+      u32x4 q[U];
 #pragma unroll
-      for (int o = 1; o < 64; o <<= 1) {
-        const uint32_t y = __shfl_up(up, o);
-        if (lane >= o) up += y;
+      for (int u = 0; u < U; ++u) {
+        q[u] = u32x4{0x7FC07FC0u, 0x7FC07FC0u, 0x7FC07FC0u, 0x7FC07FC0u};  // NaN: no match
+        if (i + u * 64 + lane < hi) q[u] = load_vec<TFE_BF16>(x, i + u * 64 + lane);
       }
-      const uint32_t first = before + up - m;
-      before += __shfl(up, 63);
-      if (nth >= first && nth < first + m) {
+#pragma unroll
+      for (int u = 0; u < U; ++u) {
         float l[8];
-        unpack<TFE_BF16>(q, l);
-        uint32_t k = first;
+        unpack<TFE_BF16>(q[u], l);
+        uint32_t all = 0, below = 0;  // matches of the 64 vectors; of the lanes before
 #pragma unroll
-        for (int j = 0; j < 8; ++j)
-          if (in(l[j]) && k++ == nth) a.token[row] = (int32_t)((i + lane) * 8 + j);
+        for (int j = 0; j < 8; ++j) {
+          const uint64_t m = __builtin_amdgcn_ballot_w64(in(l[j]));
+          all += (uint32_t)__builtin_popcountll(m);
+          below += (uint32_t)__builtin_popcountll(m & ((1ull << lane) - 1));
+        }
+        if (!found && nth < before + all) {
+          uint32_t k = before + below;
+#pragma unroll
+          for (int j = 0; j < 8; ++j)
+            if (in(l[j]) && k++ == nth) a.token[row] = (int32_t)((i + u * 64 + lane) * 8 + j);
+          found = true;
+        }
+        before += all;
       }
-      if (before > nth) break;
     }
     const uint64_t last = __builtin_amdgcn_ballot_w64(tail != ~0u && in(load1<TFE_BF16>(x, tail != ~0u ? tail : 0)));
-    if (before <= nth && tail != ~0u && ((last >> lane) & 1) &&
+    if (!found && tail != ~0u && ((last >> lane) & 1) &&
         before + (uint32_t)__builtin_popcountll(last & ((1ull << lane) - 1)) == nth)
       a.token[row] = (int32_t)tail;
   }
