@@ -1,5 +1,5 @@
-// The per-step calls of the Python binding (lookups, prefetches, head top-K)
-// as functions of a CPython module: a decode step's launch is a few
+// The per-step calls of the Python binding (lookups, prefetches, head top-K,
+// the calls on logits) as functions of a CPython module: a decode step's launch is a few
 // microseconds, of which marshalling its arguments through ctypes took about
 // half.  Each function takes the plain case -- positional arguments, exact
 // ints, floats and None, objects with data_ptr() -- and hands everything else
@@ -20,7 +20,7 @@ struct Call {
   PyObject* slow;  // the ctypes function
   void* fn;
 };
-Call g_lookup, g_multi, g_prefetch, g_scored, g_topk;
+Call g_lookup, g_multi, g_prefetch, g_scored, g_topk, g_linear, g_sample, g_loss, g_grad, g_both;
 
 // Each conversion returns false, with no exception set, for what the plain
 // case does not cover.
@@ -67,6 +67,14 @@ bool int32(PyObject* o, int32_t* out) {
   const long v = PyLong_AsLongAndOverflow(o, &over);
   if (over || v < INT32_MIN || v > INT32_MAX) return false;
   *out = (int32_t)v;
+  return true;
+}
+bool int64(PyObject* o, int64_t* out) {
+  if (!PyLong_CheckExact(o)) return false;
+  int over = 0;
+  const long long v = PyLong_AsLongLongAndOverflow(o, &over);
+  if (over) return false;
+  *out = (int64_t)v;
   return true;
 }
 bool number(PyObject* o, float* out) {
@@ -169,21 +177,133 @@ PyObject* head_topk(PyObject*, PyObject* const* a, Py_ssize_t n, PyObject* kw) {
   return status(st);
 }
 
-// bind(check, {name: (ctypes function wrapper, address)})
+PyObject* quantized_linear(PyObject*, PyObject* const* a, Py_ssize_t n, PyObject* kw) {
+  PLAIN(g_linear, 13);
+  void *x, *w, *ws, *out, *space;
+  int64_t ldx, rows, ldo, bytes;
+  int32_t dtype, odt, od, dim;
+  SLOW_UNLESS(g_linear, pointer(a[0], &x) && int32(a[1], &dtype) && int64(a[2], &ldx) &&
+                            pointer(a[3], &w) && pointer(a[4], &ws) && int64(a[5], &rows) &&
+                            int32(a[6], &od) && int32(a[7], &dim) && pointer(a[8], &out) &&
+                            int32(a[9], &odt) && int64(a[10], &ldo) && pointer(a[11], &space) &&
+                            int64(a[12], &bytes));
+  using Fn = int (*)(void*, int32_t, int64_t, void*, void*, int64_t, int32_t, int32_t, void*,
+                     int32_t, int64_t, void*, int64_t, void*);
+  int st;
+  Py_BEGIN_ALLOW_THREADS;
+  st = ((Fn)g_linear.fn)(x, dtype, ldx, w, ws, rows, od, dim, out, odt, ldo, space, bytes, s);
+  Py_END_ALLOW_THREADS;
+  return status(st);
+}
+
+PyObject* sample(PyObject*, PyObject* const* a, Py_ssize_t n, PyObject* kw) {
+  PLAIN(g_sample, 14);
+  void *l, *T, *k, *p, *m, *u, *token, *prob, *space;
+  int64_t ld, rows, bytes;
+  int32_t dtype, vocab;
+  SLOW_UNLESS(g_sample, pointer(a[0], &l) && int32(a[1], &dtype) && int64(a[2], &ld) &&
+                            int64(a[3], &rows) && int32(a[4], &vocab) && pointer(a[5], &T) &&
+                            pointer(a[6], &k) && pointer(a[7], &p) && pointer(a[8], &m) &&
+                            pointer(a[9], &u) && pointer(a[10], &token) && pointer(a[11], &prob) &&
+                            pointer(a[12], &space) && int64(a[13], &bytes));
+  using Fn = int (*)(void*, int32_t, int64_t, int64_t, int32_t, void*, void*, void*, void*, void*,
+                     void*, void*, void*, int64_t, void*);
+  int st;
+  Py_BEGIN_ALLOW_THREADS;
+  st = ((Fn)g_sample.fn)(l, dtype, ld, rows, vocab, T, k, p, m, u, token, prob, space, bytes, s);
+  Py_END_ALLOW_THREADS;
+  return status(st);
+}
+
+// What the three distillation calls begin with.
+struct Distill {
+  void *l, *ids, *t;
+  int64_t ld, rows;
+  int32_t dtype, vocab, tdtype, K;
+  float tau;
+};
+bool distill(PyObject* const* a, Distill* d) {
+  return pointer(a[0], &d->l) && int32(a[1], &d->dtype) && int64(a[2], &d->ld) &&
+         int64(a[3], &d->rows) && int32(a[4], &d->vocab) && pointer(a[5], &d->ids) &&
+         pointer(a[6], &d->t) && int32(a[7], &d->tdtype) && int32(a[8], &d->K) &&
+         number(a[9], &d->tau);
+}
+
+PyObject* distill_loss(PyObject*, PyObject* const* a, Py_ssize_t n, PyObject* kw) {
+  PLAIN(g_loss, 14);
+  Distill d;
+  void *loss, *lse, *space;
+  int64_t bytes;
+  SLOW_UNLESS(g_loss, distill(a, &d) && pointer(a[10], &loss) && pointer(a[11], &lse) &&
+                          pointer(a[12], &space) && int64(a[13], &bytes));
+  using Fn = int (*)(void*, int32_t, int64_t, int64_t, int32_t, void*, void*, int32_t, int32_t,
+                     float, void*, void*, void*, int64_t, void*);
+  int st;
+  Py_BEGIN_ALLOW_THREADS;
+  st = ((Fn)g_loss.fn)(d.l, d.dtype, d.ld, d.rows, d.vocab, d.ids, d.t, d.tdtype, d.K, d.tau, loss,
+                       lse, space, bytes, s);
+  Py_END_ALLOW_THREADS;
+  return status(st);
+}
+
+PyObject* distill_grad(PyObject*, PyObject* const* a, Py_ssize_t n, PyObject* kw) {
+  PLAIN(g_grad, 14);
+  Distill d;
+  void *lse, *weight, *grad;
+  int64_t ldg;
+  SLOW_UNLESS(g_grad, distill(a, &d) && pointer(a[10], &lse) && pointer(a[11], &weight) &&
+                          pointer(a[12], &grad) && int64(a[13], &ldg));
+  using Fn = int (*)(void*, int32_t, int64_t, int64_t, int32_t, void*, void*, int32_t, int32_t,
+                     float, void*, void*, void*, int64_t, void*);
+  int st;
+  Py_BEGIN_ALLOW_THREADS;
+  st = ((Fn)g_grad.fn)(d.l, d.dtype, d.ld, d.rows, d.vocab, d.ids, d.t, d.tdtype, d.K, d.tau, lse,
+                       weight, grad, ldg, s);
+  Py_END_ALLOW_THREADS;
+  return status(st);
+}
+
+PyObject* distill_loss_grad(PyObject*, PyObject* const* a, Py_ssize_t n, PyObject* kw) {
+  PLAIN(g_both, 17);
+  Distill d;
+  void *weight, *loss, *lse, *grad, *space;
+  int64_t ldg, bytes;
+  SLOW_UNLESS(g_both, distill(a, &d) && pointer(a[10], &weight) && pointer(a[11], &loss) &&
+                          pointer(a[12], &lse) && pointer(a[13], &grad) && int64(a[14], &ldg) &&
+                          pointer(a[15], &space) && int64(a[16], &bytes));
+  using Fn = int (*)(void*, int32_t, int64_t, int64_t, int32_t, void*, void*, int32_t, int32_t,
+                     float, void*, void*, void*, void*, int64_t, void*, int64_t, void*);
+  int st;
+  Py_BEGIN_ALLOW_THREADS;
+  st = ((Fn)g_both.fn)(d.l, d.dtype, d.ld, d.rows, d.vocab, d.ids, d.t, d.tdtype, d.K, d.tau,
+                       weight, loss, lse, grad, ldg, space, bytes, s);
+  Py_END_ALLOW_THREADS;
+  return status(st);
+}
+
+// bind(check, {name: (ctypes function wrapper, address)}); of the calls on
+// logits any may be left out, and stays as it is.
 PyObject* bind(PyObject*, PyObject* args) {
   PyObject *check, *calls;
   if (!PyArg_ParseTuple(args, "OO!", &check, &PyDict_Type, &calls)) return nullptr;
   const struct {
     const char* name;
     Call* c;
-  } all[] = {{"tfe_lookup_inject", &g_lookup},
-             {"tfe_lookup_inject_multi", &g_multi},
-             {"tfe_prefetch", &g_prefetch},
-             {"tfe_prefetch_scored", &g_scored},
-             {"tfe_head_topk", &g_topk}};
+    bool optional;
+  } all[] = {{"tfe_lookup_inject", &g_lookup, false},
+             {"tfe_lookup_inject_multi", &g_multi, false},
+             {"tfe_prefetch", &g_prefetch, false},
+             {"tfe_prefetch_scored", &g_scored, false},
+             {"tfe_head_topk", &g_topk, false},
+             {"tfe_quantized_linear", &g_linear, true},
+             {"tfe_sample", &g_sample, true},
+             {"tfe_distill_loss", &g_loss, true},
+             {"tfe_distill_grad", &g_grad, true},
+             {"tfe_distill_loss_grad", &g_both, true}};
   for (const auto& e : all) {
     PyObject* v = PyDict_GetItemString(calls, e.name);
     PyObject *f, *p;
+    if (!v && e.optional) continue;
     if (!v || !PyArg_ParseTuple(v, "OO", &f, &p)) {
       if (!PyErr_Occurred()) PyErr_SetString(PyExc_KeyError, e.name);
       return nullptr;
@@ -220,6 +340,22 @@ PyMethodDef g_methods[] = {
      "side_stream=None)\n--\n\n"},
     {"tfe_head_topk", (PyCFunction)(void (*)(void))head_topk, FAST,
      "tfe_head_topk($module, head, hidden, B, K, top_ids, top_prob, stream=None)\n--\n\n"},
+    {"tfe_quantized_linear", (PyCFunction)(void (*)(void))quantized_linear, FAST,
+     "tfe_quantized_linear($module, x, dtype, ldx, w, w_scales, rows, out_dim, dim, out, out_dtype, "
+     "ldo, workspace, workspace_bytes, stream=None)\n--\n\n"},
+    {"tfe_sample", (PyCFunction)(void (*)(void))sample, FAST,
+     "tfe_sample($module, logits, dtype, ld, rows, vocab, temperature, top_k, top_p, min_p, u, "
+     "token, prob, workspace, workspace_bytes, stream=None)\n--\n\n"},
+    {"tfe_distill_loss", (PyCFunction)(void (*)(void))distill_loss, FAST,
+     "tfe_distill_loss($module, logits, dtype, ld, rows, vocab, teacher_ids, teacher_logits, "
+     "teacher_dtype, K, temperature, loss, lse, workspace, workspace_bytes, stream=None)\n--\n\n"},
+    {"tfe_distill_grad", (PyCFunction)(void (*)(void))distill_grad, FAST,
+     "tfe_distill_grad($module, logits, dtype, ld, rows, vocab, teacher_ids, teacher_logits, "
+     "teacher_dtype, K, temperature, lse, grad_loss, grad, ldg, stream=None)\n--\n\n"},
+    {"tfe_distill_loss_grad", (PyCFunction)(void (*)(void))distill_loss_grad, FAST,
+     "tfe_distill_loss_grad($module, logits, dtype, ld, rows, vocab, teacher_ids, teacher_logits, "
+     "teacher_dtype, K, temperature, grad_loss, loss, lse, grad, ldg, workspace, workspace_bytes, "
+     "stream=None)\n--\n\n"},
     {nullptr, nullptr, 0, nullptr}};
 PyModuleDef g_module = {PyModuleDef_HEAD_INIT, "_calls", nullptr, -1, g_methods,
                         nullptr, nullptr, nullptr, nullptr};

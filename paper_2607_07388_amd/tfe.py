@@ -7,8 +7,8 @@ A negative status raises ``TfeError`` carrying ``tfe_last_error()``.
 There is no fallback: if the library cannot be built or loaded, importing
 fails.
 
-The calls a serving loop makes at every step (lookups, prefetches, head top-K)
-go through the native module ``_calls``, which takes the plain case and hands
+The calls a loop makes at every step (lookups, prefetches, head top-K, the calls
+on logits) go through the native module ``_calls``, which takes the plain case and hands
 any other to the ctypes function of the same name here.  (A batch-64 decode
 lookup from Python, back to back: 7.6 us through ctypes, 6.3 so.)
 """
@@ -397,7 +397,9 @@ def make_desc(phrase_tokens, phrase_len, n_min, n_max, vocab, values, dim, dtype
 # The per-step calls: native from here on, with the functions above for any
 # form of arguments that is not the plain one.
 _BY_CTYPES = {f.__name__: f for f in (tfe_lookup_inject, tfe_lookup_inject_multi, tfe_prefetch,
-                                      tfe_prefetch_scored, tfe_head_topk)}
+                                      tfe_prefetch_scored, tfe_head_topk, tfe_quantized_linear,
+                                      tfe_sample, tfe_distill_loss, tfe_distill_grad,
+                                      tfe_distill_loss_grad)}
 
 
 def _bind_calls():
