@@ -144,7 +144,7 @@ template <int THREADS_, uint32_t LIST_> struct Shared {
 };
 
 // Edges from the histogram in sh.e.sum (in place) or in memory.
-template <class S> __device__ void make_edges(S& sh, unsigned long long* hist) {
+template <bool SHARED, class S> __device__ void make_edges(S& sh, unsigned long long* hist) {
   constexpr int THREADS = S::THREADS, PER = kBins / THREADS;
   const int t = threadIdx.x, lane = t & 63, wave = t >> 6;
   uint32_t c[PER];
@@ -153,9 +153,9 @@ template <class S> __device__ void make_edges(S& sh, unsigned long long* hist) {
 #pragma unroll
   for (int i = 0; i < PER; ++i) {
     const uint32_t b = kBins - 1 - (t * PER + i);
-    // Other blocks of the launch may have added to it: device scope.
-    const uint64_t x = hist ? __hip_atomic_load(hist + b, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT)
-                            : sh.e.sum[b];
+    // SHARED: other blocks of the launch have added to it, device scope.
+    const uint64_t x = SHARED ? __hip_atomic_load(hist + b, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT)
+                       : hist ? hist[b] : sh.e.sum[b];
     c[i] = entry_count(x);
     w[i] = entry_sum(x, b);
     cs += c[i];
@@ -293,16 +293,35 @@ template <class S> __device__ Ranges ranges_of(S& sh, const Settings& s) {
   return r;
 }
 
-// Sorts sh.list[0 .. n), larger keys first; n <= LIST.
+// Sorts sh.list[0 .. n), larger keys first; n <= LIST.  A bitonic network; its
+// steps within 64 neighbours run in a wave's registers (an element a lane), so
+// only the longer ones need barriers.
 template <class S> __device__ void sort_list(S& sh, uint32_t n) {
-  constexpr int kThreads = S::THREADS;
+  constexpr uint32_t THREADS = S::THREADS;
+  const uint32_t lane = threadIdx.x & 63;
   uint32_t size = 64;
   while (size < n) size <<= 1;
-  for (uint32_t i = n + threadIdx.x; i < size; i += kThreads) sh.list[i] = 0;
+  for (uint32_t i = n + threadIdx.x; i < size; i += THREADS) sh.list[i] = 0;
   __syncthreads();
-  for (uint32_t k = 2; k <= size; k <<= 1)
-    for (uint32_t j = k >> 1; j; j >>= 1) {
-      for (uint32_t p = threadIdx.x; p < size / 2; p += kThreads) {
+  // Steps j, j / 2, ... 1 of stage k, j <= 32, for the waves' runs of 64.
+  auto within = [&](uint32_t k, uint32_t from) {
+    for (uint32_t i = threadIdx.x; i < size; i += THREADS) {  // whole waves
+      uint64_t x = sh.list[i];
+      for (uint32_t kk = from; kk <= k; kk <<= 1)
+        for (uint32_t j = min(kk >> 1, 32u); j; j >>= 1) {
+          const uint64_t y = __shfl_xor(x, (int)j);
+          // Descending runs where bit kk of i is clear: their lower half keeps the larger.
+          const bool larger = ((i & kk) == 0) == ((lane & j) == 0);
+          x = (x > y) == larger ? x : y;
+        }
+      sh.list[i] = x;
+    }
+    __syncthreads();
+  };
+  within(min(size, 64u), 2);
+  for (uint32_t k = 128; k <= size; k <<= 1) {
+    for (uint32_t j = k >> 1; j >= 64; j >>= 1) {
+      for (uint32_t p = threadIdx.x; p < size / 2; p += THREADS) {
         const uint32_t i = 2 * p - (p & (j - 1)), o = i + j;  // i without bit j
         const uint64_t x = sh.list[i], y = sh.list[o];
         if ((x < y) == ((i & k) == 0)) {
@@ -312,6 +331,8 @@ template <class S> __device__ void sort_list(S& sh, uint32_t n) {
       }
       __syncthreads();
     }
+    within(k, k);
+  }
 }
 
 __device__ __forceinline__ uint32_t order_bin(uint64_t key) {
@@ -863,7 +884,7 @@ __global__ __launch_bounds__(kThreads, 4) void k_row(SampleArgs a) {
     if (w != 0.f) atomicAdd((unsigned long long*)&sh.e.sum[bin_of(w)], (unsigned long long)bin_entry(w));
   });
   __syncthreads();
-  make_edges(sh, nullptr);
+  make_edges<false>(sh, nullptr);
   const Settings s = settings_of(a, row);
   const Ranges g = ranges_of(sh, s);
   collect<DT>(x, a.vocab, threadIdx.x, kThreads, r, g, [&](uint64_t key) {
@@ -942,7 +963,7 @@ __global__ __launch_bounds__(kHistThreads) void k_part_hist(SampleArgs a, uint32
     sh.n = __hip_atomic_fetch_add(&p.done, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
   __syncthreads();
   if (sh.n != parts - 1) return;
-  make_edges(sh, p.hist);
+  make_edges<true>(sh, p.hist);
   const Ranges g = ranges_of(sh, settings_of(a, row));
   if (threadIdx.x == 0) p.ranges = g;
 }
@@ -987,11 +1008,11 @@ __global__ __launch_bounds__(kFinishThreads) void k_part_finish(SampleArgs a, ui
   const Settings s = settings_of(a, row);
   if (n <= kList) {
     for (uint32_t i = threadIdx.x; i < n; i += kFinishThreads) sh.list[i] = p.list[i];
-    make_edges(sh, p.hist);
+    make_edges<false>(sh, p.hist);
     sort_list(sh, n);
     resolve(a, row, sh, s, n);
   } else {
-    make_edges(sh, p.hist);
+    make_edges<false>(sh, p.hist);
     resolve_long<DT>(a, row, r, sh, s);
   }
 }
