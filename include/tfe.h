@@ -374,9 +374,11 @@ tfe_status tfe_quantize(const void *x, int32_t dtype, int64_t ldx, int64_t rows,
 
 /* out[r, n] = sum over k of A[r, k] W[n, k], for A laid out with block_rows 1
  * and W with block_rows 128 (scales w_scales); out DEVICE [rows x out_dim] of
- * out_dtype.  Products are exact; float32 results are accumulated in float32,
+ * out_dtype.  Products are exact; float32 results are accumulated in float32.
  * bfloat16 results may be accumulated by the 8-bit matrix instruction, whose
- * sums carry about 17 bits (far below the rounding of the result).
+ * sums are off by about 1.4e-5 of a result of normally distributed terms (at
+ * worst 2^-12 of the terms' magnitudes was seen), far below their rounding.
+ * Numbers below 2^-126 may count as 0.
  * rows <= 2^20, 1 <= out_dim <= 2^20, dim <= 65536. */
 tfe_status tfe_quantized_matmul(const uint8_t *a, const uint8_t *a_scales, const uint8_t *w,
                                 const uint8_t *w_scales, int64_t rows, int32_t out_dim,
@@ -427,7 +429,7 @@ int64_t tfe_sample_workspace(int64_t rows, int32_t vocab); /* -1: bad size */
  * Entries whose id lies outside [0, vocab) are padding: their logits may hold
  * anything.  A row without an entry of finite logit has loss 0 and gradient 0.
  * A student logit of -infinity has probability 0 (the loss is +infinity where
- * the teacher gives that token weight).  1 <= K <= 256, 1 <= vocab <= 2^18,
+ * the teacher gives that token weight); +infinity or NaN makes its row NaN.  1 <= K <= 256, 1 <= vocab <= 2^18,
  * rows <= 2^20.  Softmax sums are float32.
  *   loss, lse   DEVICE float [rows] (lse of the student's row, also where the
  *               loss is 0).

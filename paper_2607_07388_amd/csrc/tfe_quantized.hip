@@ -4,6 +4,7 @@
 #include <stdint.h>
 
 #include <algorithm>
+#include <atomic>
 #include <type_traits>
 
 #include "tfe_logits.h"
@@ -359,9 +360,10 @@ __global__ __launch_bounds__(kSkinnyWaves * 64) void k_skinny(MatmulArgs a, Quan
 // one's results are written.
 // In LDS a row's eight 16-byte pieces are exchanged by its number mod 8, so that
 // the 8 lanes that an LDS cycle serves read different banks.
-// float32 results: the exact bfloat16 instruction, codes widened in registers.
+// float32 results: the bfloat16 instruction, codes widened in registers (exact
+// products, float32 sums: 1.3e-8 of the result's size off on normal numbers).
 // bfloat16 results: the scaled 8-bit instruction, twice its rate; its sums are
-// off by about 1.4e-5 of the result's size, their rounding by 2e-3.
+// off by about 1.4e-5 of the result's size, their rounding by 1.7e-3.
 #if defined(__HIP_DEVICE_COMPILE__)  // the host compiler has no buffer descriptors
 // Loads go through buffer descriptors: 32-bit offsets, and rows past a matrix'
 // last read as zeros (the whole offset is in the vector register, so that the
@@ -584,9 +586,17 @@ template <int MT, int TPW, int PC, int XDT, int DT>
 hipError_t skinny(const MatmulArgs& a, const QuantizeArgs& x, hipStream_t s) {
   const uint32_t lds = skinny_lds(a), groups = (a.n + 16 * TPW - 1) / (16 * TPW);
   auto* k = k_skinny<MT, TPW, PC, XDT, DT>;
-  const hipError_t e = hipFuncSetAttribute((const void*)k, hipFuncAttributeMaxDynamicSharedMemorySize,
-                                           (int)kSkinnyLds);
+  // Once for each device: more LDS than a kernel may have by default.
+  static std::atomic<uint64_t> told{0};
+  int dev = 0;
+  hipError_t e = hipGetDevice(&dev);
   if (e != hipSuccess) return e;
+  const uint64_t bit = 1ull << (dev & 63);
+  if (dev > 63 || !(told.load(std::memory_order_relaxed) & bit)) {
+    e = hipFuncSetAttribute((const void*)k, hipFuncAttributeMaxDynamicSharedMemorySize, (int)kSkinnyLds);
+    if (e != hipSuccess) return e;
+    told.fetch_or(bit, std::memory_order_relaxed);
+  }
   const uint32_t most = (uint32_t)compute_units() * (lds <= 81920 ? 2 : 1);
   const uint32_t want = (groups + kSkinnyWaves - 1) / kSkinnyWaves;
   k<<<dim3(std::min(most, want)), dim3(kSkinnyWaves * 64), lds, s>>>(a, x);
@@ -640,8 +650,14 @@ hipError_t launch_fp8_matmul(const MatmulArgs& a, int out_dtype, hipStream_t s) 
   if (is_skinny(a))
     return out_dtype == TFE_F32 ? skinny_rows<kCodes, TFE_F32>(a, QuantizeArgs{}, s)
                                 : skinny_rows<kCodes, TFE_BF16>(a, QuantizeArgs{}, s);
-  const uint64_t large = (uint64_t)((a.n + 255) / 256) * ((a.rows + 255) / 256);
-  if (large >= (uint64_t)compute_units() * 2) return tiles<256, 256, 2, 4>(a, out_dtype, 1, s);
+  // Large tiles where they fill the device and waste few rows.  us at 151936 x 1024,
+  // 256 x 256 / 128 x 128: bfloat16 256 rows 81 / 76, 512 135 / 144, 1024 254 / 274, 2048
+  // 454 / 510; float32 256 rows 134 / 135, 512 234 / 241, 1024 425 / 448.  257 x 40001 x 1000
+  // (three row tiles of 128 against two of 256): 59 / 29.
+  const uint32_t r256 = (a.rows + 255) / 256, r128 = (a.rows + 127) / 128;
+  const bool fills = (uint64_t)((a.n + 255) / 256) * r256 >= (uint64_t)compute_units() * 2;
+  if (fills && a.rows > 256 && r256 * 2 * 92 <= r128 * 100)
+    return tiles<256, 256, 2, 4>(a, out_dtype, 1, s);
   return tiles<128, 128, 2, 2>(a, out_dtype, 2, s);
 }
 

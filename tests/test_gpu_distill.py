@@ -98,7 +98,8 @@ def check_values(c, ids, weight, loss, lse, grad):
 
 
 SIZES = [(1, 1, 1), (2, 2, 1), (3, 5, 5), (4, 64, 7), (5, 65, 256), (7, 1000, 17), (3, 4099, 64), (300, 333, 33),
-         (2, 33333, 128), (1, 151936, 256), (5, 151936, 64), (1, 1 << 18, 3), (600, 2000, 9)]
+         (2, 33333, 128), (1, 151936, 256), (5, 151936, 64), (1, 1 << 18, 3), (600, 2000, 9), (300, 40001, 33),
+         (1001, 17000, 5)]
 
 
 @pytest.mark.parametrize("dtype,tdtype", [(F32, F32), (BF16, F32), (F32, BF16), (BF16, BF16)])

@@ -218,3 +218,37 @@ def test_captured_and_on_another_stream(rows, out_dtype):
 def test_no_rows():
     wc, wsc, _ = quantize(np.ones((4, 4)), F32, 128)
     assert tfe.tfe_quantized_linear(None, F32, 4, wc, wsc, 0, 4, 4, None, F32, 4, None, 0) == 0
+
+
+@pytest.mark.parametrize("out_dtype", [F32, BF16])
+@pytest.mark.parametrize("rows,n,dim", [(400, 70000, 130), (513, 66000, 384), (300, 66001, 520)])
+def test_large_tiles(rows, n, dim, out_dtype):
+    """Enough columns and rows for the largest tiles, with ragged ends."""
+    rng = np.random.default_rng(n)
+    ac, asc, _ = quantize(rng.standard_normal((rows, dim)), F32, 1)
+    wc, wsc, _ = quantize(rng.standard_normal((n, dim)) * 0.1, F32, 128)
+    out = torch.full((rows, n), -7.0, dtype=TORCH[out_dtype], device="cuda")
+    tfe.tfe_quantized_matmul(ac, asc, wc, wsc, rows, n, dim, out, out_dtype, n, H.cur_stream())
+    a = O.fp8_values(ac.cpu().numpy(), asc.cpu().numpy(), 1)
+    w = O.fp8_values(wc.cpu().numpy(), wsc.cpu().numpy(), 128)
+    some = np.unique(np.concatenate([np.arange(0, n, 97), np.arange(n - 300, n), np.arange(300)]))
+    at = torch.from_numpy(some).cuda()
+    check_product(out[:, at], a, w[some], out_dtype)
+
+
+@pytest.mark.parametrize("out_dtype", [F32, BF16])
+@pytest.mark.parametrize("rows", [3, 100])
+def test_extreme_scales(rows, out_dtype):
+    """Blocks at either end of the scales: hidden states of 1e-36 and of 1e30 under weights of
+    1e30 and 1e-30."""
+    rng = np.random.default_rng(rows)
+    x = rng.uniform(0.5, 1, (rows, 256)) * np.where(np.arange(rows)[:, None] % 2 == 0, 1e-36, 1e30)
+    w = rng.uniform(-1, 1, (200, 256)) * np.where(np.arange(256) < 128, 1e30, 1e-30)
+    ac, asc, seen = quantize(x, F32, 1)
+    wc, wsc, _ = quantize(w, F32, 128)
+    out = torch.empty((rows, 200), dtype=TORCH[out_dtype], device="cuda")
+    x[1::2, :128] = 0
+    ac, asc, _ = quantize(x, F32, 1)
+    tfe.tfe_quantized_matmul(ac, asc, wc, wsc, rows, 200, 256, out, out_dtype, 200, H.cur_stream())
+    check_product(out, O.fp8_values(ac.cpu().numpy(), asc.cpu().numpy(), 1),
+                  O.fp8_values(wc.cpu().numpy(), wsc.cpu().numpy(), 128), out_dtype)

@@ -6,8 +6,8 @@ the exponential is within 2^-23 and the weight rounded by half a unit of 2^31:
 below 4.2e-6 for weights that matter.  Where every comparison that an answer
 rests on is decided by more than 5e-6 of what it compares, the token has to be
 the oracle's and its probability within 1e-5.  Elsewhere (the far tail's steps are
-smaller than that) it has to lie, in the order, between the oracle's answers for
-settings and u moved by 1e-5 to either side."""
+smaller than that) it has to lie, in the order of weights known to their error,
+between the oracle's answers for settings and u moved by 1e-5 to either side."""
 import numpy as np
 import pytest
 import torch
@@ -22,6 +22,7 @@ pytestmark = pytest.mark.gpu
 F32, BF16 = tfe.TFE_F32, tfe.TFE_BF16
 TORCH = {F32: torch.float32, BF16: torch.bfloat16}
 CLEAR = 5e-6
+WEIGHT = 4.2e-6  # a weight's relative error
 
 
 class Out:
@@ -70,12 +71,12 @@ def check(l, dtype, T=None, k=None, p=None, m=None, u=None, pad=0):
             assert token[r] == want, (r, token[r], want, margin)
             assert abs(prob[r] - wp) <= 1e-5 * wp, (r, prob[r], wp)
             continue
-        order = np.empty(vocab, int)
-        order[np.lexsort((np.arange(vocab), -seen[r].astype(float)))] = np.arange(vocab)
-        near = [order[O.sample(seen[r], at[0], at[1], at[2] * (1 + i * 1e-5) if at[2] < 1 else 1.0,
-                               at[3] * (1 + j * 1e-5), at[4] + n * 1e-5)[0]]
+        near = [O.sample(seen[r], at[0], at[1], at[2] * (1 + i * 1e-5) if at[2] < 1 else 1.0,
+                         at[3] * (1 + j * 1e-5), at[4] + n * 1e-5)[0]
                 for i in (-1, 1) for j in (-1, 1) for n in (-1, 1)]
-        assert min(near) <= order[token[r]] <= max(near), (r, token[r], want, margin)
+        l64 = seen[r].astype(float)
+        w = np.exp((l64[near] - l64[token[r]]) / at[0])
+        assert w.min() <= 1 + 2 * WEIGHT and w.max() >= 1 - 2 * WEIGHT, (r, token[r], want, margin)
 
 
 def language(seed, rows, vocab, sigma=1.5):
@@ -279,3 +280,61 @@ def test_no_rows_and_no_probabilities():
     tfe.tfe_sample(t, F32, ld, 3, 100, None, None, None, None, dev([0.2, 0.5, 0.8], np.float32), token, None,
                    torch.empty(max(16, size), dtype=torch.uint8, device="cuda"), size, H.cur_stream())
     np.testing.assert_array_equal(token.cpu().numpy(), want)
+
+
+@pytest.mark.parametrize("vocab", [2999, 70001])
+@pytest.mark.parametrize("dtype", [F32, BF16])
+def test_many_rows_of_every_kind(vocab, dtype):
+    """Batches whose rows each have a block of their own: masks, infinities, NaN, flat and
+    narrow rows, logits near zero, beyond 256 and of the type's lowest value, with every
+    combination of filters."""
+    kinds, rows = 12, 132
+    rng = np.random.default_rng(vocab)
+    l = language(30, rows, vocab)
+    kind = np.arange(rows) // 11 % kinds
+    for r in range(rows):
+        k = kind[r]
+        if k == 1:
+            l[r] = 1.25
+        elif k == 2:
+            l[r, rng.random(vocab) < 0.7] = -np.inf
+        elif k == 3:
+            l[r, ::3] = np.nan
+        elif k == 4:
+            l[r, vocab // 3:] = torch.finfo(TORCH[dtype]).min
+        elif k == 5:
+            l[r] = rng.standard_normal(vocab) * 2e-3       # small ones alone
+        elif k == 6:
+            l[r] = rng.standard_normal(vocab) * 0.02       # around zero
+        elif k == 7:
+            l[r] += 300.0                                  # beyond the binned range
+        elif k == 8:
+            l[r] -= 300.0
+        elif k == 9:
+            l[r] = np.round(l[r])                          # heavy ties
+        elif k == 10:
+            l[r] = -np.abs(l[r]) - 1.0                     # no positive one
+    T, k, p, m = settings(31, rows, vocab)
+    T = np.where(kind == 11, 8.0, T)  # hot: the tail's weights matter
+    check(l, dtype, T, k, p, m, pad=vocab % 3)
+    t, ld = tensor(l, dtype)
+    u = rng.random(rows)
+    token, prob = draw(t, dtype, ld, rows, vocab, T, k, p, m, u)
+    for r0 in range(0, rows, 44):  # fewer rows: split over blocks instead
+        at = slice(r0, r0 + 44)
+        tk, pr = draw(t[at].contiguous(), dtype, ld, 44, vocab, T[at], k[at], p[at], m[at], u[at])
+        np.testing.assert_array_equal(tk, token[at])
+        np.testing.assert_array_equal(pr, prob[at])
+
+
+def test_many_rows_without_a_token():
+    rows = 140
+    l = np.full((rows, 300), -np.inf)
+    l[1::2] = np.nan
+    l[7, 3] = 2.0
+    for dtype in (F32, BF16):
+        t, ld = tensor(l, dtype)
+        token, prob = draw(t, dtype, ld, rows, 300, u=np.full(rows, 0.5))
+        assert token[7] == 3 and prob[7] == 1
+        rest = np.arange(rows) != 7
+        assert (token[rest] == -1).all() and (prob[rest] == 0).all()
