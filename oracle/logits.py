@@ -99,6 +99,11 @@ def sample(l, T, top_k, top_p, min_p, u):
     near = [abs(at - edges[0])] if n > 0 else []
     near += [abs(at - edges[1])] if edges[1] < z else []
     margin = min([margin] + [x / z for x in near])
+    # Its place among its neighbours: both weights of a comparison are off, so a gap
+    # counts as 1 / 1.7 of itself; equal logits stand in the order of their tokens.
+    for i in (n - 1, n + 1):
+        if 0 <= i < w.size and w[i] > 0 and same[i] != same[n]:
+            margin = min(margin, abs(w[i] - w[n]) / w[n] / 1.7)
     return int(order[n]), w[n] / z, margin
 
 
