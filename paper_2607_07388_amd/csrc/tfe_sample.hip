@@ -905,7 +905,7 @@ __global__ __launch_bounds__(kThreads, 4) void k_row(SampleArgs a) {
 // the kernel's end is the barrier), and a block a row finishes.
 constexpr uint32_t kMaxParts = 64;
 constexpr uint32_t kList = 8192, kPartList = 2048;
-constexpr int kMaxThreads = 256, kHistThreads = 512, kCollectThreads = 256, kFinishThreads = 1024;
+constexpr int kMaxThreads = 512, kHistThreads = 1024, kCollectThreads = 512, kFinishThreads = 1024;
 struct Part {  // a row's workspace
   unsigned long long hist[kBins];
   unsigned long long list[kList];
