@@ -10,8 +10,8 @@
 // A row is split into parts of up to 2048 16-byte vectors, each a block of 256
 // threads with eight vectors a thread in registers: many small blocks keep more
 // of memory's latency hidden than few large ones (512 rows of 151936 bfloat16,
-// loss alone: 33 us; one block of 1024 threads a row, the next row loaded while
-// one is worked on: 41).
+// loss alone: 30 us, 26 of them k_sum at 6.0 TB/s; one block of 1024 threads a row,
+// the next row loaded while one is worked on: 41).
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
@@ -300,7 +300,7 @@ __global__ __launch_bounds__(kThreads, 8) void k_loss(DistillArgs a, uint32_t pa
   if (threadIdx.x == 0) write_loss(a, row, q, lse_of(a, r));
 }
 
-// The gradient from a known log-sum-exp.
+// The gradient from a known log-sum-exp.  1023 x 40001 float32: 68 us, 4.8 TB/s.
 template <int DT, int TDT>
 __global__ __launch_bounds__(kThreads, 8) void k_grad(DistillArgs a) {
   __shared__ Shared sh;
@@ -326,6 +326,7 @@ __global__ __launch_bounds__(kThreads, 8) void k_grad(DistillArgs a) {
 // most 248, and the device has room for 1536 blocks: another one starts, until
 // the rows are whole.  The wait is bounded all the same; running out would
 // leave NaN.  (One counter alone is the limit at about 100 parts a us.)
+//   4096 x 151936 bfloat16: 450 us, 5.5 TB/s; as two launches over the same parts 645.
 //   In place: a part writes its logits' gradient only after every part, part 0
 // with all the listed tokens' logits among them, has published.
 constexpr uint32_t kPolls = 1u << 18;

@@ -17,6 +17,7 @@
 // maximum, the histogram, the collection.
 // Bound by the logits' bytes for the first pass, then by the weights' arithmetic
 // (about 27 instruction slots a logit) and the LDS additions of the second.
+// 151936 float32 logits a row: 1 row 24 us, 64 rows 53, 256 rows 100.
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
@@ -570,6 +571,7 @@ __device__ void no_token(const SampleArgs& a, uint32_t row) {
 // Logits below 2^-8 in magnitude ("small") are kept one by one for their sum; a
 // row whose answer they touch, or that has a logit of 2^8 or more, or one of
 // -2^8 or less with a weight, takes the way of float32 rows.
+// 256 rows of 151936, top-p: 52 us, that way 95; 300 of 33333: 30 and 41.
 constexpr uint32_t kFirst = 119u << 7, kHalf = 2048, kSmall = kHalf;  // the bits of 2^-8
 static_assert(2 * kHalf == kBins, "the values' counts lie where the edges do");
 __device__ __forceinline__ float value_of(uint32_t q) {  // of a bin other than kSmall
