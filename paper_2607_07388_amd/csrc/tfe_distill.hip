@@ -195,7 +195,7 @@ constexpr uint32_t kPart = kThreads * kVectors;
 constexpr uint32_t kMaxParts = kLogitsMaxVocab / 4 / kPart;
 static_assert(kMaxParts <= kThreads, "a part's sum a thread");
 
-// Workspace: eight counters, then a record for each row of a launch: its parts' running
+// Workspace: a counter for each queue, then a record for each row of a launch: its parts' running
 // sums (m in the low word, s in the high one).
 struct Record {
   unsigned long long r[kMaxParts];
@@ -319,13 +319,15 @@ __global__ __launch_bounds__(kThreads, 8) void k_grad(DistillArgs a) {
 // Both at once, the logits read once.  The parts of a row exchange their sums
 // while each keeps its logits in registers: a part publishes its sum and waits
 // for the others'.
-//   Every wait ends: rows are dealt to eight queues, and a block takes the next
-// part of its queue from a counter when it starts.  A queue's blocks that wait
-// are therefore all of its newest row (at most 31 of 32; those of its earlier
-// rows have all their parts running and need nobody else), eight queues' at
-// most 248, and the device has room for 1536 blocks: another one starts, until
-// the rows are whole.  The wait is bounded all the same; running out would
-// leave NaN.  (One counter alone is the limit at about 100 parts a us.)
+//   Every wait ends: rows are dealt to queues, and a block takes the next part
+// of its queue from a counter when it starts.  A queue's blocks that wait are
+// therefore all of its newest row (fewer than the row has parts; those of its
+// earlier rows have all their parts running and need nobody else).  There are
+// so few queues (queues_of) that theirs together are fewer than the compute
+// units, each of which has room for six: another block starts, until the rows
+// are whole, also while four streams do this at once.  The wait is bounded all
+// the same; running out would leave NaN.  (One counter alone is the limit at
+// about 100 parts a us.)
 //   4096 x 151936 bfloat16: 450 us, 5.5 TB/s; as two launches over the same parts 645.
 //   In place: a part writes its logits' gradient only after every part, part 0
 // with all the listed tokens' logits among them, has published.
@@ -336,13 +338,14 @@ __global__ __launch_bounds__(256) void k_unset(DistillArgs a, uint32_t parts) {
   if (row < a.rows) record_of(a, row).r[i - row * parts] = kUnset;
 }
 template <int DT, int TDT, bool GRAD>
-__global__ __launch_bounds__(kThreads, 6) void k_joined(DistillArgs a, uint32_t parts) {
+__global__ __launch_bounds__(kThreads, 6) void k_joined(DistillArgs a, uint32_t parts, uint32_t queues) {
   __shared__ Shared sh;
   const uint32_t t = threadIdx.x;
   const float c = a.inv_tau * kLog2e;
   uint32_t row = blockIdx.x, part = 0;
   if (parts > 1) {
-    const uint32_t queue = blockIdx.x / kQueues % kQueues;
+    // Eight neighbouring blocks, on the eight XCDs, share a queue.
+    const uint32_t queue = blockIdx.x / 8 % queues;
     if (t == 0)
       sh.ticket = __hip_atomic_fetch_add(counter_of(a, queue), 1u, __ATOMIC_RELAXED,
                                          __HIP_MEMORY_SCOPE_AGENT);
@@ -350,7 +353,7 @@ __global__ __launch_bounds__(kThreads, 6) void k_joined(DistillArgs a, uint32_t 
     const uint32_t ticket = __builtin_amdgcn_readfirstlane(sh.ticket);
     row = ticket / parts;
     part = ticket - row * parts;
-    row = row * kQueues + queue;
+    row = row * queues + queue;
     if (row >= a.rows) return;
   }
   const char* x = logits_of<DT>(a, row);
@@ -412,6 +415,11 @@ DistillArgs rows_from(DistillArgs a, uint32_t r0, uint32_t n, int dtype, int tdt
 // Rows of a launch: the grid's second axis, and 2^20 parts.
 uint32_t launch_rows(uint32_t parts) { return std::min(32768u, (1u << 20) / parts); }
 
+// Queues of the joined parts: the blocks that can wait are fewer than the compute units.
+uint32_t queues_of(uint32_t parts) {
+  return std::max(1u, std::min(kQueues, (uint32_t)compute_units() / parts));
+}
+
 template <int DT, int TDT, bool LOSS, bool GRAD> hipError_t launch(const DistillArgs& a, hipStream_t s) {
   const uint32_t parts = parts_of(DT, (int32_t)a.vocab), most = launch_rows(parts);
   const dim3 block(kThreads);
@@ -421,8 +429,9 @@ template <int DT, int TDT, bool LOSS, bool GRAD> hipError_t launch(const Distill
     if (LOSS && (GRAD || parts == 1)) {
       if (parts > 1) k_unset<<<dim3((n * parts + 255) / 256), dim3(256), 0, s>>>(b, parts);
       // As many blocks for each queue, and enough for the longest.
-      const uint32_t rounds = ((n + kQueues - 1) / kQueues * parts + kQueues - 1) / kQueues;
-      k_joined<DT, TDT, GRAD><<<dim3(parts > 1 ? rounds * kQueues * kQueues : n), block, 0, s>>>(b, parts);
+      const uint32_t queues = queues_of(parts);
+      const uint32_t rounds = ((n + queues - 1) / queues * parts + 7) / 8;
+      k_joined<DT, TDT, GRAD><<<dim3(parts > 1 ? rounds * 8 * queues : n), block, 0, s>>>(b, parts, queues);
     } else if (GRAD) {
       k_grad<DT, TDT><<<dim3(parts, n), block, 0, s>>>(b);
     } else {

@@ -451,14 +451,15 @@ __global__ __launch_bounds__(WN* WM * 64) void k_tiles(MatmulArgs a, uint32_t ti
       for (int m = 0; m < MT; ++m) acc[n][m] = f32x4{0.f, 0.f, 0.f, 0.f};
     const Tile next = find(cur.t + gridDim.x);
     for (uint32_t b = 0; b < kb; ++b) {
-      // The stage has arrived, and everybody is done with the other one.  A tile's
-      // first stage was asked for before the last tile's results were stored
-      // (more than eight stores a lane, and memory operations complete in
-      // order): those need not have landed.
+      // The stage has arrived, and everybody is done with the other one (its reads
+      // have returned: the count of LDS operations).  A tile's first stage was
+      // asked for before the last tile's results were stored (at least eight
+      // stores a lane, and memory operations complete in order): those need not
+      // have landed.
       if (stored)
-        asm volatile("s_waitcnt vmcnt(8)" ::: "memory");
+        asm volatile("s_waitcnt vmcnt(8) lgkmcnt(0)" ::: "memory");
       else
-        asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+        asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
       stored = false;
       __builtin_amdgcn_s_barrier();
       // The scales have come too; told here, or the compiler waits for them, and so
@@ -543,6 +544,7 @@ __global__ __launch_bounds__(WN* WM * 64) void k_tiles(MatmulArgs a, uint32_t ti
       // bfloat16: neighbouring lane rows exchange halves of two column tiles, so that
       // a lane stores 16 bytes and an instruction 64 of each row.
       static_assert(DT == TFE_F32 || NT % 2 == 0, "column tiles in pairs");
+      static_assert(NT * MT / 2 >= 8, "the next step's wait counts on eight stores");
       constexpr int ES = sizeof(typename Elem<DT>::T);
       const uint32_t cx = DT == TFE_F32 ? c0 : cur.n + wn + (g & 1) * 16 + (g >> 1) * 8;
       char* out = (char*)a.out + ((size_t)r0 * a.ldo + cx) * ES;
