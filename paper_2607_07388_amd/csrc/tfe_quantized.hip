@@ -365,7 +365,7 @@ __global__ __launch_bounds__(kSkinnyWaves * 64) void k_skinny(MatmulArgs a, Quan
 // products, float32 sums: 1.3e-8 of the result's size off on normal numbers).
 // bfloat16 results: the scaled 8-bit instruction, twice its rate; its sums are
 // off by about 1.4e-5 of the result's size, their rounding by 1.7e-3.
-// 2048 rows of 151936 x 1024 to bfloat16: 427 us, 1.5 PFLOP/s; the matrix cores
+// 2048 rows of 151936 x 1024 to bfloat16: 423 us, 1.5 PFLOP/s; the matrix cores
 // are busy a third of it (steps in lockstep; stores and loads add to them).
 #if defined(__HIP_DEVICE_COMPILE__)  // the host compiler has no buffer descriptors
 // Loads go through buffer descriptors: 32-bit offsets, and rows past a matrix'
@@ -386,7 +386,9 @@ __global__ __launch_bounds__(WN* WM * 64) void k_tiles(MatmulArgs a, uint32_t ti
   constexpr int LW = TN / 8 / WAVES, LX = TM / 8 / WAVES, STAGE = (TN + TM) * kFp8Block;
   static_assert(TN % (8 * WAVES) == 0 && TM % (8 * WAVES) == 0, "whole loads of either operand");
   static_assert(kFp8Block % (TN / WN) == 0 || (TN / WN) % kFp8Block == 0, "one scale of W a wave");
+  constexpr int PIECES = NT * 2;  // of 16 bytes, of a row of a wave's results in bfloat16
   __shared__ __attribute__((aligned(1024))) uint8_t lds[2 * STAGE];
+  __shared__ __attribute__((aligned(1024))) uint8_t turn[DT == TFE_BF16 ? WAVES * 16 * PIECES * 16 : 16];
   const uint32_t wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const uint32_t lane = threadIdx.x & 63, i = lane & 15, g = lane >> 4;
   const uint32_t wn = (wave % WN) * (TN / WN), wm = (wave / WN) * (TM / WM);
@@ -541,28 +543,52 @@ __global__ __launch_bounds__(WN* WM * 64) void k_tiles(MatmulArgs a, uint32_t ti
     }
     const uint32_t r0 = cur.m + wm + i, c0 = cur.n + wn + g * 4;
     if (cur.n + TN <= a.n && cur.m + TM <= a.rows) {
-      // bfloat16: neighbouring lane rows exchange halves of two column tiles, so that
-      // a lane stores 16 bytes and an instruction 64 of each row.
-      static_assert(DT == TFE_F32 || NT % 2 == 0, "column tiles in pairs");
-      static_assert(NT * MT / 2 >= 8, "the next step's wait counts on eight stores");
-      constexpr int ES = sizeof(typename Elem<DT>::T);
-      const uint32_t cx = DT == TFE_F32 ? c0 : cur.n + wn + (g & 1) * 16 + (g >> 1) * 8;
-      char* out = (char*)a.out + ((size_t)r0 * a.ldo + cx) * ES;
+      if constexpr (DT == TFE_F32) {
+        static_assert(NT * MT >= 8, "the next step's wait counts on eight stores");
+        float* out = (float*)a.out + (size_t)r0 * a.ldo + c0;
 #pragma unroll
-      for (int m = 0; m < MT; ++m) {
-        if constexpr (DT == TFE_F32) {
+        for (int m = 0; m < MT; ++m) {
 #pragma unroll
-          for (int n = 0; n < NT; ++n) store4_at<DT>(out + n * 16 * ES, acc[n][m]);
-        } else {
+          for (int n = 0; n < NT; ++n) store4_at<DT>((char*)(out + n * 16), acc[n][m]);
+          out += (size_t)a.ldo * 16;
+        }
+      } else {
+        // Sixteen rows at a time turn in the wave's own LDS, so that an instruction
+        // writes whole pieces of 128 or 256 bytes: the results of a lane's row and
+        // its three neighbours' are 64, and at an odd pitch two parts of lines.  us,
+        // so / at once: 257 x 40001 x 1000 24 / 29, 1024 x 151937 x 256 134 / 204,
+        // 1024 x 151936 x 256 97 / 109, 2048 x 151936 x 1024 the same, 256 rows of it
+        // 76 / 74.  float32 gains nothing from it (512 x 151937 x 1024: 242 / 241).
+        constexpr int ROWS = 64 / PIECES;  // of an instruction
+        static_assert(NT % 2 == 0, "column tiles in pairs");
+        static_assert(MT * 16 / ROWS >= 8, "the next step's wait counts on eight stores");
+        uint8_t* mine = turn + wave * (16 * PIECES * 16);
+        // Pieces of 16 bytes are exchanged by row, as the operands' are.
+        auto place = [&](uint32_t row, uint32_t piece) {
+          return (u32x4*)(mine + (row * PIECES + (piece ^ (row & (PIECES - 1)))) * 16);
+        };
+        uint32_t own = lane;
+        asm volatile("" : "+v"(own));  // the addresses are worked out here, not kept over the steps
+        const uint32_t row = own / PIECES, piece = own % PIECES, oi = own & 15, og = own >> 4;
+        uint16_t* out = (uint16_t*)a.out + (size_t)(cur.m + wm + row) * a.ldo + cur.n + wn + piece * 8;
+#pragma unroll
+        for (int m = 0; m < MT; ++m) {
+          // Neighbouring lane rows exchange halves of two column tiles: 16 bytes a lane.
 #pragma unroll
           for (int n = 0; n < NT; n += 2) {
             const f32x4 p = acc[n][m], q = acc[n + 1][m];
             const auto lo = __builtin_amdgcn_permlane16_swap(pack2(p[0], p[1]), pack2(q[0], q[1]), false, false);
             const auto hi = __builtin_amdgcn_permlane16_swap(pack2(p[2], p[3]), pack2(q[2], q[3]), false, false);
-            *(u32x4_a2*)(out + n * 16 * ES) = u32x4{lo[0], hi[0], lo[1], hi[1]};
+            *place(oi, n * 2 + (og & 1) * 2 + (og >> 1)) = u32x4{lo[0], hi[0], lo[1], hi[1]};
           }
+          __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+#pragma unroll
+          for (int k = 0; k < 16; k += ROWS) {
+            *(u32x4_a2*)out = *place(row + k, piece);
+            out += (size_t)a.ldo * ROWS;
+          }
+          __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
         }
-        out += (size_t)a.ldo * 16 * ES;
       }
       stored = true;
     } else {
