@@ -682,9 +682,9 @@ hipError_t launch_fp8_matmul(const MatmulArgs& a, int out_dtype, hipStream_t s) 
     return out_dtype == TFE_F32 ? skinny_rows<kCodes, TFE_F32>(a, QuantizeArgs{}, s)
                                 : skinny_rows<kCodes, TFE_BF16>(a, QuantizeArgs{}, s);
   // Large tiles where they fill the device and waste few rows.  us at 151936 x 1024,
-  // 256 x 256 / 128 x 128: bfloat16 256 rows 81 / 76, 512 135 / 144, 1024 254 / 274, 2048
-  // 454 / 510; float32 256 rows 134 / 135, 512 234 / 241, 1024 425 / 448.  257 x 40001 x 1000
-  // (three row tiles of 128 against two of 256): 59 / 29.
+  // 256 x 256 / 128 x 128: bfloat16 256 rows 77 / 74, 512 127 / 149, 1024 243 / 285, 2048
+  // 445 / 541; float32 256 rows 134 / 135, 512 234 / 241, 1024 425 / 448.  257 x 40001 x 1000
+  // (three row tiles of 128 against two of 256): 37 / 24.
   const uint32_t r256 = (a.rows + 255) / 256, r128 = (a.rows + 127) / 128;
   const bool fills = (uint64_t)((a.n + 255) / 256) * r256 >= (uint64_t)compute_units() * 2;
   if (fills && a.rows > 256 && r256 * 2 * 92 <= r128 * 100)
