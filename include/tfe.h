@@ -374,10 +374,9 @@ tfe_status tfe_quantize(const void *x, int32_t dtype, int64_t ldx, int64_t rows,
 
 /* out[r, n] = sum over k of A[r, k] W[n, k], for A laid out with block_rows 1
  * and W with block_rows 128 (scales w_scales); out DEVICE [rows x out_dim] of
- * out_dtype.  Products are exact; float32 results are accumulated in float32.
- * bfloat16 results may be accumulated by the 8-bit matrix instruction, whose
- * sums are off by about 1.4e-5 of a result of normally distributed terms (at
- * worst 2^-12 of the terms' magnitudes was seen), far below their rounding.
+ * out_dtype.  Products are exact and accumulated in float32; bfloat16 results are
+ * the float32 ones rounded to nearest even, and a row's results do not depend on
+ * the rows it comes with.
  * Numbers below 2^-126 may count as 0.
  * rows <= 2^20, 1 <= out_dim <= 2^20, dim <= 65536. */
 tfe_status tfe_quantized_matmul(const uint8_t *a, const uint8_t *a_scales, const uint8_t *w,

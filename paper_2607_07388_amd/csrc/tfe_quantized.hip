@@ -361,12 +361,15 @@ __global__ __launch_bounds__(kSkinnyWaves * 64) void k_skinny(MatmulArgs a, Quan
 // one's results are written.
 // In LDS a row's eight 16-byte pieces are exchanged by its number mod 8, so that
 // the 8 lanes that an LDS cycle serves read different banks.
-// float32 results: the bfloat16 instruction, codes widened in registers (exact
-// products, float32 sums: 1.3e-8 of the result's size off on normal numbers).
-// bfloat16 results: the scaled 8-bit instruction, twice its rate; its sums are
-// off by about 1.4e-5 of the result's size, their rounding by 1.7e-3.
-// 2048 rows of 151936 x 1024 to bfloat16: 423 us, 1.5 PFLOP/s; the matrix cores
-// are busy a third of it (steps in lockstep; stores and loads add to them).
+// Sums are float32 whatever the results' type: the bfloat16 instruction on codes
+// widened in registers (exact products; on normal numbers 1.3e-8 of the result's
+// size off), in k_skinny's order, so that a row's results do not depend on the
+// rows it comes with and bfloat16 ones are the float32 ones rounded.  The scaled
+// 8-bit instruction takes 412 us where this takes 635, but its sums are off by
+// 1.4e-5 of a normal result and up to 2^-12 of the terms' magnitudes: a result
+// small against its terms is lost.
+// 2048 rows of 151936 x 1024 to bfloat16: 635 us, 1.0 PFLOP/s; a wave widens each
+// code it multiplies, 192 conversions beside 128 products a step.
 #if defined(__HIP_DEVICE_COMPILE__)  // the host compiler has no buffer descriptors
 // Loads go through buffer descriptors: 32-bit offsets, and rows past a matrix'
 // last read as zeros (the whole offset is in the vector register, so that the
@@ -489,52 +492,22 @@ __global__ __launch_bounds__(WN* WM * 64) void k_tiles(MatmulArgs a, uint32_t ti
         scales(next, 0, sw_next, sx_next);
       }
       __builtin_amdgcn_sched_barrier(0);
-      if constexpr (DT == TFE_BF16) {
-        typedef int v8i __attribute__((ext_vector_type(8)));
-        auto operand = [&](const uint8_t* p, const uint8_t* p2, int k) {
-          const u32x4 lo = *(const u32x4*)(p + k * 16 * kFp8Block);
-          const u32x4 hi = *(const u32x4*)(p2 + k * 16 * kFp8Block);
-          return v8i{(int)lo[0], (int)lo[1], (int)lo[2], (int)lo[3],
-                     (int)hi[0], (int)hi[1], (int)hi[2], (int)hi[3]};
-        };
-        v8i xv[MT], wv = operand(lw, lw2, 0);
+      const float fw = scale_of(sw & 255u);
 #pragma unroll
-        for (int m = 0; m < MT; ++m) xv[m] = operand(lx, lx2, m);
+      for (int q = 0; q < 4; ++q) {
+        auto operand = [&](const uint8_t* p, const uint8_t* p2, int k, float f) {
+          const u32x2 v = *(const u32x2*)((q < 2 ? p : p2) + (q & 1) * 8 + k * 16 * kFp8Block);
+          return widen(v[0], v[1], f);
+        };
+        bf16x8 xv[MT];
+#pragma unroll
+        for (int m = 0; m < MT; ++m) xv[m] = operand(lx, lx2, m, scale_of(sx[m] & 255u));
 #pragma unroll
         for (int n = 0; n < NT; ++n) {
-          v8i ahead;
-          if (n + 1 < NT) ahead = operand(lw, lw2, n + 1);
+          const bf16x8 wv = operand(lw, lw2, n, fw);
 #pragma unroll
           for (int m = 0; m < MT; ++m)
-            acc[n][m] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(
-                wv, xv[m], acc[n][m], 0, 0, 0, (int)sw, 0, (int)sx[m]);
-          if (n + 1 < NT) wv = ahead;
-        }
-        // The next tile's operand is read while this one's is multiplied.
-        __builtin_amdgcn_sched_group_barrier(0x100, 2 * MT + 4, 0);
-#pragma unroll
-        for (int n = 0; n < NT; ++n) {
-          __builtin_amdgcn_sched_group_barrier(0x008, MT, 0);
-          if (n + 2 < NT) __builtin_amdgcn_sched_group_barrier(0x100, 2, 0);
-        }
-      } else {
-        const float fw = scale_of(sw & 255u);
-#pragma unroll
-        for (int q = 0; q < 4; ++q) {
-          auto operand = [&](const uint8_t* p, const uint8_t* p2, int k, float f) {
-            const u32x2 v = *(const u32x2*)((q < 2 ? p : p2) + (q & 1) * 8 + k * 16 * kFp8Block);
-            return widen(v[0], v[1], f);
-          };
-          bf16x8 xv[MT];
-#pragma unroll
-          for (int m = 0; m < MT; ++m) xv[m] = operand(lx, lx2, m, scale_of(sx[m] & 255u));
-#pragma unroll
-          for (int n = 0; n < NT; ++n) {
-            const bf16x8 wv = operand(lw, lw2, n, fw);
-#pragma unroll
-            for (int m = 0; m < MT; ++m)
-              acc[n][m] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(wv, xv[m], acc[n][m], 0, 0, 0);
-          }
+            acc[n][m] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(wv, xv[m], acc[n][m], 0, 0, 0);
         }
       }
       sw >>= 8;
@@ -556,9 +529,9 @@ __global__ __launch_bounds__(WN* WM * 64) void k_tiles(MatmulArgs a, uint32_t ti
         // Sixteen rows at a time turn in the wave's own LDS, so that an instruction
         // writes whole pieces of 128 or 256 bytes: the results of a lane's row and
         // its three neighbours' are 64, and at an odd pitch two parts of lines.  us,
-        // so / at once: 257 x 40001 x 1000 24 / 29, 1024 x 151937 x 256 134 / 204,
-        // 1024 x 151936 x 256 97 / 109, 2048 x 151936 x 1024 the same, 256 rows of it
-        // 76 / 74.  float32 gains nothing from it (512 x 151937 x 1024: 242 / 241).
+        // so / at once: 257 x 40001 x 1000 42 / 48, 1024 x 151937 x 256 162 / 227,
+        // 1024 x 151936 x 256 123 / 161, 2048 x 151936 x 1024 637 / 746, 256 rows of it
+        // 99 / 101.  float32 gains nothing from it (512 x 151937 x 1024: 242 / 241).
         constexpr int ROWS = 64 / PIECES;  // of an instruction
         static_assert(NT % 2 == 0, "column tiles in pairs");
         static_assert(MT * 16 / ROWS >= 8, "the next step's wait counts on eight stores");
@@ -682,9 +655,9 @@ hipError_t launch_fp8_matmul(const MatmulArgs& a, int out_dtype, hipStream_t s) 
     return out_dtype == TFE_F32 ? skinny_rows<kCodes, TFE_F32>(a, QuantizeArgs{}, s)
                                 : skinny_rows<kCodes, TFE_BF16>(a, QuantizeArgs{}, s);
   // Large tiles where they fill the device and waste few rows.  us at 151936 x 1024,
-  // 256 x 256 / 128 x 128: bfloat16 256 rows 77 / 74, 512 127 / 149, 1024 243 / 285, 2048
-  // 445 / 541; float32 256 rows 134 / 135, 512 234 / 241, 1024 425 / 448.  257 x 40001 x 1000
-  // (three row tiles of 128 against two of 256): 37 / 24.
+  // 256 x 256 / 128 x 128: bfloat16 256 rows 110 / 101, 512 176 / 182, 1024 339 / 355, 2048
+  // 637 / 692; float32 256 rows 128 / 107, 512 199 / 196, 1024 376 / 379.  257 x 40001 x 1000
+  // (two row tiles of 256 against three of 128): 63 / 37.
   const uint32_t r256 = (a.rows + 255) / 256, r128 = (a.rows + 127) / 128;
   const bool fills = (uint64_t)((a.n + 255) / 256) * r256 >= (uint64_t)compute_units() * 2;
   if (fills && a.rows > 256 && r256 * 2 * 92 <= r128 * 100)
