@@ -115,9 +115,10 @@ struct Teacher {
   float gap;        // sum_k q_k (log q_k - s_k / tau)
 };
 
-// Joins the block's running sums and evaluates the entries; two barriers.  Every
-// thread gets the row's sum (if `r` is given) and its entry's q; sh.q and sh.id
-// hold the entries' after the caller's next barrier.
+// Joins the block's running sums and evaluates the entries; two barriers.  Nobody
+// may still be reading `sh` from an earlier use.  Every thread gets the row's
+// sum (if `r` is given) and its entry's q; sh.q and sh.id hold the entries'
+// after the caller's next barrier.
 __device__ __forceinline__ Teacher join_block(const DistillArgs& a, const Entry& e, Shared& sh,
                                               Running* r, float c) {
   const uint32_t wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
@@ -230,7 +231,7 @@ template <int DT> struct Share {
     for (int k = 0; k < kVectors; ++k)
       if (has(k)) v[k] = load_stream<DT>(x, first + k * kThreads);
   }
-  // The block's running sum, in thread 0.
+  // The block's running sum, in every thread; `sh` may be reused after the last barrier.
   __device__ __forceinline__ Running sum(const DistillArgs& a, const char* x, bool last, float c,
                                          Shared& sh) const {
     Running r{-INFINITY, 0.f};
@@ -249,6 +250,7 @@ template <int DT> struct Share {
     __syncthreads();
     r = Running{sh.m[0], sh.s[0]};
     for (int w = 1; w < kWaves; ++w) r = join(r, Running{sh.m[w], sh.s[w]}, c);
+    __syncthreads();  // all have read: join_block writes the same words
     return r;
   }
   // The part's gradient; the listed tokens among its logits last.
