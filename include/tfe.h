@@ -436,7 +436,8 @@ int64_t tfe_sample_workspace(int64_t rows, int32_t vocab); /* -1: bad size */
  *               loss; the row's gradient is multiplied by it.  Where it is 0 the
  *               gradient is 0 whatever the logits hold.
  *   grad        DEVICE of the student's dtype, [rows x vocab], pitch ldg; may be
- *               `logits` itself when ldg = ld.
+ *               `logits` itself when ldg = ld (tfe_distill_loss_grad then reads
+ *               long rows twice), and may not overlap it otherwise.
  * tfe_distill_grad takes lse as tfe_distill_loss wrote it. */
 tfe_status tfe_distill_loss(const void *logits, int32_t dtype, int64_t ld, int64_t rows,
                             int32_t vocab, const int32_t *teacher_ids, const void *teacher_logits,

@@ -41,13 +41,14 @@ __device__ __forceinline__ Running join(Running a, Running b, float c) {
   Running r;
   r.m = fmaxf(a.m, b.m);
   const float ref = finite_max(r.m);
-  r.s = a.s * exp2_hw((a.m - ref) * c) + b.s * exp2_hw((b.m - ref) * c);
+  r.s = fmaf(a.s, exp2_hw((a.m - ref) * c), b.s * exp2_hw((b.m - ref) * c));
   return r;
 }
 __device__ __forceinline__ float lse_of(const DistillArgs& a, Running r) {
   return fmaf(r.m, a.inv_tau, log2_hw(r.s) * kLn2);
 }
-// One vector's logits into r.
+// One vector's logits into r.  (Fused operations are written out here and in
+// join: a sum has the same bits wherever it is computed.)
 template <int DT> __device__ __forceinline__ void add(Running& r, u32x4 q, float c) {
   constexpr int N = Elem<DT>::N;
   float x[N];
@@ -56,9 +57,9 @@ template <int DT> __device__ __forceinline__ void add(Running& r, u32x4 q, float
 #pragma unroll
   for (int i = 0; i < N; ++i) m = fmaxf(m, x[i]);
   const float ref = finite_max(m);
-  float s = r.s * exp2_hw((r.m - ref) * c);
+  float s = fmaf(r.s, exp2_hw((r.m - ref) * c), exp2_hw((x[0] - ref) * c));
 #pragma unroll
-  for (int i = 0; i < N; ++i) s += exp2_hw((x[i] - ref) * c);
+  for (int i = 1; i < N; ++i) s += exp2_hw((x[i] - ref) * c);
   r = Running{m, s};
 }
 __device__ __forceinline__ void add1(Running& r, float x, float c) {
@@ -107,6 +108,7 @@ struct Shared {
   int32_t id[kDistillMaxK];
   float m[kWaves], s[kWaves], t[kWaves], some[kWaves], x[kWaves], y[kWaves];
   uint32_t ticket;
+  unsigned long long missing;  // parts whose sums have not come
 };
 // What a row's entries come to.
 struct Teacher {
@@ -194,7 +196,7 @@ template <int DT> __device__ __forceinline__ char* grad_of(const DistillArgs& a,
 constexpr int kVectors = 8;  // of a thread
 constexpr uint32_t kPart = kThreads * kVectors;
 constexpr uint32_t kMaxParts = kLogitsMaxVocab / 4 / kPart;
-static_assert(kMaxParts <= kThreads, "a part's sum a thread");
+static_assert(kMaxParts <= 64, "a part's sum a lane of the first wave");
 
 // Workspace: a counter for each queue, then a record for each row of a launch: its parts' running
 // sums (m in the low word, s in the high one).
@@ -219,6 +221,41 @@ __device__ __forceinline__ Running unpacked(unsigned long long x) {
   return Running{__uint_as_float((uint32_t)x), __uint_as_float((uint32_t)(x >> 32))};
 }
 
+// The running sum of a block's logits from those of its threads (r, of whole
+// vectors) and the row's last few; in every thread.  `sh` may be reused after the
+// last barrier.
+template <int DT>
+__device__ __forceinline__ Running block_sum(const DistillArgs& a, Running r, const char* x, bool last,
+                                             float c, Shared& sh) {
+  if (last)
+    for (uint32_t i = a.vocab / Elem<DT>::N * Elem<DT>::N + threadIdx.x; i < a.vocab; i += kThreads)
+      add1(r, load1<DT>(x, i), c);
+#pragma unroll
+  for (int o = 32; o; o >>= 1) r = join(r, Running{__shfl_xor(r.m, o), __shfl_xor(r.s, o)}, c);
+  if ((threadIdx.x & 63) == 0) {
+    sh.m[threadIdx.x >> 6] = r.m;
+    sh.s[threadIdx.x >> 6] = r.s;
+  }
+  __syncthreads();
+  r = Running{sh.m[0], sh.s[0]};
+  for (int w = 1; w < kWaves; ++w) r = join(r, Running{sh.m[w], sh.s[w]}, c);
+  __syncthreads();  // all have read: join_block writes the same words
+  return r;
+}
+
+// The rest of a part's gradient: the row's last few logits, and the listed
+// tokens among the part's.
+template <int DT>
+__device__ __forceinline__ void finish_grad(const DistillArgs& a, const char* x, char* out, bool last,
+                                            bool zero, float lse, float f, const Entry& e, bool own,
+                                            const Shared& sh) {
+  if (last)
+    for (uint32_t i = a.vocab / Elem<DT>::N * Elem<DT>::N + threadIdx.x; i < a.vocab; i += kThreads)
+      store1<DT>(out, i, zero ? 0.f : scaled_softmax1(a, load1<DT>(x, i), lse, f));
+  __syncthreads();
+  if (!zero && own) write_entry<DT>(a, e, sh, out, lse, f);
+}
+
 // This thread's share of a part.
 template <int DT> struct Share {
   int first, nv;  // its first vector; the row's
@@ -231,45 +268,46 @@ template <int DT> struct Share {
     for (int k = 0; k < kVectors; ++k)
       if (has(k)) v[k] = load_stream<DT>(x, first + k * kThreads);
   }
-  // The block's running sum, in every thread; `sh` may be reused after the last barrier.
   __device__ __forceinline__ Running sum(const DistillArgs& a, const char* x, bool last, float c,
                                          Shared& sh) const {
     Running r{-INFINITY, 0.f};
 #pragma unroll
     for (int k = 0; k < kVectors; ++k)
       if (has(k)) add<DT>(r, v[k], c);
-    if (last)
-      for (uint32_t i = nv * Elem<DT>::N + threadIdx.x; i < a.vocab; i += kThreads)
-        add1(r, load1<DT>(x, i), c);
-#pragma unroll
-    for (int o = 32; o; o >>= 1) r = join(r, Running{__shfl_xor(r.m, o), __shfl_xor(r.s, o)}, c);
-    if ((threadIdx.x & 63) == 0) {
-      sh.m[threadIdx.x >> 6] = r.m;
-      sh.s[threadIdx.x >> 6] = r.s;
-    }
-    __syncthreads();
-    r = Running{sh.m[0], sh.s[0]};
-    for (int w = 1; w < kWaves; ++w) r = join(r, Running{sh.m[w], sh.s[w]}, c);
-    __syncthreads();  // all have read: join_block writes the same words
-    return r;
+    return block_sum<DT>(a, r, x, last, c, sh);
   }
   // The part's gradient; the listed tokens among its logits last.
-  template <class Own>
   __device__ __forceinline__ void grad(const DistillArgs& a, const char* x, char* out, bool last,
-                                       bool zero, float lse, float f, const Entry& e, Own own,
+                                       bool zero, float lse, float f, const Entry& e, bool own,
                                        const Shared& sh) const {
 #pragma unroll
     for (int k = 0; k < kVectors; ++k)
       if (has(k))
         store_stream<DT>(out, first + k * kThreads,
                          zero ? u32x4{0, 0, 0, 0} : scaled_softmax<DT>(a, v[k], lse, f));
-    if (last)
-      for (uint32_t i = nv * Elem<DT>::N + threadIdx.x; i < a.vocab; i += kThreads)
-        store1<DT>(out, i, zero ? 0.f : scaled_softmax1(a, load1<DT>(x, i), lse, f));
-    __syncthreads();
-    if (!zero && own) write_entry<DT>(a, e, sh, out, lse, f);
+    finish_grad<DT>(a, x, out, last, zero, lse, f, e, own, sh);
   }
 };
+// A part's running sum and its gradient, to the bit, without a place for its logits.
+template <int DT>
+__device__ __forceinline__ Running sum_of_part(const DistillArgs& a, const char* x, uint32_t part,
+                                               bool last, float c, Shared& sh) {
+  const uint32_t nv = a.vocab / Elem<DT>::N, first = part * kPart + threadIdx.x;
+  Running r{-INFINITY, 0.f};
+#pragma unroll 1
+  for (uint32_t i = first; i < min(nv, first + kPart); i += kThreads) add<DT>(r, load_vec<DT>(x, i), c);
+  return block_sum<DT>(a, r, x, last, c, sh);
+}
+template <int DT>
+__device__ __forceinline__ void grad_of_part(const DistillArgs& a, const char* x, char* out, uint32_t part,
+                                             bool last, bool zero, float lse, float f, const Entry& e,
+                                             bool own, const Shared& sh) {
+  const uint32_t nv = a.vocab / Elem<DT>::N, first = part * kPart + threadIdx.x;
+#pragma unroll 1
+  for (uint32_t i = first; i < min(nv, first + kPart); i += kThreads)
+    store_vec<DT>(out, i, zero ? u32x4{0, 0, 0, 0} : scaled_softmax<DT>(a, load_vec<DT>(x, i), lse, f));
+  finish_grad<DT>(a, x, out, last, zero, lse, f, e, own, sh);
+}
 template <int DT>
 __device__ __forceinline__ bool owns(const DistillArgs& a, const Entry& e, uint32_t part, uint32_t parts) {
   const uint32_t from = part * kPart * Elem<DT>::N;
@@ -321,26 +359,27 @@ __global__ __launch_bounds__(kThreads, 8) void k_grad(DistillArgs a) {
 // Both at once, the logits read once.  The parts of a row exchange their sums
 // while each keeps its logits in registers: a part publishes its sum and waits
 // for the others'.
-//   Every wait ends: rows are dealt to queues, and a block takes the next part
-// of its queue from a counter when it starts.  A queue's blocks that wait are
-// therefore all of its newest row (fewer than the row has parts; those of its
-// earlier rows have all their parts running and need nobody else).  There are
-// so few queues (queues_of) that theirs together are fewer than the compute
-// units, each of which has room for six: another block starts, until the rows
-// are whole, also while four streams do this at once.  The wait is bounded all
-// the same; running out would leave NaN.  (One counter alone is the limit at
+//   Nobody depends on a wait: sums that have not come after wait_limit polls, for
+// lack of room for their blocks beside other kernels, a block computes itself,
+// with the same bits.  For that the logits have to stay, so a gradient in their
+// place goes the way of two readings (k_sum, k_loss, k_grad).
+//   That waits are short: rows are dealt to queues, and a block takes the next
+// part of its queue from a counter when it starts.  A queue's blocks that wait
+// are therefore all of its newest row (fewer than the row has parts; those of
+// its earlier rows have all their parts running and need nobody else).  There
+// are so few queues (queues_of) that theirs together are fewer than the compute
+// units, each of which has room for six or more.  (One counter alone is the limit at
 // about 100 parts a us.)
 //   4096 x 151936 bfloat16: 450 us, 5.5 TB/s; as two launches over the same parts 645.
-//   In place: a part writes its logits' gradient only after every part, part 0
-// with all the listed tokens' logits among them, has published.
-constexpr uint32_t kPolls = 1u << 18;
 __global__ __launch_bounds__(256) void k_unset(DistillArgs a, uint32_t parts) {
   const uint32_t i = blockIdx.x * 256 + threadIdx.x, row = i / parts;
   if (i < kQueues) *counter_of(a, i) = 0;
   if (row < a.rows) record_of(a, row).r[i - row * parts] = kUnset;
 }
+// Blocks a compute unit: 4096 x 151936 bfloat16 506 us with six, 486 with seven; 2000 x
+// 40001 float32 126 and 133.
 template <int DT, int TDT, bool GRAD>
-__global__ __launch_bounds__(kThreads, 6) void k_joined(DistillArgs a, uint32_t parts, uint32_t queues) {
+__global__ __launch_bounds__(kThreads, DT == TFE_F32 ? 6 : 7) void k_joined(DistillArgs a, uint32_t parts, uint32_t queues) {
   __shared__ Shared sh;
   const uint32_t t = threadIdx.x;
   const float c = a.inv_tau * kLog2e;
@@ -366,25 +405,40 @@ __global__ __launch_bounds__(kThreads, 6) void k_joined(DistillArgs a, uint32_t 
   const bool own = owns<DT>(a, e, part, parts);
   if (part != 0 && own) e.s = load1<DT>(x, (uint32_t)e.id) * a.inv_tau;
   Running r = v.sum(a, x, last, c, sh);
+  unsigned long long got = packed(t == part ? r : Running{-INFINITY, 0.f});  // of part t
   if (parts > 1) {
     unsigned long long* slot = record_of(a, row).r;
-    // Every thread's loads are done before the sum is out.
-    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
-    __syncthreads();
     if (t == 0) __hip_atomic_store(slot + part, packed(r), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-    unsigned long long got = packed(Running{-INFINITY, 0.f});
-    if (t < parts) {
+    if (t < parts && t != part) {
       got = kUnset;
-      for (uint32_t n = 0; n < kPolls && got == kUnset; ++n) {
+      for (uint32_t n = 0; n < a.wait_limit && got == kUnset; ++n) {
         got = __hip_atomic_load(slot + t, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
         if (got == kUnset) __builtin_amdgcn_s_sleep(16);
       }
     }
-    r = unpacked(got);  // unset: NaN
-  } else if (t != 0) {
-    r = Running{-INFINITY, 0.f};
+    const unsigned long long missing = __builtin_amdgcn_ballot_w64(got == kUnset);
+    if (t == 0) sh.missing = missing;
   }
-  const Teacher q = join_block(a, e, sh, &r, c);
+  r = unpacked(got);
+  Teacher q = join_block(a, e, sh, &r, c);
+  if (parts > 1 && sh.missing) {
+    // Once more, with the sums that have not come; the part is read again, a vector
+    // at a time (held over this it would cost every block registers).
+    for (unsigned long long m = sh.missing; m; m &= m - 1) {
+      const uint32_t p = (uint32_t)__builtin_ctzll(m);
+      const Running other = sum_of_part<DT>(a, x, p, p == parts - 1, c, sh);
+      if (t == p) got = packed(other);
+    }
+    r = unpacked(got);
+    q = join_block(a, e, sh, &r, c);
+    const float lse = lse_of(a, r);
+    if (part == 0 && t == 0) write_loss(a, row, q, lse);
+    if (GRAD) {
+      const float g = a.weight ? a.weight[row] : 1.f;
+      grad_of_part<DT>(a, x, grad_of<DT>(a, row), part, last, !q.any || g == 0.f, lse, g * a.tau, e, own, sh);
+    }
+    return;
+  }
   const float lse = lse_of(a, r);
   if (part == 0 && t == 0) write_loss(a, row, q, lse);
   if (GRAD) {
@@ -428,18 +482,20 @@ template <int DT, int TDT, bool LOSS, bool GRAD> hipError_t launch(const Distill
   for (uint32_t r0 = 0; r0 < a.rows; r0 += most) {
     const uint32_t n = std::min(most, a.rows - r0);
     const DistillArgs b = rows_from(a, r0, n, DT, TDT);
-    if (LOSS && (GRAD || parts == 1)) {
+    const bool twice = parts > 1 && a.grad == a.logits;  // the gradient takes the logits' place
+    if (LOSS && (GRAD ? !twice : parts == 1)) {
       if (parts > 1) k_unset<<<dim3((n * parts + 255) / 256), dim3(256), 0, s>>>(b, parts);
       // As many blocks for each queue, and enough for the longest.
       const uint32_t queues = queues_of(parts);
       const uint32_t rounds = ((n + queues - 1) / queues * parts + 7) / 8;
       k_joined<DT, TDT, GRAD><<<dim3(parts > 1 ? rounds * 8 * queues : n), block, 0, s>>>(b, parts, queues);
-    } else if (GRAD) {
-      k_grad<DT, TDT><<<dim3(parts, n), block, 0, s>>>(b);
-    } else {
+      continue;
+    }
+    if (LOSS) {
       k_sum<DT, TDT><<<dim3(parts, n), block, 0, s>>>(b);
       k_loss<DT, TDT><<<dim3(n), block, 0, s>>>(b, parts);
     }
+    if (GRAD) k_grad<DT, TDT><<<dim3(parts, n), block, 0, s>>>(b);
   }
   return hipGetLastError();
 }

@@ -74,7 +74,12 @@ struct DistillArgs {
   void* grad;
   int64_t ldg;
   unsigned char* space;
+  uint32_t wait_limit;  // polls for the other parts' sums (kDistillWaitLimit)
 };
+// Polls before a block computes the sums that have not come itself (some
+// milliseconds).  The environment variable TFE_DISTILL_WAIT_LIMIT overrides it
+// per call, so that tests can force that from the host.
+constexpr uint32_t kDistillWaitLimit = 1u << 12;
 int64_t distill_space(int64_t rows, int32_t vocab);
 hipError_t launch_distill_loss(const DistillArgs& a, int dtype, int tdtype, hipStream_t s);
 hipError_t launch_distill_grad(const DistillArgs& a, int dtype, int tdtype, hipStream_t s);

@@ -3,6 +3,7 @@
 #include <hip/hip_runtime_api.h>
 #include <math.h>
 #include <stdint.h>
+#include <stdlib.h>
 
 #include <atomic>
 
@@ -329,6 +330,8 @@ tfe_status tfe_distill_loss_grad(const void* logits, int32_t dtype, int64_t ld, 
   a.grad = grad;
   a.ldg = ldg;
   a.space = (unsigned char*)workspace;
+  const char* wl = getenv("TFE_DISTILL_WAIT_LIMIT");
+  a.wait_limit = wl ? (uint32_t)strtoul(wl, nullptr, 0) : kDistillWaitLimit;
   return launched(launch_distill_loss_grad(a, dtype, teacher_dtype, (hipStream_t)stream),
                   "distillation launch");
 }
