@@ -428,10 +428,14 @@ int64_t tfe_sample_workspace(int64_t rows, int32_t vocab); /* -1: bad size */
  * Entries whose id lies outside [0, vocab) are padding: their logits may hold
  * anything.  A row without an entry of finite logit has loss 0 and gradient 0.
  * A student logit of -infinity has probability 0 (the loss is +infinity where
- * the teacher gives that token weight); +infinity or NaN makes its row NaN.  1 <= K <= 256, 1 <= vocab <= 2^18,
- * rows <= 2^20.  Softmax sums are float32.
+ * the teacher gives that token weight); where all are -infinity every
+ * probability is 0, the gradient -tau q.  A student logit of +infinity or NaN
+ * makes its row NaN.  Softmax sums are float32.  Probabilities are as exact in
+ * rows that lie far from 0 (masks of -1e9 or of the type's lowest value among
+ * them): where |lse| is above 4096 they do not rest on it.
+ * 1 <= K <= 256, 1 <= vocab <= 2^18, rows <= 2^20.
  *   loss, lse   DEVICE float [rows] (lse of the student's row, also where the
- *               loss is 0).
+ *               loss is 0; +-infinity beyond float32).
  *   grad_loss   DEVICE float [rows] or NULL (1): the gradient with respect to
  *               loss; the row's gradient is multiplied by it.  Where it is 0 the
  *               gradient is 0 whatever the logits hold.

@@ -114,9 +114,14 @@ def distill(s, ids, t, tau, weight):
     two distributions over the vocabulary."""
     s, t = np.asarray(s, np.float64) / tau, np.asarray(t, np.float64) / tau
     rows, vocab = s.shape
+    # log p from differences to the row's largest: 64 bits do not show a sum beside -1e38.
     top = s.max(1)
+    none = top == -np.inf  # the student leaves nothing: p is 0
     with np.errstate(invalid="ignore", divide="ignore"):
-        lse = top + np.log(np.exp(s - top[:, None]).sum(1))
+        logp = s - np.where(none, 0.0, top)[:, None]
+        total = np.log(np.exp(logp).sum(1))
+        lse = top + total
+        logp = np.where(none[:, None], -np.inf, logp - total[:, None])
     loss, grad = np.zeros(rows), np.zeros(s.shape)
     p, q = np.zeros(s.shape), np.zeros(s.shape)
     for r in range(rows):
@@ -128,9 +133,9 @@ def distill(s, ids, t, tau, weight):
         logq -= np.log(np.exp(logq).sum())
         qk = np.exp(logq)
         use = qk > 0
-        loss[r] = tau ** 2 * (qk[use] * (logq[use] - (s[r][at[use]] - lse[r]))).sum()
         np.add.at(q[r], at, qk)
-        p[r] = np.exp(s[r] - lse[r])
+        loss[r] = tau ** 2 * (qk[use] * (logq[use] - logp[r][at[use]])).sum()
+        p[r] = np.exp(logp[r])
         if weight[r] != 0:
             grad[r] = weight[r] * tau * (p[r] - q[r])
     return loss, lse, grad, p, q

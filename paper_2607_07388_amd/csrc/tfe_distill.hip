@@ -4,6 +4,8 @@
 //   lse = log sum_v exp(s_v / tau)       (running maximum and sum, one pass)
 //   loss = tau^2 sum_k q_k (log q_k - s_k / tau + lse)
 //   d loss / d s_v = tau (p_v - q_v),    p_v = exp(s_v / tau - lse)
+// A float32 lse far from zero does not show the sum: the loss uses the maximum
+// and the sum themselves, and p does in rows with |lse| above kFar.
 // Bound by the logits' bytes: the loss reads them, the gradient reads and
 // writes them, and both together read and write them once.
 //
@@ -47,6 +49,10 @@ __device__ __forceinline__ Running join(Running a, Running b, float c) {
 __device__ __forceinline__ float lse_of(const DistillArgs& a, Running r) {
   return fmaf(r.m, a.inv_tau, log2_hw(r.s) * kLn2);
 }
+// Rounded by 2^-12 there, and so p by as much of itself.  Every probability of a
+// row of -infinity is 0 (lse is -infinity; a row with NaN or +infinity has NaN).
+constexpr float kFar = 4096.f;
+__device__ __forceinline__ bool is_far(float lse) { return fabsf(lse) > kFar; }
 // One vector's logits into r.  (Fused operations are written out here and in
 // join: a sum has the same bits wherever it is computed.)
 template <int DT> __device__ __forceinline__ void add(Running& r, u32x4 q, float c) {
@@ -80,8 +86,18 @@ __device__ __forceinline__ float scaled_softmax1(const DistillArgs& a, float x, 
   return f * exp2_hw(fmaf(x, a.inv_tau, -lse) * kLog2e);
 }
 
-// Entry k < K of a row is thread k's: its token (-1: padding), the teacher's and
-// the student's logit over tau (-infinity for padding).
+// The same in a row that is_far, from its maximum and sum (f: already over the sum).
+template <int DT> __device__ __forceinline__ u32x4 far_softmax(u32x4 q, float ref, float c, float f) {
+  constexpr int N = Elem<DT>::N;
+  float x[N];
+  unpack<DT>(q, x);
+#pragma unroll
+  for (int i = 0; i < N; ++i) x[i] = f * exp2_hw((x[i] - ref) * c);
+  return pack<DT>(x);
+}
+
+// Entry k < K of a row is thread k's: its token (-1: padding), the teacher's
+// logit over tau (-infinity for padding) and the student's.
 struct Entry {
   int32_t id;
   float t, s;
@@ -97,7 +113,7 @@ __device__ __forceinline__ Entry entry_of(const DistillArgs& a, uint32_t row, co
     return e;
   }
   e.t = load1<TDT>(a.teacher, at) * a.inv_tau;
-  if (x) e.s = load1<DT>(x, (uint32_t)e.id) * a.inv_tau;
+  if (x) e.s = load1<DT>(x, (uint32_t)e.id);
   return e;
 }
 
@@ -114,7 +130,7 @@ struct Shared {
 struct Teacher {
   bool any;         // an entry has weight
   float q;          // this thread's entry's
-  float gap;        // sum_k q_k (log q_k - s_k / tau)
+  float gap;        // sum_k q_k (log q_k - (s_k - max) / tau), if the row's sum is given
 };
 
 // Joins the block's running sums and evaluates the entries; two barriers.  Nobody
@@ -153,8 +169,9 @@ __device__ __forceinline__ Teacher join_block(const DistillArgs& a, const Entry&
   }
   t.any = any != 0.f;
   // exp(t - max), their sum and that of exp(t - max) (t - max - s).
+  const float s = r ? (e.s - finite_max(r->m)) * a.inv_tau : 0.f;
   float x = e.t == -INFINITY ? 0.f : expf(e.t - tm);
-  const float xs = wave_add(x), ys = wave_add(x == 0.f ? 0.f : x * ((e.t - tm) - e.s));
+  const float xs = wave_add(x), ys = wave_add(x == 0.f ? 0.f : x * ((e.t - tm) - s));
   if (lane == 0) {
     sh.x[wave] = xs;
     sh.y[wave] = ys;
@@ -175,13 +192,16 @@ __device__ __forceinline__ Teacher join_block(const DistillArgs& a, const Entry&
   return t;
 }
 // The listed tokens again, with their q (an id listed twice: each writer adds
-// the same entries in the same order).
+// the same entries in the same order); p: the token's probability.
 template <int DT>
 __device__ __forceinline__ void write_entry(const DistillArgs& a, const Entry& e, const Shared& sh,
-                                            char* out, float lse, float f) {
+                                            char* out, float p, float f) {
   float q = 0.f;
   for (uint32_t k = 0; k < a.K; ++k) q += sh.id[k] == e.id ? sh.q[k] : 0.f;
-  store1<DT>(out, (uint32_t)e.id, f * (exp2_hw((e.s - lse) * kLog2e) - q));
+  store1<DT>(out, (uint32_t)e.id, f * (p - q));
+}
+__device__ __forceinline__ float p_of(const DistillArgs& a, float s, float lse) {
+  return exp2_hw((s * a.inv_tau - lse) * kLog2e);
 }
 
 template <int DT> __device__ __forceinline__ const char* logits_of(const DistillArgs& a, uint32_t row) {
@@ -253,7 +273,7 @@ __device__ __forceinline__ void finish_grad(const DistillArgs& a, const char* x,
     for (uint32_t i = a.vocab / Elem<DT>::N * Elem<DT>::N + threadIdx.x; i < a.vocab; i += kThreads)
       store1<DT>(out, i, zero ? 0.f : scaled_softmax1(a, load1<DT>(x, i), lse, f));
   __syncthreads();
-  if (!zero && own) write_entry<DT>(a, e, sh, out, lse, f);
+  if (!zero && own) write_entry<DT>(a, e, sh, out, p_of(a, e.s, lse), f);
 }
 
 // This thread's share of a part.
@@ -308,14 +328,31 @@ __device__ __forceinline__ void grad_of_part(const DistillArgs& a, const char* x
     store_vec<DT>(out, i, zero ? u32x4{0, 0, 0, 0} : scaled_softmax<DT>(a, load_vec<DT>(x, i), lse, f));
   finish_grad<DT>(a, x, out, last, zero, lse, f, e, own, sh);
 }
+// The gradient of vectors from .. to of a row that is_far, and of its last few logits.
+template <int DT>
+__device__ __forceinline__ void grad_of_far(const DistillArgs& a, const char* x, char* out, uint32_t from,
+                                            uint32_t to, bool last, Running r, float f, const Entry& e,
+                                            bool own, const Shared& sh) {
+  const float c = a.inv_tau * kLog2e, ref = finite_max(r.m), inv = r.s == 0.f ? 0.f : 1.f / r.s;
+#pragma unroll 1
+  for (uint32_t i = from + threadIdx.x; i < to; i += kThreads)
+    store_vec<DT>(out, i, far_softmax<DT>(load_vec<DT>(x, i), ref, c, f * inv));
+  if (last)
+    for (uint32_t i = a.vocab / Elem<DT>::N * Elem<DT>::N + threadIdx.x; i < a.vocab; i += kThreads)
+      store1<DT>(out, i, f * inv * exp2_hw((load1<DT>(x, i) - ref) * c));
+  __syncthreads();
+  if (own) write_entry<DT>(a, e, sh, out, exp2_hw((e.s - ref) * c) * inv, f);
+}
 template <int DT>
 __device__ __forceinline__ bool owns(const DistillArgs& a, const Entry& e, uint32_t part, uint32_t parts) {
   const uint32_t from = part * kPart * Elem<DT>::N;
   return e.id >= 0 && (uint32_t)e.id >= from && (part == parts - 1 || (uint32_t)e.id < from + kPart * Elem<DT>::N);
 }
-__device__ __forceinline__ void write_loss(const DistillArgs& a, uint32_t row, const Teacher& q, float lse) {
-  a.loss[row] = q.any ? a.tau * a.tau * (q.gap + lse) : 0.f;
-  a.lse[row] = lse;
+// No sum: the gap is infinite.
+__device__ __forceinline__ void write_loss(const DistillArgs& a, uint32_t row, const Teacher& q, Running r) {
+  const float sum = r.s == 0.f ? 0.f : log2_hw(r.s) * kLn2;
+  a.loss[row] = q.any ? a.tau * a.tau * (q.gap + sum) : 0.f;
+  a.lse[row] = lse_of(a, r);
 }
 
 // The loss of rows in several parts: the parts' sums, then a block a row.
@@ -337,7 +374,23 @@ __global__ __launch_bounds__(kThreads, 8) void k_loss(DistillArgs a, uint32_t pa
   Running r{-INFINITY, 0.f};
   if (threadIdx.x < parts) r = unpacked(record_of(a, row).r[threadIdx.x]);
   const Teacher q = join_block(a, e, sh, &r, a.inv_tau * kLog2e);
-  if (threadIdx.x == 0) write_loss(a, row, q, lse_of(a, r));
+  if (threadIdx.x == 0) write_loss(a, row, q, r);
+}
+
+// A row that is_far, by one block.
+template <int DT, int TDT>
+__device__ __noinline__ void grad_seldom(DistillArgs a, uint32_t row, uint32_t parts, float f) {
+  __shared__ Shared sh;
+  const float c = a.inv_tau * kLog2e;
+  const char* x = logits_of<DT>(a, row);
+  const Entry e = entry_of<DT, TDT>(a, row, x);
+  Running r{-INFINITY, 0.f};
+  for (uint32_t p = 0; p < parts; ++p) {
+    const Running one = sum_of_part<DT>(a, x, p, p == parts - 1, c, sh);
+    if (threadIdx.x == p) r = one;
+  }
+  join_block(a, e, sh, &r, c);
+  grad_of_far<DT>(a, x, grad_of<DT>(a, row), 0, a.vocab / Elem<DT>::N, true, r, f, e, e.id >= 0, sh);
 }
 
 // The gradient from a known log-sum-exp.  1023 x 40001 float32: 68 us, 4.8 TB/s.
@@ -350,10 +403,16 @@ __global__ __launch_bounds__(kThreads, 8) void k_grad(DistillArgs a) {
   v.load(x);
   Entry e = entry_of<DT, TDT>(a, row, nullptr);
   const bool own = owns<DT>(a, e, part, parts);
-  if (own) e.s = load1<DT>(x, (uint32_t)e.id) * a.inv_tau;
+  if (own) e.s = load1<DT>(x, (uint32_t)e.id);
   const Teacher q = join_block(a, e, sh, nullptr, 0.f);
-  const float g = a.weight ? a.weight[row] : 1.f;
-  v.grad(a, x, grad_of<DT>(a, row), part == parts - 1, !q.any || g == 0.f, a.lse[row], g * a.tau, e, own, sh);
+  const float g = a.weight ? a.weight[row] : 1.f, lse = a.lse[row];
+  const bool zero = !q.any || g == 0.f;
+  if (!zero && is_far(lse)) {
+    // One block does the row, so that nobody writes where another reads.
+    if (part == 0) grad_seldom<DT, TDT>(a, row, parts, g * a.tau);
+    return;
+  }
+  v.grad(a, x, grad_of<DT>(a, row), part == parts - 1, zero, lse, g * a.tau, e, own, sh);
 }
 
 // Both at once, the logits read once.  The parts of a row exchange their sums
@@ -375,6 +434,37 @@ __global__ __launch_bounds__(256) void k_unset(DistillArgs a, uint32_t parts) {
   const uint32_t i = blockIdx.x * 256 + threadIdx.x, row = i / parts;
   if (i < kQueues) *counter_of(a, i) = 0;
   if (row < a.rows) record_of(a, row).r[i - row * parts] = kUnset;
+}
+// A part of a row that is_far or of which sums have not come (bits of `missing`;
+// `got`: part t's sum).  The part is read again, a vector at a time, in a function
+// of its own: within the kernel this cost every block registers (4096 x 151936
+// bfloat16: 515 us where 485).
+template <int DT, int TDT>
+__device__ __noinline__ void joined_seldom(DistillArgs a, uint32_t row, uint32_t part, uint32_t parts,
+                                           unsigned long long got, unsigned long long missing) {
+  __shared__ Shared sh;
+  const float c = a.inv_tau * kLog2e;
+  const char* x = logits_of<DT>(a, row);
+  const bool last = part == parts - 1;
+  Entry e = entry_of<DT, TDT>(a, row, part == 0 ? x : nullptr);
+  const bool own = owns<DT>(a, e, part, parts);
+  if (part != 0 && own) e.s = load1<DT>(x, (uint32_t)e.id);
+  for (unsigned long long m = missing; m; m &= m - 1) {
+    const uint32_t p = (uint32_t)__builtin_ctzll(m);
+    const Running other = sum_of_part<DT>(a, x, p, p == parts - 1, c, sh);
+    if (threadIdx.x == p) got = packed(other);
+  }
+  Running r = unpacked(got);
+  const Teacher q = join_block(a, e, sh, &r, c);
+  if (part == 0 && threadIdx.x == 0) write_loss(a, row, q, r);
+  const float g = a.weight ? a.weight[row] : 1.f, lse = lse_of(a, r);
+  const bool zero = !q.any || g == 0.f;
+  char* out = grad_of<DT>(a, row);
+  const uint32_t from = part * kPart;
+  if (!zero && is_far(lse))
+    grad_of_far<DT>(a, x, out, from, min(a.vocab / Elem<DT>::N, from + kPart), last, r, g * a.tau, e, own, sh);
+  else
+    grad_of_part<DT>(a, x, out, part, last, zero, lse, g * a.tau, e, own, sh);
 }
 // Blocks a compute unit: 4096 x 151936 bfloat16 506 us with six, 486 with seven; 2000 x
 // 40001 float32 126 and 133.
@@ -403,7 +493,7 @@ __global__ __launch_bounds__(kThreads, DT == TFE_F32 ? 6 : 7) void k_joined(Dist
   v.load(x);
   Entry e = entry_of<DT, TDT>(a, row, part == 0 ? x : nullptr);
   const bool own = owns<DT>(a, e, part, parts);
-  if (part != 0 && own) e.s = load1<DT>(x, (uint32_t)e.id) * a.inv_tau;
+  if (part != 0 && own) e.s = load1<DT>(x, (uint32_t)e.id);
   Running r = v.sum(a, x, last, c, sh);
   unsigned long long got = packed(t == part ? r : Running{-INFINITY, 0.f});  // of part t
   if (parts > 1) {
@@ -420,27 +510,11 @@ __global__ __launch_bounds__(kThreads, DT == TFE_F32 ? 6 : 7) void k_joined(Dist
     if (t == 0) sh.missing = missing;
   }
   r = unpacked(got);
-  Teacher q = join_block(a, e, sh, &r, c);
-  if (parts > 1 && sh.missing) {
-    // Once more, with the sums that have not come; the part is read again, a vector
-    // at a time (held over this it would cost every block registers).
-    for (unsigned long long m = sh.missing; m; m &= m - 1) {
-      const uint32_t p = (uint32_t)__builtin_ctzll(m);
-      const Running other = sum_of_part<DT>(a, x, p, p == parts - 1, c, sh);
-      if (t == p) got = packed(other);
-    }
-    r = unpacked(got);
-    q = join_block(a, e, sh, &r, c);
-    const float lse = lse_of(a, r);
-    if (part == 0 && t == 0) write_loss(a, row, q, lse);
-    if (GRAD) {
-      const float g = a.weight ? a.weight[row] : 1.f;
-      grad_of_part<DT>(a, x, grad_of<DT>(a, row), part, last, !q.any || g == 0.f, lse, g * a.tau, e, own, sh);
-    }
-    return;
-  }
+  const Teacher q = join_block(a, e, sh, &r, c);
+  const unsigned long long missing = parts > 1 ? sh.missing : 0;
   const float lse = lse_of(a, r);
-  if (part == 0 && t == 0) write_loss(a, row, q, lse);
+  if (GRAD && (missing || is_far(lse))) return joined_seldom<DT, TDT>(a, row, part, parts, got, missing);
+  if (part == 0 && t == 0) write_loss(a, row, q, r);
   if (GRAD) {
     const float g = a.weight ? a.weight[row] : 1.f;
     v.grad(a, x, grad_of<DT>(a, row), last, !q.any || g == 0.f, lse, g * a.tau, e, own, sh);
