@@ -64,6 +64,9 @@ __device__ __forceinline__ float inverse_temperature(const SampleArgs& a, uint32
 // as much as |d| 2^-24 of the result) and the hardware's exponential: about an
 // ulp in all.  The maximum with -30, where weights are 0, also takes the NaN
 // of infinity - infinity and 0 x infinity.
+// A weight never rises as d falls, nor above 1: so gfx950's exponential and this
+// correction turned out when neighbours were compared for every float32 d from
+// -30 to 0 (an error within an ulp alone would not give it).
 __device__ __forceinline__ float weight(const Scale& r, float l) {
   const float d = fmaxf((l - r.top) * r.inv_t, -30.f);
   const float p = d * 1.44269504f;
@@ -567,7 +570,7 @@ __device__ void no_token(const SampleArgs& a, uint32_t row) {
 // that needs neither the maximum nor a weight for each logit.  All elements of a
 // bin have one weight, so the counts give the running sums exactly, and an
 // answer is a bin and a number in it; bins whose weights are equal once rounded
-// are one group.  A second pass finds the token, the group's j-th.
+// are one group, and neighbours, since weights fall with the logits.  A second pass finds the token, the group's j-th.
 // Logits below 2^-8 in magnitude ("small") are kept one by one for their sum; a
 // row whose answer they touch, or that has a logit of 2^8 or more, or one of
 // -2^8 or less with a weight, takes the way of float32 rows.
