@@ -256,11 +256,12 @@ __global__ __launch_bounds__(kSkinnyWaves * 64) void k_skinny(MatmulArgs a, Quan
   char* turn = lds + wave * kTurn;
   char* xs = lds + kSkinnyWaves * kTurn;
   u32x4 buf[2][TPW][PC][2];
-  uint32_t sbuf[2][TPW];
+  uint32_t sbuf[2];
+  static_assert(kFp8Block % (16 * TPW) == 0, "a group's rows of W lie in one block of 128");
   // Loads of one chunk (columns past the last block read the last again): 8 rows
   // of 128 bytes an instruction.  Lane l has piece l % 8 of rows l / 8 and
   // 8 + l / 8 of a tile.
-  auto load = [&](u32x4 (&v)[TPW][PC][2], uint32_t (&sw)[TPW], uint32_t grp, uint32_t ch) {
+  auto load = [&](u32x4 (&v)[TPW][PC][2], uint32_t& sw, uint32_t grp, uint32_t ch) {
 #pragma unroll
     for (int t = 0; t < TPW; ++t) {
 #pragma unroll
@@ -272,10 +273,8 @@ __global__ __launch_bounds__(kSkinnyWaves * 64) void k_skinny(MatmulArgs a, Quan
           v[t][c][q] = __builtin_nontemporal_load(
               (const u32x4*)(p + min(ch * PC + c, kb - 1) * kFp8Block));
       }
-      // A group of tiles may span two blocks of 128 rows of W.
-      const uint32_t nb = min((grp * TPW + t) * 16, a.n - 1) / kFp8Block;
-      sw[t] = *(const uint32_t*)(a.ws + (size_t)nb * a.spitch + ch * PC);
     }
+    sw = *(const uint32_t*)(a.ws + (size_t)(grp * TPW * 16 / kFp8Block) * a.spitch + ch * PC);
   };
   // A block of a tile in the operand's layout, by way of the wave's own 2 KB of
   // LDS (pieces exchanged by row, so that neither side's lanes share banks).
@@ -284,16 +283,17 @@ __global__ __launch_bounds__(kSkinnyWaves * 64) void k_skinny(MatmulArgs a, Quan
   auto operand = [&](const u32x4 (&v)[2], u32x4 (&w)[2]) {
     *(u32x4*)(turn + put) = v[0];
     *(u32x4*)(turn + 1024 + put) = v[1];
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");  // lanes read what others wrote
     w[0] = *(const u32x4*)(turn + get);
     w[1] = *(const u32x4*)(turn + (get ^ 64));
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
   };
   uint32_t grp = lo + wave;
   if (grp < hi) load(buf[0], sbuf[0], grp, 0);
   stage_rows<XDT>(a, x, MT * 16, xs, xp);
   __syncthreads();
   f32x4 acc[TPW][MT];
-  auto multiply = [&](const u32x4 (&v)[TPW][PC][2], const uint32_t (&sw)[TPW], uint32_t grp,
-                      uint32_t ch) {
+  auto multiply = [&](const u32x4 (&v)[TPW][PC][2], uint32_t sw, uint32_t grp, uint32_t ch) {
     if (ch == 0) {
 #pragma unroll
       for (int t = 0; t < TPW; ++t)
@@ -318,7 +318,7 @@ __global__ __launch_bounds__(kSkinnyWaves * 64) void k_skinny(MatmulArgs a, Quan
                                      (b * kFp8Block + q * 64 + g * 16 + h * 8) * 2);
 #pragma unroll
           for (int t = 0; t < TPW; ++t) {
-            const bf16x8 wv = widen(w[t][q][2 * h], w[t][q][2 * h + 1], scale_of(byte_of(sw[t], c)));
+            const bf16x8 wv = widen(w[t][q][2 * h], w[t][q][2 * h + 1], scale_of(byte_of(sw, c)));
 #pragma unroll
             for (int m = 0; m < MT; ++m)
               acc[t][m] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(wv, xv[m], acc[t][m], 0, 0, 0);
