@@ -97,7 +97,7 @@ template <int DT> __device__ __forceinline__ u32x4 far_softmax(u32x4 q, float re
 }
 
 // Entry k < K of a row is thread k's: its token (-1: padding), the teacher's
-// logit over tau (-infinity for padding) and the student's.
+// logit (-infinity for padding) and the student's.
 struct Entry {
   int32_t id;
   float t, s;
@@ -112,7 +112,7 @@ __device__ __forceinline__ Entry entry_of(const DistillArgs& a, uint32_t row, co
     e.id = -1;
     return e;
   }
-  e.t = load1<TDT>(a.teacher, at) * a.inv_tau;
+  e.t = load1<TDT>(a.teacher, at);
   if (x) e.s = load1<DT>(x, (uint32_t)e.id);
   return e;
 }
@@ -168,10 +168,11 @@ __device__ __forceinline__ Teacher join_block(const DistillArgs& a, const Entry&
     any = fmaxf(any, sh.some[w]);
   }
   t.any = any != 0.f;
-  // exp(t - max), their sum and that of exp(t - max) (t - max - s).
-  const float s = r ? (e.s - finite_max(r->m)) * a.inv_tau : 0.f;
-  float x = e.t == -INFINITY ? 0.f : expf(e.t - tm);
-  const float xs = wave_add(x), ys = wave_add(x == 0.f ? 0.f : x * ((e.t - tm) - s));
+  // x = exp((t - max) / tau), their sum and that of x ((t - max) / tau - s).  Differences
+  // before the division: t / tau of a list far from 0 may be rounded or infinite.
+  const float s = r ? (e.s - finite_max(r->m)) * a.inv_tau : 0.f, d = (e.t - tm) * a.inv_tau;
+  const float x = e.t == -INFINITY ? 0.f : expf(d);
+  const float xs = wave_add(x), ys = wave_add(x == 0.f ? 0.f : x * (d - s));
   if (lane == 0) {
     sh.x[wave] = xs;
     sh.y[wave] = ys;

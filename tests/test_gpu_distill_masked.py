@@ -118,3 +118,24 @@ def test_a_student_that_leaves_nothing():
     want = np.zeros((3, vocab))
     want[np.arange(2)[:, None], ids[:2]] = -tau * q
     np.testing.assert_allclose(grad.cpu().numpy(), want, rtol=1e-5, atol=0)
+
+
+@pytest.mark.parametrize("tau", [3.0, 0.3, 1.0])
+@pytest.mark.parametrize("tdtype", [F32, BF16])
+@pytest.mark.parametrize("vocab", [900, 40003])
+def test_teachers_far_from_zero(vocab, tdtype, tau):
+    """Lists whose logits lie far from 0, or at masks' values: q depends on differences alone
+    ((t - m) / tau is rounded to 2^-22 of itself, at most 104 where q is not 0)."""
+    rows = 8
+    s, ids, t, weight = inputs(vocab, rows, vocab, 40, short=False)
+    low = torch.finfo(TORCH[tdtype]).min
+    step = 8192.0 if tdtype == BF16 else 0.5  # what the type keeps there
+    for r, at in enumerate((1e6, -1e6, 3e5, -2e6)):
+        t[r] = np.round((at + np.round(t[r] * 2) * step) / step) * step
+    t[4], t[5], t[6] = low, -1e9, -low
+    t[7, ::2] = low
+    c = Call(s, ids, t, tau, F32, tdtype)
+    w = torch.from_numpy(weight).cuda()
+    loss, lse = c.loss()
+    check(c, ids, weight, loss, lse, c.grad(lse, w))
+    check(c, ids, weight, *c.both(w))
