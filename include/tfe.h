@@ -426,7 +426,9 @@ int64_t tfe_sample_workspace(int64_t rows, int32_t vocab); /* -1: bad size */
  *   loss = tau^2 sum_k q_k (log q_k - (s[id_k] / tau - lse)),
  *   d loss / d s_v = tau (exp(s_v / tau - lse) - sum of q_k with id_k = v).
  * Entries whose id lies outside [0, vocab) are padding: their logits may hold
- * anything.  A row without an entry of finite logit has loss 0 and gradient 0.
+ * anything.  A row whose entries are all padding or of logit -infinity has loss 0
+ * and gradient 0; one of +infinity or NaN makes the loss NaN, and the gradient at
+ * the listed tokens.
  * A student logit of -infinity has probability 0 (the loss is +infinity where
  * the teacher gives that token weight); where all are -infinity every
  * probability is 0, the gradient -tau q.  A student logit of +infinity or NaN

@@ -139,3 +139,21 @@ def test_teachers_far_from_zero(vocab, tdtype, tau):
     loss, lse = c.loss()
     check(c, ids, weight, loss, lse, c.grad(lse, w))
     check(c, ids, weight, *c.both(w))
+
+
+def test_infinite_teachers_are_not_hidden():
+    """NaN or +infinity in a list: the loss is NaN, and so is the gradient at the listed tokens;
+    elsewhere it is the student's.  Lists of -infinity and padding alone have no weight."""
+    vocab, tau = 33000, 2.0
+    s, _, _, _ = inputs(9, 5, vocab, 3, short=False)
+    ids = np.tile([[7, 32999, 12000]], (5, 1))
+    t = np.zeros((5, 3))
+    t[0], t[1, 1], t[2] = np.nan, np.inf, np.inf
+    t[3], ids[3, 1] = -np.inf, -1
+    c = Call(s, ids, t, tau)
+    loss, lse = c.loss()
+    for loss, lse, grad in ((loss, lse, c.grad(lse, None)), c.both(None)):
+        assert loss[:3].isnan().all() and loss[3] == 0 and torch.isfinite(loss[4]) and torch.isfinite(lse).all()
+        at = torch.from_numpy(ids[0].astype(np.int64)).cuda()
+        assert grad[:3, at].isnan().all() and grad[:3].isnan().sum() == 9
+        assert not grad[3].any() and torch.isfinite(grad[4]).all()
