@@ -421,7 +421,7 @@ int64_t tfe_sample_workspace(int64_t rows, int32_t vocab); /* -1: bad size */
 /* Distillation from a teacher's top logits.  Per row, with s the student's
  * logits (DEVICE, dtype, [rows x vocab], pitch ld), t the teacher's K top
  * logits (DEVICE, teacher_dtype, [rows x K]) of the tokens teacher_ids
- * (DEVICE int32 [rows x K]) and tau the temperature (> 0, finite):
+ * (DEVICE int32 [rows x K]) and tau the temperature (finite, from 4.3e-39 on):
  *   q = softmax(t / tau) over the row's K entries,  lse = log sum exp(s / tau),
  *   loss = tau^2 sum_k q_k (log q_k - (s[id_k] / tau - lse)),
  *   d loss / d s_v = tau (exp(s_v / tau - lse) - sum of q_k with id_k = v).

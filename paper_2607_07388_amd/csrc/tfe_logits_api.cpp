@@ -198,7 +198,9 @@ tfe_status distill_args(const void* logits, int32_t dtype, int64_t ld, int64_t r
                         float tau, DistillArgs* a) {
   TRY(distill_sizes(rows, vocab));
   NEED(K >= 1 && K <= kDistillMaxK, "K outside [1, %d]", kDistillMaxK);
-  NEED(tau > 0.f && isfinite(tau) && isfinite(1.f / tau), "temperature not positive and finite");
+  // The kernels multiply by log2(e) / tau.
+  NEED(tau > 0.f && isfinite(tau) && isfinite(1.f / tau * 1.44269504f),
+       "temperature not positive and finite, or below 4.3e-39");
   TRY(matrix(logits, dtype, ld, rows, vocab, "logits"));
   TRY(matrix(teacher, tdtype, K, rows, K, "teacher_logits"));
   if (rows == 0) return TFE_OK;
