@@ -377,7 +377,8 @@ tfe_status tfe_quantize(const void *x, int32_t dtype, int64_t ldx, int64_t rows,
  * out_dtype.  Products are exact and accumulated in float32; bfloat16 results are
  * the float32 ones rounded to nearest even, and a row's results do not depend on
  * the rows it comes with.
- * Numbers below 2^-126 may count as 0.
+ * Numbers below 2^-126 may count as 0, one that its layout rounds up to 2^128 as
+ * infinite.
  * rows <= 2^20, 1 <= out_dim <= 2^20, dim <= 65536. */
 tfe_status tfe_quantized_matmul(const uint8_t *a, const uint8_t *a_scales, const uint8_t *w,
                                 const uint8_t *w_scales, int64_t rows, int32_t out_dim,

@@ -394,7 +394,7 @@ __device__ __noinline__ void grad_seldom(DistillArgs a, uint32_t row, uint32_t p
   grad_of_far<DT>(a, x, grad_of<DT>(a, row), 0, a.vocab / Elem<DT>::N, true, r, f, e, e.id >= 0, sh);
 }
 
-// The gradient from a known log-sum-exp.  1023 x 40001 float32: 68 us, 4.8 TB/s.
+// The gradient from a known log-sum-exp.  1023 x 40001 float32: 63 us, 5.2 TB/s.
 template <int DT, int TDT>
 __global__ __launch_bounds__(kThreads, 8) void k_grad(DistillArgs a) {
   __shared__ Shared sh;
@@ -428,9 +428,9 @@ __global__ __launch_bounds__(kThreads, 8) void k_grad(DistillArgs a) {
 // are therefore all of its newest row (fewer than the row has parts; those of
 // its earlier rows have all their parts running and need nobody else).  There
 // are so few queues (queues_of) that theirs together are fewer than the compute
-// units, each of which has room for six or more.  (One counter alone is the limit at
-// about 100 parts a us.)
-//   4096 x 151936 bfloat16: 450 us, 5.5 TB/s; as two launches over the same parts 645.
+// units, each of which has room for seven.  (One counter alone is the limit at about
+// 100 parts a us.)
+//   4096 x 151936 bfloat16: 459 us, 5.4 TB/s; as two launches over the same parts 645.
 __global__ __launch_bounds__(256) void k_unset(DistillArgs a, uint32_t parts) {
   const uint32_t i = blockIdx.x * 256 + threadIdx.x, row = i / parts;
   if (i < kQueues) *counter_of(a, i) = 0;
@@ -467,10 +467,10 @@ __device__ __noinline__ void joined_seldom(DistillArgs a, uint32_t row, uint32_t
   else
     grad_of_part<DT>(a, x, out, part, last, zero, lse, g * a.tau, e, own, sh);
 }
-// Blocks a compute unit: 4096 x 151936 bfloat16 506 us with six, 486 with seven; 2000 x
-// 40001 float32 126 and 133.
+// Seven blocks a compute unit: 4096 x 151936 bfloat16 477 us where six take 498 (float32
+// the same either way).
 template <int DT, int TDT, bool GRAD>
-__global__ __launch_bounds__(kThreads, DT == TFE_F32 ? 6 : 7) void k_joined(DistillArgs a, uint32_t parts, uint32_t queues) {
+__global__ __launch_bounds__(kThreads, 7) void k_joined(DistillArgs a, uint32_t parts, uint32_t queues) {
   __shared__ Shared sh;
   const uint32_t t = threadIdx.x;
   const float c = a.inv_tau * kLog2e;

@@ -103,8 +103,9 @@ __device__ __forceinline__ u32x2 encode8(float* f, uint32_t* biased) {
   return some ? u32x2{codes4(f), codes4(f + 4)} : u32x2{pack4(f), pack4(f + 4)};
 }
 
-// Bound by a launch's latency at a head's sizes (257 x 1000: 4.7 us).
 // Blocks of one row: 16 lanes hold a block of 128.  One thread per 8 columns;
+// 257 x 1000 float32 3.2 to 4.7 us: a launch (2 to 3 us where one does next to nothing)
+// and a chain of a 64-bit division, a load and the codes' store.
 // the threads behind a row's columns write its padding of the scales.
 template <int DT> __global__ __launch_bounds__(256) void k_quantize_rows(QuantizeArgs a) {
   const uint32_t per_row = a.spitch * 16;  // threads
@@ -125,7 +126,8 @@ template <int DT> __global__ __launch_bounds__(256) void k_quantize_rows(Quantiz
 }
 
 // Blocks of 128 x 128: one block of threads each; rows beyond the last are
-// skipped.  blockIdx.y runs over the scales' whole pitch.
+// skipped.  blockIdx.y runs over the scales' whole pitch.  151936 x 1024 bfloat16: 96 us,
+// 4.9 TB/s read and written.
 template <int DT> __global__ __launch_bounds__(256) void k_quantize_tiles(QuantizeArgs a) {
   __shared__ float red[4];
   const int64_t row0 = (int64_t)blockIdx.x * kFp8Block;
@@ -201,8 +203,8 @@ __device__ __forceinline__ void store4(const MatmulArgs& a, uint32_t r, uint32_t
 // launch less), 16 bytes behind each row so that the 16 rows of an operand read
 // fall on different banks.  A wave takes TPW 16-row tiles of W at a time and
 // keeps PC blocks of 128 columns of each in flight ahead of those it
-// multiplies.  151936 x 1024: 1 row 26.6 us (5.9 TB/s of W), 64 rows 47.  Results of either type: the exact bfloat16 instruction, which
-// has time enough here.
+// multiplies.  151936 x 1024: 1 row 26 us (5.9 TB/s of W), 64 rows 46.  The exact
+// bfloat16 instruction has time enough here.
 constexpr int kCodes = 2;  // XDT of rows that are laid out already
 constexpr int kSkinnyWaves = 8;
 constexpr uint32_t kTurn = 2048;  // bytes of LDS a wave turns W's tiles in
@@ -365,11 +367,13 @@ __global__ __launch_bounds__(kSkinnyWaves * 64) void k_skinny(MatmulArgs a, Quan
 // widened in registers (exact products; on normal numbers 1.3e-8 of the result's
 // size off), in k_skinny's order, so that a row's results do not depend on the
 // rows it comes with and bfloat16 ones are the float32 ones rounded.  The scaled
-// 8-bit instruction takes 412 us where this takes 635, but its sums are off by
+// 8-bit instruction takes 412 us where this takes 636, but its sums are off by
 // 1.4e-5 of a normal result and up to 2^-12 of the terms' magnitudes: a result
 // small against its terms is lost.
-// 2048 rows of 151936 x 1024 to bfloat16: 635 us, 1.0 PFLOP/s; a wave widens each
-// code it multiplies, 192 conversions beside 128 products a step.
+// 2048 rows of 151936 x 1024 to bfloat16: 636 us, 1.0 PFLOP/s, 1024 rows to float32
+// 376; the matrix cores are busy 41%.  A wave widens the codes it multiplies, 192
+// conversions beside 128 products a step; LDS is read 8 bytes a lane, a third of the
+// time, half of that conflicts.
 #if defined(__HIP_DEVICE_COMPILE__)  // the host compiler has no buffer descriptors
 // Loads go through buffer descriptors: 32-bit offsets, and rows past a matrix'
 // last read as zeros (the whole offset is in the vector register, so that the
@@ -530,7 +534,7 @@ __global__ __launch_bounds__(WN* WM * 64) void k_tiles(MatmulArgs a, uint32_t ti
         // writes whole pieces of 128 or 256 bytes: the results of a lane's row and
         // its three neighbours' are 64, and at an odd pitch two parts of lines.  us,
         // so / at once: 257 x 40001 x 1000 42 / 48, 1024 x 151937 x 256 162 / 227,
-        // 1024 x 151936 x 256 123 / 161, 2048 x 151936 x 1024 637 / 746, 256 rows of it
+        // 1024 x 151936 x 256 123 / 161, 2048 x 151936 x 1024 636 / 746, 256 rows of it
         // 99 / 101.  float32 gains nothing from it (512 x 151937 x 1024: 242 / 241).
         constexpr int ROWS = 64 / PIECES;  // of an instruction
         static_assert(NT % 2 == 0, "column tiles in pairs");
@@ -629,6 +633,9 @@ hipError_t tiles(const MatmulArgs& a, int dt, int blocks_per_cu, hipStream_t s) 
   return hipGetLastError();
 }
 
+// us with the rows in LDS / in tiles, 151936 x 1024 to float32: 16 rows 33 / 48, 32 37 / 47,
+// 48 41 / 48, 64 46 / 50 (x 256: 24 / 20); 16 rows of 151936 x 2048 57 / 99.  Rows that do
+// not fit go to tiles: 64 of 151936 x 1152 55, 48 of x 1408 61.
 bool is_skinny(const MatmulArgs& a) { return a.rows <= 64 && skinny_lds(a) <= kSkinnyLds; }
 
 }  // namespace
@@ -656,7 +663,7 @@ hipError_t launch_fp8_matmul(const MatmulArgs& a, int out_dtype, hipStream_t s) 
                                 : skinny_rows<kCodes, TFE_BF16>(a, QuantizeArgs{}, s);
   // Large tiles where they fill the device and waste few rows.  us at 151936 x 1024,
   // 256 x 256 / 128 x 128: bfloat16 256 rows 110 / 101, 512 176 / 182, 1024 339 / 355, 2048
-  // 637 / 692; float32 256 rows 128 / 107, 512 199 / 196, 1024 376 / 379.  257 x 40001 x 1000
+  // 636 / 692; float32 256 rows 128 / 107, 512 199 / 196, 1024 376 / 379.  257 x 40001 x 1000
   // (two row tiles of 256 against three of 128): 63 / 37.
   const uint32_t r256 = (a.rows + 255) / 256, r128 = (a.rows + 127) / 128;
   const bool fills = (uint64_t)((a.n + 255) / 256) * r256 >= (uint64_t)compute_units() * 2;

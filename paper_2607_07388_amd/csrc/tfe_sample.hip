@@ -17,7 +17,8 @@
 // maximum, the histogram, the collection.
 // Bound by the logits' bytes for the first pass, then by the weights' arithmetic
 // (about 27 instruction slots a logit) and the LDS additions of the second.
-// 151936 float32 logits a row: 1 row 24 us, 64 rows 53, 256 rows 100.
+// 151936 float32 logits a row, top-k and top-p: 1 row 25 us, 64 rows 52, 256 rows 83
+// (top-p alone 96).
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
@@ -441,6 +442,7 @@ __device__ void resolve(const SampleArgs& a, uint32_t row, S& sh, const Settings
 // equal logits): the element at which the running count or sum reaches
 // `target`, twelve bits of the key at a time over the elements that share the
 // bits so far, each time over the whole row.  *sum: the sum through it.
+// 151936 equal logits: 0.8 ms for the draw alone, 2.4 with top-k and top-p.
 template <int DT, class S>
 __device__ uint64_t reach(const char* x, uint32_t vocab, const Scale& r, S& sh,
                           uint64_t target, bool by_count, uint64_t* sum) {
@@ -574,7 +576,7 @@ __device__ void no_token(const SampleArgs& a, uint32_t row) {
 // Logits below 2^-8 in magnitude ("small") are kept one by one for their sum; a
 // row whose answer they touch, or that has a logit of 2^8 or more, or one of
 // -2^8 or less with a weight, takes the way of float32 rows.
-// 256 rows of 151936, top-p: 52 us, that way 95; 300 of 33333: 30 and 41.
+// 256 rows of 151936, top-p: 50 us, that way 95; 300 of 33333: 30 and 41.
 constexpr uint32_t kFirst = 119u << 7, kHalf = 2048, kSmall = kHalf;  // the bits of 2^-8
 static_assert(2 * kHalf == kBins, "the values' counts lie where the edges do");
 __device__ __forceinline__ float value_of(uint32_t q) {  // of a bin other than kSmall
@@ -961,7 +963,7 @@ __global__ __launch_bounds__(kHistThreads) void k_part_hist(SampleArgs a, uint32
   // The last block to get here has the row's whole histogram: it finds the bins.
   // What blocks tell each other goes through device-scope atomics alone, and a
   // block counts itself in once its own are done: no fence (writing the L2s
-  // back for one took 100 us at 64 rows).
+  // back for one took 90 us at 64 rows).
   asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
   __syncthreads();
   if (threadIdx.x == 0)
@@ -1022,7 +1024,12 @@ __global__ __launch_bounds__(kFinishThreads) void k_part_finish(SampleArgs a, ui
   }
 }
 
-// Blocks a row: about 512 in all, of at least 2048 logits each.
+// Blocks a row: about 512 in all, of at least 2048 logits each; one from 128 rows on.
+// us split / one block a row, top-k and top-p, 151936 float32: 32 rows 43 / 46, 64 51 / 50,
+// 100 64 / 53, 127 72 / 57, 128 66 / 56, 192 96 / 68, 256 106 / 83, 300 146 / 130; bfloat16: 32
+// 40 / 38, 64 44 / 39, 127 58 / 43, 128 56 / 43, 256 77 / 61, 300 113 / 85; 33333 bfloat16: 32
+// 34 / 22, 128 41 / 24, 256 45 / 38.  (Fewer than 64 rows, and 64 to 127, could gain from a
+// block a row.)
 uint32_t parts_of(int64_t rows, int32_t vocab) {
   if (rows >= 128) return 1;
   const uint32_t most = std::min<uint32_t>(kMaxParts, ((uint32_t)vocab + 2047) / 2048);
@@ -1032,7 +1039,10 @@ uint32_t parts_of(int64_t rows, int32_t vocab) {
 template <int DT> hipError_t launch(const SampleArgs& a, hipStream_t s) {
   const uint32_t parts = parts_of(a.rows, (int32_t)a.vocab);
   if (parts == 1) {
-    // A short row's block leaves room for another on its compute unit.
+    // A short row's block leaves room for another on its compute unit.  us with 512 / 1024
+    // threads, top-p: 300 rows of 33333 bfloat16 31 / 50, of 65000 40 / 68 (float32 72 / 86);
+    // 128 rows of 151936 82 / 44 (101 / 80), 256 rows 86 / 50 (119 / 96), 300 rows, more than
+    // compute units, 89 / 114 (156 / 164).
     if (a.vocab <= 65536)
       k_row<DT, 512, 2048><<<dim3(a.rows), dim3(512), 0, s>>>(a);
     else
