@@ -1,0 +1,328 @@
+"""The operators that a head's learning from the tokens themselves and its integer form add, as
+cases to measure.
+
+A head learns from the tokens that came next (xent: the softmax cross entropy of its logits, which
+are not kept, with the gradients of hidden states and projection), its gradients are clipped by
+their global norm (clip), and its logits are computed from 8-bit integers with a scale for each
+token and channel (int8).  With `own` false, run() computes them in their plain form, elementary
+torch operations in 32 bits; with it true, run() calls the library.  exact() is the same in 64
+bits.  Inputs are seeded draws over the repository's vocabularies and widths."""
+import math
+import random
+
+import torch
+
+own = False
+
+VOCAB = 151936
+DTYPES = {"bf16": torch.bfloat16, "f32": torch.float32}
+TINY = 2.0 ** -100  # rows of no greater magnitude count as 0 in the integer layout
+
+
+def listed():
+    return [
+        # A few positions over a small vocabulary: the latency of one small training step.
+        {"name": "xent_16", "kind": "xent", "what": "both", "rows": 16, "vocab": 3001, "dim": 256, "grad": "bf16",
+         "pad": 0},
+        # A held-out batch of 64 positions: the loss alone, one pass over the projection.
+        {"name": "xent_loss_64", "kind": "xent", "what": "loss", "rows": 64, "vocab": VOCAB, "dim": 1024,
+         "grad": "bf16", "pad": 0},
+        # Ragged in every size, rows off their alignment, gradients kept in 32 bits for accumulation.
+        {"name": "xent_257_odd", "kind": "xent", "what": "both", "rows": 257, "vocab": 40001, "dim": 999,
+         "grad": "f32", "pad": 2},
+        # A training batch of 4096 positions: loss and both gradients.
+        {"name": "xent_4096", "kind": "xent", "what": "both", "rows": 4096, "vocab": VOCAB, "dim": 1024,
+         "grad": "bf16", "pad": 0},
+        # The head's logits for one sequence: W's bytes and a launch or two.
+        {"name": "int8_b1", "kind": "int8", "rows": 1, "vocab": VOCAB, "dim": 1024, "dtype": "bf16", "out": "f32"},
+        # A batch-64 decode step.
+        {"name": "int8_b64", "kind": "int8", "rows": 64, "vocab": VOCAB, "dim": 1024, "dtype": "bf16", "out": "f32"},
+        # A ragged batch over a vocabulary and a width that end inside a tile; f32 hidden states.
+        {"name": "int8_257_odd", "kind": "int8", "rows": 257, "vocab": 40001, "dim": 1000, "dtype": "f32",
+         "out": "bf16"},
+        # All positions of two short prompts at once, as a scorer needs them.
+        {"name": "int8_2048", "kind": "int8", "rows": 2048, "vocab": VOCAB, "dim": 1024, "dtype": "bf16",
+         "out": "bf16"},
+        # A handful of small gradients: launches are what counts.
+        {"name": "clip_small", "kind": "clip", "what": "clip", "tensors": 12, "total": 50000, "dtype": "f32",
+         "ragged": False},
+        # The gradients of a model of many parameters, matrices and vectors, packed one behind the other.
+        {"name": "clip_many_odd", "kind": "clip", "what": "clip", "tensors": 300, "total": 60000000, "dtype": "f32",
+         "ragged": True},
+        # The head's gradient and a few more, in bfloat16.
+        {"name": "clip_head", "kind": "clip", "what": "clip", "tensors": 4, "total": VOCAB * 1024, "dtype": "bf16",
+         "ragged": False},
+        # The norm alone, of what one rank of several holds.
+        {"name": "norm_head", "kind": "clip", "what": "norm", "tensors": 4, "total": VOCAB * 1024, "dtype": "f32",
+         "ragged": False},
+    ]
+
+
+def _log(rng, lo, hi):
+    return int(round(math.exp(rng.uniform(math.log(lo), math.log(hi)))))
+
+
+def draw(rng):
+    kind = rng.choice(["xent", "xent", "int8", "clip"])
+    if kind == "clip":
+        dtype = rng.choice(["bf16", "f32"])
+        tensors = _log(rng, 1, 400)
+        return {"kind": kind, "what": rng.choice(["clip", "clip", "norm"]), "tensors": tensors,
+                "total": max(tensors * 8, _log(rng, 10000, VOCAB * 1024 if dtype == "bf16" else VOCAB * 512)),
+                "dtype": dtype, "ragged": rng.choice([False, True])}
+    vocab = rng.choice([VOCAB, _log(rng, 1000, VOCAB), _log(rng, 1000, VOCAB)])
+    dim = rng.choice([1024, rng.randint(200, 1024)])
+    if kind == "int8":
+        return {"kind": kind, "rows": _log(rng, 1, 2048), "vocab": vocab, "dim": dim,
+                "dtype": rng.choice(["bf16", "f32"]), "out": rng.choice(["bf16", "f32"])}
+    grad = rng.choice(["bf16", "bf16", "f32"])
+    return {"kind": kind, "what": rng.choice(["loss", "grad", "both", "both"]),
+            "rows": _log(rng, 1, 4096 if grad == "bf16" else 2048), "vocab": vocab, "dim": dim, "grad": grad,
+            "pad": rng.choice([0, 0, rng.randint(1, 64)])}
+
+
+# ---- inputs ----------------------------------------------------------------------------------
+
+
+def _gen(seed, tag):
+    g = torch.Generator(device="cuda")
+    g.manual_seed((int(seed) * 1000003 + tag) & 0x7FFFFFFFFFFF)
+    return g
+
+
+def _normal(seed, tag, rows, cols, sigma, dtype, pad=0):
+    out = torch.empty((rows, cols + pad), dtype=dtype, device="cuda")
+    g = _gen(seed, tag)
+    per = max(1, (1 << 26) // (cols + pad))
+    for at in range(0, rows, per):
+        n = min(per, rows - at)
+        out[at:at + n] = torch.randn((n, cols + pad), generator=g, device="cuda") * sigma
+    return out[:, :cols]
+
+
+def _sizes(case):
+    """Sizes of the gradients, the same for every seed: a few matrices hold most of the elements;
+    whole vectors of 64 unless the case is ragged."""
+    rng, n = random.Random(case["tensors"] * 7919 + case["total"]), case["tensors"]
+    weights = [math.exp(rng.uniform(-4, 4)) for _ in range(n)]
+    each = case["total"] / sum(weights)
+    sizes = [max(1, int(w * each)) for w in weights]
+    return [s + (s & 1 ^ 1) for s in sizes] if case["ragged"] else [-(-s // 64) * 64 for s in sizes]
+
+
+def prepare(case, seed):
+    c = case
+    s = {"case": c, "stream": torch.cuda.current_stream().cuda_stream}
+    if c["kind"] == "xent":
+        rows, vocab, dim = c["rows"], c["vocab"], c["dim"]
+        g, f32 = _gen(seed, 3), dict(dtype=torch.float32, device="cuda")
+        s["x"] = _normal(seed, 1, rows, dim, 1.0, torch.bfloat16, c["pad"])
+        s["w"] = _normal(seed, 2, vocab, dim, 0.1, torch.bfloat16, c["pad"])
+        # Next tokens as text has them, frequent ones often; every eleventh position has none.
+        rank = torch.exp(torch.rand(rows, generator=g, device="cuda") * math.log(vocab)).long().clamp(max=vocab) - 1
+        s["targets"] = (rank * 7919 % vocab).int()
+        s["targets"][7::11] = -1
+        s["weight"] = torch.rand(rows, generator=g, device="cuda") + 0.5
+        s["loss"], s["lse"] = torch.empty(rows, **f32), torch.empty(rows, **f32)
+        if c["what"] == "grad":
+            for at in range(0, rows, 512):
+                s["lse"][at:at + 512] = torch.logsumexp(s["x"][at:at + 512].float() @ s["w"].float().t(), 1)
+        if c["what"] != "loss":
+            kind = dict(dtype=DTYPES[c["grad"]], device="cuda")
+            s["grad_x"], s["grad_w"] = torch.empty((rows, dim), **kind), torch.empty((vocab, dim), **kind)
+    elif c["kind"] == "int8":
+        s["x"] = _normal(seed, 1, c["rows"], c["dim"], 1.0, DTYPES[c["dtype"]])
+        wide = -(-c["dim"] // 128) * 128
+        s["w"] = torch.zeros((c["vocab"], wide), dtype=torch.int8, device="cuda")
+        s["w_scales"] = torch.empty(c["vocab"], dtype=torch.float32, device="cuda")
+        w = _normal(seed, 2, c["vocab"], c["dim"], 0.1, torch.bfloat16)
+        for at in range(0, c["vocab"], 1 << 15):
+            codes, scales = _codes(w[at:at + (1 << 15)].float())
+            s["w"][at:at + (1 << 15), :c["dim"]], s["w_scales"][at:at + (1 << 15)] = codes.to(torch.int8), scales
+        s["out"] = torch.empty((c["rows"], c["vocab"]), dtype=DTYPES[c["out"]], device="cuda")
+    else:
+        sizes = _sizes(c)
+        flat = _normal(seed, 4, 1, sum(sizes), 3.0 / math.sqrt(sum(sizes)), DTYPES[c["dtype"]])[0]
+        s["flat"], s["out"] = flat, torch.empty_like(flat)
+        s["grads"], s["outs"] = list(flat.split(sizes)), list(s["out"].split(sizes))
+        s["max_norm"], s["norm"] = 1.0, torch.empty(1, dtype=torch.float32, device="cuda")
+    return s
+
+
+# ---- one pass ----------------------------------------------------------------------------------
+
+
+def run(state):
+    kind = state["case"]["kind"]
+    if own:
+        return {"xent": _own_xent, "int8": _own_int8, "clip": _own_clip}[kind](state)
+    return {"xent": _xent, "int8": _int8, "clip": _clip}[kind](state)
+
+
+def _number(dtype):
+    return 1 if dtype == torch.bfloat16 else 0
+
+
+def _space(s, size):
+    """The workspace that a program keeps from its first call on."""
+    if "space" not in s:
+        s["space"] = torch.empty(max(16, size()), dtype=torch.uint8, device="cuda")
+    return s["space"], s["space"].numel()
+
+
+def _own_xent(s):
+    from paper_2607_07388_amd import tfe
+    x, w, what = s["x"], s["w"], s["case"]["what"]
+    rows, dim = x.shape
+    vocab = w.shape[0]
+    space = _space(s, lambda: tfe.tfe_cross_entropy_workspace(rows, vocab, dim))
+    head = (x, x.stride(0), w, w.stride(0), s["targets"], rows, vocab, dim)
+    if what == "loss":
+        tfe.tfe_cross_entropy_loss(*head, s["loss"], s["lse"], *space, s["stream"])
+        return s["loss"], s["lse"]
+    grads = (s["grad_x"], dim, s["grad_w"], dim, _number(s["grad_w"].dtype), 0)
+    if what == "grad":
+        tfe.tfe_cross_entropy_grad(*head, s["lse"], s["weight"], *grads, *space, s["stream"])
+        return s["grad_x"], s["grad_w"]
+    tfe.tfe_cross_entropy_loss_grad(*head, s["weight"], s["loss"], s["lse"], *grads, *space, s["stream"])
+    return s["loss"], s["lse"], s["grad_x"], s["grad_w"]
+
+
+def _own_int8(s):
+    from paper_2607_07388_amd import tfe
+    x, out = s["x"], s["out"]
+    rows, dim = x.shape
+    space = _space(s, lambda: tfe.tfe_int8_workspace(rows, dim))
+    tfe.tfe_int8_linear(x, _number(x.dtype), x.stride(0), s["w"], s["w_scales"], rows, out.shape[1], dim, out,
+                        _number(out.dtype), out.shape[1], *space, s["stream"])
+    return out
+
+
+def _own_clip(s):
+    from paper_2607_07388_amd import tfe
+    if "list" not in s:  # the gradients' places: made once, as a program does
+        s["list"] = tfe.make_grad_tensors([(g, o, 1, g.numel(), g.numel(), g.numel(), _number(g.dtype))
+                                           for g, o in zip(s["grads"], s["outs"])])
+    n = len(s["grads"])
+    space = _space(s, lambda: tfe.tfe_grad_workspace(s["list"], n))
+    if s["case"]["what"] == "norm":
+        tfe.tfe_grad_norm(s["list"], n, s["norm"], *space, s["stream"])
+        return s["norm"]
+    tfe.tfe_grad_norm_clip(s["list"], n, s["max_norm"], s["norm"], *space, s["stream"])
+    return s["norm"], s["out"]
+
+
+def _xent(s):
+    x, w, what = s["x"].float(), s["w"].float(), s["case"]["what"]
+    z = x @ w.t()
+    some = s["targets"] >= 0
+    at = s["targets"].clamp(min=0).long()[:, None]
+    if what == "grad":
+        lse = s["lse"]
+    else:
+        top = z.amax(1, keepdim=True)
+        lse = top[:, 0] + torch.log(torch.exp(z - top).sum(1))
+        loss = torch.where(some, lse - z.gather(1, at)[:, 0], torch.zeros_like(lse))
+        if what == "loss":
+            return loss, lse
+    z = torch.exp(z - lse[:, None])
+    z.scatter_add_(1, at, torch.full_like(lse, -1.0)[:, None])
+    z *= torch.where(some, s["weight"], torch.zeros_like(lse))[:, None]
+    grad_x, grad_w = (z @ w).to(s["grad_x"].dtype), (z.t() @ x).to(s["grad_w"].dtype)
+    return (grad_x, grad_w) if what == "grad" else (loss, lse, grad_x, grad_w)
+
+
+def _codes(x):
+    """Codes (as float32 numbers) and scales of rows: code = round(x * (127 / the row's largest))."""
+    top = x.abs().amax(1)
+    some = top > TINY
+    inverse = torch.where(some, 127.0 / top, torch.zeros_like(top))
+    return torch.round(x * inverse[:, None]), torch.where(some, top / 127.0, torch.zeros_like(top))
+
+
+def _int8(s):
+    x, scales = _codes(s["x"].float())
+    sums = x @ s["w"][:, :x.shape[1]].float().t()  # below 2^24: exact
+    return (sums * scales[:, None] * s["w_scales"]).to(s["out"].dtype)
+
+
+def _clip(s):
+    sums = torch.stack([g.float().square().sum(dtype=torch.float64) for g in s["grads"]])
+    norm = sums.sum().sqrt()
+    if s["case"]["what"] == "norm":
+        return norm.float().view(1)
+    by = (s["max_norm"] / norm).clamp(max=1.0).float()
+    return norm.float().view(1), torch.cat([(g.float() * by).to(g.dtype) for g in s["grads"]])
+
+
+# ---- in 64 bits --------------------------------------------------------------------------------
+
+
+def exact(case, seed):
+    s = prepare(case, seed)
+    return {"xent": _exact_xent, "int8": _exact_int8, "clip": _exact_clip}[case["kind"]](s)
+
+
+def _exact_xent(s):
+    what, rows = s["case"]["what"], s["x"].shape[0]
+    w = s["w"].double().contiguous()
+    loss = torch.zeros(rows, dtype=torch.float64, device="cuda")
+    lse = torch.zeros_like(loss)
+    grad_x = torch.empty((rows, w.shape[1]), dtype=torch.float64, device="cuda")
+    grad_w = torch.zeros_like(w) if what != "loss" else None
+    for a in range(0, rows, 1024):
+        b = min(a + 1024, rows)
+        x, t = s["x"][a:b].double(), s["targets"][a:b].long()
+        z = torch.mm(x, w.t())
+        lse[a:b] = s["lse"][a:b].double() if what == "grad" else torch.logsumexp(z, 1)
+        there = t >= 0
+        picked = z[torch.arange(b - a, device="cuda"), t.clamp(min=0)]
+        loss[a:b] = (lse[a:b] - picked) * there
+        if grad_w is None:
+            continue
+        d = (z - lse[a:b, None]).exp()
+        d[torch.arange(b - a, device="cuda"), t.clamp(min=0)] -= 1.0
+        d *= (s["weight"][a:b].double() * there)[:, None]
+        grad_x[a:b] = torch.mm(d, w)
+        grad_w += torch.mm(d.t().contiguous(), x)
+    return {"loss": (loss, lse), "grad": (grad_x, grad_w), "both": (loss, lse, grad_x, grad_w)}[what]
+
+
+def _exact_int8(s):
+    # The codes follow from the definition's two float32 roundings; their product is in 64 bits.
+    x = s["x"].float()
+    top = x.abs().max(1, keepdim=True).values
+    codes = torch.round((x.double() * (127.0 / top).double()).float().double())
+    codes, scale = codes * (top > TINY), (top / 127.0).double() * (top > TINY)
+    out = torch.empty(s["out"].shape, dtype=torch.float64, device="cuda")
+    per = 1 << 14
+    for n in range(0, out.shape[1], per):
+        w = s["w"][n:n + per, :x.shape[1]].double() * s["w_scales"][n:n + per, None].double()
+        out[:, n:n + per] = torch.mm(codes * scale, w.t().contiguous())
+    return out
+
+
+def _exact_clip(s):
+    flat = s["flat"].double()
+    norm = torch.linalg.vector_norm(flat).view(1)
+    if s["case"]["what"] == "norm":
+        return norm
+    return norm, flat * min(1.0, s["max_norm"] / float(norm))
+
+
+# ---- what a pass cannot do without -------------------------------------------------------------
+
+
+def work(case):
+    size = {"bf16": 2, "f32": 4}
+    if case["kind"] == "clip":
+        total = sum(_sizes(case))
+        return {"bytes": total * size[case["dtype"]] * (1 if case["what"] == "norm" else 2), "flops": 3 * total}
+    rows, vocab, dim = case["rows"], case["vocab"], case["dim"]
+    if case["kind"] == "int8":
+        return {"bytes": vocab * (-(-dim // 128) * 128 + 4) + rows * dim * size[case["dtype"]]
+                + rows * vocab * size[case["out"]], "flops": 2 * rows * vocab * dim}
+    both = (rows + vocab) * dim
+    if case["what"] == "loss":
+        return {"bytes": 2 * both + 12 * rows, "flops": 2 * rows * vocab * dim}
+    return {"bytes": (2 + size[case["grad"]]) * both + 16 * rows, "flops": 6 * rows * vocab * dim}
