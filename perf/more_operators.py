@@ -192,9 +192,9 @@ def _own_int8(s):
     from paper_2607_07388_amd import tfe
     x, out = s["x"], s["out"]
     rows, dim = x.shape
-    space = _space(s, lambda: tfe.tfe_int8_workspace(rows, dim))
-    tfe.tfe_int8_linear(x, _number(x.dtype), x.stride(0), s["w"], s["w_scales"], rows, out.shape[1], dim, out,
-                        _number(out.dtype), out.shape[1], *space, s["stream"])
+    space = _space(s, lambda: tfe.tfe_integer_workspace(rows, dim))
+    tfe.tfe_integer_linear(x, _number(x.dtype), x.stride(0), s["w"], s["w_scales"], rows, out.shape[1], dim, out,
+                           _number(out.dtype), out.shape[1], *space, s["stream"])
     return out
 
 
