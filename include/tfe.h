@@ -463,6 +463,108 @@ tfe_status tfe_distill_loss_grad(const void *logits, int32_t dtype, int64_t ld, 
                                  int64_t workspace_bytes, void *stream);
 int64_t tfe_distill_workspace(int64_t rows, int32_t vocab); /* -1: bad size */
 
+/* ---- The head learned from tokens, and served in integers -------------------
+ * What a program does next to the calls above: the head's projection learned
+ * from the tokens that came next, its gradients kept in bounds, and its logits
+ * by 8-bit integers.  The rules above hold here too: no state, the caller's
+ * workspace, kernels only, matrices row-major with a pitch, any host thread. */
+
+/* Softmax cross entropy over the vocabulary, the logits computed in pieces and
+ * not kept.  With z = H W^T (hidden DEVICE bfloat16 [rows x dim], pitch ldh; w
+ * DEVICE bfloat16 [vocab x dim], pitch ldw; products exact, sums float32) and t
+ * the row's target (DEVICE int32 [rows]):
+ *   lse = log sum_v exp z_v,   loss = lse - z_t,
+ *   dz_v = g (exp(z_v - lse) - [v = t]),   d hidden = dz W,   d w = dz^T H.
+ * A row whose target lies outside [0, vocab) has none: loss 0 and gradient 0 (its
+ * lse is computed).
+ *   loss, lse   DEVICE float [rows].
+ *   grad_loss   DEVICE float [rows] or NULL (1): g, the gradient with respect to
+ *               loss.  Where it is 0 the row has gradient 0.  Neither such a
+ *               row nor one without a target takes part in d w, whatever its
+ *               hidden state holds.
+ *   grad_hidden, grad_w  DEVICE of grad_dtype, [rows x dim] and [vocab x dim],
+ *               pitches ldgh and ldgw; apart from each other and every input.
+ *               Sums are float32.  For TFE_BF16 results dz is rounded to
+ *               bfloat16 before the products with W and H, for TFE_F32 ones to
+ *               the sum of two bfloat16 numbers (17 bits), at twice the products.
+ *   accumulate  not 0: grad_w (TFE_F32 only) is added to, not written.
+ * A row with a logit of +infinity or NaN has a loss and gradients that are NaN,
+ * and grad_w with it.  Results do not change from call to call.
+ * tfe_cross_entropy_grad takes lse as tfe_cross_entropy_loss wrote it.
+ * Pointers 16-byte aligned, with pitches and dim multiples of 8 (and pitches up
+ * to 2^21), are read in place; others are copied in pieces first.
+ * 1 <= vocab <= 2^18, 1 <= dim <= 16384, rows <= 2^20. */
+tfe_status tfe_cross_entropy_loss(const void *hidden, int64_t ldh, const void *w, int64_t ldw,
+                                  const int32_t *targets, int64_t rows, int32_t vocab,
+                                  int32_t dim, float *loss, float *lse, void *workspace,
+                                  int64_t workspace_bytes, void *stream);
+tfe_status tfe_cross_entropy_grad(const void *hidden, int64_t ldh, const void *w, int64_t ldw,
+                                  const int32_t *targets, int64_t rows, int32_t vocab,
+                                  int32_t dim, const float *lse, const float *grad_loss,
+                                  void *grad_hidden, int64_t ldgh, void *grad_w, int64_t ldgw,
+                                  int32_t grad_dtype, int32_t accumulate, void *workspace,
+                                  int64_t workspace_bytes, void *stream);
+/* Both in one call. */
+tfe_status tfe_cross_entropy_loss_grad(const void *hidden, int64_t ldh, const void *w, int64_t ldw,
+                                       const int32_t *targets, int64_t rows, int32_t vocab,
+                                       int32_t dim, const float *grad_loss, float *loss,
+                                       float *lse, void *grad_hidden, int64_t ldgh, void *grad_w,
+                                       int64_t ldgw, int32_t grad_dtype, int32_t accumulate,
+                                       void *workspace, int64_t workspace_bytes, void *stream);
+int64_t tfe_cross_entropy_workspace(int64_t rows, int32_t vocab, int32_t dim); /* -1: bad size */
+
+/* One gradient: `rows` rows of `cols` elements, ldg apart (ldo in `out`).  `out`
+ * is where its clipped form goes: `grad` itself, at the same pitch, or memory
+ * apart from every gradient; tfe_grad_norm does not look at it. */
+typedef struct {
+  const void *grad; /* DEVICE, dtype */
+  void *out;        /* DEVICE, dtype */
+  int64_t rows, cols, ldg, ldo;
+  int32_t dtype;    /* TFE_F32 or TFE_BF16 */
+} tfe_grad_tensor;
+
+/* The norm of n tensors (HOST array, read during the call) taken as one vector:
+ * norm (DEVICE float [1]) = sqrt(sum of squares), summed in float64. */
+tfe_status tfe_grad_norm(const tfe_grad_tensor *tensors, int64_t n, float *norm, void *workspace,
+                         int64_t workspace_bytes, void *stream);
+/* out = grad * min(1, max_norm / norm), for a norm that is on the device (of
+ * these tensors, or joined from several ranks'); products are float32, rounded
+ * once.  A norm that is 0, infinite or NaN changes nothing (out = grad): the
+ * caller sees it in norm.  Where nothing changes and out is grad nothing is
+ * written.  0 <= max_norm, finite. */
+tfe_status tfe_grad_clip(const tfe_grad_tensor *tensors, int64_t n, float max_norm,
+                         const float *norm, void *stream);
+/* Both in one call. */
+tfe_status tfe_grad_norm_clip(const tfe_grad_tensor *tensors, int64_t n, float max_norm,
+                              float *norm, void *workspace, int64_t workspace_bytes,
+                              void *stream);
+int64_t tfe_grad_workspace(const tfe_grad_tensor *tensors, int64_t n); /* -1: bad tensors */
+
+/* Integer layout.  A matrix [rows x dim] becomes
+ *   codes   DEVICE int8 [rows x P], P = dim rounded up to 128, zero from column
+ *           dim on; 16-byte aligned;
+ *   scales  DEVICE float [rows],
+ * value = code * scale: one scale for each token (hidden states) or output
+ * channel (rows of W).  With m the largest finite |x| of the row,
+ *   scale = m / 127,  code = x * (127 * (1 / m)) rounded to nearest even,
+ * the quotients and products each rounded to float32.  Rows with m <= 2^-100 have scale and
+ * codes 0; infinities become +-127; a row with a NaN has scale NaN.
+ * dim <= 65536, rows <= 2^20. */
+tfe_status tfe_integer_quantize(const void *x, int32_t dtype, int64_t ldx, int64_t rows, int32_t dim,
+                             int8_t *codes, float *scales, void *stream);
+/* out[r, n] = ((sum over k of a[r, k] w[n, k]) * a_scales[r]) * w_scales[n]: the
+ * sum exact in 32-bit integers, the products float32, rounded to out_dtype; codes in
+ * [-127, 127].  rows <= 2^20, 1 <= out_dim <= 2^20, dim <= 65536. */
+tfe_status tfe_integer_matmul(const int8_t *a, const float *a_scales, const int8_t *w,
+                           const float *w_scales, int64_t rows, int32_t out_dim, int32_t dim,
+                           void *out, int32_t out_dtype, int64_t ldo, void *stream);
+/* tfe_integer_quantize of x and tfe_integer_matmul in one call. */
+tfe_status tfe_integer_linear(const void *x, int32_t dtype, int64_t ldx, const int8_t *w,
+                           const float *w_scales, int64_t rows, int32_t out_dim, int32_t dim,
+                           void *out, int32_t out_dtype, int64_t ldo, void *workspace,
+                           int64_t workspace_bytes, void *stream);
+int64_t tfe_integer_workspace(int64_t rows, int32_t dim); /* -1: bad size */
+
 /* ---- Offline phrase-table construction -----------------------------------
  * Paper: Sec. 4.2 (candidate phrases mined from a corpus and selected by
  * frequency; n-gram extraction is the dominant construction cost reported in

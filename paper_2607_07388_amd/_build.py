@@ -11,9 +11,9 @@ SO = os.path.join(HERE, "libtfe.so")
 CALLS = os.path.join(HERE, "_calls.so")
 ROCM_INC = os.path.join(os.environ.get("ROCM_PATH", "/opt/rocm"), "include")
 
-SOURCES = ["tfe_api.cpp", "tfe_head_api.cpp", "tfe_logits_api.cpp", "tfe_host.cpp", "tfe_stage.cpp",
-           "tfe_build.hip", "tfe_distill.hip", "tfe_head.hip",
-           "tfe_head_noalloc.hip", "tfe_quantized.hip", "tfe_sample.hip", "tfe_lookup.hip", "tfe_multi.hip", "tfe_tiered.hip"]
+SOURCES = ["tfe_api.cpp", "tfe_head_api.cpp", "tfe_logits_api.cpp", "tfe_learn_api.cpp", "tfe_host.cpp", "tfe_stage.cpp",
+           "tfe_build.hip", "tfe_cross_entropy.hip", "tfe_distill.hip", "tfe_grad_norm.hip", "tfe_head.hip",
+           "tfe_head_noalloc.hip", "tfe_int8.hip", "tfe_quantized.hip", "tfe_sample.hip", "tfe_lookup.hip", "tfe_multi.hip", "tfe_tiered.hip"]
 
 HIP_FLAGS = ["--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-Wall",
              # Packed-FP32 instructions stay off: ordinary float code only.

@@ -21,6 +21,7 @@ struct Call {
   void* fn;
 };
 Call g_lookup, g_multi, g_prefetch, g_scored, g_topk, g_linear, g_sample, g_loss, g_grad, g_both;
+Call g_xent, g_xent_grad, g_xent_both, g_norm, g_clip, g_norm_clip, g_int8;
 
 // Each conversion returns false, with no exception set, for what the plain
 // case does not cover.
@@ -281,6 +282,143 @@ PyObject* distill_loss_grad(PyObject*, PyObject* const* a, Py_ssize_t n, PyObjec
   return status(st);
 }
 
+PyObject* integer_linear(PyObject*, PyObject* const* a, Py_ssize_t n, PyObject* kw) {
+  PLAIN(g_int8, 13);
+  void *x, *w, *ws, *out, *space;
+  int64_t ldx, rows, ldo, bytes;
+  int32_t dtype, odt, od, dim;
+  SLOW_UNLESS(g_int8, pointer(a[0], &x) && int32(a[1], &dtype) && int64(a[2], &ldx) &&
+                            pointer(a[3], &w) && pointer(a[4], &ws) && int64(a[5], &rows) &&
+                            int32(a[6], &od) && int32(a[7], &dim) && pointer(a[8], &out) &&
+                            int32(a[9], &odt) && int64(a[10], &ldo) && pointer(a[11], &space) &&
+                            int64(a[12], &bytes));
+  using Fn = int (*)(void*, int32_t, int64_t, void*, void*, int64_t, int32_t, int32_t, void*,
+                     int32_t, int64_t, void*, int64_t, void*);
+  int st;
+  Py_BEGIN_ALLOW_THREADS;
+  st = ((Fn)g_int8.fn)(x, dtype, ldx, w, ws, rows, od, dim, out, odt, ldo, space, bytes, s);
+  Py_END_ALLOW_THREADS;
+  return status(st);
+}
+
+// The arguments that the cross entropy calls begin with.
+struct Xent {
+  void *h, *w, *t;
+  int64_t ldh, ldw, rows;
+  int32_t vocab, dim;
+};
+bool xent(PyObject* const* a, Xent* x) {
+  return pointer(a[0], &x->h) && int64(a[1], &x->ldh) && pointer(a[2], &x->w) &&
+         int64(a[3], &x->ldw) && pointer(a[4], &x->t) && int64(a[5], &x->rows) &&
+         int32(a[6], &x->vocab) && int32(a[7], &x->dim);
+}
+// Gradients and workspace, from a on.
+struct XentGrads {
+  void *gx, *gw, *space;
+  int64_t ldgx, ldgw, bytes;
+  int32_t dtype, add;
+};
+bool xent_grads(PyObject* const* a, XentGrads* g) {
+  return pointer(a[0], &g->gx) && int64(a[1], &g->ldgx) && pointer(a[2], &g->gw) &&
+         int64(a[3], &g->ldgw) && int32(a[4], &g->dtype) && int32(a[5], &g->add) &&
+         pointer(a[6], &g->space) && int64(a[7], &g->bytes);
+}
+
+PyObject* cross_entropy_loss(PyObject*, PyObject* const* a, Py_ssize_t n, PyObject* kw) {
+  PLAIN(g_xent, 12);
+  Xent x;
+  void *loss, *lse, *space;
+  int64_t bytes;
+  SLOW_UNLESS(g_xent, xent(a, &x) && pointer(a[8], &loss) && pointer(a[9], &lse) &&
+                          pointer(a[10], &space) && int64(a[11], &bytes));
+  using Fn = int (*)(void*, int64_t, void*, int64_t, void*, int64_t, int32_t, int32_t, void*, void*,
+                     void*, int64_t, void*);
+  int st;
+  Py_BEGIN_ALLOW_THREADS;
+  st = ((Fn)g_xent.fn)(x.h, x.ldh, x.w, x.ldw, x.t, x.rows, x.vocab, x.dim, loss, lse, space, bytes,
+                       s);
+  Py_END_ALLOW_THREADS;
+  return status(st);
+}
+
+PyObject* cross_entropy_grad(PyObject*, PyObject* const* a, Py_ssize_t n, PyObject* kw) {
+  PLAIN(g_xent_grad, 18);
+  Xent x;
+  XentGrads g;
+  void *lse, *weight;
+  SLOW_UNLESS(g_xent_grad, xent(a, &x) && pointer(a[8], &lse) && pointer(a[9], &weight) &&
+                               xent_grads(a + 10, &g));
+  using Fn = int (*)(void*, int64_t, void*, int64_t, void*, int64_t, int32_t, int32_t, void*, void*,
+                     void*, int64_t, void*, int64_t, int32_t, int32_t, void*, int64_t, void*);
+  int st;
+  Py_BEGIN_ALLOW_THREADS;
+  st = ((Fn)g_xent_grad.fn)(x.h, x.ldh, x.w, x.ldw, x.t, x.rows, x.vocab, x.dim, lse, weight, g.gx,
+                            g.ldgx, g.gw, g.ldgw, g.dtype, g.add, g.space, g.bytes, s);
+  Py_END_ALLOW_THREADS;
+  return status(st);
+}
+
+PyObject* cross_entropy_loss_grad(PyObject*, PyObject* const* a, Py_ssize_t n, PyObject* kw) {
+  PLAIN(g_xent_both, 19);
+  Xent x;
+  XentGrads g;
+  void *weight, *loss, *lse;
+  SLOW_UNLESS(g_xent_both, xent(a, &x) && pointer(a[8], &weight) && pointer(a[9], &loss) &&
+                               pointer(a[10], &lse) && xent_grads(a + 11, &g));
+  using Fn = int (*)(void*, int64_t, void*, int64_t, void*, int64_t, int32_t, int32_t, void*, void*,
+                     void*, void*, int64_t, void*, int64_t, int32_t, int32_t, void*, int64_t, void*);
+  int st;
+  Py_BEGIN_ALLOW_THREADS;
+  st = ((Fn)g_xent_both.fn)(x.h, x.ldh, x.w, x.ldw, x.t, x.rows, x.vocab, x.dim, weight, loss, lse,
+                            g.gx, g.ldgx, g.gw, g.ldgw, g.dtype, g.add, g.space, g.bytes, s);
+  Py_END_ALLOW_THREADS;
+  return status(st);
+}
+
+PyObject* grad_norm(PyObject*, PyObject* const* a, Py_ssize_t n, PyObject* kw) {
+  PLAIN(g_norm, 5);
+  void *list, *norm, *space;
+  int64_t count, bytes;
+  SLOW_UNLESS(g_norm, pointer(a[0], &list) && int64(a[1], &count) && pointer(a[2], &norm) &&
+                          pointer(a[3], &space) && int64(a[4], &bytes));
+  using Fn = int (*)(void*, int64_t, void*, void*, int64_t, void*);
+  int st;
+  Py_BEGIN_ALLOW_THREADS;
+  st = ((Fn)g_norm.fn)(list, count, norm, space, bytes, s);
+  Py_END_ALLOW_THREADS;
+  return status(st);
+}
+
+PyObject* grad_clip(PyObject*, PyObject* const* a, Py_ssize_t n, PyObject* kw) {
+  PLAIN(g_clip, 4);
+  void *list, *norm;
+  int64_t count;
+  float most;
+  SLOW_UNLESS(g_clip, pointer(a[0], &list) && int64(a[1], &count) && number(a[2], &most) &&
+                          pointer(a[3], &norm));
+  using Fn = int (*)(void*, int64_t, float, void*, void*);
+  int st;
+  Py_BEGIN_ALLOW_THREADS;
+  st = ((Fn)g_clip.fn)(list, count, most, norm, s);
+  Py_END_ALLOW_THREADS;
+  return status(st);
+}
+
+PyObject* grad_norm_clip(PyObject*, PyObject* const* a, Py_ssize_t n, PyObject* kw) {
+  PLAIN(g_norm_clip, 6);
+  void *list, *norm, *space;
+  int64_t count, bytes;
+  float most;
+  SLOW_UNLESS(g_norm_clip, pointer(a[0], &list) && int64(a[1], &count) && number(a[2], &most) &&
+                               pointer(a[3], &norm) && pointer(a[4], &space) && int64(a[5], &bytes));
+  using Fn = int (*)(void*, int64_t, float, void*, void*, int64_t, void*);
+  int st;
+  Py_BEGIN_ALLOW_THREADS;
+  st = ((Fn)g_norm_clip.fn)(list, count, most, norm, space, bytes, s);
+  Py_END_ALLOW_THREADS;
+  return status(st);
+}
+
 // bind(check, {name: (ctypes function wrapper, address)}); of the calls on
 // logits any may be left out, and stays as it is.
 PyObject* bind(PyObject*, PyObject* args) {
@@ -299,7 +437,14 @@ PyObject* bind(PyObject*, PyObject* args) {
              {"tfe_sample", &g_sample, true},
              {"tfe_distill_loss", &g_loss, true},
              {"tfe_distill_grad", &g_grad, true},
-             {"tfe_distill_loss_grad", &g_both, true}};
+             {"tfe_distill_loss_grad", &g_both, true},
+             {"tfe_cross_entropy_loss", &g_xent, true},
+             {"tfe_cross_entropy_grad", &g_xent_grad, true},
+             {"tfe_cross_entropy_loss_grad", &g_xent_both, true},
+             {"tfe_grad_norm", &g_norm, true},
+             {"tfe_grad_clip", &g_clip, true},
+             {"tfe_grad_norm_clip", &g_norm_clip, true},
+             {"tfe_integer_linear", &g_int8, true}};
   for (const auto& e : all) {
     PyObject* v = PyDict_GetItemString(calls, e.name);
     PyObject *f, *p;
@@ -356,6 +501,28 @@ PyMethodDef g_methods[] = {
      "tfe_distill_loss_grad($module, logits, dtype, ld, rows, vocab, teacher_ids, teacher_logits, "
      "teacher_dtype, K, temperature, grad_loss, loss, lse, grad, ldg, workspace, workspace_bytes, "
      "stream=None)\n--\n\n"},
+    {"tfe_cross_entropy_loss", (PyCFunction)(void (*)(void))cross_entropy_loss, FAST,
+     "tfe_cross_entropy_loss($module, hidden, ldh, w, ldw, targets, rows, vocab, dim, loss, "
+     "lse, workspace, workspace_bytes, stream=None)\n--\n\n"},
+    {"tfe_cross_entropy_grad", (PyCFunction)(void (*)(void))cross_entropy_grad, FAST,
+     "tfe_cross_entropy_grad($module, hidden, ldh, w, ldw, targets, rows, vocab, dim, lse, "
+     "grad_loss, grad_hidden, ldgh, grad_w, ldgw, grad_dtype, accumulate, workspace, "
+     "workspace_bytes, stream=None)\n--\n\n"},
+    {"tfe_cross_entropy_loss_grad", (PyCFunction)(void (*)(void))cross_entropy_loss_grad, FAST,
+     "tfe_cross_entropy_loss_grad($module, hidden, ldh, w, ldw, targets, rows, vocab, dim, "
+     "grad_loss, loss, lse, grad_hidden, ldgh, grad_w, ldgw, grad_dtype, accumulate, "
+     "workspace, workspace_bytes, stream=None)\n--\n\n"},
+    {"tfe_grad_norm", (PyCFunction)(void (*)(void))grad_norm, FAST,
+     "tfe_grad_norm($module, tensors, n, norm, workspace, workspace_bytes, "
+     "stream=None)\n--\n\n"},
+    {"tfe_grad_clip", (PyCFunction)(void (*)(void))grad_clip, FAST,
+     "tfe_grad_clip($module, tensors, n, max_norm, norm, stream=None)\n--\n\n"},
+    {"tfe_grad_norm_clip", (PyCFunction)(void (*)(void))grad_norm_clip, FAST,
+     "tfe_grad_norm_clip($module, tensors, n, max_norm, norm, workspace, workspace_bytes, "
+     "stream=None)\n--\n\n"},
+    {"tfe_integer_linear", (PyCFunction)(void (*)(void))integer_linear, FAST,
+     "tfe_integer_linear($module, x, dtype, ldx, w, w_scales, rows, out_dim, dim, out, "
+     "out_dtype, ldo, workspace, workspace_bytes, stream=None)\n--\n\n"},
     {nullptr, nullptr, 0, nullptr}};
 PyModuleDef g_module = {PyModuleDef_HEAD_INIT, "_calls", nullptr, -1, g_methods,
                         nullptr, nullptr, nullptr, nullptr};

@@ -1,0 +1,588 @@
+// Softmax cross entropy of the head's logits z = H W^T (H the hidden states
+// [rows x dim], W the projection [vocab x dim], bfloat16), which are computed
+// in tiles and not kept:
+//   lse_r = log sum_v exp z_rv,  loss_r = lse_r - z_rt,
+//   dz_rv = weight_r (exp(z_rv - lse_r) - [v = t]),  dH = dz W,  dW = dz^T H.
+#include <float.h>
+#include <hip/hip_runtime.h>
+#include <stdint.h>
+
+#include <algorithm>
+#include <atomic>
+
+#include "tfe_gemm.h"
+#include "tfe_learn.h"
+#include "tfe_rows.h"
+
+namespace tfe {
+namespace {
+
+using gemm::Bf16;
+using gemm::Operand;
+using gemm::Tile;
+using rows::pack2;
+using rows::u32x4;
+typedef gemm::f32x4 f32x4;
+typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
+typedef float f32x2 __attribute__((ext_vector_type(2)));
+
+// A matrix in memory as the tiles read it.
+struct Matrix {
+  const uint16_t* at;
+  uint32_t ld, rows, cols;
+};
+__device__ __forceinline__ Operand along(const Matrix& m, uint32_t row) {
+  return Operand{(const char*)(m.at + (size_t)row * m.ld), m.ld * 2, m.rows > row ? m.rows - row : 0u, m.cols};
+}
+__device__ __forceinline__ Operand across(const Matrix& m, uint32_t col) {
+  return Operand{(const char*)(m.at + col), m.ld * 2, m.rows, m.cols > col ? m.cols - col : 0u};
+}
+
+// Blocks go to the 8 XCDs in turn; place t of them as if each XCD took a run of
+// neighbouring places, so that those share its L2.  `total` is a multiple of 8.
+__device__ __forceinline__ uint32_t place_of(uint32_t t, uint32_t total) {
+  return (t & 7) * (total >> 3) + (t >> 3);
+}
+
+// ---- rows in aligned order -------------------------------------------------------
+
+// Copies rows, with zeros behind their columns; rows whose target is none or
+// whose weight is 0 (targets given) become zeros, so that whatever they hold
+// takes no part in dW.
+struct PackArgs {
+  const uint16_t* x;
+  int64_t ldx;
+  uint32_t rows, cols, pitch;
+  const int32_t* targets;
+  const float* weight;
+  uint32_t vocab;
+  uint16_t* out;
+};
+__global__ __launch_bounds__(256) void k_pack(PackArgs a) {
+  const uint32_t per = a.pitch / 8;
+  const uint64_t n = (uint64_t)a.rows * per;
+  for (uint64_t at = (uint64_t)blockIdx.x * 256 + threadIdx.x; at < n; at += (uint64_t)gridDim.x * 256) {
+    const uint32_t r = (uint32_t)(at / per), c = (uint32_t)(at - (uint64_t)r * per) * 8;
+    u32x4 v{0, 0, 0, 0};
+    const bool none = a.targets && ((uint32_t)a.targets[r] >= a.vocab || (a.weight && a.weight[r] == 0.f));
+    if (!none) {
+      const uint16_t* x = a.x + (size_t)r * a.ldx + c;
+      if (c + 8 <= a.cols) {
+        v = *(const rows::u32x4_a2*)x;
+      } else {
+#pragma unroll
+        for (int j = 0; j < 8; ++j)
+          if (c + j < a.cols) v[j / 2] |= (uint32_t)x[j] << (16 * (j & 1));
+      }
+    }
+    *(u32x4*)(a.out + (size_t)r * a.pitch + c) = v;
+  }
+}
+
+// ---- logits: their sums, or dz -----------------------------------------------------
+
+struct LogitsArgs {
+  Matrix w, h;      // h: the rows of this launch
+  uint32_t tiles_q, total;
+  uint32_t vocab0;  // of w's first row
+  const int32_t* targets;
+  // sums
+  f32x2* part;      // [slab][rows of the launch]
+  uint32_t slab0;
+  float* picked;    // the target's logit
+  // dz
+  const float* lse;
+  const float* weight;
+  uint32_t vocab;
+  uint16_t* dz;     // [planes][rows][pitch]
+  uint32_t pitch;
+  uint64_t plane;
+};
+
+template <int TP, int TQ, int WP, int WQ>
+__device__ __forceinline__ bool logits_tile(const LogitsArgs& a, Tile<Bf16, TP, TQ, WP, WQ, false, false>& t,
+                                            uint32_t* p0, uint32_t* q0, char* lds) {
+  const uint32_t place = place_of(blockIdx.x, a.total);
+  *p0 = place / a.tiles_q * TP;
+  *q0 = place % a.tiles_q * TQ;
+  if (*p0 >= a.w.rows) return false;
+  t.clear();
+  const Operand p = along(a.w, *p0), q = along(a.h, *q0);
+  t.run(p, q, 0, (a.w.cols * 2 + gemm::kStep - 1) / gemm::kStep, lds);
+  return true;
+}
+
+// Columns of a slab: those of one wave.
+constexpr int kSlab = 128;
+
+template <int TP, int TQ, int WP, int WQ>
+__global__ __launch_bounds__(WP* WQ * 64) void k_sums(LogitsArgs a) {
+  extern __shared__ __attribute__((aligned(1024))) char lds[];
+  Tile<Bf16, TP, TQ, WP, WQ, false, false> t;
+  static_assert(TP / WP == kSlab, "a wave's columns are a slab");
+  uint32_t p0, q0;
+  if (!logits_tile<TP, TQ, WP, WQ>(a, t, &p0, &q0, lds)) return;
+  const uint32_t c0 = p0 + t.wp + t.g * 4, slab = a.slab0 + (p0 + t.wp) / kSlab;
+#pragma unroll
+  for (int m = 0; m < t.MT; ++m) {
+    const uint32_t r = q0 + t.wq + m * 16 + t.i;
+    float top = -FLT_MAX, sum = 0.f;
+#pragma unroll
+    for (int n = 0; n < t.NT; ++n)
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        if (c0 + n * 16 + j >= a.w.rows) t.acc[n][m][j] = -INFINITY;
+        top = fmaxf(top, t.acc[n][m][j]);
+      }
+    top = fmaxf(top, __shfl_xor(top, 16));
+    top = fmaxf(top, __shfl_xor(top, 32));
+#pragma unroll
+    for (int n = 0; n < t.NT; ++n)
+#pragma unroll
+      for (int j = 0; j < 4; ++j) sum += __expf(t.acc[n][m][j] - top);
+    sum += __shfl_xor(sum, 16);
+    sum += __shfl_xor(sum, 32);
+    if (r < a.h.rows) {
+      if (t.g == 0 && p0 + t.wp < a.w.rows) a.part[(size_t)slab * a.h.rows + r] = f32x2{top, sum};
+      const uint32_t at = (uint32_t)a.targets[r] - a.vocab0 - c0;
+      if (at < (uint32_t)kSlab && (at & 12) == 0) {
+        float z = 0.f;
+#pragma unroll
+        for (int n = 0; n < t.NT; ++n)
+#pragma unroll
+          for (int j = 0; j < 4; ++j) z = at == (uint32_t)(n * 16 + j) ? t.acc[n][m][j] : z;
+        if (c0 + at < a.w.rows) a.picked[r] = z;
+      }
+    }
+  }
+}
+
+// A block joins the slabs of 16 rows.
+struct JoinArgs {
+  const f32x2* part;
+  uint32_t slabs, rows, vocab;
+  const int32_t* targets;
+  const float* picked;
+  float* loss;
+  float* lse;
+};
+__global__ __launch_bounds__(1024) void k_join(JoinArgs a) {
+  __shared__ f32x2 red[64][17];
+  const uint32_t i = threadIdx.x & 15, y = threadIdx.x >> 4, r = blockIdx.x * 16 + i;
+  float top = -FLT_MAX, sum = 0.f;
+  if (r < a.rows)
+    for (uint32_t k = y; k < a.slabs; k += 64) {
+      const f32x2 v = a.part[(size_t)k * a.rows + r];
+      const float m = fmaxf(top, v[0]);
+      sum = sum * __expf(top - m) + v[1] * __expf(v[0] - m);
+      top = m;
+    }
+  red[y][i] = f32x2{top, sum};
+  __syncthreads();
+  if (y != 0 || r >= a.rows) return;
+  for (int k = 1; k < 64; ++k) top = fmaxf(top, red[k][i][0]);
+  sum = 0.f;
+  for (int k = 0; k < 64; ++k) sum += red[k][i][1] * __expf(red[k][i][0] - top);
+  const float rest = logf(sum);
+  a.lse[r] = top + rest;
+  a.loss[r] = (uint32_t)a.targets[r] < a.vocab ? (top - a.picked[r]) + rest : 0.f;
+}
+
+template <int TP, int TQ, int WP, int WQ, int PLANES>
+__global__ __launch_bounds__(WP* WQ * 64) void k_dz(LogitsArgs a) {
+  extern __shared__ __attribute__((aligned(1024))) char lds[];
+  Tile<Bf16, TP, TQ, WP, WQ, false, false> t;
+  uint32_t p0, q0;
+  if (!logits_tile<TP, TQ, WP, WQ>(a, t, &p0, &q0, lds)) return;
+  const uint32_t c0 = p0 + t.wp + t.g * 4;
+#pragma unroll
+  for (int m = 0; m < t.MT; ++m) {
+    const uint32_t r = q0 + t.wq + m * 16 + t.i;
+    if (r >= a.h.rows) continue;
+    const uint32_t target = (uint32_t)a.targets[r];
+    const float lse = a.lse[r];
+    const float weight = target < a.vocab ? (a.weight ? a.weight[r] : 1.f) : 0.f;
+    const uint32_t at = target - a.vocab0 - c0;
+    uint16_t* out = a.dz + (size_t)r * a.pitch + c0;
+#pragma unroll
+    for (int n = 0; n < t.NT; ++n) {
+      float d[4], e[4];
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        float v = __expf(t.acc[n][m][j] - lse);
+        if (at == (uint32_t)(n * 16 + j)) v -= 1.f;
+        d[j] = weight == 0.f || c0 + n * 16 + j >= a.w.rows ? 0.f : v * weight;
+        if (PLANES == 2) e[j] = d[j] - (float)(__bf16)d[j];
+      }
+      if (c0 + n * 16 < a.pitch) {
+        *(u32x2*)(out + n * 16) = u32x2{pack2(d[0], d[1]), pack2(d[2], d[3])};
+        if (PLANES == 2) *(u32x2*)(out + a.plane + n * 16) = u32x2{pack2(e[0], e[1]), pack2(e[2], e[3])};
+      }
+    }
+  }
+}
+
+// ---- gradients -----------------------------------------------------------------------
+
+struct GradHArgs {
+  Matrix w, dz;  // a piece of the vocabulary
+  uint32_t planes;
+  uint64_t plane;
+  uint32_t tiles_p, tiles_q, splits, total, dim;
+  float* sums;  // [splits][rows][pitch]
+  uint32_t pitch;
+  bool add;
+};
+template <int TP, int TQ, int WP, int WQ>
+__global__ __launch_bounds__(WP* WQ * 64) void k_grad_h(GradHArgs a) {
+  extern __shared__ __attribute__((aligned(1024))) char lds[];
+  Tile<Bf16, TP, TQ, WP, WQ, true, false> t;
+  const uint32_t place = place_of(blockIdx.x, a.total), tiles = a.tiles_p * a.tiles_q;
+  const uint32_t split = place / tiles, in = place % tiles;
+  if (split >= a.splits) return;
+  const uint32_t p0 = in % a.tiles_p * TP, q0 = in / a.tiles_p * TQ;
+  const uint32_t steps = (a.w.rows + 63) / 64;
+  const uint32_t s0 = (uint32_t)((uint64_t)steps * split / a.splits);
+  const uint32_t s1 = (uint32_t)((uint64_t)steps * (split + 1) / a.splits);
+  t.clear();
+  for (uint32_t k = 0; k < a.planes; ++k) {
+    Matrix dz = a.dz;
+    dz.at += k * a.plane;
+    t.run(across(a.w, p0), along(dz, q0), s0, s1, lds);
+  }
+  const uint32_t c0 = p0 + t.wp + t.g * 4;
+#pragma unroll
+  for (int m = 0; m < t.MT; ++m) {
+    const uint32_t r = q0 + t.wq + m * 16 + t.i;
+    if (r >= a.dz.rows) continue;
+    float* out = a.sums + ((size_t)split * a.dz.rows + r) * a.pitch + c0;
+#pragma unroll
+    for (int n = 0; n < t.NT; ++n)
+      if (c0 + n * 16 < a.pitch) {
+        f32x4 v = t.acc[n][m];
+        if (a.add) v += *(const f32x4*)(out + n * 16);
+        *(f32x4*)(out + n * 16) = v;
+      }
+  }
+}
+struct FinishArgs {
+  const float* sums;
+  uint32_t splits, rows, pitch, dim;
+  void* out;
+  int64_t ldo;
+  const int32_t* targets;
+  const float* weight;
+  uint32_t vocab;
+};
+template <int DT> __global__ __launch_bounds__(256) void k_finish_h(FinishArgs a) {
+  const uint32_t per = a.pitch / 4;
+  const uint64_t n = (uint64_t)a.rows * per;
+  for (uint64_t at = (uint64_t)blockIdx.x * 256 + threadIdx.x; at < n; at += (uint64_t)gridDim.x * 256) {
+    const uint32_t r = (uint32_t)(at / per), c = (uint32_t)(at - (uint64_t)r * per) * 4;
+    f32x4 v{0, 0, 0, 0};
+    for (uint32_t k = 0; k < a.splits; ++k)
+      v += *(const f32x4*)(a.sums + ((size_t)k * a.rows + r) * a.pitch + c);
+    // 0 x an infinity of W is not a gradient of a row without one.
+    const bool none = (uint32_t)a.targets[r] >= a.vocab || (a.weight && a.weight[r] == 0.f);
+    char* out = (char*)a.out + ((size_t)r * a.ldo) * sizeof(typename rows::Elem<DT>::T);
+#pragma unroll
+    for (int j = 0; j < 4; ++j)
+      if (c + j < a.dim) rows::store1<DT>(out, c + j, none ? 0.f : v[j]);
+  }
+}
+
+struct GradWArgs {
+  Matrix h, dz;  // dz's columns are a piece of the vocabulary
+  uint32_t planes;
+  uint64_t plane;
+  uint32_t tiles_p, total, dim, vocab;  // vocab: of the piece
+  void* out;
+  int64_t ldo;
+  bool add;
+};
+template <int TP, int TQ, int WP, int WQ, int DT>
+__global__ __launch_bounds__(WP* WQ * 64) void k_grad_w(GradWArgs a) {
+  typedef typename rows::Elem<DT>::T T;
+  extern __shared__ __attribute__((aligned(1024))) char lds[];
+  Tile<Bf16, TP, TQ, WP, WQ, true, true> t;
+  const uint32_t place = place_of(blockIdx.x, a.total);
+  const uint32_t p0 = place % a.tiles_p * TP, q0 = place / a.tiles_p * TQ;
+  if (q0 >= a.vocab) return;
+  t.clear();
+  for (uint32_t k = 0; k < a.planes; ++k) {
+    Matrix dz = a.dz;
+    dz.at += k * a.plane;
+    t.run(across(a.h, p0), across(dz, q0), 0, (a.h.rows + 63) / 64, lds);
+  }
+  const uint32_t c0 = p0 + t.wp + t.g * 4;
+#pragma unroll
+  for (int m = 0; m < t.MT; ++m) {
+    const uint32_t v = q0 + t.wq + m * 16 + t.i;
+    if (v >= a.vocab) continue;
+    T* out = (T*)a.out + (size_t)v * a.ldo + c0;
+#pragma unroll
+    for (int n = 0; n < t.NT; ++n) {
+      f32x4 x = t.acc[n][m];
+      typedef f32x4 f4 __attribute__((aligned(4)));
+      typedef u32x2 u2 __attribute__((aligned(2)));
+      if (c0 + n * 16 + 4 <= a.dim) {
+        if constexpr (DT == TFE_F32) {
+          if (a.add) x += *(const f4*)(out + n * 16);
+          *(f4*)(out + n * 16) = x;
+        } else {
+          *(u2*)(out + n * 16) = u2{pack2(x[0], x[1]), pack2(x[2], x[3])};
+        }
+      } else {
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+          if (c0 + n * 16 + j < a.dim) {
+            const float old = DT == TFE_F32 && a.add ? rows::load1<DT>(out, n * 16 + j) : 0.f;
+            rows::store1<DT>(out, n * 16 + j, x[j] + old);
+          }
+      }
+    }
+  }
+}
+
+// ---- launches ------------------------------------------------------------------------
+
+// What lies where in the workspace, and how the work is cut.
+struct Plan {
+  uint32_t pitch;        // of packed rows and of dH's sums: dim rounded up to 64
+  uint32_t piece;        // columns of the vocabulary at a time
+  uint32_t chunk;        // rows at a time whose slabs' sums are kept
+  uint32_t splits;       // of dH's sums over the vocabulary
+  uint32_t tile;         // rows of a tile
+  int64_t h, masked, w, part, picked, dz, sums, bytes;
+};
+
+int64_t take(int64_t* at, int64_t bytes) {
+  const int64_t here = *at;
+  *at += (bytes + 255) / 256 * 256;
+  return here;
+}
+uint32_t up(uint32_t x, uint32_t to) { return (x + to - 1) / to * to; }
+
+Plan plan_of(int64_t n_rows, int32_t n_vocab, int32_t n_dim) {
+  const uint32_t rows = (uint32_t)n_rows, vocab = (uint32_t)n_vocab, dim = (uint32_t)n_dim;
+  Plan p{};
+  p.pitch = up(dim, 64);
+  p.tile = rows > 128 ? 256 : rows > 64 ? 128 : 64;
+  const uint32_t most = std::max<uint32_t>(2048, (uint32_t)std::min<int64_t>((1 << 27) / n_rows, 1 << 18) / 256 * 256);
+  const uint32_t pieces = (vocab + most - 1) / most;
+  p.piece = up((vocab + pieces - 1) / pieces, 256);
+  p.chunk = std::min<uint32_t>(rows, 16384);
+  const uint32_t tiles = ((dim + 255) / 256) * ((rows + p.tile - 1) / p.tile);
+  p.splits = std::max<uint32_t>(1, std::min<uint32_t>((uint32_t)compute_units() / tiles, p.piece / 256));
+  int64_t at = 0;
+  p.h = take(&at, (int64_t)rows * p.pitch * 2);
+  p.masked = take(&at, (int64_t)rows * p.pitch * 2);
+  p.w = take(&at, (int64_t)p.piece * p.pitch * 2);
+  p.part = take(&at, (int64_t)((vocab + p.piece - 1) / p.piece * p.piece / kSlab) * p.chunk * 8);
+  p.picked = take(&at, (int64_t)rows * 4);
+  p.dz = take(&at, (int64_t)rows * (p.piece + 64) * 4);
+  p.sums = take(&at, (int64_t)p.splits * rows * p.pitch * 4);
+  p.bytes = at;
+  return p;
+}
+
+// 16-byte loads of whole rows.
+bool direct(const void* p, int64_t ld, uint32_t dim) {
+  return ((uintptr_t)p & 15) == 0 && ld % 8 == 0 && dim % 8 == 0 && ld <= kXentMaxPitch;
+}
+
+hipError_t pack(const uint16_t* x, int64_t ldx, uint32_t rows, uint32_t cols, uint32_t pitch,
+                const XentArgs* masked, uint16_t* out, hipStream_t s) {
+  PackArgs a{x, ldx, rows, cols, pitch, nullptr, nullptr, 0, out};
+  if (masked) a.targets = masked->targets, a.weight = masked->weight, a.vocab = masked->vocab;
+  const uint64_t n = (uint64_t)rows * (pitch / 8);
+  k_pack<<<dim3((uint32_t)std::min<uint64_t>((n + 255) / 256, 8192)), dim3(256), 0, s>>>(a);
+  return hipGetLastError();
+}
+
+// More LDS than a kernel may have by default: told once for each device.
+template <class K> hipError_t allow(K* k, int bytes, std::atomic<uint64_t>* told) {
+  int dev = 0;
+  hipError_t e = hipGetDevice(&dev);
+  if (e != hipSuccess) return e;
+  const uint64_t bit = 1ull << (dev & 63);
+  if (dev > 63 || !(told->load(std::memory_order_relaxed) & bit)) {
+    e = hipFuncSetAttribute((const void*)k, hipFuncAttributeMaxDynamicSharedMemorySize, bytes);
+    if (e != hipSuccess) return e;
+    told->fetch_or(bit, std::memory_order_relaxed);
+  }
+  return hipSuccess;
+}
+#define LAUNCH(T, kernel, blocks, s, args)                                          \
+  do {                                                                              \
+    static std::atomic<uint64_t> told_{0};                                          \
+    const hipError_t e_ = allow(kernel, T::LDS, &told_);                            \
+    if (e_ != hipSuccess) return e_;                                                \
+    kernel<<<dim3(blocks), dim3(T::THREADS), T::LDS, s>>>(args);                    \
+    return hipGetLastError();                                                       \
+  } while (0)
+
+template <int TP, int TQ, int WP, int WQ> hipError_t sums(LogitsArgs a, hipStream_t s) {
+  typedef Tile<Bf16, TP, TQ, WP, WQ, false, false> T;
+  a.tiles_q = (a.h.rows + TQ - 1) / TQ;
+  a.total = up((a.w.rows + TP - 1) / TP * a.tiles_q, 8);
+  auto* k = k_sums<TP, TQ, WP, WQ>;
+  LAUNCH(T, k, a.total, s, a);
+}
+template <int TP, int TQ, int WP, int WQ, int PLANES> hipError_t dz(LogitsArgs a, hipStream_t s) {
+  typedef Tile<Bf16, TP, TQ, WP, WQ, false, false> T;
+  a.tiles_q = (a.h.rows + TQ - 1) / TQ;
+  a.total = up((a.w.rows + TP - 1) / TP * a.tiles_q, 8);
+  auto* k = k_dz<TP, TQ, WP, WQ, PLANES>;
+  LAUNCH(T, k, a.total, s, a);
+}
+template <int TP, int TQ, int WP, int WQ> hipError_t grad_h(GradHArgs a, hipStream_t s) {
+  typedef Tile<Bf16, TP, TQ, WP, WQ, true, false> T;
+  a.tiles_p = (a.dim + TP - 1) / TP;
+  a.tiles_q = (a.dz.rows + TQ - 1) / TQ;
+  a.total = up(a.tiles_p * a.tiles_q * a.splits, 8);
+  auto* k = k_grad_h<TP, TQ, WP, WQ>;
+  LAUNCH(T, k, a.total, s, a);
+}
+template <int TP, int TQ, int WP, int WQ, int DT> hipError_t grad_w(GradWArgs a, hipStream_t s) {
+  typedef Tile<Bf16, TP, TQ, WP, WQ, true, true> T;
+  a.tiles_p = (a.dim + TP - 1) / TP;
+  a.total = up(a.tiles_p * ((a.vocab + TQ - 1) / TQ), 8);
+  auto* k = k_grad_w<TP, TQ, WP, WQ, DT>;
+  LAUNCH(T, k, a.total, s, a);
+}
+
+// dW of no rows.
+__global__ __launch_bounds__(256) void k_zero(char* out, uint64_t pitch, uint32_t bytes) {
+  char* row = out + blockIdx.x * pitch;
+  for (uint32_t c = threadIdx.x * 2; c < bytes; c += 512) *(uint16_t*)(row + c) = 0;
+}
+hipError_t zero(const XentArgs& a, hipStream_t s) {
+  const uint32_t size = a.gdtype == TFE_F32 ? 4 : 2;
+  k_zero<<<dim3(a.vocab), dim3(256), 0, s>>>((char*)a.gw, (uint64_t)a.ldgw * size, a.dim * size);
+  return hipGetLastError();
+}
+
+#define TRY_HIP(call)                        \
+  do {                                       \
+    const hipError_t te_ = (call);           \
+    if (te_ != hipSuccess) return te_;       \
+  } while (0)
+
+// Rows [v0, v0 + n) of W as the tiles take them.
+hipError_t piece_of_w(const XentArgs& a, const Plan& p, uint32_t v0, uint32_t n, Matrix* m, hipStream_t s) {
+  const uint16_t* at = a.w + (size_t)v0 * a.ldw;
+  if (direct(a.w, a.ldw, a.dim)) {
+    *m = Matrix{at, (uint32_t)a.ldw, n, a.dim};
+    return hipSuccess;
+  }
+  uint16_t* to = (uint16_t*)(a.space + p.w);
+  *m = Matrix{to, p.pitch, n, p.pitch};
+  return pack(at, a.ldw, n, a.dim, p.pitch, nullptr, to, s);
+}
+
+}  // namespace
+
+int64_t xent_space(int64_t rows, int32_t vocab, int32_t dim) {
+  return rows == 0 ? 0 : plan_of(rows, vocab, dim).bytes;
+}
+
+hipError_t launch_xent_loss(const XentArgs& a, hipStream_t s) {
+  const Plan p = plan_of(a.rows, a.vocab, a.dim);
+  Matrix h{a.hidden, (uint32_t)a.ldh, a.rows, a.dim};
+  if (!direct(a.hidden, a.ldh, a.dim)) {
+    uint16_t* to = (uint16_t*)(a.space + p.h);
+    TRY_HIP(pack(a.hidden, a.ldh, a.rows, a.dim, p.pitch, nullptr, to, s));
+    h = Matrix{to, p.pitch, a.rows, p.pitch};
+  }
+  const uint32_t step = direct(a.w, a.ldw, a.dim) ? a.vocab : p.piece;
+  for (uint32_t r0 = 0; r0 < a.rows; r0 += p.chunk) {
+    LogitsArgs l{};
+    l.h = h;
+    l.h.at += (size_t)r0 * h.ld;
+    l.h.rows = std::min(p.chunk, a.rows - r0);
+    l.targets = a.targets + r0;
+    l.part = (f32x2*)(a.space + p.part);
+    l.picked = (float*)(a.space + p.picked) + r0;
+    for (uint32_t v0 = 0; v0 < a.vocab; v0 += step) {
+      TRY_HIP(piece_of_w(a, p, v0, std::min(step, a.vocab - v0), &l.w, s));
+      l.vocab0 = v0;
+      l.slab0 = v0 / kSlab;
+      TRY_HIP((p.tile == 256   ? sums<256, 256, 2, 4>(l, s)
+               : p.tile == 128 ? sums<256, 128, 2, 2>(l, s)
+                               : sums<256, 64, 2, 2>(l, s)));
+    }
+    JoinArgs j{l.part, (a.vocab + kSlab - 1) / kSlab, l.h.rows, a.vocab, l.targets, l.picked,
+               a.loss + r0, a.lse + r0};
+    k_join<<<dim3((l.h.rows + 15) / 16), dim3(1024), 0, s>>>(j);
+    TRY_HIP(hipGetLastError());
+  }
+  return hipSuccess;
+}
+
+hipError_t launch_xent_grad(const XentArgs& a, hipStream_t s) {
+  if (a.rows == 0) return a.accumulate ? hipSuccess : zero(a, s);
+  const Plan p = plan_of(a.rows, a.vocab, a.dim);
+  const bool f32 = a.gdtype == TFE_F32;
+  uint16_t* masked = (uint16_t*)(a.space + p.masked);
+  TRY_HIP(pack(a.hidden, a.ldh, a.rows, a.dim, p.pitch, &a, masked, s));
+  const Matrix h{masked, p.pitch, a.rows, p.pitch};
+  for (uint32_t v0 = 0; v0 < a.vocab; v0 += p.piece) {
+    const uint32_t n = std::min(p.piece, a.vocab - v0);
+    LogitsArgs l{};
+    l.h = h;
+    TRY_HIP(piece_of_w(a, p, v0, n, &l.w, s));
+    l.vocab0 = v0;
+    l.targets = a.targets;
+    l.lse = a.lse;
+    l.weight = a.weight;
+    l.vocab = a.vocab;
+    l.dz = (uint16_t*)(a.space + p.dz);
+    l.pitch = p.piece + 64;
+    l.plane = (uint64_t)a.rows * l.pitch;
+    l.h.cols = l.w.cols;  // zeros from dim on
+    if (f32)
+      TRY_HIP((p.tile == 256   ? dz<256, 256, 2, 4, 2>(l, s)
+               : p.tile == 128 ? dz<256, 128, 2, 2, 2>(l, s)
+                               : dz<256, 64, 2, 2, 2>(l, s)));
+    else
+      TRY_HIP((p.tile == 256   ? dz<256, 256, 2, 4, 1>(l, s)
+               : p.tile == 128 ? dz<256, 128, 2, 2, 1>(l, s)
+                               : dz<256, 64, 2, 2, 1>(l, s)));
+    const Matrix d{l.dz, l.pitch, a.rows, up(n, 64)};
+    GradHArgs gh{};
+    gh.w = l.w;
+    gh.dz = d;
+    gh.planes = f32 ? 2 : 1;
+    gh.plane = l.plane;
+    gh.splits = p.splits;
+    gh.dim = a.dim;
+    gh.sums = (float*)(a.space + p.sums);
+    gh.pitch = p.pitch;
+    gh.add = v0 != 0;
+    TRY_HIP((p.tile == 256   ? grad_h<256, 256, 2, 4>(gh, s)
+             : p.tile == 128 ? grad_h<256, 128, 2, 2>(gh, s)
+                             : grad_h<256, 64, 2, 2>(gh, s)));
+    GradWArgs gw{};
+    gw.h = h;
+    gw.dz = d;
+    gw.planes = gh.planes;
+    gw.plane = l.plane;
+    gw.dim = a.dim;
+    gw.vocab = n;
+    gw.ldo = a.ldgw;
+    gw.add = a.accumulate;
+    gw.out = (char*)a.gw + (size_t)v0 * a.ldgw * (f32 ? 4 : 2);
+    TRY_HIP((f32 ? grad_w<256, 256, 2, 4, TFE_F32>(gw, s) : grad_w<256, 256, 2, 4, TFE_BF16>(gw, s)));
+  }
+  FinishArgs f{(float*)(a.space + p.sums), p.splits, a.rows, p.pitch, a.dim, a.gx, a.ldgx, a.targets,
+               a.weight, a.vocab};
+  const uint32_t blocks = (uint32_t)std::min<uint64_t>(((uint64_t)a.rows * (p.pitch / 4) + 255) / 256, 8192);
+  if (f32)
+    k_finish_h<TFE_F32><<<dim3(blocks), dim3(256), 0, s>>>(f);
+  else
+    k_finish_h<TFE_BF16><<<dim3(blocks), dim3(256), 0, s>>>(f);
+  return hipGetLastError();
+}
+
+}  // namespace tfe

@@ -1,0 +1,209 @@
+// Tile products on the matrix cores, for the calls that learn and serve the
+// head: sums over k of P(p, k) Q(q, k), P and Q of bfloat16 or 8-bit integers.
+// An operand lies in memory with k along its rows (`Across` false: row p holds
+// P(p, .)) or with k as the row number (true: row k holds P(., k)).
+#pragma once
+#include <hip/hip_runtime.h>
+#include <stdint.h>
+
+namespace tfe {
+namespace gemm {
+
+typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
+typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
+typedef short s16x4 __attribute__((ext_vector_type(4)));
+typedef float f32x4 __attribute__((ext_vector_type(4)));
+typedef int i32x4 __attribute__((ext_vector_type(4)));
+
+struct Bf16 {
+  typedef f32x4 Acc;
+  static constexpr int BYTES = 2;
+};
+struct Int8 {
+  typedef i32x4 Acc;
+  static constexpr int BYTES = 1;
+};
+
+// An operand of one tile.  Rows along k: `at` is its first row, `rows` the rows
+// there are from it on and `cols` the length of k.  k across: `at` is the
+// tile's first column of row k = 0, `rows` the length of k and `cols` the
+// columns there are from the tile's first on.  16-byte aligned, `pitch` in bytes
+// a multiple of 16, and cols * BYTES a multiple of 16: a 16-byte load is inside
+// or outside as a whole.
+struct Operand {
+  const char* at;
+  uint32_t pitch, rows, cols;
+};
+
+constexpr int kStep = 128;  // bytes of k a step: 64 bfloat16 or 128 integers
+
+// T rows (or columns) of an operand, kStep bytes of k deep, in LDS.
+// Rows along k: 128 bytes each, its eight 16-byte pieces exchanged by the row's
+// number mod 8.  k across (bfloat16): 64 rows of T numbers, in 32-byte pieces (the
+// 16 columns that a transposing read takes from a row) exchanged by the row's
+// number, so that the four rows it reads at once lie on different banks.
+template <class E, int T, bool ACROSS, int WAVES> struct Side {
+  static constexpr int SIZE = T * kStep;
+  static constexpr int LOADS = SIZE / 1024 / WAVES;
+  static_assert(SIZE % (1024 * WAVES) == 0, "whole loads of every wave");
+  static_assert(!ACROSS || E::BYTES == 2, "the transposing read is one of 16-bit numbers");
+  static constexpr uint32_t ROW = ACROSS ? T * 2 : kStep;  // bytes of an LDS row
+  static constexpr uint32_t PER = 1024 / ROW;              // rows of a load instruction
+
+  __device__ static __forceinline__ uint32_t turned(uint32_t k) {
+    return T >= 128 ? k & 7 : (k >> 1) & 3;
+  }
+
+  uint32_t from;   // this lane's byte offset within the rows of its first load
+  uint32_t piece;  // its 16-byte piece of a row (rows along k), or byte of a row
+
+  __device__ __forceinline__ void init(uint32_t wave, uint32_t lane, uint32_t pitch) {
+    const uint32_t r = lane / (ROW / 16), c = lane % (ROW / 16);
+    const uint32_t row = wave * PER + r;
+    if (ACROSS) {
+      static_assert(!ACROSS || WAVES * PER % 8 == 0, "rows of a wave's loads are turned alike");
+      piece = (((c >> 1) ^ turned(row)) << 5) + ((c & 1) << 4);
+    } else {
+      piece = (c ^ (row & 7)) << 4;
+    }
+    from = row * pitch + piece;
+  }
+#if defined(__HIP_DEVICE_COMPILE__)
+  // Loads of step `s` (k from s * kStep bytes on) into `to`.
+  __device__ __forceinline__ void load(const Operand& o, uint32_t s, char* to, uint32_t wave) const {
+    typedef __attribute__((address_space(3))) void* Lds;
+    if (ACROSS) {
+      const uint32_t k = s * (kStep / 2), left = o.rows > k ? min(o.rows - k, 64u) : 0u;
+      const uint32_t bytes = left ? (left - 1) * o.pitch + min(o.cols * 2, o.pitch) : 0u;
+      const auto d = __builtin_amdgcn_make_buffer_rsrc((void*)(o.at + (size_t)k * o.pitch), 0, (int)bytes,
+                                                       0x00020000);
+#pragma unroll
+      for (int c = 0; c < LOADS; ++c)
+        __builtin_amdgcn_raw_ptr_buffer_load_lds(d, (Lds)(to + (c * WAVES + wave) * 1024), 16,
+                                                 (int)(from + c * WAVES * PER * o.pitch), 0, 0, 0);
+    } else {
+      const uint32_t rows = min(o.rows, (uint32_t)T), len = o.cols * E::BYTES;
+      const uint32_t bytes = rows ? (rows - 1) * o.pitch + len : 0u;
+      const auto d = __builtin_amdgcn_make_buffer_rsrc((void*)o.at, 0, (int)bytes, 0x00020000);
+      const uint32_t k = s * kStep;
+      // Past the row's end: an offset beyond every descriptor's range.
+      const bool out = k + piece >= len;
+#pragma unroll
+      for (int c = 0; c < LOADS; ++c)
+        __builtin_amdgcn_raw_ptr_buffer_load_lds(
+            d, (Lds)(to + (c * WAVES + wave) * 1024), 16,
+            (int)(out ? 0x7FFFFFF0u : from + k + c * WAVES * PER * o.pitch), 0, 0, 0);
+    }
+  }
+  // The 16 rows (columns) from 16 t + `first` on, `first` a multiple of the
+  // wave's part: lane (g, i) gets row i's 16 bytes of k at 64 h + 16 g.
+  __device__ static __forceinline__ u32x4 operand(const char* lds, uint32_t first, int t, int h,
+                                                  uint32_t i, uint32_t g) {
+    if (ACROSS) {
+      typedef __attribute__((address_space(3))) s16x4* Lds;
+      const uint32_t k = g * 8 + (i >> 2);
+      u32x4 r;
+#pragma unroll
+      for (int q = 0; q < 2; ++q) {
+        const uint32_t f = turned(k + q * 4);
+        const char* p = lds + (k + h * 32 + q * 4) * ROW + (((first / 16 + t) ^ f) << 5) + (i & 3) * 8;
+        const s16x4 v = __builtin_amdgcn_ds_read_tr16_b64_v4i16((Lds)p);
+        const u32x2 w = __builtin_bit_cast(u32x2, v);
+        r[2 * q] = w[0];
+        r[2 * q + 1] = w[1];
+      }
+      return r;
+    }
+    return *(const u32x4*)(lds + (first + t * 16 + i) * kStep + (((h * 4 + g) ^ (i & 7)) << 4));
+  }
+#endif
+};
+
+template <class E>
+__device__ __forceinline__ typename E::Acc multiply(u32x4 p, u32x4 q, typename E::Acc c) {
+#if defined(__HIP_DEVICE_COMPILE__)
+  if constexpr (E::BYTES == 2)
+    return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, p),
+                                                   __builtin_bit_cast(bf16x8, q), c, 0, 0, 0);
+  else
+    return __builtin_amdgcn_mfma_i32_16x16x64_i8(__builtin_bit_cast(i32x4, p),
+                                                 __builtin_bit_cast(i32x4, q), c, 0, 0, 0);
+#else
+  return c;
+#endif
+}
+
+// A block of WP x WQ waves and its tile of TP x TQ sums.  Lane (g, i) of a wave
+// holds in acc[n][m][j] the sum at p = wp + 16 n + 4 g + j, q = wq + 16 m + i.
+template <class E, int TP, int TQ, int WP, int WQ, bool PA, bool QA> struct Tile {
+  static constexpr int WAVES = WP * WQ, NT = TP / WP / 16, MT = TQ / WQ / 16;
+  static constexpr int THREADS = WAVES * 64;
+  typedef Side<E, TP, PA, WAVES> P;
+  typedef Side<E, TQ, QA, WAVES> Q;
+  static constexpr int STAGE = P::SIZE + Q::SIZE, LDS = 2 * STAGE;
+  typename E::Acc acc[NT][MT];
+  uint32_t wave, lane, i, g, wp, wq;
+
+  __device__ __forceinline__ Tile() {
+    wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    lane = threadIdx.x & 63;
+    i = lane & 15;
+    g = lane >> 4;
+    wp = (wave % WP) * (TP / WP);
+    wq = (wave / WP) * (TQ / WQ);
+  }
+  __device__ __forceinline__ void clear() {
+#pragma unroll
+    for (int n = 0; n < NT; ++n)
+#pragma unroll
+      for (int m = 0; m < MT; ++m) acc[n][m] = typename E::Acc{0, 0, 0, 0};
+  }
+  // Adds steps [s0, s1) of the operands: one step's loads under way while the
+  // one before is multiplied.
+  __device__ __forceinline__ void run(const Operand& p, const Operand& q, uint32_t s0, uint32_t s1,
+                                      char* lds) {
+#if defined(__HIP_DEVICE_COMPILE__)
+    P sp;
+    Q sq;
+    sp.init(wave, lane, p.pitch);
+    sq.init(wave, lane, q.pitch);
+    if (s0 < s1) {
+      sp.load(p, s0, lds, wave);
+      sq.load(q, s0, lds + P::SIZE, wave);
+    }
+    uint32_t at = 0;
+    for (uint32_t s = s0; s < s1; ++s) {
+      // The stage has arrived, and every wave's reads of the other one have returned.
+      asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
+      __builtin_amdgcn_s_barrier();
+      __builtin_amdgcn_sched_barrier(0);
+      const char* from = lds + at;
+      at = STAGE - at;
+      if (s + 1 < s1) {
+        sp.load(p, s + 1, lds + at, wave);
+        sq.load(q, s + 1, lds + at + P::SIZE, wave);
+      }
+      __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        u32x4 qv[MT];
+#pragma unroll
+        for (int m = 0; m < MT; ++m) qv[m] = Q::operand(from + P::SIZE, wq, m, h, i, g);
+#pragma unroll
+        for (int n = 0; n < NT; ++n) {
+          const u32x4 pv = P::operand(from, wp, n, h, i, g);
+#pragma unroll
+          for (int m = 0; m < MT; ++m) acc[n][m] = multiply<E>(pv, qv[m], acc[n][m]);
+        }
+      }
+    }
+    // The LDS may be written again, by loads or by the caller.
+    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+    __builtin_amdgcn_s_barrier();
+#endif
+  }
+};
+
+}  // namespace gemm
+}  // namespace tfe

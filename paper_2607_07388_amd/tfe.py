@@ -60,6 +60,12 @@ class tfe_stats(ctypes.Structure):
         return {n: int(getattr(self, n)) for n, _ in self._fields_}
 
 
+class tfe_grad_tensor(ctypes.Structure):
+    _fields_ = [("grad", ctypes.c_void_p), ("out", ctypes.c_void_p), ("rows", ctypes.c_int64),
+                ("cols", ctypes.c_int64), ("ldg", ctypes.c_int64), ("ldo", ctypes.c_int64),
+                ("dtype", ctypes.c_int32)]
+
+
 class TfeError(RuntimeError):
     def __init__(self, status, msg):
         super().__init__("libtfe status %d: %s" % (status, msg))
@@ -123,6 +129,22 @@ def _load():
         "tfe_distill_loss_grad": ([vp, i32, i64, i64, i32, vp, vp, i32, i32, ctypes.c_float, vp,
                                    vp, vp, vp, i64, vp, i64, vp], ctypes.c_int),
         "tfe_distill_workspace": ([i64, i32], i64),
+        "tfe_cross_entropy_loss": ([vp, i64, vp, i64, vp, i64, i32, i32, vp, vp, vp, i64, vp],
+                                   ctypes.c_int),
+        "tfe_cross_entropy_grad": ([vp, i64, vp, i64, vp, i64, i32, i32, vp, vp, vp, i64, vp, i64,
+                                    i32, i32, vp, i64, vp], ctypes.c_int),
+        "tfe_cross_entropy_loss_grad": ([vp, i64, vp, i64, vp, i64, i32, i32, vp, vp, vp, vp, i64,
+                                         vp, i64, i32, i32, vp, i64, vp], ctypes.c_int),
+        "tfe_cross_entropy_workspace": ([i64, i32, i32], i64),
+        "tfe_grad_norm": ([vp, i64, vp, vp, i64, vp], ctypes.c_int),
+        "tfe_grad_clip": ([vp, i64, ctypes.c_float, vp, vp], ctypes.c_int),
+        "tfe_grad_norm_clip": ([vp, i64, ctypes.c_float, vp, vp, i64, vp], ctypes.c_int),
+        "tfe_grad_workspace": ([vp, i64], i64),
+        "tfe_integer_quantize": ([vp, i32, i64, i64, i32, vp, vp, vp], ctypes.c_int),
+        "tfe_integer_matmul": ([vp, vp, vp, vp, i64, i32, i32, vp, i32, i64, vp], ctypes.c_int),
+        "tfe_integer_linear": ([vp, i32, i64, vp, vp, i64, i32, i32, vp, i32, i64, vp, i64, vp],
+                            ctypes.c_int),
+        "tfe_integer_workspace": ([i64, i32], i64),
         "tfe_ngram_release": ([], ctypes.c_int),
         "tfe_ngram_top": ([vp, i64, i32, i32, i64, i64, vp, vp, ctypes.POINTER(i64), vp],
                           ctypes.c_int),
@@ -152,6 +174,10 @@ EXPORTED = ("tfe_table_load", "tfe_table_free", "tfe_lookup_inject", "tfe_lookup
             "tfe_quantize", "tfe_quantized_matmul", "tfe_quantized_linear", "tfe_quantized_workspace",
             "tfe_sample", "tfe_sample_workspace", "tfe_distill_loss", "tfe_distill_grad",
             "tfe_distill_loss_grad", "tfe_distill_workspace",
+            "tfe_cross_entropy_loss", "tfe_cross_entropy_grad", "tfe_cross_entropy_loss_grad",
+            "tfe_cross_entropy_workspace", "tfe_grad_norm", "tfe_grad_clip", "tfe_grad_norm_clip",
+            "tfe_grad_workspace", "tfe_integer_quantize", "tfe_integer_matmul", "tfe_integer_linear",
+            "tfe_integer_workspace",
             "tfe_ngram_top", "tfe_ngram_release",
             "tfe_get_stats", "tfe_reset_stats", "tfe_residency", "tfe_last_error",
             "tfe_memory_held", "tfe_index_capacity",
@@ -329,6 +355,100 @@ def tfe_distill_workspace(rows, vocab):
     return _check(lib.tfe_distill_workspace(rows, vocab))
 
 
+def tfe_cross_entropy_loss(hidden, ldh, w, ldw, targets, rows, vocab, dim, loss, lse, workspace,
+                           workspace_bytes, stream=None):
+    return _check(lib.tfe_cross_entropy_loss(addr(hidden), ldh, addr(w), ldw, addr(targets), rows,
+                                             vocab, dim, addr(loss), addr(lse), addr(workspace),
+                                             workspace_bytes, stream_handle(stream)))
+
+
+def tfe_cross_entropy_grad(hidden, ldh, w, ldw, targets, rows, vocab, dim, lse, grad_loss,
+                           grad_hidden, ldgh, grad_w, ldgw, grad_dtype, accumulate, workspace,
+                           workspace_bytes, stream=None):
+    return _check(lib.tfe_cross_entropy_grad(addr(hidden), ldh, addr(w), ldw, addr(targets), rows,
+                                             vocab, dim, addr(lse), addr(grad_loss),
+                                             addr(grad_hidden), ldgh, addr(grad_w), ldgw,
+                                             grad_dtype, accumulate, addr(workspace),
+                                             workspace_bytes, stream_handle(stream)))
+
+
+def tfe_cross_entropy_loss_grad(hidden, ldh, w, ldw, targets, rows, vocab, dim, grad_loss, loss,
+                                lse, grad_hidden, ldgh, grad_w, ldgw, grad_dtype, accumulate,
+                                workspace, workspace_bytes, stream=None):
+    return _check(lib.tfe_cross_entropy_loss_grad(addr(hidden), ldh, addr(w), ldw, addr(targets),
+                                                  rows, vocab, dim, addr(grad_loss), addr(loss),
+                                                  addr(lse), addr(grad_hidden), ldgh,
+                                                  addr(grad_w), ldgw, grad_dtype, accumulate,
+                                                  addr(workspace), workspace_bytes,
+                                                  stream_handle(stream)))
+
+
+def tfe_cross_entropy_workspace(rows, vocab, dim):
+    """Bytes of workspace a tfe_cross_entropy_loss or _grad call of this size needs."""
+    return _check(lib.tfe_cross_entropy_workspace(rows, vocab, dim))
+
+
+class GradTensors:
+    """The array that the gradient norm and clipping take, with the tensors it points to."""
+
+    def __init__(self, tensors):
+        self.kept = [t[:2] for t in tensors]
+        self.array = (tfe_grad_tensor * max(1, len(tensors)))(
+            *(tfe_grad_tensor(addr(g), addr(o), *rest) for g, o, *rest in tensors))
+        self.address = ctypes.addressof(self.array)
+
+    def data_ptr(self):
+        return self.address
+
+
+def make_grad_tensors(tensors):
+    """Entries (grad, out, rows, cols, ldg, ldo, dtype), one a tensor; out may be grad."""
+    return GradTensors(tensors)
+
+
+def tfe_grad_norm(tensors, n, norm, workspace, workspace_bytes, stream=None):
+    return _check(lib.tfe_grad_norm(addr(tensors), n, addr(norm), addr(workspace),
+                                    workspace_bytes, stream_handle(stream)))
+
+
+def tfe_grad_clip(tensors, n, max_norm, norm, stream=None):
+    return _check(lib.tfe_grad_clip(addr(tensors), n, max_norm, addr(norm), stream_handle(stream)))
+
+
+def tfe_grad_norm_clip(tensors, n, max_norm, norm, workspace, workspace_bytes, stream=None):
+    return _check(lib.tfe_grad_norm_clip(addr(tensors), n, max_norm, addr(norm), addr(workspace),
+                                         workspace_bytes, stream_handle(stream)))
+
+
+def tfe_grad_workspace(tensors, n):
+    """Bytes of workspace a tfe_grad_norm(_clip) call of these tensors needs."""
+    return _check(lib.tfe_grad_workspace(addr(tensors), n))
+
+
+def tfe_integer_quantize(x, dtype, ldx, rows, dim, codes, scales, stream=None):
+    return _check(lib.tfe_integer_quantize(addr(x), dtype, ldx, rows, dim, addr(codes), addr(scales),
+                                        stream_handle(stream)))
+
+
+def tfe_integer_matmul(a, a_scales, w, w_scales, rows, out_dim, dim, out, out_dtype, ldo,
+                    stream=None):
+    return _check(lib.tfe_integer_matmul(addr(a), addr(a_scales), addr(w), addr(w_scales), rows,
+                                      out_dim, dim, addr(out), out_dtype, ldo,
+                                      stream_handle(stream)))
+
+
+def tfe_integer_linear(x, dtype, ldx, w, w_scales, rows, out_dim, dim, out, out_dtype, ldo,
+                    workspace, workspace_bytes, stream=None):
+    return _check(lib.tfe_integer_linear(addr(x), dtype, ldx, addr(w), addr(w_scales), rows, out_dim,
+                                      dim, addr(out), out_dtype, ldo, addr(workspace),
+                                      workspace_bytes, stream_handle(stream)))
+
+
+def tfe_integer_workspace(rows, dim):
+    """Bytes of workspace a tfe_integer_linear call of this size needs."""
+    return _check(lib.tfe_integer_workspace(rows, dim))
+
+
 def tfe_ngram_top(tokens, n_tokens, vocab, n, skip, top, out_tuples, out_counts, stream=None):
     """Returns the number of ranks written."""
     w = ctypes.c_int64(0)
@@ -399,7 +519,10 @@ def make_desc(phrase_tokens, phrase_len, n_min, n_max, vocab, values, dim, dtype
 _BY_CTYPES = {f.__name__: f for f in (tfe_lookup_inject, tfe_lookup_inject_multi, tfe_prefetch,
                                       tfe_prefetch_scored, tfe_head_topk, tfe_quantized_linear,
                                       tfe_sample, tfe_distill_loss, tfe_distill_grad,
-                                      tfe_distill_loss_grad)}
+                                      tfe_distill_loss_grad, tfe_cross_entropy_loss,
+                                      tfe_cross_entropy_grad, tfe_cross_entropy_loss_grad,
+                                      tfe_grad_norm, tfe_grad_clip, tfe_grad_norm_clip,
+                                      tfe_integer_linear)}
 
 
 def _bind_calls():

@@ -1,0 +1,284 @@
+"""Softmax cross entropy without kept logits, through the C ABI, against the 64-bit oracle.
+
+Bounds, u = 2^-24.  A logit is a float32 sum of dim exact products: off by at most
+E = dim u max_v sum |x w|.  lse adds the sum of exponentials: at most 300 additions deep, and an
+exponential at distance d from the maximum off by 2 u d + 2 u relative, weighted by e^-d: in all
+below 400 u; two roundings of its own size.  The loss is lse minus a logit: 2 E + 400 u + 4 u of
+the parts.  A number of dz = g (p - [t]) is off by g p (2 E + 400 u) + 2 u g, and is rounded by
+2^-8 of itself for bfloat16 gradients, by 2^-16 for float32 ones (two bfloat16 numbers: what the
+first leaves, at most 2^-8, rounded by 2^-8 of it).  The gradients' sums add these by the
+magnitudes they are multiplied with, n u sum |dz| |.| for n additions, and one last rounding."""
+import numpy as np
+import pytest
+import torch
+
+from oracle import learn as O
+from paper_2607_07388_amd import tfe
+
+from . import harness as H
+
+pytestmark = pytest.mark.gpu
+
+F32, BF16 = tfe.TFE_F32, tfe.TFE_BF16
+TORCH = {F32: torch.float32, BF16: torch.bfloat16}
+U = 2.0 ** -24
+
+
+def device(x, pad=0, shift=0):
+    """x as bfloat16 rows `pad` elements further apart, `shift` elements into an allocation; what lies between is NaN."""
+    rows, cols = x.shape
+    t = torch.full((rows * (cols + pad) + shift,), float("nan"), dtype=torch.bfloat16, device="cuda")
+    t = t[shift:].view(rows, cols + pad)
+    t[:, :cols] = torch.from_numpy(np.ascontiguousarray(x, np.float32)).cuda().bfloat16()
+    return t
+
+
+def empty(rows, cols, dtype, pad=0, fill=-7.0):
+    return torch.full((rows, cols + pad), fill, dtype=TORCH[dtype], device="cuda")
+
+
+class Case:
+    def __init__(self, rows, vocab, dim, seed=1, pad=0, shift=0, spread=0.3):
+        rng = np.random.default_rng(seed + rows + vocab + dim)
+        self.rows, self.vocab, self.dim, self.pad, self.shift = rows, vocab, dim, pad, shift
+        self.x = device(rng.standard_normal((rows, dim)), pad, shift)
+        self.w = device(rng.standard_normal((vocab, dim)) * spread, pad, shift)
+        t = rng.integers(0, vocab, rows)
+        if rows > 2:
+            t[rng.random(rows) < 0.2] = -1
+            t[rows // 2] = vocab
+        self.t = torch.from_numpy(t.astype(np.int32)).cuda()
+        self.g = torch.from_numpy(rng.random(rows).astype(np.float32) + 0.5).cuda()
+        if rows > 5:
+            self.g[3] = 0
+        self.size = tfe.tfe_cross_entropy_workspace(rows, vocab, dim)
+
+    def space(self):
+        return torch.full((self.size,), 0x7F, dtype=torch.uint8, device="cuda"), self.size
+
+    def head(self):
+        ld = self.dim + self.pad
+        return self.x, ld, self.w, ld, self.t, self.rows, self.vocab, self.dim
+
+    def loss(self):
+        loss, lse = (torch.full((self.rows,), -7.0, device="cuda") for _ in range(2))
+        tfe.tfe_cross_entropy_loss(*self.head(), loss, lse, *self.space(), H.cur_stream())
+        return loss, lse
+
+    def both(self, dtype, weight=True, accumulate=None, out_pad=0):
+        loss, lse = (torch.full((self.rows,), -7.0, device="cuda") for _ in range(2))
+        gx = empty(self.rows, self.dim, dtype, out_pad)
+        gw = empty(self.vocab, self.dim, dtype, out_pad) if accumulate is None else accumulate.clone()
+        tfe.tfe_cross_entropy_loss_grad(*self.head(), self.g if weight else None, loss, lse, gx, self.dim + out_pad, gw,
+                                        self.dim + out_pad, dtype, 0 if accumulate is None else 1, *self.space(),
+                                        H.cur_stream())
+        return loss, lse, gx, gw
+
+    def grad(self, dtype, lse, weight=True):
+        gx, gw = empty(self.rows, self.dim, dtype), empty(self.vocab, self.dim, dtype)
+        tfe.tfe_cross_entropy_grad(*self.head(), lse, self.g if weight else None, gx, self.dim, gw, self.dim, dtype, 0,
+                                   *self.space(), H.cur_stream())
+        return gx, gw
+
+    def oracle(self, weight=True):
+        x, w = (a[:, :self.dim].float().cpu().numpy().astype(np.float64) for a in (self.x, self.w))
+        g = self.g.cpu().numpy().astype(np.float64) if weight else np.ones(self.rows)
+        return x, w, self.t.cpu().numpy(), g
+
+    def check(self, got, dtype=None, weight=True):
+        x, w, t, g = self.oracle(weight)
+        loss, lse, dx, dw, dz = O.cross_entropy(x, w, t, g)
+        e = self.dim * U * (np.abs(x) @ np.abs(w).T).max(1)
+        bound = 2 * e + 400 * U + 8 * U * np.abs(lse) + 4 * U * np.abs(loss)
+        if got[0] is not None:
+            near(got[0], loss, bound)
+            near(got[1], lse, bound)
+        if dtype is None:
+            return
+        rho, last = (2.0 ** -8, 2.0 ** -8) if dtype == BF16 else (2.0 ** -16, U)
+        live = np.where((t >= 0) & (t < self.vocab), g, 0.0)[:, None]
+        p = np.exp(x @ w.T - lse[:, None])
+        off = live * (p * (2 * e + 400 * U + 8 * U * np.abs(lse))[:, None] + 2 * U) + (rho + 2 * U) * np.abs(dz)
+        size = np.abs(dz)
+        for k, (want, err, mag, n) in enumerate(((dx, off @ np.abs(w), size @ np.abs(w), self.vocab),
+                                                  (dw, off.T @ np.abs(x), size.T @ np.abs(x), self.rows))):
+            full = got[2 + k]
+            near(full[:, :self.dim], want, (1 + last) * (err + 2 * n * U * mag) + last * np.abs(want) + 1e-30)
+            if full.shape[1] > self.dim:
+                assert (full[:, self.dim:] == -7).all()
+
+
+def near(got, want, bound):
+    got = got.double().cpu().numpy()
+    assert np.isfinite(got).all()
+    worst = (np.abs(got - want) - bound).max()
+    assert worst <= 0, "%g beyond the bound" % worst
+
+
+# One row and one token; rows of every tile; widths and vocabularies that end inside a tile;
+# pitches and starts that are aligned, and not.
+SHAPES = [(1, 1, 1, 0, 0), (1, 2, 8, 0, 0), (2, 300, 64, 0, 0), (3, 257, 7, 1, 1), (16, 3001, 256, 0, 0),
+          (17, 129, 72, 8, 0), (63, 255, 64, 0, 8), (64, 1000, 120, 0, 0), (65, 129, 72, 5, 3), (100, 700, 200, 8, 8),
+          (128, 777, 1000, 0, 0), (129, 515, 65, 0, 0), (200, 2500, 96, 16, 0), (257, 1111, 130, 3, 1),
+          (300, 5000, 320, 0, 0), (513, 640, 1024, 0, 0), (40, 64, 2048, 0, 0)]
+
+
+@pytest.mark.parametrize("rows,vocab,dim,pad,shift", SHAPES)
+def test_loss(rows, vocab, dim, pad, shift):
+    c = Case(rows, vocab, dim, pad=pad, shift=shift)
+    c.check(c.loss())
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("rows,vocab,dim,pad,shift", SHAPES)
+def test_loss_and_gradients(rows, vocab, dim, pad, shift, dtype):
+    c = Case(rows, vocab, dim, pad=pad, shift=shift)
+    c.check(c.both(dtype, out_pad=pad), dtype)
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("rows,vocab,dim", [(5, 400, 33), (100, 3000, 128), (300, 1000, 64)])
+def test_parts_are_the_whole(rows, vocab, dim, dtype):
+    """Loss and gradient in two calls are those of one, to the bit, and repeat; no weights are ones."""
+    c = Case(rows, vocab, dim)
+    for weight in (True, False):
+        loss, lse, gx, gw = c.both(dtype, weight)
+        c.check((loss, lse, gx, gw), dtype, weight)
+        a, b = c.loss()
+        assert torch.equal(a, loss) and torch.equal(b, lse)
+        for _ in range(2):
+            x, w = c.grad(dtype, lse, weight)
+            assert torch.equal(x, gx) and torch.equal(w, gw)
+
+
+@pytest.mark.parametrize("rows,vocab,dim", [(3, 100, 24), (70, 900, 100), (400, 700, 136)])
+def test_accumulated(rows, vocab, dim):
+    c = Case(rows, vocab, dim)
+    *_, gw = c.both(F32)
+    old = torch.randn((vocab, dim), device="cuda")
+    *_, more = c.both(F32, accumulate=old)
+    assert torch.equal(more, gw + old)
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("rows", [6, 150, 260])
+def test_rows_that_take_no_part(rows, dtype):
+    """Rows without a target or of weight 0 may hold anything; the others do not change."""
+    c = Case(rows, 600, 88)
+    want = c.both(dtype)
+    none = (c.t < 0) | (c.t >= c.vocab) | (c.g == 0)
+    assert none.any() and not none.all()
+    bad = none.nonzero()[:, 0]
+    c.x[bad[::2]] = float("nan")
+    c.x[bad[1::2]] = float("inf")
+    got = c.both(dtype)
+    assert torch.equal(got[2], want[2]) and torch.equal(got[3], want[3])
+    assert (got[2][none] == 0).all() and torch.equal(got[0][~none], want[0][~none])
+    nowhere = (c.t < 0) | (c.t >= c.vocab)
+    assert (got[0][nowhere] == 0).all()
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+def test_no_row_takes_part(dtype):
+    c = Case(70, 300, 40)
+    c.t.fill_(-1)
+    c.x.fill_(float("nan"))
+    loss, _, gx, gw = c.both(dtype)
+    assert (loss == 0).all() and (gx == 0).all() and (gw == 0).all()
+
+
+@pytest.mark.parametrize("dtype,accumulate", [(F32, 0), (BF16, 0), (F32, 1)])
+def test_zero_rows(dtype, accumulate):
+    gw = empty(33, 7, dtype, 3)
+    w = device(np.ones((33, 7)))
+    tfe.tfe_cross_entropy_loss_grad(None, 7, w, 7, None, 0, 33, 7, None, None, None, None, 7, gw, 10, dtype, accumulate,
+                                    None, 0, H.cur_stream())
+    assert (gw[:, :7] == (-7 if accumulate else 0)).all() and (gw[:, 7:] == -7).all()
+
+
+@pytest.mark.parametrize("rows", [6, 200, 300])
+def test_nan_is_not_hidden(rows):
+    c = Case(rows, 500, 64)
+    live = ((c.t >= 0) & (c.t < c.vocab) & (c.g != 0)).nonzero()[:, 0]
+    want = c.both(F32)
+    r = int(live[1])
+    for bad in (float("nan"), float("inf")):
+        c.x[r, 5] = bad
+        loss, lse, gx, gw = c.both(F32)
+        assert loss[r].isnan() and lse[r].isnan() and gx[r].isnan().all() and gw[:, 5].isnan().all()
+        others = torch.arange(rows, device="cuda") != r
+        assert torch.equal(loss[others], want[0][others]) and torch.equal(gx[others], want[2][others])
+
+
+@pytest.mark.parametrize("scale", [30.0, 1000.0])
+@pytest.mark.parametrize("rows", [9, 140])
+def test_confident_rows(rows, scale):
+    """Logits hundreds and thousands apart: probabilities are 0 and 1 almost everywhere."""
+    c = Case(rows, 300, 64, spread=scale)
+    with torch.no_grad():
+        z = c.x[:, :64].double() @ c.w[:, :64].double().t()
+        c.t[::3] = z.argmax(1)[::3].int()
+    c.check(c.both(F32), F32)
+    c.check(c.both(BF16), BF16)
+
+
+def torch_oracle(c, weight):
+    """loss, lse, dx, dw in float64 on the GPU, for sizes that numpy takes long over."""
+    x, w = c.x[:, :c.dim].double(), c.w[:, :c.dim].double()
+    z = torch.mm(x, w.t().contiguous())
+    lse = z.logsumexp(1)
+    there = (c.t >= 0) & (c.t < c.vocab)
+    at = torch.where(there, c.t, torch.zeros_like(c.t)).long()[:, None]
+    loss = torch.where(there, lse - z.gather(1, at)[:, 0], torch.zeros_like(lse))
+    z = (z - lse[:, None]).exp_()
+    z.scatter_add_(1, at, -torch.ones_like(lse)[:, None])
+    z *= (weight.double() * there)[:, None]
+    return loss, lse, torch.mm(z, w), torch.mm(z.t().contiguous(), x)
+
+
+def rel(got, want):
+    return float((got.double() - want).norm() / want.norm())
+
+
+# More rows than sums are kept of at once; vocabularies of several pieces, also copied ones.
+@pytest.mark.parametrize("rows,vocab,dim,pad,dtype", [
+    (17000, 300, 24, 0, BF16), (2100, 70001, 64, 0, F32), (2100, 70001, 63, 2, BF16), (9000, 17000, 40, 0, BF16),
+    (40, 262144, 64, 0, BF16), (1, 151936, 1024, 0, F32), (700, 151936, 128, 0, BF16)])
+def test_large(rows, vocab, dim, pad, dtype):
+    """Norms of the errors: each float32 logit is off by a few U of a sum of |x w| of about 10, so
+    loss and lse by far less than 1e-5; independent roundings of dz by at most 2^-8 (2^-16) of it
+    leave the gradients off by no more than that of their norm, and the last rounding adds as much."""
+    c = Case(rows, vocab, dim, pad=pad)
+    want = torch_oracle(c, c.g)
+    got = c.both(dtype)
+    some = (c.t >= 0) & (c.t < c.vocab)
+    assert rel(got[1], want[1]) < 1e-5 and (not some.any() or rel(got[0], want[0]) < 1e-5)
+    most = 2.0 ** -7 if dtype == BF16 else 2.0 ** -15
+    assert rel(got[2], want[2]) < most and rel(got[3], want[3]) < most
+
+
+@pytest.mark.parametrize("rows,dtype", [(4, BF16), (64, F32), (300, BF16)])
+def test_captured_and_on_another_stream(rows, dtype):
+    """Captured in a graph and replayed on inputs that change in between, and on a stream of its own."""
+    cases = [Case(rows, 1500, 128, seed=s) for s in range(3)]
+    want = [c.both(dtype) for c in cases]
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        got = cases[1].both(dtype)
+    side.synchronize()
+    assert all(torch.equal(a, b) for a, b in zip(got, want[1]))
+    c = Case(rows, 1500, 128, seed=9)
+    loss, lse = torch.empty(rows, device="cuda"), torch.empty(rows, device="cuda")
+    gx, gw, space = empty(rows, 128, dtype), empty(1500, 128, dtype), c.space()
+    torch.cuda.synchronize()
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g):
+        tfe.tfe_cross_entropy_loss_grad(*c.head(), c.g, loss, lse, gx, 128, gw, 128, dtype, 0, *space, H.cur_stream())
+    for k in (1, 2, 0, 1):
+        for a in ("x", "w", "t", "g"):
+            getattr(c, a).copy_(getattr(cases[k], a))
+        g.replay()
+        cases[0].both(dtype)
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip((loss, lse, gx, gw), want[k]))
