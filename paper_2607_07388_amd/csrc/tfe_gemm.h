@@ -42,8 +42,10 @@ constexpr int kStep = 128;  // bytes of k a step: 64 bfloat16 or 128 integers
 // Rows along k: 128 bytes each, its eight 16-byte pieces exchanged by the row's
 // number mod 8.  k across (bfloat16): 64 rows of T numbers, in 32-byte pieces (the
 // 16 columns that a transposing read takes from a row) exchanged by the row's
-// number, so that the four rows it reads at once lie on different banks.
-template <class E, int T, bool ACROSS, int WAVES> struct Side {
+// number, so that the eight rows that are read at once (k to k + 3 and k + 8 to
+// k + 11) lie on different banks.
+// HALF: the T rows are 64 of each 128, from `shift` (0 or 64) on.
+template <class E, int T, bool ACROSS, int WAVES, bool HALF = false> struct Side {
   static constexpr int SIZE = T * kStep;
   static constexpr int LOADS = SIZE / 1024 / WAVES;
   static_assert(SIZE % (1024 * WAVES) == 0, "whole loads of every wave");
@@ -52,7 +54,7 @@ template <class E, int T, bool ACROSS, int WAVES> struct Side {
   static constexpr uint32_t PER = 1024 / ROW;              // rows of a load instruction
 
   __device__ static __forceinline__ uint32_t turned(uint32_t k) {
-    return T >= 128 ? k & 7 : (k >> 1) & 3;
+    return T >= 128 ? (k & 3) | (k >> 1 & 4) : (k >> 1 & 1) | (k >> 2 & 2);
   }
 
   uint32_t from;   // this lane's byte offset within the rows of its first load
@@ -62,8 +64,10 @@ template <class E, int T, bool ACROSS, int WAVES> struct Side {
     const uint32_t r = lane / (ROW / 16), c = lane % (ROW / 16);
     const uint32_t row = wave * PER + r;
     if (ACROSS) {
-      static_assert(!ACROSS || WAVES * PER % 8 == 0, "rows of a wave's loads are turned alike");
+      // Rows of a wave's loads are turned alike, or alternately.
+      static_assert(!ACROSS || WAVES * PER % 16 == 0 || (WAVES * PER == 8 && T >= 128), "16 rows repeat");
       piece = (((c >> 1) ^ turned(row)) << 5) + ((c & 1) << 4);
+      if (HALF) piece += piece & 128;
     } else {
       piece = (c ^ (row & 7)) << 4;
     }
@@ -71,19 +75,25 @@ template <class E, int T, bool ACROSS, int WAVES> struct Side {
   }
 #if defined(__HIP_DEVICE_COMPILE__)
   // Loads of step `s` (k from s * kStep bytes on) into `to`.
-  __device__ __forceinline__ void load(const Operand& o, uint32_t s, char* to, uint32_t wave) const {
+  __device__ __forceinline__ void load(const Operand& o, uint32_t s, char* to, uint32_t wave,
+                                       uint32_t shift = 0) const {
     typedef __attribute__((address_space(3))) void* Lds;
+    // Rows between a wave's loads.
+    constexpr uint32_t APART = HALF && !ACROSS ? 128 : WAVES * PER;
+    static_assert(!HALF || ACROSS || WAVES * PER == 64, "a load of every wave is 64 rows");
+    const uint32_t start = from + shift * (ACROSS ? 2 : o.pitch);
     if (ACROSS) {
       const uint32_t k = s * (kStep / 2), left = o.rows > k ? min(o.rows - k, 64u) : 0u;
       const uint32_t bytes = left ? (left - 1) * o.pitch + min(o.cols * 2, o.pitch) : 0u;
       const auto d = __builtin_amdgcn_make_buffer_rsrc((void*)(o.at + (size_t)k * o.pitch), 0, (int)bytes,
                                                        0x00020000);
+      const uint32_t other = WAVES * PER == 8 ? start - piece + (piece ^ 128) : start;
 #pragma unroll
       for (int c = 0; c < LOADS; ++c)
         __builtin_amdgcn_raw_ptr_buffer_load_lds(d, (Lds)(to + (c * WAVES + wave) * 1024), 16,
-                                                 (int)(from + c * WAVES * PER * o.pitch), 0, 0, 0);
+                                                 (int)((c & 1 ? other : start) + c * APART * o.pitch), 0, 0, 0);
     } else {
-      const uint32_t rows = min(o.rows, (uint32_t)T), len = o.cols * E::BYTES;
+      const uint32_t rows = min(o.rows, (uint32_t)(HALF ? 2 * T : T)), len = o.cols * E::BYTES;
       const uint32_t bytes = rows ? (rows - 1) * o.pitch + len : 0u;
       const auto d = __builtin_amdgcn_make_buffer_rsrc((void*)o.at, 0, (int)bytes, 0x00020000);
       const uint32_t k = s * kStep;
@@ -93,7 +103,7 @@ template <class E, int T, bool ACROSS, int WAVES> struct Side {
       for (int c = 0; c < LOADS; ++c)
         __builtin_amdgcn_raw_ptr_buffer_load_lds(
             d, (Lds)(to + (c * WAVES + wave) * 1024), 16,
-            (int)(out ? 0x7FFFFFF0u : from + k + c * WAVES * PER * o.pitch), 0, 0, 0);
+            (int)(out ? 0x7FFFFFF0u : start + k + c * APART * o.pitch), 0, 0, 0);
     }
   }
   // The 16 rows (columns) from 16 t + `first` on, `first` a multiple of the
@@ -106,8 +116,7 @@ template <class E, int T, bool ACROSS, int WAVES> struct Side {
       u32x4 r;
 #pragma unroll
       for (int q = 0; q < 2; ++q) {
-        const uint32_t f = turned(k + q * 4);
-        const char* p = lds + (k + h * 32 + q * 4) * ROW + (((first / 16 + t) ^ f) << 5) + (i & 3) * 8;
+        const char* p = lds + (k + h * 32 + q * 4) * ROW + (((first / 16 + t) ^ turned(k)) << 5) + (i & 3) * 8;
         const s16x4 v = __builtin_amdgcn_ds_read_tr16_b64_v4i16((Lds)p);
         const u32x2 w = __builtin_bit_cast(u32x2, v);
         r[2 * q] = w[0];
@@ -142,6 +151,7 @@ template <class E, int TP, int TQ, int WP, int WQ, bool PA, bool QA> struct Tile
   typedef Side<E, TP, PA, WAVES> P;
   typedef Side<E, TQ, QA, WAVES> Q;
   static constexpr int STAGE = P::SIZE + Q::SIZE, LDS = 2 * STAGE;
+  static constexpr bool LARGE = TP == 256 && TQ == 256 && WP == 2 && WQ == 4;
   typename E::Acc acc[NT][MT];
   uint32_t wave, lane, i, g, wp, wq;
 
@@ -159,19 +169,124 @@ template <class E, int TP, int TQ, int WP, int WQ, bool PA, bool QA> struct Tile
 #pragma unroll
       for (int m = 0; m < MT; ++m) acc[n][m] = typename E::Acc{0, 0, 0, 0};
   }
-  // Adds steps [s0, s1) of the operands: one step's loads under way while the
-  // one before is multiplied.
+  // Adds steps [s0, s1) of the operands.  The LDS may be written afterwards.
   __device__ __forceinline__ void run(const Operand& p, const Operand& q, uint32_t s0, uint32_t s1,
+                                      char* lds) {
+    if (s0 >= s1) return;
+    if constexpr (LARGE)
+      in_turns(p, q, s0, s1, lds);
+    else
+      together(p, q, s0, s1, lds);
+  }
+
+ private:
+  // Large tiles: the waves take turns.  While the four of one group (one on each
+  // SIMD) multiply, the other four read LDS and ask for loads; a barrier ends each
+  // turn.  A wave's step is two such pairs of turns: its rows of P's first half with
+  // all of Q, then P's second half.  A half's place in LDS is loaded again, for
+  // the step after next, in the turn after every wave has read it, so a load is a
+  // whole step under way; a turn waits for the loads of the step before alone.
+  __device__ __forceinline__ void in_turns(const Operand& p, const Operand& q, uint32_t s0, uint32_t s1,
+                                           char* lds) {
+#if defined(__HIP_DEVICE_COMPILE__)
+    typedef Side<E, 128, PA, WAVES, true> Half;
+    constexpr int HALF = Half::SIZE;
+    static_assert(NT == 8 && MT == 4 && Half::LOADS == 2 && Q::LOADS == 4, "what the waits count");
+    Half sp;
+    Q sq;
+    sp.init(wave, lane, p.pitch);
+    sq.init(wave, lane, q.pitch);
+    // A stage: P's halves, then Q.
+    auto load_first = [&](uint32_t s, char* to) {
+      sp.load(p, s, to, wave, 0);
+      sq.load(q, s, to + 2 * HALF, wave);
+    };
+    auto load_second = [&](uint32_t s, char* to) { sp.load(p, s, to + HALF, wave, 64); };
+    u32x4 pv[2][4], qv[2][4];
+    auto read_p = [&](const char* from) {
+#pragma unroll
+      for (int h = 0; h < 2; ++h)
+#pragma unroll
+        for (int n = 0; n < 4; ++n) pv[h][n] = Half::operand(from, wp / 2, n, h, i, g);
+    };
+    auto read_q = [&](const char* from) {
+#pragma unroll
+      for (int h = 0; h < 2; ++h)
+#pragma unroll
+        for (int m = 0; m < 4; ++m) qv[h][m] = Q::operand(from + 2 * HALF, wq, m, h, i, g);
+    };
+    auto products = [&](int half) {
+      __builtin_amdgcn_s_setprio(1);
+#pragma unroll
+      for (int h = 0; h < 2; ++h)
+#pragma unroll
+        for (int n = 0; n < 4; ++n)
+#pragma unroll
+          for (int m = 0; m < 4; ++m) {
+            typename E::Acc& c = acc[half * 4 + n][m];
+            c = multiply<E>(pv[h][n], qv[h][m], c);
+          }
+      __builtin_amdgcn_s_setprio(0);
+    };
+    // Ends a turn; `kept` of the loads asked for last may still be under way.
+    auto turn = [] {
+      __builtin_amdgcn_sched_barrier(0);
+      __builtin_amdgcn_s_barrier();
+      __builtin_amdgcn_sched_barrier(0);
+    };
+    auto arrived = [](bool all) {
+      __builtin_amdgcn_sched_barrier(0);
+      if (all)
+        asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
+      else
+        asm volatile("s_waitcnt vmcnt(8) lgkmcnt(0)" ::: "memory");
+    };
+    load_first(s0, lds);
+    load_second(s0, lds);
+    if (s0 + 1 < s1) {
+      load_first(s0 + 1, lds + STAGE);
+      asm volatile("s_waitcnt vmcnt(6)" ::: "memory");
+    } else {
+      asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+    }
+    __builtin_amdgcn_s_barrier();
+    const bool second = wave >= 4;
+    if (second) turn();
+    uint32_t at = 0;
+    for (uint32_t s = s0; s < s1; ++s) {
+      const char* from = lds + at;
+      // All but the last 8 loads of a wave: the other stage's first half and Q (6) and
+      // second half (2), of this step or the next.
+      read_p(from);
+      read_q(from);
+      if (s + 1 < s1) load_second(s + 1, lds + (STAGE - at));
+      arrived(s + 1 >= s1);
+      turn();
+      products(0);
+      turn();
+      read_p(from + HALF);
+      if (s + 2 < s1) load_first(s + 2, lds + at);
+      arrived(s + 2 >= s1);
+      turn();
+      products(1);
+      turn();
+      at = STAGE - at;
+    }
+    if (!second) turn();
+#endif
+  }
+
+  // Smaller tiles: one step's loads are under way while the one before is
+  // multiplied.
+  __device__ __forceinline__ void together(const Operand& p, const Operand& q, uint32_t s0, uint32_t s1,
                                       char* lds) {
 #if defined(__HIP_DEVICE_COMPILE__)
     P sp;
     Q sq;
     sp.init(wave, lane, p.pitch);
     sq.init(wave, lane, q.pitch);
-    if (s0 < s1) {
-      sp.load(p, s0, lds, wave);
-      sq.load(q, s0, lds + P::SIZE, wave);
-    }
+    sp.load(p, s0, lds, wave);
+    sq.load(q, s0, lds + P::SIZE, wave);
     uint32_t at = 0;
     for (uint32_t s = s0; s < s1; ++s) {
       // The stage has arrived, and every wave's reads of the other one have returned.
