@@ -99,17 +99,56 @@ struct LogitsArgs {
   uint64_t plane;
 };
 
-template <int TP, int TQ, int WP, int WQ>
-__device__ __forceinline__ bool logits_tile(const LogitsArgs& a, Tile<Bf16, TP, TQ, WP, WQ, false, false>& t,
-                                            uint32_t* p0, uint32_t* q0, char* lds) {
-  const uint32_t place = place_of(blockIdx.x, a.total);
-  *p0 = place / a.tiles_q * TP;
-  *q0 = place % a.tiles_q * TQ;
-  if (*p0 >= a.w.rows) return false;
-  t.clear();
-  const Operand p = along(a.w, *p0), q = along(a.h, *q0);
-  t.run(p, q, 0, (a.w.cols * 2 + gemm::kStep - 1) / gemm::kStep, lds);
-  return true;
+// Tile t of a launch: its first column and row; false behind the last.
+__device__ __forceinline__ bool logits_tile(const LogitsArgs& a, uint32_t t, uint32_t tp, uint32_t tq,
+                                            uint32_t* p0, uint32_t* q0) {
+  if (t >= a.total) return false;
+  const uint32_t place = place_of(t, a.total);
+  *p0 = place / a.tiles_q * tp;
+  *q0 = place % a.tiles_q * tq;
+  return *p0 < a.w.rows;
+}
+__device__ __forceinline__ gemm::Segment logits_segment(const LogitsArgs& a, uint32_t p0, uint32_t q0) {
+  return gemm::Segment{along(a.w, p0), along(a.h, q0), 0, (a.w.cols * 2 + gemm::kStep - 1) / gemm::kStep};
+}
+// What a tile's rows have: targets, and for dz lse and weights, T::TQ numbers each.
+template <int TQ> constexpr int kInfo = TQ * 12;
+
+// A block's tiles: t, t + the grid and so on.  Places behind the last column
+// are at the end of the last XCD's run, where a block's later tiles are too.
+// done(p0, q0, info) has the rows' numbers in LDS.
+template <class T, int TP, int TQ, int STORES, bool DZ, class Done>
+__device__ __forceinline__ void logits_tiles(const LogitsArgs& a, T& tile, char* lds, Done done) {
+  uint32_t t = blockIdx.x, p0, q0, np0 = 0, nq0 = 0;
+  if (!logits_tile(a, t, TP, TQ, &p0, &q0)) return;
+  tile.clear();
+  tile.template run<STORES>(
+      logits_segment(a, p0, q0),
+      [&](gemm::Segment* s) {
+        t += gridDim.x;
+        const bool more = logits_tile(a, t, TP, TQ, &np0, &nq0);
+        if (more) *s = logits_segment(a, np0, nq0);
+        return more;
+      },
+      [&](uint32_t odd) {
+        char* to = lds + T::LDS + odd * kInfo<TQ>;
+        static_assert(T::WAVES * 64 >= TQ, "a wave for each 64 rows");
+        if (tile.wave < TQ / 64) {
+          gemm::load_numbers(a.targets, q0, a.h.rows, tile.wave, to);
+          if (DZ) {
+            gemm::load_numbers(a.lse, q0, a.h.rows, tile.wave, to + TQ * 4);
+            if (a.weight) gemm::load_numbers(a.weight, q0, a.h.rows, tile.wave, to + TQ * 8);
+          }
+        }
+      },
+      [&](uint32_t odd) {
+        const bool stored = done(p0, q0, lds + T::LDS + odd * kInfo<TQ>);
+        p0 = np0;
+        q0 = nq0;
+        tile.clear();
+        return stored;
+      },
+      lds);
 }
 
 // Columns of a slab: those of one wave.
@@ -117,44 +156,52 @@ constexpr int kSlab = 128;
 
 template <int TP, int TQ, int WP, int WQ>
 __global__ __launch_bounds__(WP* WQ * 64) void k_sums(LogitsArgs a) {
+  typedef Tile<Bf16, TP, TQ, WP, WQ, false, false> T;
   extern __shared__ __attribute__((aligned(1024))) char lds[];
-  Tile<Bf16, TP, TQ, WP, WQ, false, false> t;
+  T t;
   static_assert(TP / WP == kSlab, "a wave's columns are a slab");
-  uint32_t p0, q0;
-  if (!logits_tile<TP, TQ, WP, WQ>(a, t, &p0, &q0, lds)) return;
-  const uint32_t c0 = p0 + t.wp + t.g * 4, slab = a.slab0 + (p0 + t.wp) / kSlab;
+  logits_tiles<T, TP, TQ, 0, false>(a, t, lds, [&](uint32_t p0, uint32_t q0, const char* info) {
+    const uint32_t c0 = p0 + t.wp + t.g * 4, slab = a.slab0 + (p0 + t.wp) / kSlab;
+    if (p0 + t.wp + kSlab > a.w.rows) {
 #pragma unroll
-  for (int m = 0; m < t.MT; ++m) {
-    const uint32_t r = q0 + t.wq + m * 16 + t.i;
-    float top = -FLT_MAX, sum = 0.f;
+      for (int n = 0; n < t.NT; ++n)
 #pragma unroll
-    for (int n = 0; n < t.NT; ++n)
+        for (int j = 0; j < 4; ++j)
+          if (c0 + n * 16 + j >= a.w.rows)
 #pragma unroll
-      for (int j = 0; j < 4; ++j) {
-        if (c0 + n * 16 + j >= a.w.rows) t.acc[n][m][j] = -INFINITY;
-        top = fmaxf(top, t.acc[n][m][j]);
-      }
-    top = fmaxf(top, __shfl_xor(top, 16));
-    top = fmaxf(top, __shfl_xor(top, 32));
+            for (int m = 0; m < t.MT; ++m) t.acc[n][m][j] = -INFINITY;
+    }
 #pragma unroll
-    for (int n = 0; n < t.NT; ++n)
+    for (int m = 0; m < t.MT; ++m) {
+      const uint32_t in = t.wq + m * 16 + t.i, r = q0 + in;
+      float top = -FLT_MAX, sum = 0.f;
 #pragma unroll
-      for (int j = 0; j < 4; ++j) sum += __expf(t.acc[n][m][j] - top);
-    sum += __shfl_xor(sum, 16);
-    sum += __shfl_xor(sum, 32);
-    if (r < a.h.rows) {
-      if (t.g == 0 && p0 + t.wp < a.w.rows) a.part[(size_t)slab * a.h.rows + r] = f32x2{top, sum};
-      const uint32_t at = (uint32_t)a.targets[r] - a.vocab0 - c0;
-      if (at < (uint32_t)kSlab && (at & 12) == 0) {
-        float z = 0.f;
+      for (int n = 0; n < t.NT; ++n)
 #pragma unroll
-        for (int n = 0; n < t.NT; ++n)
+        for (int j = 0; j < 4; ++j) top = fmaxf(top, t.acc[n][m][j]);
+      top = fmaxf(top, __shfl_xor(top, 16));
+      top = fmaxf(top, __shfl_xor(top, 32));
 #pragma unroll
-          for (int j = 0; j < 4; ++j) z = at == (uint32_t)(n * 16 + j) ? t.acc[n][m][j] : z;
-        if (c0 + at < a.w.rows) a.picked[r] = z;
+      for (int n = 0; n < t.NT; ++n)
+#pragma unroll
+        for (int j = 0; j < 4; ++j) sum += __expf(t.acc[n][m][j] - top);
+      sum += __shfl_xor(sum, 16);
+      sum += __shfl_xor(sum, 32);
+      if (r < a.h.rows) {
+        if (t.g == 0 && p0 + t.wp < a.w.rows) a.part[(size_t)slab * a.h.rows + r] = f32x2{top, sum};
+        const uint32_t at = ((const uint32_t*)info)[in] - a.vocab0 - c0;
+        if (at < (uint32_t)kSlab && (at & 12) == 0) {
+          float z = 0.f;
+#pragma unroll
+          for (int n = 0; n < t.NT; ++n)
+#pragma unroll
+            for (int j = 0; j < 4; ++j) z = at == (uint32_t)(n * 16 + j) ? t.acc[n][m][j] : z;
+          if (c0 + at < a.w.rows) a.picked[r] = z;
+        }
       }
     }
-  }
+    return false;
+  });
 }
 
 // A block joins the slabs of 16 rows.
@@ -188,38 +235,76 @@ __global__ __launch_bounds__(1024) void k_join(JoinArgs a) {
   a.loss[r] = (uint32_t)a.targets[r] < a.vocab ? (top - a.picked[r]) + rest : 0.f;
 }
 
+// Two tiles of 16 columns of a row, each lane's 4 + 4, as 16 bytes of bfloat16 at
+// column piece_of(g): lanes of neighbouring rows of 16 exchange halves.
+__device__ __forceinline__ u32x4 pair_of(const float* p, const float* q) {
+#if defined(__HIP_DEVICE_COMPILE__)
+  const auto lo = __builtin_amdgcn_permlane16_swap(pack2(p[0], p[1]), pack2(q[0], q[1]), false, false);
+  const auto hi = __builtin_amdgcn_permlane16_swap(pack2(p[2], p[3]), pack2(q[2], q[3]), false, false);
+  return u32x4{lo[0], hi[0], lo[1], hi[1]};
+#else
+  return u32x4{};
+#endif
+}
+__device__ __forceinline__ uint32_t piece_of(uint32_t g) { return (g & 1) * 16 + (g >> 1) * 8; }
+
 template <int TP, int TQ, int WP, int WQ, int PLANES>
 __global__ __launch_bounds__(WP* WQ * 64) void k_dz(LogitsArgs a) {
+  typedef Tile<Bf16, TP, TQ, WP, WQ, false, false> T;
   extern __shared__ __attribute__((aligned(1024))) char lds[];
-  Tile<Bf16, TP, TQ, WP, WQ, false, false> t;
-  uint32_t p0, q0;
-  if (!logits_tile<TP, TQ, WP, WQ>(a, t, &p0, &q0, lds)) return;
-  const uint32_t c0 = p0 + t.wp + t.g * 4;
+  T t;
+  constexpr int STORES = T::MT * T::NT / 2 * PLANES;
+  logits_tiles<T, TP, TQ, STORES, true>(a, t, lds, [&](uint32_t p0, uint32_t q0, const char* info) {
+    const uint32_t c0 = p0 + t.wp + t.g * 4;
+    // All of a wave's columns are stored (the pitch is as long as the tiles are wide); beyond
+    // the vocabulary zeros.
+    const bool ends = p0 + TP > a.w.rows, all = q0 + TQ <= a.h.rows;
 #pragma unroll
-  for (int m = 0; m < t.MT; ++m) {
-    const uint32_t r = q0 + t.wq + m * 16 + t.i;
-    if (r >= a.h.rows) continue;
-    const uint32_t target = (uint32_t)a.targets[r];
-    const float lse = a.lse[r];
-    const float weight = target < a.vocab ? (a.weight ? a.weight[r] : 1.f) : 0.f;
-    const uint32_t at = target - a.vocab0 - c0;
-    uint16_t* out = a.dz + (size_t)r * a.pitch + c0;
+    for (int m = 0; m < t.MT; ++m) {
+      const uint32_t in = t.wq + m * 16 + t.i, r = q0 + in;
+      const uint32_t target = ((const uint32_t*)info)[in];
+      const float lse = ((const float*)info)[TQ + in];
+      const float given = a.weight ? ((const float*)info)[2 * TQ + in] : 1.f;
+      const float weight = target < a.vocab ? given : 0.f;
+      const uint32_t at = target - a.vocab0 - c0;
+      const bool hit = at < (uint32_t)(TP / WP) && (at & 12) == 0;
 #pragma unroll
-    for (int n = 0; n < t.NT; ++n) {
-      float d[4], e[4];
+      for (int n = 0; n < t.NT; ++n)
 #pragma unroll
-      for (int j = 0; j < 4; ++j) {
-        float v = __expf(t.acc[n][m][j] - lse);
-        if (at == (uint32_t)(n * 16 + j)) v -= 1.f;
-        d[j] = weight == 0.f || c0 + n * 16 + j >= a.w.rows ? 0.f : v * weight;
-        if (PLANES == 2) e[j] = d[j] - (float)(__bf16)d[j];
+        for (int j = 0; j < 4; ++j) t.acc[n][m][j] = __expf(t.acc[n][m][j] - lse);
+      if (__builtin_amdgcn_ballot_w64(hit)) {
+#pragma unroll
+        for (int n = 0; n < t.NT; ++n)
+#pragma unroll
+          for (int j = 0; j < 4; ++j) t.acc[n][m][j] -= at == (uint32_t)(n * 16 + j) ? 1.f : 0.f;
       }
-      if (c0 + n * 16 < a.pitch) {
-        *(u32x2*)(out + n * 16) = u32x2{pack2(d[0], d[1]), pack2(d[2], d[3])};
-        if (PLANES == 2) *(u32x2*)(out + a.plane + n * 16) = u32x2{pack2(e[0], e[1]), pack2(e[2], e[3])};
+      // Rows without a gradient are zeros, whatever their probabilities.
+      if (__builtin_amdgcn_ballot_w64(weight == 0.f)) {
+#pragma unroll
+        for (int n = 0; n < t.NT; ++n)
+#pragma unroll
+          for (int j = 0; j < 4; ++j) t.acc[n][m][j] = weight == 0.f ? 0.f : t.acc[n][m][j];
+      }
+      uint16_t* out = a.dz + (size_t)r * a.pitch + p0 + t.wp + piece_of(t.g);
+#pragma unroll
+      for (int n = 0; n < t.NT; n += 2) {
+        float d[8], e[8];
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+          d[j] = t.acc[n + j / 4][m][j & 3] * weight;
+          if (ends && c0 + (n + j / 4) * 16 + (j & 3) >= a.w.rows) d[j] = 0.f;
+          if (PLANES == 2) e[j] = d[j] - (float)(__bf16)d[j];
+        }
+        const u32x4 v = pair_of(d, d + 4);
+        if (all || r < a.h.rows) *(u32x4*)(out + n * 16) = v;
+        if (PLANES == 2) {
+          const u32x4 w = pair_of(e, e + 4);
+          if (all || r < a.h.rows) *(u32x4*)(out + a.plane + n * 16) = w;
+        }
       }
     }
-  }
+    return all;
+  });
 }
 
 // ---- gradients -----------------------------------------------------------------------
@@ -245,11 +330,21 @@ __global__ __launch_bounds__(WP* WQ * 64) void k_grad_h(GradHArgs a) {
   const uint32_t s0 = (uint32_t)((uint64_t)steps * split / a.splits);
   const uint32_t s1 = (uint32_t)((uint64_t)steps * (split + 1) / a.splits);
   t.clear();
-  for (uint32_t k = 0; k < a.planes; ++k) {
-    Matrix dz = a.dz;
-    dz.at += k * a.plane;
-    t.run(across(a.w, p0), along(dz, q0), s0, s1, lds);
-  }
+  Matrix dz = a.dz;
+  uint32_t plane = 0;
+  // The operands end with the split.
+  Matrix w = a.w;
+  w.rows = min(w.rows, s1 * 64);
+  dz.cols = min(dz.cols, s1 * 64);
+  t.template run<0>(
+      gemm::Segment{across(w, p0), along(dz, q0), s0, s1},
+      [&](gemm::Segment* s) {
+        if (++plane >= a.planes) return false;
+        dz.at += a.plane;
+        s->q = along(dz, q0);
+        return true;
+      },
+      [](uint32_t) {}, [](uint32_t) { return false; }, lds);
   const uint32_t c0 = p0 + t.wp + t.g * 4;
 #pragma unroll
   for (int m = 0; m < t.MT; ++m) {
@@ -309,11 +404,17 @@ __global__ __launch_bounds__(WP* WQ * 64) void k_grad_w(GradWArgs a) {
   const uint32_t p0 = place % a.tiles_p * TP, q0 = place / a.tiles_p * TQ;
   if (q0 >= a.vocab) return;
   t.clear();
-  for (uint32_t k = 0; k < a.planes; ++k) {
-    Matrix dz = a.dz;
-    dz.at += k * a.plane;
-    t.run(across(a.h, p0), across(dz, q0), 0, (a.h.rows + 63) / 64, lds);
-  }
+  Matrix dz = a.dz;
+  uint32_t plane = 0;
+  t.template run<0>(
+      gemm::Segment{across(a.h, p0), across(dz, q0), 0, (a.h.rows + 63) / 64},
+      [&](gemm::Segment* s) {
+        if (++plane >= a.planes) return false;
+        dz.at += a.plane;
+        s->q = across(dz, q0);
+        return true;
+      },
+      [](uint32_t) {}, [](uint32_t) { return false; }, lds);
   const uint32_t c0 = p0 + t.wp + t.g * 4;
 #pragma unroll
   for (int m = 0; m < t.MT; ++m) {
@@ -368,9 +469,8 @@ Plan plan_of(int64_t n_rows, int32_t n_vocab, int32_t n_dim) {
   Plan p{};
   p.pitch = up(dim, 64);
   p.tile = rows > 128 ? 256 : rows > 64 ? 128 : 64;
-  const uint32_t most = std::max<uint32_t>(2048, (uint32_t)std::min<int64_t>((1 << 27) / n_rows, 1 << 18) / 256 * 256);
-  const uint32_t pieces = (vocab + most - 1) / most;
-  p.piece = up((vocab + pieces - 1) / pieces, 256);
+  const int64_t most = std::max<int64_t>(2048, (1 << 27) / n_rows / 256 * 256);
+  p.piece = (uint32_t)std::min<int64_t>(most, up(vocab, 256));
   p.chunk = std::min<uint32_t>(rows, 16384);
   const uint32_t tiles = ((dim + 255) / 256) * ((rows + p.tile - 1) / p.tile);
   p.splits = std::max<uint32_t>(1, std::min<uint32_t>((uint32_t)compute_units() / tiles, p.piece / 256));
@@ -413,28 +513,33 @@ template <class K> hipError_t allow(K* k, int bytes, std::atomic<uint64_t>* told
   }
   return hipSuccess;
 }
-#define LAUNCH(T, kernel, blocks, s, args)                                          \
+#define LAUNCH(T, INFO, kernel, blocks, s, args)                                    \
   do {                                                                              \
     static std::atomic<uint64_t> told_{0};                                          \
-    const hipError_t e_ = allow(kernel, T::LDS, &told_);                            \
+    const hipError_t e_ = allow(kernel, T::LDS + INFO, &told_);                            \
     if (e_ != hipSuccess) return e_;                                                \
-    kernel<<<dim3(blocks), dim3(T::THREADS), T::LDS, s>>>(args);                    \
+    kernel<<<dim3(blocks), dim3(T::THREADS), T::LDS + INFO, s>>>(args);             \
     return hipGetLastError();                                                       \
   } while (0)
+
+// Blocks of a launch whose blocks take one tile after another.
+template <class T> uint32_t blocks(uint32_t total, int info) {
+  return std::min<uint32_t>(total, up(compute_units() * (163840 / (T::LDS + info)), 8));
+}
 
 template <int TP, int TQ, int WP, int WQ> hipError_t sums(LogitsArgs a, hipStream_t s) {
   typedef Tile<Bf16, TP, TQ, WP, WQ, false, false> T;
   a.tiles_q = (a.h.rows + TQ - 1) / TQ;
   a.total = up((a.w.rows + TP - 1) / TP * a.tiles_q, 8);
   auto* k = k_sums<TP, TQ, WP, WQ>;
-  LAUNCH(T, k, a.total, s, a);
+  LAUNCH(T, 2 * kInfo<TQ>, k, blocks<T>(a.total, 2 * kInfo<TQ>), s, a);
 }
 template <int TP, int TQ, int WP, int WQ, int PLANES> hipError_t dz(LogitsArgs a, hipStream_t s) {
   typedef Tile<Bf16, TP, TQ, WP, WQ, false, false> T;
   a.tiles_q = (a.h.rows + TQ - 1) / TQ;
   a.total = up((a.w.rows + TP - 1) / TP * a.tiles_q, 8);
   auto* k = k_dz<TP, TQ, WP, WQ, PLANES>;
-  LAUNCH(T, k, a.total, s, a);
+  LAUNCH(T, 2 * kInfo<TQ>, k, blocks<T>(a.total, 2 * kInfo<TQ>), s, a);
 }
 template <int TP, int TQ, int WP, int WQ> hipError_t grad_h(GradHArgs a, hipStream_t s) {
   typedef Tile<Bf16, TP, TQ, WP, WQ, true, false> T;
@@ -442,14 +547,14 @@ template <int TP, int TQ, int WP, int WQ> hipError_t grad_h(GradHArgs a, hipStre
   a.tiles_q = (a.dz.rows + TQ - 1) / TQ;
   a.total = up(a.tiles_p * a.tiles_q * a.splits, 8);
   auto* k = k_grad_h<TP, TQ, WP, WQ>;
-  LAUNCH(T, k, a.total, s, a);
+  LAUNCH(T, 0, k, a.total, s, a);
 }
 template <int TP, int TQ, int WP, int WQ, int DT> hipError_t grad_w(GradWArgs a, hipStream_t s) {
   typedef Tile<Bf16, TP, TQ, WP, WQ, true, true> T;
   a.tiles_p = (a.dim + TP - 1) / TP;
   a.total = up(a.tiles_p * ((a.vocab + TQ - 1) / TQ), 8);
   auto* k = k_grad_w<TP, TQ, WP, WQ, DT>;
-  LAUNCH(T, k, a.total, s, a);
+  LAUNCH(T, 0, k, a.total, s, a);
 }
 
 // dW of no rows.
@@ -510,7 +615,7 @@ hipError_t launch_xent_loss(const XentArgs& a, hipStream_t s) {
       l.slab0 = v0 / kSlab;
       TRY_HIP((p.tile == 256   ? sums<256, 256, 2, 4>(l, s)
                : p.tile == 128 ? sums<256, 128, 2, 2>(l, s)
-                               : sums<256, 64, 2, 2>(l, s)));
+                               : sums<128, 64, 1, 4>(l, s)));
     }
     JoinArgs j{l.part, (a.vocab + kSlab - 1) / kSlab, l.h.rows, a.vocab, l.targets, l.picked,
                a.loss + r0, a.lse + r0};
@@ -544,11 +649,11 @@ hipError_t launch_xent_grad(const XentArgs& a, hipStream_t s) {
     if (f32)
       TRY_HIP((p.tile == 256   ? dz<256, 256, 2, 4, 2>(l, s)
                : p.tile == 128 ? dz<256, 128, 2, 2, 2>(l, s)
-                               : dz<256, 64, 2, 2, 2>(l, s)));
+                               : dz<128, 64, 1, 4, 2>(l, s)));
     else
       TRY_HIP((p.tile == 256   ? dz<256, 256, 2, 4, 1>(l, s)
                : p.tile == 128 ? dz<256, 128, 2, 2, 1>(l, s)
-                               : dz<256, 64, 2, 2, 1>(l, s)));
+                               : dz<128, 64, 1, 4, 1>(l, s)));
     const Matrix d{l.dz, l.pitch, a.rows, up(n, 64)};
     GradHArgs gh{};
     gh.w = l.w;

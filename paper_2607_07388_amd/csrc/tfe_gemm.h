@@ -143,6 +143,31 @@ __device__ __forceinline__ typename E::Acc multiply(u32x4 p, u32x4 q, typename E
 #endif
 }
 
+// Numbers of four bytes from `first` on (those that there are, and zeros) into LDS:
+// 64 of each wave that takes part, 64 `part` behind the first.
+__device__ __forceinline__ void load_numbers(const void* array, uint32_t first, uint32_t count, uint32_t part,
+                                             char* to) {
+#if defined(__HIP_DEVICE_COMPILE__)
+  typedef __attribute__((address_space(3))) void* Lds;
+  const uint32_t left = count > first ? min(count - first, 1u << 20) : 0u;
+  const auto d = __builtin_amdgcn_make_buffer_rsrc((void*)((const char*)array + (size_t)first * 4), 0,
+                                                   (int)(left * 4), 0x00020000);
+  __builtin_amdgcn_raw_ptr_buffer_load_lds(d, (Lds)(to + part * 256), 4,
+                                           (int)(part * 256 + (threadIdx.x & 63) * 4), 0, 0, 0);
+#endif
+}
+
+// Steps [s0, s1) of a tile's operands.
+struct Segment {
+  Operand p, q;
+  uint32_t s0, s1;
+};
+__device__ __forceinline__ Segment no_segment(const Segment& like) {
+  Segment r = like;  // reads as zeros
+  r.p.rows = r.p.cols = r.q.rows = r.q.cols = 0;
+  return r;
+}
+
 // A block of WP x WQ waves and its tile of TP x TQ sums.  Lane (g, i) of a wave
 // holds in acc[n][m][j] the sum at p = wp + 16 n + 4 g + j, q = wq + 16 m + i.
 template <class E, int TP, int TQ, int WP, int WQ, bool PA, bool QA> struct Tile {
@@ -150,8 +175,12 @@ template <class E, int TP, int TQ, int WP, int WQ, bool PA, bool QA> struct Tile
   static constexpr int THREADS = WAVES * 64;
   typedef Side<E, TP, PA, WAVES> P;
   typedef Side<E, TQ, QA, WAVES> Q;
-  static constexpr int STAGE = P::SIZE + Q::SIZE, LDS = 2 * STAGE;
   static constexpr bool LARGE = TP == 256 && TQ == 256 && WP == 2 && WQ == 4;
+  static constexpr int STAGE = P::SIZE + Q::SIZE;
+  // Behind the stages: two tiles' numbers of their rows and columns, INFO bytes each.
+  static constexpr int LDS = 2 * STAGE;
+  // Steps of a segment: fewer are followed by zeros.
+  static constexpr uint32_t LEAST = 4;
   typename E::Acc acc[NT][MT];
   uint32_t wave, lane, i, g, wp, wq;
 
@@ -169,40 +198,50 @@ template <class E, int TP, int TQ, int WP, int WQ, bool PA, bool QA> struct Tile
 #pragma unroll
       for (int m = 0; m < MT; ++m) acc[n][m] = typename E::Acc{0, 0, 0, 0};
   }
-  // Adds steps [s0, s1) of the operands.  The LDS may be written afterwards.
-  __device__ __forceinline__ void run(const Operand& p, const Operand& q, uint32_t s0, uint32_t s1,
-                                      char* lds) {
-    if (s0 >= s1) return;
-    if constexpr (LARGE)
-      in_turns(p, q, s0, s1, lds);
-    else
-      together(p, q, s0, s1, lds);
+  // Adds one segment after another: `next` gives the one behind (false: none), `begin`
+  // is called when a segment's first step is about to be read, and may ask for loads into
+  // the LDS behind the stages, of a place for odd and one for even segments; `done` when a
+  // segment's sums are in acc, where those loads have come.  Neither may wait for other
+  // waves.  `done` returns whether it has stored at least STORES times (memory operations
+  // of each wave), which then need not have landed when the next segment's first step is.
+  // A segment of fewer than LEAST steps ends where its operands end.
+  template <int STORES, class Next, class Begin, class Done>
+  __device__ __forceinline__ void run(Segment cur, Next next, Begin begin, Done done, char* lds) {
+    if constexpr (LARGE) {
+      in_turns<STORES>(cur, next, begin, done, lds);
+    } else {
+      uint32_t odd = 0;
+      for (bool more = true; more; odd ^= 1) {
+        Segment nxt = cur;
+        more = next(&nxt);
+        begin(odd);
+        together(cur.p, cur.q, cur.s0, cur.s1, lds);
+        done(odd);
+        cur = nxt;
+      }
+    }
   }
 
  private:
   // Large tiles: the waves take turns.  While the four of one group (one on each
   // SIMD) multiply, the other four read LDS and ask for loads; a barrier ends each
   // turn.  A wave's step is two such pairs of turns: its rows of P's first half with
-  // all of Q, then P's second half.  A half's place in LDS is loaded again, for
-  // the step after next, in the turn after every wave has read it, so a load is a
-  // whole step under way; a turn waits for the loads of the step before alone.
-  __device__ __forceinline__ void in_turns(const Operand& p, const Operand& q, uint32_t s0, uint32_t s1,
-                                           char* lds) {
+  // all of Q, then P's second half.  A place in LDS is loaded again, for the step
+  // after next, in the turn after every wave has read it, so a load is a whole step
+  // under way.  Loads run on over the segments: a tile's first ones are under way
+  // while the last one's results are written.
+  template <int STORES, class Next, class Begin, class Done>
+  __device__ __forceinline__ void in_turns(Segment cur, Next next, Begin begin, Done done, char* lds) {
 #if defined(__HIP_DEVICE_COMPILE__)
     typedef Side<E, 128, PA, WAVES, true> Half;
     constexpr int HALF = Half::SIZE;
     static_assert(NT == 8 && MT == 4 && Half::LOADS == 2 && Q::LOADS == 4, "what the waits count");
     Half sp;
     Q sq;
-    sp.init(wave, lane, p.pitch);
-    sq.init(wave, lane, q.pitch);
-    // A stage: P's halves, then Q.
-    auto load_first = [&](uint32_t s, char* to) {
-      sp.load(p, s, to, wave, 0);
-      sq.load(q, s, to + 2 * HALF, wave);
-    };
-    auto load_second = [&](uint32_t s, char* to) { sp.load(p, s, to + HALF, wave, 64); };
+    sp.init(wave, lane, cur.p.pitch);
+    sq.init(wave, lane, cur.q.pitch);
     u32x4 pv[2][4], qv[2][4];
+    // A stage: P's halves, then Q.
     auto read_p = [&](const char* from) {
 #pragma unroll
       for (int h = 0; h < 2; ++h)
@@ -228,52 +267,86 @@ template <class E, int TP, int TQ, int WP, int WQ, bool PA, bool QA> struct Tile
           }
       __builtin_amdgcn_s_setprio(0);
     };
-    // Ends a turn; `kept` of the loads asked for last may still be under way.
     auto turn = [] {
       __builtin_amdgcn_sched_barrier(0);
       __builtin_amdgcn_s_barrier();
       __builtin_amdgcn_sched_barrier(0);
     };
-    auto arrived = [](bool all) {
-      __builtin_amdgcn_sched_barrier(0);
-      if (all)
-        asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
-      else
-        asm volatile("s_waitcnt vmcnt(8) lgkmcnt(0)" ::: "memory");
-    };
-    load_first(s0, lds);
-    load_second(s0, lds);
-    if (s0 + 1 < s1) {
-      load_first(s0 + 1, lds + STAGE);
-      asm volatile("s_waitcnt vmcnt(6)" ::: "memory");
-    } else {
-      asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
-    }
+    sp.load(cur.p, cur.s0, lds, wave, 0);
+    sq.load(cur.q, cur.s0, lds + 2 * HALF, wave);
+    sp.load(cur.p, cur.s0, lds + HALF, wave, 64);
+    sp.load(cur.p, cur.s0 + 1, lds + STAGE, wave, 0);
+    sq.load(cur.q, cur.s0 + 1, lds + STAGE + 2 * HALF, wave);
+    wait_loads<6>();  // the first step is there
     __builtin_amdgcn_s_barrier();
     const bool second = wave >= 4;
     if (second) turn();
-    uint32_t at = 0;
-    for (uint32_t s = s0; s < s1; ++s) {
-      const char* from = lds + at;
-      // All but the last 8 loads of a wave: the other stage's first half and Q (6) and
-      // second half (2), of this step or the next.
-      read_p(from);
-      read_q(from);
-      if (s + 1 < s1) load_second(s + 1, lds + (STAGE - at));
-      arrived(s + 1 >= s1);
-      turn();
-      products(0);
-      turn();
-      read_p(from + HALF);
-      if (s + 2 < s1) load_first(s + 2, lds + at);
-      arrived(s + 2 >= s1);
-      turn();
-      products(1);
-      turn();
-      at = STAGE - at;
+    uint32_t at = 0, odd = 0;
+    bool stored = false;
+    for (bool more = true; more; odd ^= 1) {
+      Segment nxt = cur;
+      more = next(&nxt);
+      if (!more) nxt = no_segment(cur);
+      begin(odd);
+      const uint32_t steps = max(cur.s1 - cur.s0, LEAST);
+      // Step j from this segment's first on, and whose.
+      auto whose = [&](uint32_t j, uint32_t* s) {
+        const bool in = j < steps;
+        *s = in ? cur.s0 + j : nxt.s0 + j - steps;
+        return in;
+      };
+      for (uint32_t j = 0; j < steps; ++j) {
+        char* const from = lds + at;
+        uint32_t s;
+        read_p(from);
+        read_q(from);
+        {
+          const Operand p = whose(j + 1, &s) ? cur.p : nxt.p;
+          sp.load(p, s, lds + (STAGE - at) + HALF, wave, 64);
+        }
+        // This step's second half of P is there: behind it were asked for the next step's
+        // first half and Q (6), and what this turn asked for (2).
+        if (STORES && stored && j == 0)
+          wait_loads<(8 + STORES < 63 ? 8 + STORES : 63)>();
+        else
+          wait_loads<8>();
+        turn();
+        products(0);
+        turn();
+        read_p(from + HALF);
+        {
+          const bool in = whose(j + 2, &s);
+          const Operand p = in ? cur.p : nxt.p, q = in ? cur.q : nxt.q;
+          sp.load(p, s, from, wave, 0);
+          sq.load(q, s, from + 2 * HALF, wave);
+        }
+        // The next step's first half and Q are there: behind them were asked for its second
+        // half (2) and what this turn asked for (6).
+        if (STORES && stored && j == 0)
+          wait_loads<(8 + STORES < 63 ? 8 + STORES : 63)>();
+        else
+          wait_loads<8>();
+        turn();
+        products(1);
+        turn();
+        at = STAGE - at;
+      }
+      __builtin_amdgcn_sched_barrier(0);
+      stored = done(odd);
+      __builtin_amdgcn_sched_barrier(0);
+      cur = nxt;
     }
     if (!second) turn();
+    // Loads of zeros may still be under way.
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
 #endif
+  }
+  // This wave's LDS reads have returned, and all but its last N memory operations.
+  template <int N> __device__ static __forceinline__ void wait_loads() {
+    static_assert(N < 64, "the counter's range");
+    __builtin_amdgcn_sched_barrier(0);
+    asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" ::"n"(N) : "memory");
+    __builtin_amdgcn_sched_barrier(0);
   }
 
   // Smaller tiles: one step's loads are under way while the one before is
@@ -281,6 +354,7 @@ template <class E, int TP, int TQ, int WP, int WQ, bool PA, bool QA> struct Tile
   __device__ __forceinline__ void together(const Operand& p, const Operand& q, uint32_t s0, uint32_t s1,
                                       char* lds) {
 #if defined(__HIP_DEVICE_COMPILE__)
+    if (s0 >= s1) return;
     P sp;
     Q sq;
     sp.init(wave, lane, p.pitch);

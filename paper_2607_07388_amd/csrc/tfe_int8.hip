@@ -83,6 +83,19 @@ template <int DT> __global__ __launch_bounds__(256) void k_int8_quantize(Int8Qua
 
 // ---- product -----------------------------------------------------------------
 
+// Two tiles of 16 columns of a row, each lane's 4 + 4, as 16 bytes of bfloat16 at
+// column piece_of(g): lanes of neighbouring rows of 16 exchange halves.
+__device__ __forceinline__ u32x4 pair_of(const float* p, const float* q) {
+#if defined(__HIP_DEVICE_COMPILE__)
+  const auto lo = __builtin_amdgcn_permlane16_swap(pack2(p[0], p[1]), pack2(q[0], q[1]), false, false);
+  const auto hi = __builtin_amdgcn_permlane16_swap(pack2(p[2], p[3]), pack2(q[2], q[3]), false, false);
+  return u32x4{lo[0], hi[0], lo[1], hi[1]};
+#else
+  return u32x4{};
+#endif
+}
+__device__ __forceinline__ uint32_t piece_of(uint32_t g) { return (g & 1) * 16 + (g >> 1) * 8; }
+
 struct TileArgs {
   Int8MatmulArgs m;
   uint32_t tiles_q, total;
@@ -90,70 +103,121 @@ struct TileArgs {
 
 template <int TP, int TQ, int WP, int WQ, int DT>
 __global__ __launch_bounds__(WP* WQ * 64) void k_int8_tiles(TileArgs b) {
-  typedef typename Elem<DT>::T T;
+  typedef typename Elem<DT>::T E;
+  typedef Tile<Int8, TP, TQ, WP, WQ, false, false> T;
+  typedef f32x4 V4;
+  typedef f32x4 V4_a4 __attribute__((aligned(4)));
+  typedef u32x2 u32x2_a2 __attribute__((aligned(2)));
   extern __shared__ __attribute__((aligned(1024))) char lds[];
   const Int8MatmulArgs& a = b.m;
-  Tile<Int8, TP, TQ, WP, WQ, false, false> t;
-  const uint32_t place = (blockIdx.x & 7) * (b.total >> 3) + (blockIdx.x >> 3);
-  const uint32_t p0 = place / b.tiles_q * TP, q0 = place % b.tiles_q * TQ;
-  if (p0 >= a.n) return;
+  T t;
+  auto find = [&](uint32_t at, uint32_t* p0, uint32_t* q0) {
+    if (at >= b.total) return false;
+    const uint32_t place = (at & 7) * (b.total >> 3) + (at >> 3);
+    *p0 = place / b.tiles_q * TP;
+    *q0 = place % b.tiles_q * TQ;
+    return *p0 < a.n;
+  };
+  auto segment = [&](uint32_t p0, uint32_t q0) {
+    return gemm::Segment{Operand{(const char*)a.w + (size_t)p0 * a.pitch, a.pitch, a.n - p0, a.pitch},
+                         Operand{(const char*)a.a + (size_t)q0 * a.pitch, a.pitch, a.rows - q0, a.pitch}, 0,
+                         a.pitch / gemm::kStep};
+  };
+  uint32_t at = blockIdx.x, p0, q0, np0 = 0, nq0 = 0;
+  if (!find(at, &p0, &q0)) return;
   t.clear();
-  t.run(Operand{(const char*)a.w + (size_t)p0 * a.pitch, a.pitch, a.n - p0, a.pitch},
-        Operand{(const char*)a.a + (size_t)q0 * a.pitch, a.pitch, a.rows - q0, a.pitch}, 0,
-        a.pitch / gemm::kStep, lds);
-  const uint32_t c0 = p0 + t.wp + t.g * 4;
+  // The rows' scales, then the columns'.
+  constexpr int INFO = (TQ + TP) * 4;
+  constexpr int STORES = DT == TFE_F32 ? T::NT * T::MT : T::NT * T::MT / 2;
+  auto write = [&](const char* info) {
+    const float* as = (const float*)info + t.wq + t.i;
+    const f32x4* ws = (const f32x4*)(info + TQ * 4) + t.wp / 4 + t.g;
+    const bool all = p0 + TP <= a.n && q0 + TQ <= a.rows;
+    V4 w[T::NT];
 #pragma unroll
-  for (int n = 0; n < t.NT; ++n) {
-    float ws[4];
+    for (int n = 0; n < T::NT; ++n) w[n] = ws[n * 4];
 #pragma unroll
-    for (int j = 0; j < 4; ++j) ws[j] = a.ws[min(c0 + n * 16 + j, a.n - 1)];
-#pragma unroll
-    for (int m = 0; m < t.MT; ++m) {
+    for (int m = 0; m < T::MT; ++m) {
       const uint32_t r = q0 + t.wq + m * 16 + t.i;
-      if (r >= a.rows) continue;
-      const float as = a.as[r];
-      T* out = (T*)a.out + (size_t)r * a.ldo + c0 + n * 16;
-      f32x4 v;
+      const float x = as[m * 16];
 #pragma unroll
-      for (int j = 0; j < 4; ++j) v[j] = (float)t.acc[n][m][j] * as * ws[j];
-      typedef f32x4 f4 __attribute__((aligned(4)));
-      typedef u32x2 u2 __attribute__((aligned(2)));
-      if (c0 + n * 16 + 4 <= a.n) {
-        if constexpr (DT == TFE_F32)
-          *(f4*)out = v;
-        else
-          *(u2*)out = u2{pack2(v[0], v[1]), pack2(v[2], v[3])};
-      } else {
+      for (int n = 0; n < T::NT; n += 2) {
+        V4 v[2];
 #pragma unroll
-        for (int j = 0; j < 4; ++j)
-          if (c0 + n * 16 + j < a.n) store1<DT>(out, j, v[j]);
+        for (int h = 0; h < 2; ++h)
+#pragma unroll
+          for (int j = 0; j < 4; ++j) v[h][j] = (float)t.acc[n + h][m][j] * x * w[n + h][j];
+        if (DT == TFE_F32 || !all) {
+#pragma unroll
+          for (int h = 0; h < 2; ++h) {
+            const uint32_t c = p0 + t.wp + t.g * 4 + (n + h) * 16;
+            E* out = (E*)a.out + (size_t)r * a.ldo + c;
+            if (all || (r < a.rows && c + 4 <= a.n)) {
+              if constexpr (DT == TFE_F32)
+                *(V4_a4*)out = v[h];
+              else
+                *(u32x2_a2*)out = u32x2{pack2(v[h][0], v[h][1]), pack2(v[h][2], v[h][3])};
+            } else if (r < a.rows) {
+#pragma unroll
+              for (int j = 0; j < 4; ++j)
+                if (c + j < a.n) store1<DT>(out, j, v[h][j]);
+            }
+          }
+        } else {
+          E* out = (E*)a.out + (size_t)r * a.ldo + p0 + t.wp + n * 16 + piece_of(t.g);
+          *(u32x4_a2*)out = pair_of((const float*)&v[0], (const float*)&v[1]);
+        }
       }
     }
-  }
+    return all;
+  };
+  t.template run<STORES>(
+      segment(p0, q0),
+      [&](gemm::Segment* s) {
+        at += gridDim.x;
+        const bool more = find(at, &np0, &nq0);
+        if (more) *s = segment(np0, nq0);
+        return more;
+      },
+      [&](uint32_t odd) {
+        char* to = lds + T::LDS + odd * INFO;
+        static_assert(TP / 64 <= T::WAVES && TQ / 64 <= T::WAVES, "a wave for each 64 scales");
+        if (t.wave < TQ / 64) gemm::load_numbers(a.as, q0, a.rows, t.wave, to);
+        if (t.wave < TP / 64) gemm::load_numbers(a.ws, p0, a.n, t.wave, to + TQ * 4);
+      },
+      [&](uint32_t odd) {
+        const bool stored = write(lds + T::LDS + odd * INFO);
+        p0 = np0;
+        q0 = nq0;
+        t.clear();
+        return stored;
+      },
+      lds);
 }
 
 template <int TP, int TQ, int WP, int WQ, int DT>
 hipError_t tiles(const Int8MatmulArgs& m, hipStream_t s) {
   typedef Tile<Int8, TP, TQ, WP, WQ, false, false> T;
   auto* k = k_int8_tiles<TP, TQ, WP, WQ, DT>;
+  constexpr int LDS = T::LDS + 2 * (TP + TQ) * 4;
   static std::atomic<uint64_t> told{0};
   int dev = 0;
   hipError_t e = hipGetDevice(&dev);
   if (e != hipSuccess) return e;
   const uint64_t bit = 1ull << (dev & 63);
   if (dev > 63 || !(told.load(std::memory_order_relaxed) & bit)) {
-    e = hipFuncSetAttribute((const void*)k, hipFuncAttributeMaxDynamicSharedMemorySize, T::LDS);
+    e = hipFuncSetAttribute((const void*)k, hipFuncAttributeMaxDynamicSharedMemorySize, LDS);
     if (e != hipSuccess) return e;
     told.fetch_or(bit, std::memory_order_relaxed);
   }
   TileArgs a{m, (m.rows + TQ - 1) / TQ, 0};
   a.total = ((m.n + TP - 1) / TP * a.tiles_q + 7) / 8 * 8;
-  k<<<dim3(a.total), dim3(T::THREADS), T::LDS, s>>>(a);
+  k<<<dim3(std::min<uint32_t>(a.total, (compute_units() * (163840 / LDS) + 7) / 8 * 8)), dim3(T::THREADS), LDS, s>>>(a);
   return hipGetLastError();
 }
 
 template <int DT> hipError_t matmul(const Int8MatmulArgs& a, hipStream_t s) {
-  if (a.rows <= 64) return tiles<256, 64, 2, 2, DT>(a, s);
+  if (a.rows <= 64) return tiles<128, 64, 1, 4, DT>(a, s);
   if (a.rows <= 256) return tiles<128, 128, 2, 2, DT>(a, s);
   return tiles<256, 256, 2, 4, DT>(a, s);
 }
