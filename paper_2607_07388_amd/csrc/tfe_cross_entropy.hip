@@ -32,11 +32,30 @@ struct Matrix {
   uint32_t ld, rows, cols;
 };
 __device__ __forceinline__ Operand along(const Matrix& m, uint32_t row) {
-  return Operand{(const char*)(m.at + (size_t)row * m.ld), m.ld * 2, m.rows > row ? m.rows - row : 0u, m.cols};
+  return Operand{(const char*)(m.at + (size_t)row * m.ld), m.ld * 2, m.rows > row ? m.rows - row : 0u, m.cols, 0, 0};
 }
 __device__ __forceinline__ Operand across(const Matrix& m, uint32_t col) {
-  return Operand{(const char*)(m.at + col), m.ld * 2, m.rows, m.cols > col ? m.cols - col : 0u};
+  return Operand{(const char*)(m.at + col), m.ld * 2, m.rows, m.cols > col ? m.cols - col : 0u, 0, 0};
 }
+
+// dz of a piece of the vocabulary, in blocks of 2^log rows x 64 columns, `blocks` beside
+// each other: 128 bytes of each of 4096 rows a long pitch apart took the products that
+// read them 20 us longer of 235, and writing them 30 of 285.
+struct Dz {
+  uint16_t* at;
+  uint64_t plane;  // elements to the second numbers of float32 gradients
+  uint32_t log, blocks, rows, cols;  // rows and columns of whole blocks
+  __device__ __forceinline__ size_t block(uint32_t row, uint32_t col) const {
+    return ((size_t)(row >> log) * blocks + (col >> 6)) * (gemm::block_bytes(log) / 2);
+  }
+  // Steps [s0, s1) of `row`'s tile, k along the rows.
+  __device__ __forceinline__ Operand along(uint32_t p, uint32_t row, uint32_t s1) const {
+    return Operand{(const char*)(at + p * plane + block(row, 0)), 128, 1u << log, min(cols, s1 * 64), log, blocks};
+  }
+  __device__ __forceinline__ Operand across(uint32_t p, uint32_t col) const {
+    return Operand{(const char*)(at + p * plane + block(0, col)), 128, rows, cols - col, log, blocks};
+  }
+};
 
 // Blocks go to the 8 XCDs in turn; place t of them as if each XCD took a run of
 // neighbouring places, so that those share its L2.  `total` is a multiple of 8.
@@ -94,9 +113,7 @@ struct LogitsArgs {
   const float* lse;
   const float* weight;
   uint32_t vocab;
-  uint16_t* dz;     // [planes][rows][pitch]
-  uint32_t pitch;
-  uint64_t plane;
+  Dz dz;
 };
 
 // Tile t of a launch: its first column and row; false behind the last.
@@ -256,16 +273,16 @@ __global__ __launch_bounds__(WP* WQ * 64) void k_dz(LogitsArgs a) {
   constexpr int STORES = T::MT * T::NT / 2 * PLANES;
   logits_tiles<T, TP, TQ, STORES, true>(a, t, lds, [&](uint32_t p0, uint32_t q0, const char* info) {
     const uint32_t c0 = p0 + t.wp + t.g * 4;
-    // All of a wave's columns are stored (the pitch is as long as the tiles are wide); beyond
-    // the vocabulary zeros.
-    const bool ends = p0 + TP > a.w.rows, all = q0 + TQ <= a.h.rows;
+    // Whole blocks are written: zeros beyond the vocabulary and the rows.
+    const bool ends = p0 + TP > a.w.rows;
+    uint16_t* const tile = a.dz.at + a.dz.block(q0, p0 + t.wp) + piece_of(t.g);
 #pragma unroll
     for (int m = 0; m < t.MT; ++m) {
-      const uint32_t in = t.wq + m * 16 + t.i, r = q0 + in;
+      const uint32_t in = t.wq + m * 16 + t.i;
       const uint32_t target = ((const uint32_t*)info)[in];
       const float lse = ((const float*)info)[TQ + in];
       const float given = a.weight ? ((const float*)info)[2 * TQ + in] : 1.f;
-      const float weight = target < a.vocab ? given : 0.f;
+      const float weight = target < a.vocab && q0 + in < a.h.rows ? given : 0.f;
       const uint32_t at = target - a.vocab0 - c0;
       const bool hit = at < (uint32_t)(TP / WP) && (at & 12) == 0;
 #pragma unroll
@@ -285,7 +302,7 @@ __global__ __launch_bounds__(WP* WQ * 64) void k_dz(LogitsArgs a) {
 #pragma unroll
           for (int j = 0; j < 4; ++j) t.acc[n][m][j] = weight == 0.f ? 0.f : t.acc[n][m][j];
       }
-      uint16_t* out = a.dz + (size_t)r * a.pitch + p0 + t.wp + piece_of(t.g);
+      uint16_t* const row = tile + in * 64;
 #pragma unroll
       for (int n = 0; n < t.NT; n += 2) {
         float d[8], e[8];
@@ -295,25 +312,22 @@ __global__ __launch_bounds__(WP* WQ * 64) void k_dz(LogitsArgs a) {
           if (ends && c0 + (n + j / 4) * 16 + (j & 3) >= a.w.rows) d[j] = 0.f;
           if (PLANES == 2) e[j] = d[j] - (float)(__bf16)d[j];
         }
-        const u32x4 v = pair_of(d, d + 4);
-        if (all || r < a.h.rows) *(u32x4*)(out + n * 16) = v;
-        if (PLANES == 2) {
-          const u32x4 w = pair_of(e, e + 4);
-          if (all || r < a.h.rows) *(u32x4*)(out + a.plane + n * 16) = w;
-        }
+        uint16_t* const out = row + (n / 4) * (gemm::block_bytes(__builtin_ctz(TQ)) / 2) + (n & 2) * 16;
+        *(u32x4*)out = pair_of(d, d + 4);
+        if (PLANES == 2) *(u32x4*)(out + a.dz.plane) = pair_of(e, e + 4);
       }
     }
-    return all;
+    return true;
   });
 }
 
 // ---- gradients -----------------------------------------------------------------------
 
 struct GradHArgs {
-  Matrix w, dz;  // a piece of the vocabulary
+  Matrix w;  // a piece of the vocabulary
+  Dz dz;
   uint32_t planes;
-  uint64_t plane;
-  uint32_t tiles_p, tiles_q, splits, total, dim;
+  uint32_t tiles_p, tiles_q, splits, total, dim, rows;
   float* sums;  // [splits][rows][pitch]
   uint32_t pitch;
   bool add;
@@ -330,18 +344,15 @@ __global__ __launch_bounds__(WP* WQ * 64) void k_grad_h(GradHArgs a) {
   const uint32_t s0 = (uint32_t)((uint64_t)steps * split / a.splits);
   const uint32_t s1 = (uint32_t)((uint64_t)steps * (split + 1) / a.splits);
   t.clear();
-  Matrix dz = a.dz;
-  uint32_t plane = 0;
   // The operands end with the split.
   Matrix w = a.w;
   w.rows = min(w.rows, s1 * 64);
-  dz.cols = min(dz.cols, s1 * 64);
+  uint32_t plane = 0;
   t.template run<0>(
-      gemm::Segment{across(w, p0), along(dz, q0), s0, s1},
+      gemm::Segment{across(w, p0), a.dz.along(0, q0, s1), s0, s1},
       [&](gemm::Segment* s) {
         if (++plane >= a.planes) return false;
-        dz.at += a.plane;
-        s->q = along(dz, q0);
+        s->q = a.dz.along(plane, q0, s1);
         return true;
       },
       [](uint32_t) {}, [](uint32_t) { return false; }, lds);
@@ -349,8 +360,8 @@ __global__ __launch_bounds__(WP* WQ * 64) void k_grad_h(GradHArgs a) {
 #pragma unroll
   for (int m = 0; m < t.MT; ++m) {
     const uint32_t r = q0 + t.wq + m * 16 + t.i;
-    if (r >= a.dz.rows) continue;
-    float* out = a.sums + ((size_t)split * a.dz.rows + r) * a.pitch + c0;
+    if (r >= a.rows) continue;
+    float* out = a.sums + ((size_t)split * a.rows + r) * a.pitch + c0;
 #pragma unroll
     for (int n = 0; n < t.NT; ++n)
       if (c0 + n * 16 < a.pitch) {
@@ -387,9 +398,9 @@ template <int DT> __global__ __launch_bounds__(256) void k_finish_h(FinishArgs a
 }
 
 struct GradWArgs {
-  Matrix h, dz;  // dz's columns are a piece of the vocabulary
+  Matrix h;
+  Dz dz;  // of a piece of the vocabulary
   uint32_t planes;
-  uint64_t plane;
   uint32_t tiles_p, total, dim, vocab;  // vocab: of the piece
   void* out;
   int64_t ldo;
@@ -404,14 +415,12 @@ __global__ __launch_bounds__(WP* WQ * 64) void k_grad_w(GradWArgs a) {
   const uint32_t p0 = place % a.tiles_p * TP, q0 = place / a.tiles_p * TQ;
   if (q0 >= a.vocab) return;
   t.clear();
-  Matrix dz = a.dz;
   uint32_t plane = 0;
   t.template run<0>(
-      gemm::Segment{across(a.h, p0), across(dz, q0), 0, (a.h.rows + 63) / 64},
+      gemm::Segment{across(a.h, p0), a.dz.across(0, q0), 0, (a.h.rows + 63) / 64},
       [&](gemm::Segment* s) {
         if (++plane >= a.planes) return false;
-        dz.at += a.plane;
-        s->q = across(dz, q0);
+        s->q = a.dz.across(plane, q0);
         return true;
       },
       [](uint32_t) {}, [](uint32_t) { return false; }, lds);
@@ -454,6 +463,8 @@ struct Plan {
   uint32_t chunk;        // rows at a time whose slabs' sums are kept
   uint32_t splits;       // of dH's sums over the vocabulary
   uint32_t tile;         // rows of a tile
+  uint32_t log;          // dz is in blocks of 2^log = tile rows
+  int64_t plane;         // its bytes, of which there are two for float32 gradients
   int64_t h, masked, w, part, picked, dz, sums, bytes;
 };
 
@@ -480,7 +491,9 @@ Plan plan_of(int64_t n_rows, int32_t n_vocab, int32_t n_dim) {
   p.w = take(&at, (int64_t)p.piece * p.pitch * 2);
   p.part = take(&at, (int64_t)((vocab + p.piece - 1) / p.piece * p.piece / kSlab) * p.chunk * 8);
   p.picked = take(&at, (int64_t)rows * 4);
-  p.dz = take(&at, (int64_t)rows * (p.piece + 64) * 4);
+  p.log = p.tile == 256 ? 8 : p.tile == 128 ? 7 : 6;
+  p.plane = (int64_t)(up(rows, p.tile) / p.tile) * (p.piece / 64) * gemm::block_bytes(p.log);
+  p.dz = take(&at, p.plane * 2);
   p.sums = take(&at, (int64_t)p.splits * rows * p.pitch * 4);
   p.bytes = at;
   return p;
@@ -544,7 +557,7 @@ template <int TP, int TQ, int WP, int WQ, int PLANES> hipError_t dz(LogitsArgs a
 template <int TP, int TQ, int WP, int WQ> hipError_t grad_h(GradHArgs a, hipStream_t s) {
   typedef Tile<Bf16, TP, TQ, WP, WQ, true, false> T;
   a.tiles_p = (a.dim + TP - 1) / TP;
-  a.tiles_q = (a.dz.rows + TQ - 1) / TQ;
+  a.tiles_q = (a.rows + TQ - 1) / TQ;
   a.total = up(a.tiles_p * a.tiles_q * a.splits, 8);
   auto* k = k_grad_h<TP, TQ, WP, WQ>;
   LAUNCH(T, 0, k, a.total, s, a);
@@ -642,9 +655,8 @@ hipError_t launch_xent_grad(const XentArgs& a, hipStream_t s) {
     l.lse = a.lse;
     l.weight = a.weight;
     l.vocab = a.vocab;
-    l.dz = (uint16_t*)(a.space + p.dz);
-    l.pitch = p.piece + 64;
-    l.plane = (uint64_t)a.rows * l.pitch;
+    // Rows of whole tiles, columns of whole steps of this piece (memory: of whole tiles).
+    l.dz = Dz{(uint16_t*)(a.space + p.dz), (uint64_t)p.plane / 2, p.log, p.piece / 64, up(a.rows, p.tile), up(n, 64)};
     l.h.cols = l.w.cols;  // zeros from dim on
     if (f32)
       TRY_HIP((p.tile == 256   ? dz<256, 256, 2, 4, 2>(l, s)
@@ -654,12 +666,11 @@ hipError_t launch_xent_grad(const XentArgs& a, hipStream_t s) {
       TRY_HIP((p.tile == 256   ? dz<256, 256, 2, 4, 1>(l, s)
                : p.tile == 128 ? dz<256, 128, 2, 2, 1>(l, s)
                                : dz<128, 64, 1, 4, 1>(l, s)));
-    const Matrix d{l.dz, l.pitch, a.rows, up(n, 64)};
     GradHArgs gh{};
     gh.w = l.w;
-    gh.dz = d;
+    gh.dz = l.dz;
+    gh.rows = a.rows;
     gh.planes = f32 ? 2 : 1;
-    gh.plane = l.plane;
     gh.splits = p.splits;
     gh.dim = a.dim;
     gh.sums = (float*)(a.space + p.sums);
@@ -670,9 +681,8 @@ hipError_t launch_xent_grad(const XentArgs& a, hipStream_t s) {
                              : grad_h<256, 64, 2, 2>(gh, s)));
     GradWArgs gw{};
     gw.h = h;
-    gw.dz = d;
+    gw.dz = l.dz;
     gw.planes = gh.planes;
-    gw.plane = l.plane;
     gw.dim = a.dim;
     gw.vocab = n;
     gw.ldo = a.ldgw;

@@ -25,15 +25,24 @@ struct Int8 {
   static constexpr int BYTES = 1;
 };
 
+// Bytes from a block of 2^log rows x 128 bytes to the next: a power of two apart, the
+// blocks that are read at once would lie in the same channels of memory.
+__host__ __device__ constexpr uint32_t block_bytes(uint32_t log) { return (128u << log) + 1024; }
+
 // An operand of one tile.  Rows along k: `at` is its first row, `rows` the rows
 // there are from it on and `cols` the length of k.  k across: `at` is the
 // tile's first column of row k = 0, `rows` the length of k and `cols` the
 // columns there are from the tile's first on.  16-byte aligned, `pitch` in bytes
 // a multiple of 16, and cols * BYTES a multiple of 16: a 16-byte load is inside
 // or outside as a whole.
+// log > 0: a matrix in blocks of 2^log rows x 128 bytes, `blocks` of them beside each
+// other, each as one piece of memory (pitch 128): what a step reads lies together
+// whichever way it runs.  rows and cols are whole blocks, and all of it is there.
 struct Operand {
   const char* at;
   uint32_t pitch, rows, cols;
+  uint32_t log, blocks;
+  __device__ __forceinline__ uint32_t group() const { return log ? block_bytes(log) : 128u; }
 };
 
 constexpr int kStep = 128;  // bytes of k a step: 64 bfloat16 or 128 integers
@@ -60,19 +69,24 @@ template <class E, int T, bool ACROSS, int WAVES, bool HALF = false> struct Side
   uint32_t from;   // this lane's byte offset within the rows of its first load
   uint32_t piece;  // its 16-byte piece of a row (rows along k), or byte of a row
 
-  __device__ __forceinline__ void init(uint32_t wave, uint32_t lane, uint32_t pitch) {
+  __device__ __forceinline__ void init(uint32_t wave, uint32_t lane, const Operand& o) {
     const uint32_t r = lane / (ROW / 16), c = lane % (ROW / 16);
     const uint32_t row = wave * PER + r;
     if (ACROSS) {
       // Rows of a wave's loads are turned alike, or alternately.
       static_assert(!ACROSS || WAVES * PER % 16 == 0 || (WAVES * PER == 8 && T >= 128), "16 rows repeat");
       piece = (((c >> 1) ^ turned(row)) << 5) + ((c & 1) << 4);
+      // 64 columns are a group in memory.
       if (HALF) piece += piece & 128;
+      piece = (piece >> 7) * o.group() + (piece & 127);
     } else {
       piece = (c ^ (row & 7)) << 4;
     }
-    from = row * pitch + piece;
+    from = row * o.pitch + piece;
   }
+  // What is left behind k, by scalar instructions: an unsigned difference that saturates
+  // is a vector one, and a descriptor in vector registers is loaded with in a loop.
+  __device__ static __forceinline__ int behind(uint32_t all, uint32_t k) { return max((int)(all - k), 0); }
 #if defined(__HIP_DEVICE_COMPILE__)
   // Loads of step `s` (k from s * kStep bytes on) into `to`.
   __device__ __forceinline__ void load(const Operand& o, uint32_t s, char* to, uint32_t wave,
@@ -81,29 +95,31 @@ template <class E, int T, bool ACROSS, int WAVES, bool HALF = false> struct Side
     // Rows between a wave's loads.
     constexpr uint32_t APART = HALF && !ACROSS ? 128 : WAVES * PER;
     static_assert(!HALF || ACROSS || WAVES * PER == 64, "a load of every wave is 64 rows");
-    const uint32_t start = from + shift * (ACROSS ? 2 : o.pitch);
     if (ACROSS) {
-      const uint32_t k = s * (kStep / 2), left = o.rows > k ? min(o.rows - k, 64u) : 0u;
-      const uint32_t bytes = left ? (left - 1) * o.pitch + min(o.cols * 2, o.pitch) : 0u;
-      const auto d = __builtin_amdgcn_make_buffer_rsrc((void*)(o.at + (size_t)k * o.pitch), 0, (int)bytes,
-                                                       0x00020000);
+      const uint32_t k = s * (kStep / 2), left = (uint32_t)min(behind(o.rows, k), 64);
+      const size_t away = o.log ? (size_t)(k >> o.log) * o.blocks * o.group() + (k & ((1u << o.log) - 1)) * 128
+                                : (size_t)k * o.pitch;
+      const uint32_t bytes = !left ? 0u : o.log ? 0x7FFFFFF0u : (left - 1) * o.pitch + min(o.cols * 2, o.pitch);
+      const auto d = __builtin_amdgcn_make_buffer_rsrc((void*)(o.at + away), 0, (int)bytes, 0x00020000);
+      const uint32_t start = from + (shift >> 6) * o.group();
+      // Alternately turned rows are those of operands that are not in blocks.
       const uint32_t other = WAVES * PER == 8 ? start - piece + (piece ^ 128) : start;
 #pragma unroll
       for (int c = 0; c < LOADS; ++c)
         __builtin_amdgcn_raw_ptr_buffer_load_lds(d, (Lds)(to + (c * WAVES + wave) * 1024), 16,
                                                  (int)((c & 1 ? other : start) + c * APART * o.pitch), 0, 0, 0);
     } else {
-      const uint32_t rows = min(o.rows, (uint32_t)(HALF ? 2 * T : T)), len = o.cols * E::BYTES;
-      const uint32_t bytes = rows ? (rows - 1) * o.pitch + len : 0u;
-      const auto d = __builtin_amdgcn_make_buffer_rsrc((void*)o.at, 0, (int)bytes, 0x00020000);
-      const uint32_t k = s * kStep;
+      const uint32_t k = s * kStep, left = (uint32_t)behind(o.cols * E::BYTES, k);
+      const uint32_t rows = left ? min(o.rows, (uint32_t)(HALF ? 2 * T : T)) : 0u;
+      const uint32_t bytes = rows ? (rows - 1) * o.pitch + min(left, (uint32_t)kStep) : 0u;
+      const size_t away = o.log ? (size_t)s * o.group() : k;
+      const auto d = __builtin_amdgcn_make_buffer_rsrc((void*)(o.at + away), 0, (int)bytes, 0x00020000);
       // Past the row's end: an offset beyond every descriptor's range.
-      const bool out = k + piece >= len;
+      const uint32_t start = piece < left ? from + shift * o.pitch : 0x70000000u;
 #pragma unroll
       for (int c = 0; c < LOADS; ++c)
-        __builtin_amdgcn_raw_ptr_buffer_load_lds(
-            d, (Lds)(to + (c * WAVES + wave) * 1024), 16,
-            (int)(out ? 0x7FFFFFF0u : start + k + c * APART * o.pitch), 0, 0, 0);
+        __builtin_amdgcn_raw_ptr_buffer_load_lds(d, (Lds)(to + (c * WAVES + wave) * 1024), 16,
+                                                 (int)(start + c * APART * o.pitch), 0, 0, 0);
     }
   }
   // The 16 rows (columns) from 16 t + `first` on, `first` a multiple of the
@@ -236,10 +252,14 @@ template <class E, int TP, int TQ, int WP, int WQ, bool PA, bool QA> struct Tile
     typedef Side<E, 128, PA, WAVES, true> Half;
     constexpr int HALF = Half::SIZE;
     static_assert(NT == 8 && MT == 4 && Half::LOADS == 2 && Q::LOADS == 4, "what the waits count");
+    // Q with k across lies in groups of 64 columns: a load of blocks is one piece of memory
+    // (rows of all 256 took the product that reads them 265 us instead of 230).
+    typedef Side<E, QA ? 64 : TQ, QA, WAVES> Part;
+    static_assert(!QA || (Part::LOADS == 1 && TQ / WQ == 64), "a wave's columns are a group");
     Half sp;
-    Q sq;
-    sp.init(wave, lane, cur.p.pitch);
-    sq.init(wave, lane, cur.q.pitch);
+    Part sq;
+    sp.init(wave, lane, cur.p);
+    sq.init(wave, lane, cur.q);
     u32x4 pv[2][4], qv[2][4];
     // A stage: P's halves, then Q.
     auto read_p = [&](const char* from) {
@@ -252,7 +272,13 @@ template <class E, int TP, int TQ, int WP, int WQ, bool PA, bool QA> struct Tile
 #pragma unroll
       for (int h = 0; h < 2; ++h)
 #pragma unroll
-        for (int m = 0; m < 4; ++m) qv[h][m] = Q::operand(from + 2 * HALF, wq, m, h, i, g);
+        for (int m = 0; m < 4; ++m)
+          qv[h][m] = QA ? Part::operand(from + 2 * HALF + wq / 64 * Part::SIZE, 0, m, h, i, g)
+                        : Part::operand(from + 2 * HALF, wq, m, h, i, g);
+    };
+    auto load_q = [&](const Operand& o, uint32_t s, char* to) {
+#pragma unroll
+      for (int c = 0; c < TQ / (QA ? 64 : TQ); ++c) sq.load(o, s, to + c * Part::SIZE, wave, c * 64);
     };
     auto products = [&](int half) {
       __builtin_amdgcn_s_setprio(1);
@@ -273,16 +299,16 @@ template <class E, int TP, int TQ, int WP, int WQ, bool PA, bool QA> struct Tile
       __builtin_amdgcn_sched_barrier(0);
     };
     sp.load(cur.p, cur.s0, lds, wave, 0);
-    sq.load(cur.q, cur.s0, lds + 2 * HALF, wave);
+    load_q(cur.q, cur.s0, lds + 2 * HALF);
     sp.load(cur.p, cur.s0, lds + HALF, wave, 64);
     sp.load(cur.p, cur.s0 + 1, lds + STAGE, wave, 0);
-    sq.load(cur.q, cur.s0 + 1, lds + STAGE + 2 * HALF, wave);
+    load_q(cur.q, cur.s0 + 1, lds + STAGE + 2 * HALF);
     wait_loads<6>();  // the first step is there
     __builtin_amdgcn_s_barrier();
     const bool second = wave >= 4;
     if (second) turn();
     uint32_t at = 0, odd = 0;
-    bool stored = false;
+    bool stored = false, ahead = false;
     for (bool more = true; more; odd ^= 1) {
       Segment nxt = cur;
       more = next(&nxt);
@@ -300,13 +326,14 @@ template <class E, int TP, int TQ, int WP, int WQ, bool PA, bool QA> struct Tile
         uint32_t s;
         read_p(from);
         read_q(from);
-        {
+        if (!ahead) {
           const Operand p = whose(j + 1, &s) ? cur.p : nxt.p;
           sp.load(p, s, lds + (STAGE - at) + HALF, wave, 64);
         }
+        ahead = false;
         // This step's second half of P is there: behind it were asked for the next step's
-        // first half and Q (6), and what this turn asked for (2).
-        if (STORES && stored && j == 0)
+        // first half and Q (6), and its second half (2).
+        if (STORES && stored && j < 2)
           wait_loads<(8 + STORES < 63 ? 8 + STORES : 63)>();
         else
           wait_loads<8>();
@@ -318,7 +345,7 @@ template <class E, int TP, int TQ, int WP, int WQ, bool PA, bool QA> struct Tile
           const bool in = whose(j + 2, &s);
           const Operand p = in ? cur.p : nxt.p, q = in ? cur.q : nxt.q;
           sp.load(p, s, from, wave, 0);
-          sq.load(q, s, from + 2 * HALF, wave);
+          load_q(q, s, from + 2 * HALF);
         }
         // The next step's first half and Q are there: behind them were asked for its second
         // half (2) and what this turn asked for (6).
@@ -330,6 +357,12 @@ template <class E, int TP, int TQ, int WP, int WQ, bool PA, bool QA> struct Tile
         products(1);
         turn();
         at = STAGE - at;
+      }
+      // The next segment's second step: every wave has read what lies in its place, and
+      // asked for now it does not wait for the results' stores.
+      if (STORES) {
+        sp.load(nxt.p, nxt.s0 + 1, lds + (STAGE - at) + HALF, wave, 64);
+        ahead = true;
       }
       __builtin_amdgcn_sched_barrier(0);
       stored = done(odd);
@@ -357,8 +390,8 @@ template <class E, int TP, int TQ, int WP, int WQ, bool PA, bool QA> struct Tile
     if (s0 >= s1) return;
     P sp;
     Q sq;
-    sp.init(wave, lane, p.pitch);
-    sq.init(wave, lane, q.pitch);
+    sp.init(wave, lane, p);
+    sq.init(wave, lane, q);
     sp.load(p, s0, lds, wave);
     sq.load(q, s0, lds + P::SIZE, wave);
     uint32_t at = 0;
