@@ -173,7 +173,7 @@ constexpr int kSlab = 128;
 
 template <int TP, int TQ, int WP, int WQ>
 __global__ __launch_bounds__(WP* WQ * 64) void k_sums(LogitsArgs a) {
-  typedef Tile<Bf16, TP, TQ, WP, WQ, false, false> T;
+  typedef Tile<Bf16, TP, TQ, WP, WQ, false, false, false> T;
   extern __shared__ __attribute__((aligned(1024))) char lds[];
   T t;
   static_assert(TP / WP == kSlab, "a wave's columns are a slab");
@@ -267,7 +267,7 @@ __device__ __forceinline__ uint32_t piece_of(uint32_t g) { return (g & 1) * 16 +
 
 template <int TP, int TQ, int WP, int WQ, int PLANES>
 __global__ __launch_bounds__(WP* WQ * 64) void k_dz(LogitsArgs a) {
-  typedef Tile<Bf16, TP, TQ, WP, WQ, false, false> T;
+  typedef Tile<Bf16, TP, TQ, WP, WQ, false, false, false> T;
   extern __shared__ __attribute__((aligned(1024))) char lds[];
   T t;
   constexpr int STORES = T::MT * T::NT / 2 * PLANES;
@@ -335,7 +335,7 @@ struct GradHArgs {
 template <int TP, int TQ, int WP, int WQ>
 __global__ __launch_bounds__(WP* WQ * 64) void k_grad_h(GradHArgs a) {
   extern __shared__ __attribute__((aligned(1024))) char lds[];
-  Tile<Bf16, TP, TQ, WP, WQ, true, false> t;
+  Tile<Bf16, TP, TQ, WP, WQ, true, false, true> t;
   const uint32_t place = place_of(blockIdx.x, a.total), tiles = a.tiles_p * a.tiles_q;
   const uint32_t split = place / tiles, in = place % tiles;
   if (split >= a.splits) return;
@@ -410,7 +410,7 @@ template <int TP, int TQ, int WP, int WQ, int DT>
 __global__ __launch_bounds__(WP* WQ * 64) void k_grad_w(GradWArgs a) {
   typedef typename rows::Elem<DT>::T T;
   extern __shared__ __attribute__((aligned(1024))) char lds[];
-  Tile<Bf16, TP, TQ, WP, WQ, true, true> t;
+  Tile<Bf16, TP, TQ, WP, WQ, true, true, true> t;
   const uint32_t place = place_of(blockIdx.x, a.total);
   const uint32_t p0 = place % a.tiles_p * TP, q0 = place / a.tiles_p * TQ;
   if (q0 >= a.vocab) return;
@@ -541,21 +541,21 @@ template <class T> uint32_t blocks(uint32_t total, int info) {
 }
 
 template <int TP, int TQ, int WP, int WQ> hipError_t sums(LogitsArgs a, hipStream_t s) {
-  typedef Tile<Bf16, TP, TQ, WP, WQ, false, false> T;
+  typedef Tile<Bf16, TP, TQ, WP, WQ, false, false, false> T;
   a.tiles_q = (a.h.rows + TQ - 1) / TQ;
   a.total = up((a.w.rows + TP - 1) / TP * a.tiles_q, 8);
   auto* k = k_sums<TP, TQ, WP, WQ>;
   LAUNCH(T, 2 * kInfo<TQ>, k, blocks<T>(a.total, 2 * kInfo<TQ>), s, a);
 }
 template <int TP, int TQ, int WP, int WQ, int PLANES> hipError_t dz(LogitsArgs a, hipStream_t s) {
-  typedef Tile<Bf16, TP, TQ, WP, WQ, false, false> T;
+  typedef Tile<Bf16, TP, TQ, WP, WQ, false, false, false> T;
   a.tiles_q = (a.h.rows + TQ - 1) / TQ;
   a.total = up((a.w.rows + TP - 1) / TP * a.tiles_q, 8);
   auto* k = k_dz<TP, TQ, WP, WQ, PLANES>;
   LAUNCH(T, 2 * kInfo<TQ>, k, blocks<T>(a.total, 2 * kInfo<TQ>), s, a);
 }
 template <int TP, int TQ, int WP, int WQ> hipError_t grad_h(GradHArgs a, hipStream_t s) {
-  typedef Tile<Bf16, TP, TQ, WP, WQ, true, false> T;
+  typedef Tile<Bf16, TP, TQ, WP, WQ, true, false, true> T;
   a.tiles_p = (a.dim + TP - 1) / TP;
   a.tiles_q = (a.rows + TQ - 1) / TQ;
   a.total = up(a.tiles_p * a.tiles_q * a.splits, 8);
@@ -563,7 +563,7 @@ template <int TP, int TQ, int WP, int WQ> hipError_t grad_h(GradHArgs a, hipStre
   LAUNCH(T, 0, k, a.total, s, a);
 }
 template <int TP, int TQ, int WP, int WQ, int DT> hipError_t grad_w(GradWArgs a, hipStream_t s) {
-  typedef Tile<Bf16, TP, TQ, WP, WQ, true, true> T;
+  typedef Tile<Bf16, TP, TQ, WP, WQ, true, true, true> T;
   a.tiles_p = (a.dim + TP - 1) / TP;
   a.total = up(a.tiles_p * ((a.vocab + TQ - 1) / TQ), 8);
   auto* k = k_grad_w<TP, TQ, WP, WQ, DT>;

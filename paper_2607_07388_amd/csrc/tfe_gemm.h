@@ -35,14 +35,13 @@ __host__ __device__ constexpr uint32_t block_bytes(uint32_t log) { return (128u 
 // columns there are from the tile's first on.  16-byte aligned, `pitch` in bytes
 // a multiple of 16, and cols * BYTES a multiple of 16: a 16-byte load is inside
 // or outside as a whole.
-// log > 0: a matrix in blocks of 2^log rows x 128 bytes, `blocks` of them beside each
-// other, each as one piece of memory (pitch 128): what a step reads lies together
-// whichever way it runs.  rows and cols are whole blocks, and all of it is there.
+// In blocks (a Side's BLOCKS): 2^log rows x 128 bytes as one piece of memory each (pitch
+// 128), `blocks` of them beside each other: what a step reads lies together whichever
+// way it runs.  rows and cols are whole blocks, and all of it is there.
 struct Operand {
   const char* at;
   uint32_t pitch, rows, cols;
   uint32_t log, blocks;
-  __device__ __forceinline__ uint32_t group() const { return log ? block_bytes(log) : 128u; }
 };
 
 constexpr int kStep = 128;  // bytes of k a step: 64 bfloat16 or 128 integers
@@ -54,11 +53,12 @@ constexpr int kStep = 128;  // bytes of k a step: 64 bfloat16 or 128 integers
 // number, so that the eight rows that are read at once (k to k + 3 and k + 8 to
 // k + 11) lie on different banks.
 // HALF: the T rows are 64 of each 128, from `shift` (0 or 64) on.
-template <class E, int T, bool ACROSS, int WAVES, bool HALF = false> struct Side {
+template <class E, int T, bool ACROSS, bool BLOCKS, int WAVES, bool HALF = false> struct Side {
   static constexpr int SIZE = T * kStep;
   static constexpr int LOADS = SIZE / 1024 / WAVES;
   static_assert(SIZE % (1024 * WAVES) == 0, "whole loads of every wave");
   static_assert(!ACROSS || E::BYTES == 2, "the transposing read is one of 16-bit numbers");
+  static_assert(!ACROSS || !BLOCKS || T == 64, "across blocks, a load is of one block");
   static constexpr uint32_t ROW = ACROSS ? T * 2 : kStep;  // bytes of an LDS row
   static constexpr uint32_t PER = 1024 / ROW;              // rows of a load instruction
 
@@ -76,46 +76,85 @@ template <class E, int T, bool ACROSS, int WAVES, bool HALF = false> struct Side
       // Rows of a wave's loads are turned alike, or alternately.
       static_assert(!ACROSS || WAVES * PER % 16 == 0 || (WAVES * PER == 8 && T >= 128), "16 rows repeat");
       piece = (((c >> 1) ^ turned(row)) << 5) + ((c & 1) << 4);
-      // 64 columns are a group in memory.
       if (HALF) piece += piece & 128;
-      piece = (piece >> 7) * o.group() + (piece & 127);
     } else {
       piece = (c ^ (row & 7)) << 4;
     }
     from = row * o.pitch + piece;
   }
-  // What is left behind k, by scalar instructions: an unsigned difference that saturates
-  // is a vector one, and a descriptor in vector registers is loaded with in a loop.
-  __device__ static __forceinline__ int behind(uint32_t all, uint32_t k) { return max((int)(all - k), 0); }
+
+  // Where a step's k begins, and what is left of it (rows, or bytes along the rows), in
+  // scalar registers (a limit may be applied by a vector instruction, and a descriptor in
+  // vector registers is loaded with in a loop: told to be the same in all lanes).  A turn's scalar instructions take time that its loads do not have:
+  // the next step's place is added up, not worked out.
+  struct Cursor {
+    const char* at;
+    int left;
+    uint32_t fixed;  // bytes to the last row, or of the columns that there are
+    uint32_t step, pitch;
+    uint32_t phase, phases, jump;  // across blocks of more rows than a step
+  };
+  __device__ static __forceinline__ Cursor start(const Operand& o, uint32_t s) {
+    Cursor c{};
+    c.pitch = o.pitch;
+    if (ACROSS) {
+      const uint32_t k = s * (kStep / 2);
+      c.left = max((int)(o.rows - k), 0);
+      if (BLOCKS) {
+        const uint32_t wide = o.blocks * block_bytes(o.log);
+        c.phases = 1u << (o.log - 6);
+        c.phase = s & (c.phases - 1);
+        c.step = 64 * 128;
+        c.jump = wide - (128u << o.log);
+        c.at = o.at + (size_t)(k >> o.log) * wide + c.phase * c.step;
+        c.fixed = 128;
+      } else {
+        c.step = 64 * o.pitch;
+        c.at = o.at + (size_t)k * o.pitch;
+        c.fixed = min(o.cols * 2, o.pitch);
+      }
+    } else {
+      c.left = max((int)(o.cols * E::BYTES - s * kStep), 0);
+      c.step = BLOCKS ? block_bytes(o.log) : kStep;
+      c.at = o.at + (size_t)s * c.step;
+      const uint32_t rows = min(o.rows, (uint32_t)(HALF ? 2 * T : T));
+      c.fixed = rows ? (rows - 1) * o.pitch : 0u;
+      if (!rows) c.left = 0;
+    }
+    return c;
+  }
+  __device__ static __forceinline__ void advance(Cursor* c) {
+    c->at += c->step;
+    c->left = max(c->left - (ACROSS ? kStep / 2 : kStep), 0);
+    if (ACROSS && BLOCKS) {
+      c->phase = c->phase + 1 == c->phases ? 0 : c->phase + 1;
+      if (c->phase == 0) c->at += c->jump;
+    }
+  }
 #if defined(__HIP_DEVICE_COMPILE__)
-  // Loads of step `s` (k from s * kStep bytes on) into `to`.
-  __device__ __forceinline__ void load(const Operand& o, uint32_t s, char* to, uint32_t wave,
-                                       uint32_t shift = 0) const {
+  // A step's loads into `to`; across blocks `shift` is in bytes.
+  __device__ __forceinline__ void load(const Cursor& o, char* to, uint32_t wave, uint32_t shift = 0) const {
     typedef __attribute__((address_space(3))) void* Lds;
     // Rows between a wave's loads.
     constexpr uint32_t APART = HALF && !ACROSS ? 128 : WAVES * PER;
     static_assert(!HALF || ACROSS || WAVES * PER == 64, "a load of every wave is 64 rows");
     if (ACROSS) {
-      const uint32_t k = s * (kStep / 2), left = (uint32_t)min(behind(o.rows, k), 64);
-      const size_t away = o.log ? (size_t)(k >> o.log) * o.blocks * o.group() + (k & ((1u << o.log) - 1)) * 128
-                                : (size_t)k * o.pitch;
-      const uint32_t bytes = !left ? 0u : o.log ? 0x7FFFFFF0u : (left - 1) * o.pitch + min(o.cols * 2, o.pitch);
-      const auto d = __builtin_amdgcn_make_buffer_rsrc((void*)(o.at + away), 0, (int)bytes, 0x00020000);
-      const uint32_t start = from + (shift >> 6) * o.group();
-      // Alternately turned rows are those of operands that are not in blocks.
+      const int rows = min(o.left, 64);
+      // (rows - 1) * pitch + fixed, of no rows 0.  All of the blocks is there.
+      const int bytes = __builtin_amdgcn_readfirstlane(
+          BLOCKS ? (rows ? 0x7FFFFFF0 : 0) : max((int)(rows * o.pitch - (o.pitch - o.fixed)), 0));
+      const auto d = __builtin_amdgcn_make_buffer_rsrc((void*)o.at, 0, bytes, 0x00020000);
+      const uint32_t start = from + (BLOCKS ? shift : shift * 2);
       const uint32_t other = WAVES * PER == 8 ? start - piece + (piece ^ 128) : start;
 #pragma unroll
       for (int c = 0; c < LOADS; ++c)
         __builtin_amdgcn_raw_ptr_buffer_load_lds(d, (Lds)(to + (c * WAVES + wave) * 1024), 16,
                                                  (int)((c & 1 ? other : start) + c * APART * o.pitch), 0, 0, 0);
     } else {
-      const uint32_t k = s * kStep, left = (uint32_t)behind(o.cols * E::BYTES, k);
-      const uint32_t rows = left ? min(o.rows, (uint32_t)(HALF ? 2 * T : T)) : 0u;
-      const uint32_t bytes = rows ? (rows - 1) * o.pitch + min(left, (uint32_t)kStep) : 0u;
-      const size_t away = o.log ? (size_t)s * o.group() : k;
-      const auto d = __builtin_amdgcn_make_buffer_rsrc((void*)(o.at + away), 0, (int)bytes, 0x00020000);
+      const int bytes = __builtin_amdgcn_readfirstlane((int)o.fixed + min(o.left, kStep));
+      const auto d = __builtin_amdgcn_make_buffer_rsrc((void*)o.at, 0, bytes, 0x00020000);
       // Past the row's end: an offset beyond every descriptor's range.
-      const uint32_t start = piece < left ? from + shift * o.pitch : 0x70000000u;
+      const uint32_t start = (int)piece < o.left ? from + shift * o.pitch : 0x70000000u;
 #pragma unroll
       for (int c = 0; c < LOADS; ++c)
         __builtin_amdgcn_raw_ptr_buffer_load_lds(d, (Lds)(to + (c * WAVES + wave) * 1024), 16,
@@ -186,13 +225,16 @@ __device__ __forceinline__ Segment no_segment(const Segment& like) {
 
 // A block of WP x WQ waves and its tile of TP x TQ sums.  Lane (g, i) of a wave
 // holds in acc[n][m][j] the sum at p = wp + 16 n + 4 g + j, q = wq + 16 m + i.
-template <class E, int TP, int TQ, int WP, int WQ, bool PA, bool QA> struct Tile {
+// PA, QA: k runs across P, Q; QB: Q lies in blocks.
+template <class E, int TP, int TQ, int WP, int WQ, bool PA, bool QA, bool QB> struct Tile {
   static constexpr int WAVES = WP * WQ, NT = TP / WP / 16, MT = TQ / WQ / 16;
   static constexpr int THREADS = WAVES * 64;
-  typedef Side<E, TP, PA, WAVES> P;
-  typedef Side<E, TQ, QA, WAVES> Q;
+  typedef Side<E, TP, PA, false, WAVES> P;
+  typedef Side<E, QA && QB ? 64 : TQ, QA, QB, WAVES> Q;
   static constexpr bool LARGE = TP == 256 && TQ == 256 && WP == 2 && WQ == 4;
-  static constexpr int STAGE = P::SIZE + Q::SIZE;
+  static constexpr int PARTS = QA && QB ? TQ / 64 : 1;  // blocks of a step across them
+  static_assert(PARTS == 1 || TQ / WQ == 64, "a wave's columns are a block's");
+  static constexpr int STAGE = P::SIZE + Q::SIZE * PARTS;
   // Behind the stages: two tiles' numbers of their rows and columns, INFO bytes each.
   static constexpr int LDS = 2 * STAGE;
   // Steps of a segment: fewer are followed by zeros.
@@ -249,17 +291,14 @@ template <class E, int TP, int TQ, int WP, int WQ, bool PA, bool QA> struct Tile
   template <int STORES, class Next, class Begin, class Done>
   __device__ __forceinline__ void in_turns(Segment cur, Next next, Begin begin, Done done, char* lds) {
 #if defined(__HIP_DEVICE_COMPILE__)
-    typedef Side<E, 128, PA, WAVES, true> Half;
+    typedef Side<E, 128, PA, false, WAVES, true> Half;
     constexpr int HALF = Half::SIZE;
-    static_assert(NT == 8 && MT == 4 && Half::LOADS == 2 && Q::LOADS == 4, "what the waits count");
-    // Q with k across lies in groups of 64 columns: a load of blocks is one piece of memory
-    // (rows of all 256 took the product that reads them 265 us instead of 230).
-    typedef Side<E, QA ? 64 : TQ, QA, WAVES> Part;
-    static_assert(!QA || (Part::LOADS == 1 && TQ / WQ == 64), "a wave's columns are a group");
+    static_assert(NT == 8 && MT == 4 && Half::LOADS == 2 && Q::LOADS * PARTS == 4, "what the waits count");
     Half sp;
-    Part sq;
+    Q sq;
     sp.init(wave, lane, cur.p);
     sq.init(wave, lane, cur.q);
+    const uint32_t block = block_bytes(cur.q.log);
     u32x4 pv[2][4], qv[2][4];
     // A stage: P's halves, then Q.
     auto read_p = [&](const char* from) {
@@ -273,12 +312,11 @@ template <class E, int TP, int TQ, int WP, int WQ, bool PA, bool QA> struct Tile
       for (int h = 0; h < 2; ++h)
 #pragma unroll
         for (int m = 0; m < 4; ++m)
-          qv[h][m] = QA ? Part::operand(from + 2 * HALF + wq / 64 * Part::SIZE, 0, m, h, i, g)
-                        : Part::operand(from + 2 * HALF, wq, m, h, i, g);
+          qv[h][m] = q_operand(from + 2 * HALF, m, h);
     };
-    auto load_q = [&](const Operand& o, uint32_t s, char* to) {
+    auto load_q = [&](const typename Q::Cursor& c, char* to) {
 #pragma unroll
-      for (int c = 0; c < TQ / (QA ? 64 : TQ); ++c) sq.load(o, s, to + c * Part::SIZE, wave, c * 64);
+      for (int k = 0; k < PARTS; ++k) sq.load(c, to + k * Q::SIZE, wave, k * block);
     };
     auto products = [&](int half) {
       __builtin_amdgcn_s_setprio(1);
@@ -298,11 +336,19 @@ template <class E, int TP, int TQ, int WP, int WQ, bool PA, bool QA> struct Tile
       __builtin_amdgcn_s_barrier();
       __builtin_amdgcn_sched_barrier(0);
     };
-    sp.load(cur.p, cur.s0, lds, wave, 0);
-    load_q(cur.q, cur.s0, lds + 2 * HALF);
-    sp.load(cur.p, cur.s0, lds + HALF, wave, 64);
-    sp.load(cur.p, cur.s0 + 1, lds + STAGE, wave, 0);
-    load_q(cur.q, cur.s0 + 1, lds + STAGE + 2 * HALF);
+    // The next loads' places: P's first half and Q two steps on, P's second half one.
+    auto first = Half::start(cur.p, cur.s0), other = first;
+    auto cq = Q::start(cur.q, cur.s0);
+    sp.load(first, lds, wave, 0);
+    load_q(cq, lds + 2 * HALF);
+    sp.load(other, lds + HALF, wave, 64);
+    Half::advance(&first);
+    Half::advance(&other);
+    Q::advance(&cq);
+    sp.load(first, lds + STAGE, wave, 0);
+    load_q(cq, lds + STAGE + 2 * HALF);
+    Half::advance(&first);
+    Q::advance(&cq);
     wait_loads<6>();  // the first step is there
     __builtin_amdgcn_s_barrier();
     const bool second = wave >= 4;
@@ -315,20 +361,14 @@ template <class E, int TP, int TQ, int WP, int WQ, bool PA, bool QA> struct Tile
       if (!more) nxt = no_segment(cur);
       begin(odd);
       const uint32_t steps = max(cur.s1 - cur.s0, LEAST);
-      // Step j from this segment's first on, and whose.
-      auto whose = [&](uint32_t j, uint32_t* s) {
-        const bool in = j < steps;
-        *s = in ? cur.s0 + j : nxt.s0 + j - steps;
-        return in;
-      };
       for (uint32_t j = 0; j < steps; ++j) {
         char* const from = lds + at;
-        uint32_t s;
         read_p(from);
         read_q(from);
+        if (j + 1 == steps) other = Half::start(nxt.p, nxt.s0);
         if (!ahead) {
-          const Operand p = whose(j + 1, &s) ? cur.p : nxt.p;
-          sp.load(p, s, lds + (STAGE - at) + HALF, wave, 64);
+          sp.load(other, lds + (STAGE - at) + HALF, wave, 64);
+          Half::advance(&other);
         }
         ahead = false;
         // This step's second half of P is there: behind it were asked for the next step's
@@ -341,12 +381,14 @@ template <class E, int TP, int TQ, int WP, int WQ, bool PA, bool QA> struct Tile
         products(0);
         turn();
         read_p(from + HALF);
-        {
-          const bool in = whose(j + 2, &s);
-          const Operand p = in ? cur.p : nxt.p, q = in ? cur.q : nxt.q;
-          sp.load(p, s, from, wave, 0);
-          load_q(q, s, from + 2 * HALF);
+        if (j + 2 == steps) {
+          first = Half::start(nxt.p, nxt.s0);
+          cq = Q::start(nxt.q, nxt.s0);
         }
+        sp.load(first, from, wave, 0);
+        load_q(cq, from + 2 * HALF);
+        Half::advance(&first);
+        Q::advance(&cq);
         // The next step's first half and Q are there: behind them were asked for its second
         // half (2) and what this turn asked for (6).
         if (STORES && stored && j == 0)
@@ -361,7 +403,8 @@ template <class E, int TP, int TQ, int WP, int WQ, bool PA, bool QA> struct Tile
       // The next segment's second step: every wave has read what lies in its place, and
       // asked for now it does not wait for the results' stores.
       if (STORES) {
-        sp.load(nxt.p, nxt.s0 + 1, lds + (STAGE - at) + HALF, wave, 64);
+        sp.load(other, lds + (STAGE - at) + HALF, wave, 64);
+        Half::advance(&other);
         ahead = true;
       }
       __builtin_amdgcn_sched_barrier(0);
@@ -374,6 +417,12 @@ template <class E, int TP, int TQ, int WP, int WQ, bool PA, bool QA> struct Tile
     asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
 #endif
   }
+#if defined(__HIP_DEVICE_COMPILE__)
+  __device__ __forceinline__ u32x4 q_operand(const char* from, int m, int h) const {
+    if (PARTS > 1) return Q::operand(from + wq / 64 * Q::SIZE, 0, m, h, i, g);
+    return Q::operand(from, wq, m, h, i, g);
+  }
+#endif
   // This wave's LDS reads have returned, and all but its last N memory operations.
   template <int N> __device__ static __forceinline__ void wait_loads() {
     static_assert(N < 64, "the counter's range");
@@ -385,15 +434,24 @@ template <class E, int TP, int TQ, int WP, int WQ, bool PA, bool QA> struct Tile
   // Smaller tiles: one step's loads are under way while the one before is
   // multiplied.
   __device__ __forceinline__ void together(const Operand& p, const Operand& q, uint32_t s0, uint32_t s1,
-                                      char* lds) {
+                                           char* lds) {
 #if defined(__HIP_DEVICE_COMPILE__)
     if (s0 >= s1) return;
     P sp;
     Q sq;
     sp.init(wave, lane, p);
     sq.init(wave, lane, q);
-    sp.load(p, s0, lds, wave);
-    sq.load(q, s0, lds + P::SIZE, wave);
+    auto cp = P::start(p, s0);
+    auto cq = Q::start(q, s0);
+    const uint32_t block = block_bytes(q.log);
+    auto load = [&](char* to) {
+      sp.load(cp, to, wave);
+#pragma unroll
+      for (int k = 0; k < PARTS; ++k) sq.load(cq, to + P::SIZE + k * Q::SIZE, wave, k * block);
+      P::advance(&cp);
+      Q::advance(&cq);
+    };
+    load(lds);
     uint32_t at = 0;
     for (uint32_t s = s0; s < s1; ++s) {
       // The stage has arrived, and every wave's reads of the other one have returned.
@@ -402,16 +460,13 @@ template <class E, int TP, int TQ, int WP, int WQ, bool PA, bool QA> struct Tile
       __builtin_amdgcn_sched_barrier(0);
       const char* from = lds + at;
       at = STAGE - at;
-      if (s + 1 < s1) {
-        sp.load(p, s + 1, lds + at, wave);
-        sq.load(q, s + 1, lds + at + P::SIZE, wave);
-      }
+      if (s + 1 < s1) load(lds + at);
       __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
       for (int h = 0; h < 2; ++h) {
         u32x4 qv[MT];
 #pragma unroll
-        for (int m = 0; m < MT; ++m) qv[m] = Q::operand(from + P::SIZE, wq, m, h, i, g);
+        for (int m = 0; m < MT; ++m) qv[m] = q_operand(from + P::SIZE, m, h);
 #pragma unroll
         for (int n = 0; n < NT; ++n) {
           const u32x4 pv = P::operand(from, wp, n, h, i, g);

@@ -104,7 +104,7 @@ struct TileArgs {
 template <int TP, int TQ, int WP, int WQ, int DT>
 __global__ __launch_bounds__(WP* WQ * 64) void k_int8_tiles(TileArgs b) {
   typedef typename Elem<DT>::T E;
-  typedef Tile<Int8, TP, TQ, WP, WQ, false, false> T;
+  typedef Tile<Int8, TP, TQ, WP, WQ, false, false, false> T;
   typedef f32x4 V4;
   typedef f32x4 V4_a4 __attribute__((aligned(4)));
   typedef u32x2 u32x2_a2 __attribute__((aligned(2)));
@@ -198,7 +198,7 @@ __global__ __launch_bounds__(WP* WQ * 64) void k_int8_tiles(TileArgs b) {
 
 template <int TP, int TQ, int WP, int WQ, int DT>
 hipError_t tiles(const Int8MatmulArgs& m, hipStream_t s) {
-  typedef Tile<Int8, TP, TQ, WP, WQ, false, false> T;
+  typedef Tile<Int8, TP, TQ, WP, WQ, false, false, false> T;
   auto* k = k_int8_tiles<TP, TQ, WP, WQ, DT>;
   constexpr int LDS = T::LDS + 2 * (TP + TQ) * 4;
   static std::atomic<uint64_t> told{0};
