@@ -230,24 +230,34 @@ struct JoinArgs {
   float* loss;
   float* lse;
 };
+__device__ __forceinline__ f32x2 joined(f32x2 x, f32x2 y) {
+  const float top = fmaxf(x[0], y[0]);
+  return f32x2{top, x[1] * __expf(x[0] - top) + y[1] * __expf(y[0] - top)};
+}
 __global__ __launch_bounds__(1024) void k_join(JoinArgs a) {
-  __shared__ f32x2 red[64][17];
+  constexpr int LANES = 64, DEEP = 8;  // slabs of a row at a time, and of a thread under way
+  __shared__ f32x2 red[LANES][17];
   const uint32_t i = threadIdx.x & 15, y = threadIdx.x >> 4, r = blockIdx.x * 16 + i;
-  float top = -FLT_MAX, sum = 0.f;
+  const f32x2 none{-FLT_MAX, 0.f};
+  f32x2 sum = none;
   if (r < a.rows)
-    for (uint32_t k = y; k < a.slabs; k += 64) {
-      const f32x2 v = a.part[(size_t)k * a.rows + r];
-      const float m = fmaxf(top, v[0]);
-      sum = sum * __expf(top - m) + v[1] * __expf(v[0] - m);
-      top = m;
+    for (uint32_t k = y; k < a.slabs; k += LANES * DEEP) {
+      f32x2 v[DEEP];
+#pragma unroll
+      for (uint32_t j = 0; j < DEEP; ++j)
+        v[j] = k + j * LANES < a.slabs ? a.part[(size_t)(k + j * LANES) * a.rows + r] : none;
+#pragma unroll
+      for (int j = 0; j < DEEP; ++j) sum = joined(sum, v[j]);
     }
-  red[y][i] = f32x2{top, sum};
+  red[y][i] = sum;
   __syncthreads();
+#pragma unroll 1
+  for (uint32_t half = LANES / 2; half; half >>= 1) {
+    if (y < half) red[y][i] = joined(red[y][i], red[y + half][i]);
+    __syncthreads();
+  }
   if (y != 0 || r >= a.rows) return;
-  for (int k = 1; k < 64; ++k) top = fmaxf(top, red[k][i][0]);
-  sum = 0.f;
-  for (int k = 0; k < 64; ++k) sum += red[k][i][1] * __expf(red[k][i][0] - top);
-  const float rest = logf(sum);
+  const float top = red[0][i][0], rest = logf(red[0][i][1]);
   a.lse[r] = top + rest;
   a.loss[r] = (uint32_t)a.targets[r] < a.vocab ? (top - a.picked[r]) + rest : 0.f;
 }
@@ -380,14 +390,28 @@ struct FinishArgs {
   const float* weight;
   uint32_t vocab;
 };
-template <int DT> __global__ __launch_bounds__(256) void k_finish_h(FinishArgs a) {
+// 64 splits of 64 rows x 1024: 33 us where a thread waited for one after another.
+template <int DT> __global__ __launch_bounds__(64) void k_finish_h(FinishArgs a) {
   const uint32_t per = a.pitch / 4;
   const uint64_t n = (uint64_t)a.rows * per;
-  for (uint64_t at = (uint64_t)blockIdx.x * 256 + threadIdx.x; at < n; at += (uint64_t)gridDim.x * 256) {
+  for (uint64_t at = (uint64_t)blockIdx.x * 64 + threadIdx.x; at < n; at += (uint64_t)gridDim.x * 64) {
     const uint32_t r = (uint32_t)(at / per), c = (uint32_t)(at - (uint64_t)r * per) * 4;
     f32x4 v{0, 0, 0, 0};
-    for (uint32_t k = 0; k < a.splits; ++k)
-      v += *(const f32x4*)(a.sums + ((size_t)k * a.rows + r) * a.pitch + c);
+    const float* from = a.sums + (size_t)r * a.pitch + c;
+    const size_t apart = (size_t)a.rows * a.pitch;
+    uint32_t k = 0;
+    for (; k + 16 <= a.splits; k += 16, from += 16 * apart) {
+      f32x4 x[16];
+#pragma unroll
+      for (int j = 0; j < 16; ++j) x[j] = *(const f32x4*)(from + j * apart);
+#pragma unroll
+      for (int j = 0; j < 16; ++j) v += x[j];
+    }
+    f32x4 x[16];
+#pragma unroll
+    for (uint32_t j = 0; j < 16; ++j) x[j] = k + j < a.splits ? *(const f32x4*)(from + j * apart) : f32x4{0, 0, 0, 0};
+#pragma unroll
+    for (int j = 0; j < 16; ++j) v += x[j];
     // 0 x an infinity of W is not a gradient of a row without one.
     const bool none = (uint32_t)a.targets[r] >= a.vocab || (a.weight && a.weight[r] == 0.f);
     char* out = (char*)a.out + ((size_t)r * a.ldo) * sizeof(typename rows::Elem<DT>::T);
@@ -408,53 +432,109 @@ struct GradWArgs {
 };
 template <int TP, int TQ, int WP, int WQ, int DT>
 __global__ __launch_bounds__(WP* WQ * 64) void k_grad_w(GradWArgs a) {
-  typedef typename rows::Elem<DT>::T T;
+  typedef typename rows::Elem<DT>::T E;
+  typedef Tile<Bf16, TP, TQ, WP, WQ, true, true, true> T;
+  typedef f32x4 f4 __attribute__((aligned(4)));
   extern __shared__ __attribute__((aligned(1024))) char lds[];
-  Tile<Bf16, TP, TQ, WP, WQ, true, true, true> t;
-  const uint32_t place = place_of(blockIdx.x, a.total);
-  const uint32_t p0 = place % a.tiles_p * TP, q0 = place / a.tiles_p * TQ;
-  if (q0 >= a.vocab) return;
+  T t;
+  // A block's tiles, and of each its planes: one segment behind the other.
+  struct Place {
+    uint32_t t, plane, p0, q0;
+  };
+  auto find = [&](Place* x) {
+    if (x->t >= a.total) return false;
+    const uint32_t place = place_of(x->t, a.total);
+    x->p0 = place % a.tiles_p * TP;
+    x->q0 = place / a.tiles_p * TQ;
+    return x->q0 < a.vocab;
+  };
+  auto segment = [&](const Place& x) {
+    return gemm::Segment{across(a.h, x.p0), a.dz.across(x.plane, x.q0), 0, (a.h.rows + 63) / 64};
+  };
+  Place cur{blockIdx.x, 0, 0, 0}, nxt;
+  if (!find(&cur)) return;
+  constexpr int STORES = DT == TFE_F32 ? T::NT * T::MT : T::NT * T::MT / 2;
   t.clear();
-  uint32_t plane = 0;
-  t.template run<0>(
-      gemm::Segment{across(a.h, p0), a.dz.across(0, q0), 0, (a.h.rows + 63) / 64},
-      [&](gemm::Segment* s) {
-        if (++plane >= a.planes) return false;
-        s->q = a.dz.across(plane, q0);
-        return true;
-      },
-      [](uint32_t) {}, [](uint32_t) { return false; }, lds);
-  const uint32_t c0 = p0 + t.wp + t.g * 4;
+  auto write = [&](uint32_t p0, uint32_t q0) {
+    const bool all = p0 + TP <= a.dim && q0 + TQ <= a.vocab;
 #pragma unroll
-  for (int m = 0; m < t.MT; ++m) {
-    const uint32_t v = q0 + t.wq + m * 16 + t.i;
-    if (v >= a.vocab) continue;
-    T* out = (T*)a.out + (size_t)v * a.ldo + c0;
+    for (int m = 0; m < T::MT; ++m) {
+      const uint32_t v = q0 + t.wq + m * 16 + t.i;
+      E* const row = (E*)a.out + (size_t)v * a.ldo + p0 + t.wp;
 #pragma unroll
-    for (int n = 0; n < t.NT; ++n) {
-      f32x4 x = t.acc[n][m];
-      typedef f32x4 f4 __attribute__((aligned(4)));
-      typedef u32x2 u2 __attribute__((aligned(2)));
-      if (c0 + n * 16 + 4 <= a.dim) {
-        if constexpr (DT == TFE_F32) {
-          if (a.add) x += *(const f4*)(out + n * 16);
-          *(f4*)(out + n * 16) = x;
-        } else {
-          *(u2*)(out + n * 16) = u2{pack2(x[0], x[1]), pack2(x[2], x[3])};
-        }
-      } else {
+      for (int n = 0; n < T::NT; n += 2) {
+        if (DT == TFE_F32 || !all) {
 #pragma unroll
-        for (int j = 0; j < 4; ++j)
-          if (c0 + n * 16 + j < a.dim) {
-            const float old = DT == TFE_F32 && a.add ? rows::load1<DT>(out, n * 16 + j) : 0.f;
-            rows::store1<DT>(out, n * 16 + j, x[j] + old);
+          for (int h = 0; h < 2; ++h) {
+            const uint32_t c = (n + h) * 16 + t.g * 4, left = a.dim - min(a.dim, p0 + t.wp + c);
+            f32x4 x = t.acc[n + h][m];
+            if (all || (v < a.vocab && left >= 4)) {
+              if constexpr (DT == TFE_F32) {
+                if (a.add) x += *(const f4*)(row + c);
+                *(f4*)(row + c) = x;
+              } else {
+                typedef u32x2 u2 __attribute__((aligned(2)));
+                *(u2*)(row + c) = u2{pack2(x[0], x[1]), pack2(x[2], x[3])};
+              }
+            } else if (v < a.vocab) {
+#pragma unroll
+              for (uint32_t j = 0; j < 4; ++j)
+                if (j < left) {
+                  const float old = DT == TFE_F32 && a.add ? rows::load1<DT>(row, c + j) : 0.f;
+                  rows::store1<DT>(row, c + j, x[j] + old);
+                }
+            }
           }
+        } else {
+          // They pass by: nothing reads them soon.
+          __builtin_nontemporal_store(pair_of((const float*)&t.acc[n][m], (const float*)&t.acc[n + 1][m]),
+                                      (rows::u32x4_a2*)(row + n * 16 + piece_of(t.g)));
+        }
       }
     }
-  }
+    return all;
+  };
+  t.template run<STORES>(
+      segment(cur),
+      [&](gemm::Segment* s) {
+        nxt = cur;
+        if (++nxt.plane == a.planes) nxt.plane = 0, nxt.t += gridDim.x;
+        const bool more = find(&nxt);
+        if (more) *s = segment(nxt);
+        return more;
+      },
+      [](uint32_t) {},
+      [&](uint32_t) {
+        bool stored = false;
+        if (cur.plane + 1 == a.planes) {
+          stored = write(cur.p0, cur.q0);
+          t.clear();
+        }
+        cur = nxt;
+        return stored;
+      },
+      lds);
 }
 
 // ---- launches ------------------------------------------------------------------------
+
+// Rows of a tile of logits.  Loss and gradients in us with tiles of 64 / 128 / 256 rows
+// (and 128 / 256 / 256 columns), dim 1024: 100 rows of vocabulary 3001 48 / 73 / 78, of 70000
+// 166 / 194 / 190, of 151936 429 / 394 / 421; 200 rows of 20000 97 / 103 / 108, of 151936
+// 647 / 549 / 452; 700 rows of 3000 70 / 90 / 98, of 20000 211 / 191 / 152.
+uint32_t tile_of(uint32_t rows, uint32_t vocab) {
+  const uint32_t cus = (uint32_t)compute_units(), wide = (vocab + 255) / 256;
+  if (rows > 128 && wide * ((rows + 255) / 256) * 4 >= cus * 3) return 256;
+  return rows > 64 && rows <= 128 && wide >= cus * 2 ? 128 : 64;
+}
+// Whether dW is cut into tiles of 128 x 128, of 256 x 256 otherwise.  Loss and gradients in
+// us, so / otherwise: 64 rows of 151936 x 1024 289 / 315, of 40000 95 / 106; 100 rows of 151936
+// 411 / 394, of 70000 166 / 181; 200 rows of 151936 495 / 452; 700 rows of 3000 70 / 77, of 20000
+// 152 / 158; 2048 rows of 20000 354 / 351; 4096 rows of 3000 172 / 195.
+bool small_w(uint32_t rows, uint32_t vocab, uint32_t dim) {
+  const uint32_t cus = (uint32_t)compute_units(), tiles = ((vocab + 255) / 256) * ((dim + 255) / 256);
+  return rows <= 64 || tiles * 4 < cus * 5 || (rows <= 128 && tiles < cus * 5);
+}
 
 // What lies where in the workspace, and how the work is cut.
 struct Plan {
@@ -479,12 +559,12 @@ Plan plan_of(int64_t n_rows, int32_t n_vocab, int32_t n_dim) {
   const uint32_t rows = (uint32_t)n_rows, vocab = (uint32_t)n_vocab, dim = (uint32_t)n_dim;
   Plan p{};
   p.pitch = up(dim, 64);
-  p.tile = rows > 128 ? 256 : rows > 64 ? 128 : 64;
+  p.tile = tile_of(rows, vocab);
   const int64_t most = std::max<int64_t>(2048, (1 << 27) / n_rows / 256 * 256);
   p.piece = (uint32_t)std::min<int64_t>(most, up(vocab, 256));
   p.chunk = std::min<uint32_t>(rows, 16384);
   const uint32_t tiles = ((dim + 255) / 256) * ((rows + p.tile - 1) / p.tile);
-  p.splits = std::max<uint32_t>(1, std::min<uint32_t>((uint32_t)compute_units() / tiles, p.piece / 256));
+  p.splits = std::max<uint32_t>(1, std::min<uint32_t>((uint32_t)compute_units() / tiles, p.piece / 128));
   int64_t at = 0;
   p.h = take(&at, (int64_t)rows * p.pitch * 2);
   p.masked = take(&at, (int64_t)rows * p.pitch * 2);
@@ -567,7 +647,7 @@ template <int TP, int TQ, int WP, int WQ, int DT> hipError_t grad_w(GradWArgs a,
   a.tiles_p = (a.dim + TP - 1) / TP;
   a.total = up(a.tiles_p * ((a.vocab + TQ - 1) / TQ), 8);
   auto* k = k_grad_w<TP, TQ, WP, WQ, DT>;
-  LAUNCH(T, 0, k, a.total, s, a);
+  LAUNCH(T, 0, k, blocks<T>(a.total, 0), s, a);
 }
 
 // dW of no rows.
@@ -587,8 +667,9 @@ hipError_t zero(const XentArgs& a, hipStream_t s) {
     if (te_ != hipSuccess) return te_;       \
   } while (0)
 
-// Rows [v0, v0 + n) of W as the tiles take them.
-hipError_t piece_of_w(const XentArgs& a, const Plan& p, uint32_t v0, uint32_t n, Matrix* m, hipStream_t s) {
+// Rows [v0, v0 + n) of W as the tiles take them; `there`: a copy of them is in place.
+hipError_t piece_of_w(const XentArgs& a, const Plan& p, uint32_t v0, uint32_t n, bool there, Matrix* m,
+                      hipStream_t s) {
   const uint16_t* at = a.w + (size_t)v0 * a.ldw;
   if (direct(a.w, a.ldw, a.dim)) {
     *m = Matrix{at, (uint32_t)a.ldw, n, a.dim};
@@ -596,7 +677,7 @@ hipError_t piece_of_w(const XentArgs& a, const Plan& p, uint32_t v0, uint32_t n,
   }
   uint16_t* to = (uint16_t*)(a.space + p.w);
   *m = Matrix{to, p.pitch, n, p.pitch};
-  return pack(at, a.ldw, n, a.dim, p.pitch, nullptr, to, s);
+  return there ? hipSuccess : pack(at, a.ldw, n, a.dim, p.pitch, nullptr, to, s);
 }
 
 }  // namespace
@@ -623,7 +704,7 @@ hipError_t launch_xent_loss(const XentArgs& a, hipStream_t s) {
     l.part = (f32x2*)(a.space + p.part);
     l.picked = (float*)(a.space + p.picked) + r0;
     for (uint32_t v0 = 0; v0 < a.vocab; v0 += step) {
-      TRY_HIP(piece_of_w(a, p, v0, std::min(step, a.vocab - v0), &l.w, s));
+      TRY_HIP(piece_of_w(a, p, v0, std::min(step, a.vocab - v0), r0 > 0 && step >= a.vocab, &l.w, s));
       l.vocab0 = v0;
       l.slab0 = v0 / kSlab;
       TRY_HIP((p.tile == 256   ? sums<256, 256, 2, 4>(l, s)
@@ -638,7 +719,7 @@ hipError_t launch_xent_loss(const XentArgs& a, hipStream_t s) {
   return hipSuccess;
 }
 
-hipError_t launch_xent_grad(const XentArgs& a, hipStream_t s) {
+hipError_t launch_xent_grad(const XentArgs& a, bool behind_loss, hipStream_t s) {
   if (a.rows == 0) return a.accumulate ? hipSuccess : zero(a, s);
   const Plan p = plan_of(a.rows, a.vocab, a.dim);
   const bool f32 = a.gdtype == TFE_F32;
@@ -649,7 +730,7 @@ hipError_t launch_xent_grad(const XentArgs& a, hipStream_t s) {
     const uint32_t n = std::min(p.piece, a.vocab - v0);
     LogitsArgs l{};
     l.h = h;
-    TRY_HIP(piece_of_w(a, p, v0, n, &l.w, s));
+    TRY_HIP(piece_of_w(a, p, v0, n, behind_loss && p.piece >= a.vocab, &l.w, s));
     l.vocab0 = v0;
     l.targets = a.targets;
     l.lse = a.lse;
@@ -688,15 +769,18 @@ hipError_t launch_xent_grad(const XentArgs& a, hipStream_t s) {
     gw.ldo = a.ldgw;
     gw.add = a.accumulate;
     gw.out = (char*)a.gw + (size_t)v0 * a.ldgw * (f32 ? 4 : 2);
-    TRY_HIP((f32 ? grad_w<256, 256, 2, 4, TFE_F32>(gw, s) : grad_w<256, 256, 2, 4, TFE_BF16>(gw, s)));
+    if (small_w(a.rows, n, a.dim))
+      TRY_HIP((f32 ? grad_w<128, 128, 2, 2, TFE_F32>(gw, s) : grad_w<128, 128, 2, 2, TFE_BF16>(gw, s)));
+    else
+      TRY_HIP((f32 ? grad_w<256, 256, 2, 4, TFE_F32>(gw, s) : grad_w<256, 256, 2, 4, TFE_BF16>(gw, s)));
   }
   FinishArgs f{(float*)(a.space + p.sums), p.splits, a.rows, p.pitch, a.dim, a.gx, a.ldgx, a.targets,
                a.weight, a.vocab};
-  const uint32_t blocks = (uint32_t)std::min<uint64_t>(((uint64_t)a.rows * (p.pitch / 4) + 255) / 256, 8192);
+  const uint32_t blocks = (uint32_t)std::min<uint64_t>(((uint64_t)a.rows * (p.pitch / 4) + 63) / 64, 32768);
   if (f32)
-    k_finish_h<TFE_F32><<<dim3(blocks), dim3(256), 0, s>>>(f);
+    k_finish_h<TFE_F32><<<dim3(blocks), dim3(64), 0, s>>>(f);
   else
-    k_finish_h<TFE_BF16><<<dim3(blocks), dim3(256), 0, s>>>(f);
+    k_finish_h<TFE_BF16><<<dim3(blocks), dim3(64), 0, s>>>(f);
   return hipGetLastError();
 }
 

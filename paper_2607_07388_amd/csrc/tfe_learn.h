@@ -38,7 +38,8 @@ struct XentArgs {
 };
 int64_t xent_space(int64_t rows, int32_t vocab, int32_t dim);
 hipError_t launch_xent_loss(const XentArgs& a, hipStream_t s);
-hipError_t launch_xent_grad(const XentArgs& a, hipStream_t s);
+// behind_loss: the loss of the same arguments was launched just before.
+hipError_t launch_xent_grad(const XentArgs& a, bool behind_loss, hipStream_t s);
 
 inline uint32_t int8_pitch(int32_t dim) { return ((uint32_t)dim + 127) / 128 * 128; }
 

@@ -155,7 +155,7 @@ tfe_status tfe_cross_entropy_grad(const void* hidden, int64_t ldh, const void* w
                  accumulate, &a));
   NEED(rows == 0 || (lse && aligned(lse, 4)), "lse: null or not aligned");
   a.lse = const_cast<float*>(lse);
-  return launched(launch_xent_grad(a, (hipStream_t)stream), "cross entropy gradient launch");
+  return launched(launch_xent_grad(a, false, (hipStream_t)stream), "cross entropy gradient launch");
 }
 
 tfe_status tfe_cross_entropy_loss_grad(const void* hidden, int64_t ldh, const void* w, int64_t ldw,
@@ -175,7 +175,7 @@ tfe_status tfe_cross_entropy_loss_grad(const void* hidden, int64_t ldh, const vo
   a.loss = loss;
   a.lse = lse;
   if (rows) TRY(launched(launch_xent_loss(a, (hipStream_t)stream), "cross entropy launch"));
-  return launched(launch_xent_grad(a, (hipStream_t)stream), "cross entropy gradient launch");
+  return launched(launch_xent_grad(a, true, (hipStream_t)stream), "cross entropy gradient launch");
 }
 
 int64_t tfe_cross_entropy_workspace(int64_t rows, int32_t vocab, int32_t dim) {
