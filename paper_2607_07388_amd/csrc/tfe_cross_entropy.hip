@@ -77,10 +77,10 @@ struct PackArgs {
   uint32_t vocab;
   uint16_t* out;
 };
-__global__ __launch_bounds__(256) void k_pack(PackArgs a) {
+template <int THREADS> __device__ __forceinline__ void packed(const PackArgs& a, uint32_t block, uint32_t blocks) {
   const uint32_t per = a.pitch / 8;
   const uint64_t n = (uint64_t)a.rows * per;
-  for (uint64_t at = (uint64_t)blockIdx.x * 256 + threadIdx.x; at < n; at += (uint64_t)gridDim.x * 256) {
+  for (uint64_t at = (uint64_t)block * THREADS + threadIdx.x; at < n; at += (uint64_t)blocks * THREADS) {
     const uint32_t r = (uint32_t)(at / per), c = (uint32_t)(at - (uint64_t)r * per) * 8;
     u32x4 v{0, 0, 0, 0};
     const bool none = a.targets && ((uint32_t)a.targets[r] >= a.vocab || (a.weight && a.weight[r] == 0.f));
@@ -97,6 +97,7 @@ __global__ __launch_bounds__(256) void k_pack(PackArgs a) {
     *(u32x4*)(a.out + (size_t)r * a.pitch + c) = v;
   }
 }
+__global__ __launch_bounds__(256) void k_pack(PackArgs a) { packed<256>(a, blockIdx.x, gridDim.x); }
 
 // ---- logits: their sums, or dz -----------------------------------------------------
 
@@ -114,6 +115,7 @@ struct LogitsArgs {
   const float* weight;
   uint32_t vocab;
   Dz dz;
+  float* rest;      // what the rounding of a row's dz at its target leaves
 };
 
 // Tile t of a launch: its first column and row; false behind the last.
@@ -304,6 +306,14 @@ __global__ __launch_bounds__(WP* WQ * 64) void k_dz(LogitsArgs a) {
         for (int n = 0; n < t.NT; ++n)
 #pragma unroll
           for (int j = 0; j < 4; ++j) t.acc[n][m][j] -= at == (uint32_t)(n * 16 + j) ? 1.f : 0.f;
+        float d = 0.f;
+#pragma unroll
+        for (int n = 0; n < T::NT; ++n)
+#pragma unroll
+          for (int j = 0; j < 4; ++j) d = at == (uint32_t)(n * 16 + j) ? t.acc[n][m][j] * weight : d;
+        float e = d - (float)(__bf16)d;
+        if (PLANES == 2) e -= (float)(__bf16)e;
+        if (hit && q0 + in < a.h.rows) a.rest[q0 + in] = weight == 0.f ? 0.f : e;
       }
       // Rows without a gradient are zeros, whatever their probabilities.
       if (__builtin_amdgcn_ballot_w64(weight == 0.f)) {
@@ -332,6 +342,67 @@ __global__ __launch_bounds__(WP* WQ * 64) void k_dz(LogitsArgs a) {
 }
 
 // ---- gradients -----------------------------------------------------------------------
+
+// dz at a row's target is most of its dz (p - 1 beside small p), and its rounding most
+// of the gradients' error: 0.0027 of their norm in bfloat16, 0.0018 with what it leaves
+// (`rest`) added in float32.  For dW the rows are listed by their target's 128 columns;
+// where more than kListed rows share those, their roundings average out, and none is added.
+constexpr uint32_t kBucket = 128, kListed = 32, kMostBuckets = (1 << 18) / kBucket;
+
+struct ListArgs {
+  const int32_t* targets;
+  const float* weight;
+  uint32_t rows, vocab;
+  uint32_t* start;  // [buckets + 1]
+  uint32_t* order;  // [rows]: row numbers, a bucket's in any order
+};
+__device__ __forceinline__ void list_rows(const ListArgs& a) {
+  __shared__ uint32_t count[kMostBuckets], sums[1024];
+  const uint32_t buckets = (a.vocab + kBucket - 1) / kBucket, tid = threadIdx.x;
+  constexpr uint32_t EACH = kMostBuckets / 1024;
+  auto bucket_of = [&](uint32_t r) {
+    const uint32_t t = (uint32_t)a.targets[r];
+    return t < a.vocab && !(a.weight && a.weight[r] == 0.f) ? t / kBucket : kMostBuckets;
+  };
+  for (uint32_t b = tid; b < kMostBuckets; b += 1024) count[b] = 0;
+  __syncthreads();
+  for (uint32_t r = tid; r < a.rows; r += 1024) {
+    const uint32_t b = bucket_of(r);
+    if (b < kMostBuckets) atomicAdd(&count[b], 1u);
+  }
+  __syncthreads();
+  uint32_t mine = 0;
+  for (uint32_t k = 0; k < EACH; ++k) mine += count[tid * EACH + k];
+  sums[tid] = mine;
+  __syncthreads();
+  for (uint32_t o = 1; o < 1024; o <<= 1) {
+    const uint32_t x = tid >= o ? sums[tid - o] : 0u;
+    __syncthreads();
+    sums[tid] += x;
+    __syncthreads();
+  }
+  uint32_t at = sums[tid] - mine;
+  for (uint32_t k = 0; k < EACH; ++k) {
+    const uint32_t b = tid * EACH + k, n = count[b];
+    count[b] = at;
+    if (b <= buckets) a.start[b] = at;
+    at += n;
+  }
+  if (tid == 1023 && buckets == kMostBuckets) a.start[buckets] = at;
+  __syncthreads();
+  for (uint32_t r = tid; r < a.rows; r += 1024) {
+    const uint32_t b = bucket_of(r);
+    if (b < kMostBuckets) a.order[atomicAdd(&count[b], 1u)] = r;
+  }
+}
+
+// The rows that take part packed, and listed by the last block.
+__global__ __launch_bounds__(1024) void k_prepare(PackArgs a, ListArgs l) {
+  if (blockIdx.x + 1 == gridDim.x)
+    list_rows(l);
+  else
+    packed<1024>(a, blockIdx.x, gridDim.x - 1);
+}
 
 struct GradHArgs {
   Matrix w;  // a piece of the vocabulary
@@ -389,6 +460,9 @@ struct FinishArgs {
   const int32_t* targets;
   const float* weight;
   uint32_t vocab;
+  const float* rest;
+  const uint16_t* w;
+  int64_t ldw;
 };
 // 64 splits of 64 rows x 1024: 33 us where a thread waited for one after another.
 template <int DT> __global__ __launch_bounds__(64) void k_finish_h(FinishArgs a) {
@@ -413,11 +487,15 @@ template <int DT> __global__ __launch_bounds__(64) void k_finish_h(FinishArgs a)
 #pragma unroll
     for (int j = 0; j < 16; ++j) v += x[j];
     // 0 x an infinity of W is not a gradient of a row without one.
-    const bool none = (uint32_t)a.targets[r] >= a.vocab || (a.weight && a.weight[r] == 0.f);
+    const uint32_t target = (uint32_t)a.targets[r];
+    const bool none = target >= a.vocab || (a.weight && a.weight[r] == 0.f);
+    const float rest = none ? 0.f : a.rest[r];
+    const uint16_t* const at_w = a.w + (size_t)(none ? 0 : target) * a.ldw;
     char* out = (char*)a.out + ((size_t)r * a.ldo) * sizeof(typename rows::Elem<DT>::T);
 #pragma unroll
     for (int j = 0; j < 4; ++j)
-      if (c + j < a.dim) rows::store1<DT>(out, c + j, none ? 0.f : v[j]);
+      if (c + j < a.dim)
+        rows::store1<DT>(out, c + j, none ? 0.f : fmaf(rest, rows::load1<TFE_BF16>(at_w, c + j), v[j]));
   }
 }
 
@@ -426,6 +504,12 @@ struct GradWArgs {
   Dz dz;  // of a piece of the vocabulary
   uint32_t planes;
   uint32_t tiles_p, total, dim, vocab;  // vocab: of the piece
+  uint32_t vocab0;
+  const int32_t* targets;
+  const float* rest;
+  const uint32_t* start;
+  const uint32_t* order;
+  uint32_t buckets;
   void* out;
   int64_t ldo;
   bool add;
@@ -454,19 +538,79 @@ __global__ __launch_bounds__(WP* WQ * 64) void k_grad_w(GradWArgs a) {
   Place cur{blockIdx.x, 0, 0, 0}, nxt;
   if (!find(&cur)) return;
   constexpr int STORES = DT == TFE_F32 ? T::NT * T::MT : T::NT * T::MT / 2;
+  static_assert(TQ / WQ == 64 && kListed <= 64, "a wave's columns lie in one bucket, its rows in a wave");
   t.clear();
+  // The lane's numbers, worked out anew in each tile: kept over the steps, what follows from
+  // them would take the registers of the sums.
+  auto lane_of = [&](uint32_t* i, uint32_t* g) {
+    uint32_t own = t.lane;
+    asm volatile("" : "+v"(own));
+    *i = own & 15;
+    *g = own >> 4;
+    return own;
+  };
+  auto add_rests = [&](uint32_t p0, uint32_t q0, const char* info) {
+    uint32_t i, g;
+    const uint32_t lane = lane_of(&i, &g);
+    // Of the tile's first bucket on.
+    const uint32_t* starts = (const uint32_t*)info + (t.wq / kBucket);
+    const uint32_t from = __builtin_amdgcn_readfirstlane(starts[0]);
+    const uint32_t n = __builtin_amdgcn_readfirstlane(starts[1]) - from;
+    if (n == 0 || n > kListed) return;
+    uint32_t row = 0, target = 0;
+    float rest = 0.f;
+    if (lane < n) {
+      row = a.order[from + lane];
+      target = (uint32_t)a.targets[row];
+      rest = a.rest[row];
+    }
+    const uint32_t first = a.vocab0 + q0 + t.wq;
+    // In the order of their numbers, so that sums do not change from call to call.
+    uint32_t rank = lane < n ? 0 : lane;
+#pragma unroll 1
+    for (uint32_t k = 0; k < n; ++k)
+      rank += lane < n && (uint32_t)__builtin_amdgcn_readlane(row, k) < row;
+    row = __builtin_amdgcn_ds_permute(rank * 4, row);
+    target = __builtin_amdgcn_ds_permute(rank * 4, target);
+    rest = __int_as_float(__builtin_amdgcn_ds_permute(rank * 4, __float_as_int(rest)));
+    uint64_t mine = __builtin_amdgcn_ballot_w64(lane < n && target - first < 64u);
+    while (mine) {
+      const int l = __builtin_ctzll(mine);
+      mine &= mine - 1;
+      const uint32_t r = __builtin_amdgcn_readlane(row, l), in = __builtin_amdgcn_readlane(target, l) - first;
+      const float by = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(rest), l));
+      const uint16_t* x = a.h.at + (size_t)r * a.h.ld + p0 + t.wp + g * 4;
+      u32x2 y[T::NT];
+#pragma unroll
+      for (int n = 0; n < T::NT; ++n)
+        y[n] = p0 + t.wp + n * 16 + g * 4 < a.h.cols ? *(const u32x2*)(x + n * 16) : u32x2{0, 0};
+      // Every sum is added to, most of them 0: a choice among them would put them in memory.
+#pragma unroll
+      for (int m = 0; m < T::MT; ++m) {
+        const float f = in == (uint32_t)m * 16 + i ? by : 0.f;
+#pragma unroll
+        for (int n = 0; n < T::NT; ++n)
+#pragma unroll
+          for (int j = 0; j < 4; ++j)
+            t.acc[n][m][j] =
+                fmaf(f, __uint_as_float(j & 1 ? y[n][j / 2] & 0xFFFF0000u : y[n][j / 2] << 16), t.acc[n][m][j]);
+      }
+    }
+  };
   auto write = [&](uint32_t p0, uint32_t q0) {
+    uint32_t i, g;
+    lane_of(&i, &g);
     const bool all = p0 + TP <= a.dim && q0 + TQ <= a.vocab;
 #pragma unroll
     for (int m = 0; m < T::MT; ++m) {
-      const uint32_t v = q0 + t.wq + m * 16 + t.i;
+      const uint32_t v = q0 + t.wq + m * 16 + i;
       E* const row = (E*)a.out + (size_t)v * a.ldo + p0 + t.wp;
 #pragma unroll
       for (int n = 0; n < T::NT; n += 2) {
         if (DT == TFE_F32 || !all) {
 #pragma unroll
           for (int h = 0; h < 2; ++h) {
-            const uint32_t c = (n + h) * 16 + t.g * 4, left = a.dim - min(a.dim, p0 + t.wp + c);
+            const uint32_t c = (n + h) * 16 + g * 4, left = a.dim - min(a.dim, p0 + t.wp + c);
             f32x4 x = t.acc[n + h][m];
             if (all || (v < a.vocab && left >= 4)) {
               if constexpr (DT == TFE_F32) {
@@ -488,7 +632,7 @@ __global__ __launch_bounds__(WP* WQ * 64) void k_grad_w(GradWArgs a) {
         } else {
           // They pass by: nothing reads them soon.
           __builtin_nontemporal_store(pair_of((const float*)&t.acc[n][m], (const float*)&t.acc[n + 1][m]),
-                                      (rows::u32x4_a2*)(row + n * 16 + piece_of(t.g)));
+                                      (rows::u32x4_a2*)(row + n * 16 + piece_of(g)));
         }
       }
     }
@@ -503,10 +647,15 @@ __global__ __launch_bounds__(WP* WQ * 64) void k_grad_w(GradWArgs a) {
         if (more) *s = segment(nxt);
         return more;
       },
-      [](uint32_t) {},
-      [&](uint32_t) {
+      [&](uint32_t odd) {
+        if (t.wave == 0)
+          gemm::load_numbers(a.start, (a.vocab0 + cur.q0) / kBucket, a.buckets + 1, 0, lds + T::LDS + odd * 256);
+      },
+      [&](uint32_t odd) {
         bool stored = false;
         if (cur.plane + 1 == a.planes) {
+          add_rests(cur.p0, cur.q0, lds + T::LDS + odd * 256);
+          __builtin_amdgcn_sched_barrier(0);
           stored = write(cur.p0, cur.q0);
           t.clear();
         }
@@ -545,7 +694,7 @@ struct Plan {
   uint32_t tile;         // rows of a tile
   uint32_t log;          // dz is in blocks of 2^log = tile rows
   int64_t plane;         // its bytes, of which there are two for float32 gradients
-  int64_t h, masked, w, part, picked, dz, sums, bytes;
+  int64_t h, masked, w, part, picked, rest, start, order, dz, sums, bytes;
 };
 
 int64_t take(int64_t* at, int64_t bytes) {
@@ -571,6 +720,9 @@ Plan plan_of(int64_t n_rows, int32_t n_vocab, int32_t n_dim) {
   p.w = take(&at, (int64_t)p.piece * p.pitch * 2);
   p.part = take(&at, (int64_t)((vocab + p.piece - 1) / p.piece * p.piece / kSlab) * p.chunk * 8);
   p.picked = take(&at, (int64_t)rows * 4);
+  p.rest = take(&at, (int64_t)rows * 4);
+  p.start = take(&at, (kMostBuckets + 1) * 4);
+  p.order = take(&at, (int64_t)rows * 4);
   p.log = p.tile == 256 ? 8 : p.tile == 128 ? 7 : 6;
   p.plane = (int64_t)(up(rows, p.tile) / p.tile) * (p.piece / 64) * gemm::block_bytes(p.log);
   p.dz = take(&at, p.plane * 2);
@@ -585,9 +737,8 @@ bool direct(const void* p, int64_t ld, uint32_t dim) {
 }
 
 hipError_t pack(const uint16_t* x, int64_t ldx, uint32_t rows, uint32_t cols, uint32_t pitch,
-                const XentArgs* masked, uint16_t* out, hipStream_t s) {
-  PackArgs a{x, ldx, rows, cols, pitch, nullptr, nullptr, 0, out};
-  if (masked) a.targets = masked->targets, a.weight = masked->weight, a.vocab = masked->vocab;
+                uint16_t* out, hipStream_t s) {
+  const PackArgs a{x, ldx, rows, cols, pitch, nullptr, nullptr, 0, out};
   const uint64_t n = (uint64_t)rows * (pitch / 8);
   k_pack<<<dim3((uint32_t)std::min<uint64_t>((n + 255) / 256, 8192)), dim3(256), 0, s>>>(a);
   return hipGetLastError();
@@ -647,7 +798,7 @@ template <int TP, int TQ, int WP, int WQ, int DT> hipError_t grad_w(GradWArgs a,
   a.tiles_p = (a.dim + TP - 1) / TP;
   a.total = up(a.tiles_p * ((a.vocab + TQ - 1) / TQ), 8);
   auto* k = k_grad_w<TP, TQ, WP, WQ, DT>;
-  LAUNCH(T, 0, k, blocks<T>(a.total, 0), s, a);
+  LAUNCH(T, 512, k, blocks<T>(a.total, 512), s, a);
 }
 
 // dW of no rows.
@@ -677,7 +828,7 @@ hipError_t piece_of_w(const XentArgs& a, const Plan& p, uint32_t v0, uint32_t n,
   }
   uint16_t* to = (uint16_t*)(a.space + p.w);
   *m = Matrix{to, p.pitch, n, p.pitch};
-  return there ? hipSuccess : pack(at, a.ldw, n, a.dim, p.pitch, nullptr, to, s);
+  return there ? hipSuccess : pack(at, a.ldw, n, a.dim, p.pitch, to, s);
 }
 
 }  // namespace
@@ -691,7 +842,7 @@ hipError_t launch_xent_loss(const XentArgs& a, hipStream_t s) {
   Matrix h{a.hidden, (uint32_t)a.ldh, a.rows, a.dim};
   if (!direct(a.hidden, a.ldh, a.dim)) {
     uint16_t* to = (uint16_t*)(a.space + p.h);
-    TRY_HIP(pack(a.hidden, a.ldh, a.rows, a.dim, p.pitch, nullptr, to, s));
+    TRY_HIP(pack(a.hidden, a.ldh, a.rows, a.dim, p.pitch, to, s));
     h = Matrix{to, p.pitch, a.rows, p.pitch};
   }
   const uint32_t step = direct(a.w, a.ldw, a.dim) ? a.vocab : p.piece;
@@ -724,8 +875,12 @@ hipError_t launch_xent_grad(const XentArgs& a, bool behind_loss, hipStream_t s) 
   const Plan p = plan_of(a.rows, a.vocab, a.dim);
   const bool f32 = a.gdtype == TFE_F32;
   uint16_t* masked = (uint16_t*)(a.space + p.masked);
-  TRY_HIP(pack(a.hidden, a.ldh, a.rows, a.dim, p.pitch, &a, masked, s));
   const Matrix h{masked, p.pitch, a.rows, p.pitch};
+  const PackArgs packed{a.hidden, a.ldh, a.rows, a.dim, p.pitch, a.targets, a.weight, a.vocab, masked};
+  const ListArgs list{a.targets, a.weight, a.rows, a.vocab, (uint32_t*)(a.space + p.start), (uint32_t*)(a.space + p.order)};
+  const uint64_t pieces = ((uint64_t)a.rows * (p.pitch / 8) + 1023) / 1024;
+  k_prepare<<<dim3((uint32_t)std::min<uint64_t>(pieces, 2048) + 1), dim3(1024), 0, s>>>(packed, list);
+  TRY_HIP(hipGetLastError());
   for (uint32_t v0 = 0; v0 < a.vocab; v0 += p.piece) {
     const uint32_t n = std::min(p.piece, a.vocab - v0);
     LogitsArgs l{};
@@ -736,6 +891,7 @@ hipError_t launch_xent_grad(const XentArgs& a, bool behind_loss, hipStream_t s) 
     l.lse = a.lse;
     l.weight = a.weight;
     l.vocab = a.vocab;
+    l.rest = (float*)(a.space + p.rest);
     // Rows of whole tiles, columns of whole steps of this piece (memory: of whole tiles).
     l.dz = Dz{(uint16_t*)(a.space + p.dz), (uint64_t)p.plane / 2, p.log, p.piece / 64, up(a.rows, p.tile), up(n, 64)};
     l.h.cols = l.w.cols;  // zeros from dim on
@@ -766,6 +922,12 @@ hipError_t launch_xent_grad(const XentArgs& a, bool behind_loss, hipStream_t s) 
     gw.planes = gh.planes;
     gw.dim = a.dim;
     gw.vocab = n;
+    gw.vocab0 = v0;
+    gw.targets = a.targets;
+    gw.rest = l.rest;
+    gw.start = list.start;
+    gw.order = list.order;
+    gw.buckets = (a.vocab + kBucket - 1) / kBucket;
     gw.ldo = a.ldgw;
     gw.add = a.accumulate;
     gw.out = (char*)a.gw + (size_t)v0 * a.ldgw * (f32 ? 4 : 2);
@@ -775,7 +937,7 @@ hipError_t launch_xent_grad(const XentArgs& a, bool behind_loss, hipStream_t s) 
       TRY_HIP((f32 ? grad_w<256, 256, 2, 4, TFE_F32>(gw, s) : grad_w<256, 256, 2, 4, TFE_BF16>(gw, s)));
   }
   FinishArgs f{(float*)(a.space + p.sums), p.splits, a.rows, p.pitch, a.dim, a.gx, a.ldgx, a.targets,
-               a.weight, a.vocab};
+               a.weight, a.vocab, (const float*)(a.space + p.rest), a.w, a.ldw};
   const uint32_t blocks = (uint32_t)std::min<uint64_t>(((uint64_t)a.rows * (p.pitch / 4) + 63) / 64, 32768);
   if (f32)
     k_finish_h<TFE_F32><<<dim3(blocks), dim3(64), 0, s>>>(f);

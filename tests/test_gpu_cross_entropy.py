@@ -257,6 +257,33 @@ def test_large(rows, vocab, dim, pad, dtype):
     assert rel(got[2], want[2]) < most and rel(got[3], want[3]) < most
 
 
+@pytest.mark.parametrize("rows", [5, 100, 300])
+def test_target_roundings_are_not_lost(rows):
+    """With 3000 tokens nearly as likely as each other dz is (1 - p) at the target beside p of
+    1/3000: what its rounding leaves is added in float32.  The others' roundings, of at most 2^-8
+    of 1/sqrt(3000) of dz' norm (2^-16 for float32 gradients), are what is left beside the results'
+    own rounding (none in float32, whose sums are off by less than 2^-20)."""
+    c = Case(rows, 3000, 200, spread=0.02)
+    want = torch_oracle(c, c.g)
+    _, _, gx, gw = c.both(BF16)
+    for got, exact in ((gx, want[2]), (gw, want[3])):
+        own = rel(exact.bfloat16(), exact)
+        assert rel(got, exact) <= own + 2.0 ** -8 / 50
+    _, _, gx, gw = c.both(F32)
+    assert rel(gx, want[2]) <= 2.0 ** -16 / 50 + 2.0 ** -20 and rel(gw, want[3]) <= 2.0 ** -16 / 50 + 2.0 ** -20
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("rows,same", [(33, 1), (200, 1), (200, 3), (1000, 20), (70, 2)])
+def test_common_targets(rows, same, dtype):
+    """Few tokens are everybody's targets: more rows than are listed share a block of columns."""
+    c = Case(rows, 700, 72)
+    c.t = (c.t % same * 130 % 700).int()
+    got = c.both(dtype)
+    c.check(got, dtype)
+    assert all(torch.equal(a, b) for a, b in zip(got, c.both(dtype)))
+
+
 @pytest.mark.parametrize("rows,dtype", [(4, BF16), (64, F32), (300, BF16)])
 def test_captured_and_on_another_stream(rows, dtype):
     """Captured in a graph and replayed on inputs that change in between, and on a stream of its own."""
