@@ -196,25 +196,246 @@ __global__ __launch_bounds__(WP* WQ * 64) void k_int8_tiles(TileArgs b) {
       lds);
 }
 
+// More LDS than a kernel may have by default: told once for each device.
+template <class K> hipError_t allow(K* k, int bytes, std::atomic<uint64_t>* told) {
+  int dev = 0;
+  hipError_t e = hipGetDevice(&dev);
+  if (e != hipSuccess) return e;
+  const uint64_t bit = 1ull << (dev & 63);
+  if (dev > 63 || !(told->load(std::memory_order_relaxed) & bit)) {
+    e = hipFuncSetAttribute((const void*)k, hipFuncAttributeMaxDynamicSharedMemorySize, bytes);
+    if (e != hipSuccess) return e;
+    told->fetch_or(bit, std::memory_order_relaxed);
+  }
+  return hipSuccess;
+}
+
 template <int TP, int TQ, int WP, int WQ, int DT>
 hipError_t tiles(const Int8MatmulArgs& m, hipStream_t s) {
   typedef Tile<Int8, TP, TQ, WP, WQ, false, false, false> T;
   auto* k = k_int8_tiles<TP, TQ, WP, WQ, DT>;
   constexpr int LDS = T::LDS + 2 * (TP + TQ) * 4;
   static std::atomic<uint64_t> told{0};
-  int dev = 0;
-  hipError_t e = hipGetDevice(&dev);
+  const hipError_t e = allow(k, LDS, &told);
   if (e != hipSuccess) return e;
-  const uint64_t bit = 1ull << (dev & 63);
-  if (dev > 63 || !(told.load(std::memory_order_relaxed) & bit)) {
-    e = hipFuncSetAttribute((const void*)k, hipFuncAttributeMaxDynamicSharedMemorySize, LDS);
-    if (e != hipSuccess) return e;
-    told.fetch_or(bit, std::memory_order_relaxed);
-  }
   TileArgs a{m, (m.rows + TQ - 1) / TQ, 0};
   a.total = ((m.n + TP - 1) / TP * a.tiles_q + 7) / 8 * 8;
   k<<<dim3(std::min<uint32_t>(a.total, (compute_units() * (163840 / LDS) + 7) / 8 * 8)), dim3(T::THREADS), LDS, s>>>(a);
   return hipGetLastError();
+}
+
+// Few rows (at most 16 MT): bound by W's bytes, read once, as the other 8-bit product of few
+// rows.  The rows' codes lie in LDS, 16 bytes behind each so that the 16 rows of an operand
+// read fall on different banks; a wave takes TPW 16-row tiles of W at a time, 8 rows of
+// 128 bytes a load instruction, and keeps PC blocks of 128 columns of each in flight ahead of
+// those it multiplies.  With XDT a float type the rows are hidden states, laid out by every block
+// itself beside its first loads of W: one launch less.
+constexpr int kCodes = 2;  // XDT of rows that are laid out already
+constexpr int kSkinnyWaves = 8;
+constexpr uint32_t kTurn = 2048;  // bytes of LDS a wave turns W's tiles in
+constexpr uint32_t kSkinnyLds = 135168 + kSkinnyWaves * kTurn;
+constexpr uint32_t kPrepared = 16;  // rows that every block lays out itself
+
+struct SkinnyArgs {
+  Int8MatmulArgs m;
+  Int8QuantizeArgs x;
+};
+
+// A wave lays rows out: a lane has 8 columns of each 512, the row's first PER x 512 in registers.
+template <int DT>
+__device__ __forceinline__ void stage_row(const Int8QuantizeArgs& x, uint32_t row, uint32_t lane, char* to,
+                                          float* scale) {
+  constexpr int PER = 2;
+  const char* in = (const char*)x.x + (size_t)row * x.ldx * sizeof(typename Elem<DT>::T);
+  float f[PER][8], top = 0.f;
+  bool nan = false;
+#pragma unroll
+  for (int k = 0; k < PER; ++k) {
+    load8<DT>(in, x.dim, k * 512 + lane * 8, f[k]);
+    largest8(f[k], &top, &nan);
+  }
+  for (uint32_t c = PER * 512 + lane * 8; c < x.dim; c += 512) {
+    float g[8];
+    load8<DT>(in, x.dim, c, g);
+    largest8(g, &top, &nan);
+  }
+  top = wave_max(top);
+  nan = __builtin_amdgcn_ballot_w64(nan) != 0;
+  const bool some = top > kInt8Least;
+  const float inverse = some ? 1.f / top * 127.f : 0.f;
+#pragma unroll
+  for (int k = 0; k < PER; ++k) {
+    const uint32_t c = k * 512 + lane * 8;
+    if (c < x.pitch) *(u32x2*)(to + c) = some ? codes8(f[k], inverse) : u32x2{0, 0};
+  }
+  for (uint32_t c = PER * 512 + lane * 8; c < x.pitch; c += 512) {
+    float g[8];
+    load8<DT>(in, x.dim, c, g);
+    *(u32x2*)(to + c) = some ? codes8(g, inverse) : u32x2{0, 0};
+  }
+  if (lane == 0) *scale = nan ? NAN : some ? top / 127.f : 0.f;
+}
+
+template <int MT, int TPW, int PC, int XDT, int DT>
+__global__ __launch_bounds__(kSkinnyWaves * 64) void k_int8_skinny(SkinnyArgs b) {
+  typedef typename Elem<DT>::T E;
+  extern __shared__ __attribute__((aligned(16))) char lds[];
+  __shared__ float scales[MT * 16];
+  const Int8MatmulArgs& a = b.m;
+  const uint32_t wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const uint32_t lane = threadIdx.x & 63, i = lane & 15, g = lane >> 4;
+  const uint32_t xp = a.pitch + 16, kb = a.pitch / 128, chunks = (kb + PC - 1) / PC;
+  const uint32_t groups = (a.n + 16 * TPW - 1) / (16 * TPW);
+  const uint32_t lo = (uint32_t)((uint64_t)groups * blockIdx.x / gridDim.x);
+  const uint32_t hi = (uint32_t)((uint64_t)groups * (blockIdx.x + 1) / gridDim.x);
+  char* turn = lds + wave * kTurn;
+  char* xs = lds + kSkinnyWaves * kTurn;
+  u32x4 buf[2][TPW][PC][2];
+  f32x4 ws[2][TPW];
+  // Loads of one chunk (columns past the last block read the last again): lane l has piece
+  // l % 8 of rows l / 8 and 8 + l / 8 of a tile.
+  auto load = [&](u32x4 (&v)[TPW][PC][2], f32x4 (&w)[TPW], uint32_t grp, uint32_t ch) {
+#pragma unroll
+    for (int t = 0; t < TPW; ++t) {
+#pragma unroll
+      for (int q = 0; q < 2; ++q) {
+        const uint32_t row = (grp * TPW + t) * 16 + q * 8 + (lane >> 3);
+        const char* p = (const char*)a.w + (size_t)min(row, a.n - 1) * a.pitch + (lane & 7) * 16;
+#pragma unroll
+        for (int c = 0; c < PC; ++c)
+          v[t][c][q] = __builtin_nontemporal_load((const u32x4*)(p + min(ch * PC + c, kb - 1) * 128));
+      }
+      // The columns' scales, with their last chunk.
+      if (ch + 1 == chunks) {
+        const uint32_t n = (grp * TPW + t) * 16 + g * 4;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) w[t][j] = a.ws[min(n + j, a.n - 1)];
+      }
+    }
+  };
+  // A block of a tile in the operand's layout, by way of the wave's own 2 KB of LDS (pieces
+  // exchanged by row, so that neither side's lanes share banks).
+  const uint32_t put = (lane >> 3) * 128 + ((lane & 7) ^ (lane >> 3)) * 16;
+  const uint32_t get = i * 128 + (g ^ (i & 7)) * 16;
+  auto operand = [&](const u32x4 (&v)[2], u32x4 (&w)[2]) {
+    *(u32x4*)(turn + put) = v[0];
+    *(u32x4*)(turn + 1024 + put) = v[1];
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");  // lanes read what others wrote
+    w[0] = *(const u32x4*)(turn + get);
+    w[1] = *(const u32x4*)(turn + (get ^ 64));
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+  };
+  uint32_t grp = lo + wave;
+  if (grp < hi) load(buf[0], ws[0], grp, 0);
+  if constexpr (XDT == kCodes) {
+    const uint32_t per = a.pitch / 16;
+    for (uint32_t t = threadIdx.x; t < MT * 16 * per; t += kSkinnyWaves * 64) {
+      const uint32_t r = t / per, c = (t - r * per) * 16;
+      *(u32x4*)(xs + r * xp + c) = r < a.rows ? *(const u32x4*)(a.a + (size_t)r * a.pitch + c) : u32x4{0, 0, 0, 0};
+    }
+    if (threadIdx.x < MT * 16) scales[threadIdx.x] = threadIdx.x < a.rows ? a.as[threadIdx.x] : 0.f;
+  } else {
+    for (uint32_t r = wave; r < a.rows; r += kSkinnyWaves) stage_row<XDT>(b.x, r, lane, xs + r * xp, scales + r);
+    const uint32_t per = a.pitch / 16, from = a.rows * per;
+    for (uint32_t t = from + threadIdx.x; t < MT * 16 * per; t += kSkinnyWaves * 64)
+      *(u32x4*)(xs + t / per * xp + t % per * 16) = u32x4{0, 0, 0, 0};
+  }
+  __syncthreads();
+  i32x4 acc[TPW][MT];
+  auto multiply = [&](const u32x4 (&v)[TPW][PC][2], const f32x4 (&sw)[TPW], uint32_t grp, uint32_t ch) {
+    if (ch == 0) {
+#pragma unroll
+      for (int t = 0; t < TPW; ++t)
+#pragma unroll
+        for (int m = 0; m < MT; ++m) acc[t][m] = i32x4{0, 0, 0, 0};
+    }
+#pragma unroll
+    for (int c = 0; c < PC; ++c) {
+      const uint32_t blk = ch * PC + c;
+      if (blk >= kb) break;
+      u32x4 w[TPW][2];
+#pragma unroll
+      for (int t = 0; t < TPW; ++t) operand(v[t][c], w[t]);
+#pragma unroll
+      for (int q = 0; q < 2; ++q) {
+        u32x4 xv[MT];
+#pragma unroll
+        for (int m = 0; m < MT; ++m)
+          xv[m] = *(const u32x4*)(xs + (m * 16 + i) * xp + blk * 128 + q * 64 + g * 16);
+#pragma unroll
+        for (int t = 0; t < TPW; ++t)
+#pragma unroll
+          for (int m = 0; m < MT; ++m) acc[t][m] = gemm::multiply<Int8>(w[t][q], xv[m], acc[t][m]);
+      }
+    }
+    if (ch + 1 == chunks) {
+#pragma unroll
+      for (int t = 0; t < TPW; ++t)
+#pragma unroll
+        for (int m = 0; m < MT; ++m) {
+          const uint32_t r = m * 16 + i, n = (grp * TPW + t) * 16 + g * 4;
+          if (r >= a.rows) continue;
+          const float x = scales[r];
+          f32x4 y;
+#pragma unroll
+          for (int j = 0; j < 4; ++j) y[j] = (float)acc[t][m][j] * x * sw[t][j];
+          E* out = (E*)a.out + (size_t)r * a.ldo + n;
+          typedef f32x4 f4 __attribute__((aligned(4)));
+          typedef u32x2 u2 __attribute__((aligned(2)));
+          if (n + 4 <= a.n) {
+            if constexpr (DT == TFE_F32)
+              *(f4*)out = y;
+            else
+              *(u2*)out = u2{pack2(y[0], y[1]), pack2(y[2], y[3])};
+          } else {
+#pragma unroll
+            for (int j = 0; j < 4; ++j)
+              if (n + j < a.n) store1<DT>(out, j, y[j]);
+          }
+        }
+    }
+  };
+  uint32_t ch = 0;
+  // Two chunks a turn: the buffers stay in registers by name.
+  while (grp < hi) {
+    uint32_t ng = grp, nc = ch + 1;
+    if (nc == chunks) nc = 0, ng += kSkinnyWaves;
+    if (ng < hi) load(buf[1], ws[1], ng, nc);
+    multiply(buf[0], ws[0], grp, ch);
+    grp = ng, ch = nc;
+    if (grp >= hi) break;
+    nc = ch + 1;
+    if (nc == chunks) nc = 0, ng += kSkinnyWaves;
+    if (ng < hi) load(buf[0], ws[0], ng, nc);
+    multiply(buf[1], ws[1], grp, ch);
+    grp = ng, ch = nc;
+  }
+}
+
+uint32_t skinny_lds(const Int8MatmulArgs& a) {
+  return (a.rows + 15) / 16 * 16 * (a.pitch + 16) + kSkinnyWaves * kTurn;
+}
+bool is_skinny(const Int8MatmulArgs& a) { return a.rows <= 64 && skinny_lds(a) <= kSkinnyLds; }
+
+template <int MT, int TPW, int PC, int XDT, int DT>
+hipError_t skinny(const Int8MatmulArgs& a, const Int8QuantizeArgs& x, hipStream_t s) {
+  const uint32_t lds = skinny_lds(a), groups = (a.n + 16 * TPW - 1) / (16 * TPW);
+  auto* k = k_int8_skinny<MT, TPW, PC, XDT, DT>;
+  static std::atomic<uint64_t> told{0};
+  const hipError_t e = allow(k, (int)kSkinnyLds, &told);
+  if (e != hipSuccess) return e;
+  const uint32_t most = (uint32_t)compute_units() * (lds <= 81000 ? 2 : 1);
+  const uint32_t want = (groups + kSkinnyWaves - 1) / kSkinnyWaves;
+  k<<<dim3(std::min(most, want)), dim3(kSkinnyWaves * 64), lds, s>>>(SkinnyArgs{a, x});
+  return hipGetLastError();
+}
+template <int DT> hipError_t skinny_rows(const Int8MatmulArgs& a, hipStream_t s) {
+  switch ((a.rows + 15) / 16) {
+    case 1: return skinny<1, 1, 4, kCodes, DT>(a, Int8QuantizeArgs{}, s);
+    case 2: return skinny<2, 2, 4, kCodes, DT>(a, Int8QuantizeArgs{}, s);
+    case 3: return skinny<3, 2, 4, kCodes, DT>(a, Int8QuantizeArgs{}, s);
+    default: return skinny<4, 2, 4, kCodes, DT>(a, Int8QuantizeArgs{}, s);
+  }
 }
 
 // Tiles of 256 x 256 where they fill the device and waste few rows, of 128 x 64 where those
@@ -223,6 +444,7 @@ hipError_t tiles(const Int8MatmulArgs& m, hipStream_t s) {
 // of 151936 69 / 67 / 71, 257 87 / 84 / 90, 400 120 / 109 / 99, 600 174 / 147 / 132; 700 rows of 3000
 // 13 / 15 / 26, of 20000 30 / 31 / 32; 1024 rows of 151936 to float32 436 / 372 / 250.
 template <int DT> hipError_t matmul(const Int8MatmulArgs& a, hipStream_t s) {
+  if (is_skinny(a)) return skinny_rows<DT>(a, s);
   const uint32_t cus = (uint32_t)compute_units(), r128 = (a.rows + 127) / 128, r256 = (a.rows + 255) / 256;
   if (a.rows > 256 && (uint64_t)((a.n + 255) / 256) * r256 >= cus * 2 && r256 * 200 <= r128 * 125)
     return tiles<256, 256, 2, 4, DT>(a, s);
@@ -247,6 +469,13 @@ hipError_t launch_int8_matmul(const Int8MatmulArgs& a, int out_dtype, hipStream_
 
 hipError_t launch_int8_linear(const Int8QuantizeArgs& x, const Int8MatmulArgs& a, int dtype,
                               int out_dtype, hipStream_t s) {
+  if (a.rows <= kPrepared && is_skinny(a)) {
+    if (dtype == TFE_F32)
+      return out_dtype == TFE_F32 ? skinny<1, 1, 4, TFE_F32, TFE_F32>(a, x, s)
+                                  : skinny<1, 1, 4, TFE_F32, TFE_BF16>(a, x, s);
+    return out_dtype == TFE_F32 ? skinny<1, 1, 4, TFE_BF16, TFE_F32>(a, x, s)
+                                : skinny<1, 1, 4, TFE_BF16, TFE_BF16>(a, x, s);
+  }
   const hipError_t e = launch_int8_quantize(x, dtype, s);
   return e == hipSuccess ? launch_int8_matmul(a, out_dtype, s) : e;
 }
