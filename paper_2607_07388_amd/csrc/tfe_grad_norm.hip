@@ -215,15 +215,15 @@ template <int SLOTS> __global__ __launch_bounds__(kThreads) void k_clip(Batch<SL
           [&](const Slot& t, uint64_t at, uint64_t n) { scale<kThreads>(t, at, n, f); });
 }
 
-// Runs `go` with batches of up to SLOTS tensors that have elements.
-template <int SLOTS, class F> hipError_t batches_of(const GradArgs& a, F go) {
+// Runs `go` with batches of up to SLOTS tensors that have elements; `out`: theirs is used.
+template <int SLOTS, class F> hipError_t batches_of(const GradArgs& a, bool out, F go) {
   Batch<SLOTS> b;
   b.slots = b.units = 0;
   for (int64_t k = 0; k < a.n; ++k) {
     const tfe_grad_tensor& g = a.tensors[k];
     const uint64_t n = (uint64_t)g.rows * g.cols;
     if (n == 0) continue;
-    const bool whole = g.rows == 1 || (g.ldg == g.cols && g.ldo == g.cols);
+    const bool whole = g.rows == 1 || (g.ldg == g.cols && (!out || g.ldo == g.cols));
     b.slot[b.slots++] = Slot{(const char*)g.grad, (char*)g.out, n, b.units, whole ? 0 : (uint32_t)g.cols,
                              (uint32_t)g.ldg, (uint32_t)g.ldo, g.dtype};
     b.units += (uint32_t)((n + kUnit - 1) / kUnit);
@@ -235,8 +235,8 @@ template <int SLOTS, class F> hipError_t batches_of(const GradArgs& a, F go) {
   }
   return b.slots ? go(b) : hipSuccess;
 }
-template <class F> hipError_t batches(const GradArgs& a, F go) {
-  return a.n <= kShort ? batches_of<kShort>(a, go) : batches_of<kSlots>(a, go);
+template <class F> hipError_t batches(const GradArgs& a, bool out, F go) {
+  return a.n <= kShort ? batches_of<kShort>(a, out, go) : batches_of<kSlots>(a, out, go);
 }
 
 template <int SLOTS, bool PASS> void sums(const Batch<SLOTS>& b, uint32_t blocks, double* part, hipStream_t s) {
@@ -244,7 +244,7 @@ template <int SLOTS, bool PASS> void sums(const Batch<SLOTS>& b, uint32_t blocks
 }
 hipError_t partials(const GradArgs& a, bool pass, uint32_t* parts, hipStream_t s) {
   *parts = 0;
-  return batches(a, [&](const auto& b) {
+  return batches(a, false, [&](const auto& b) {
     const uint32_t blocks = std::min(b.units, kParts);
     double* part = (double*)a.space + *parts;
     pass ? sums<sizeof(b.slot) / sizeof(Slot), true>(b, blocks, part, s)
@@ -258,7 +258,7 @@ hipError_t join(const GradArgs& a, uint32_t parts, hipStream_t s) {
   return hipGetLastError();
 }
 hipError_t clip(const GradArgs& a, const double* part, uint32_t parts, hipStream_t s) {
-  return batches(a, [&](const auto& b) {
+  return batches(a, true, [&](const auto& b) {
     k_clip<<<dim3(std::min(b.units, kBlocks)), dim3(kThreads), 0, s>>>(
         b, ClipArgs{part, parts, a.norm, a.max_norm});
     return hipGetLastError();

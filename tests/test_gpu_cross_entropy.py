@@ -136,6 +136,22 @@ def test_loss_and_gradients(rows, vocab, dim, pad, shift, dtype):
     c.check(c.both(dtype, out_pad=pad), dtype)
 
 
+@pytest.mark.parametrize("rows,vocab", [(9, 400), (100, 3000), (300, 1000)])
+@pytest.mark.parametrize("which", ["x", "w"])
+def test_one_operand_off_its_alignment(which, rows, vocab):
+    c = Case(rows, vocab, 72)
+    want = c.both(F32)
+    rows_, cols = (rows if which == "x" else vocab), 72
+    t = device(getattr(c, which).float().cpu().numpy(), pad=3, shift=5)
+    args = list(c.head())
+    at = 0 if which == "x" else 2
+    args[at], args[at + 1] = t, cols + 3
+    loss, lse = (torch.empty(rows, device="cuda") for _ in range(2))
+    gx, gw = empty(rows, 72, F32), empty(vocab, 72, F32)
+    tfe.tfe_cross_entropy_loss_grad(*args, c.g, loss, lse, gx, 72, gw, 72, F32, 0, *c.space(), H.cur_stream())
+    assert all(torch.equal(a, b) for a, b in zip((loss, lse, gx, gw), want))
+
+
 @pytest.mark.parametrize("dtype", [F32, BF16])
 @pytest.mark.parametrize("rows,vocab,dim", [(5, 400, 33), (100, 3000, 128), (300, 1000, 64)])
 def test_parts_are_the_whole(rows, vocab, dim, dtype):
@@ -243,7 +259,7 @@ def rel(got, want):
 # More rows than sums are kept of at once; vocabularies of several pieces, also copied ones.
 @pytest.mark.parametrize("rows,vocab,dim,pad,dtype", [
     (17000, 300, 24, 0, BF16), (2100, 70001, 64, 0, F32), (2100, 70001, 63, 2, BF16), (9000, 17000, 40, 0, BF16),
-    (40, 262144, 64, 0, BF16), (1, 151936, 1024, 0, F32), (700, 151936, 128, 0, BF16)])
+    (40, 262144, 64, 0, BF16), (30000, 151936, 24, 0, BF16), (1, 151936, 1024, 0, F32), (700, 151936, 128, 0, BF16)])
 def test_large(rows, vocab, dim, pad, dtype):
     """Norms of the errors: each float32 logit is off by a few U of a sum of |x w| of about 10, so
     loss and lse by far less than 1e-5; independent roundings of dz by at most 2^-8 (2^-16) of it

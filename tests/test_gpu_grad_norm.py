@@ -191,3 +191,25 @@ def test_captured_and_on_another_stream(name):
         c2.clip(1.0)
         torch.cuda.synchronize()
         assert torch.equal(c.norm, norm) and all(torch.equal(x, y) for x, y in zip(c.outs, outs))
+
+
+def test_norm_does_not_look_at_out():
+    g = torch.randn((700, 96), device="cuda")
+    t = tfe.make_grad_tensors([(g, None, 700, 96, 96, 0, F32), (g, None, 1, 700 * 96, 0, 0, F32)])
+    size, norm = tfe.tfe_grad_workspace(t, 2), torch.zeros(1, device="cuda")
+    tfe.tfe_grad_norm(t, 2, norm, torch.empty(size, dtype=torch.uint8, device="cuda"), size, H.cur_stream())
+    want = O.grad_norm([g.cpu().numpy()] * 2)
+    assert abs(float(norm) - want) <= 2.0 ** -23 * want
+
+
+def test_more_than_2_to_the_32_elements():
+    n = (1 << 32) + 4099
+    g = torch.ones(n, dtype=torch.bfloat16, device="cuda")
+    g[-1] = 3.0
+    t = tfe.make_grad_tensors([(g, g, 1, n, n, n, BF16)])
+    size, norm = tfe.tfe_grad_workspace(t, 1), torch.zeros(1, device="cuda")
+    tfe.tfe_grad_norm_clip(t, 1, 32768.0, norm, torch.empty(size, dtype=torch.uint8, device="cuda"), size, H.cur_stream())
+    want = np.sqrt(n + 8.0)
+    assert abs(float(norm) - want) <= 2.0 ** -23 * want
+    by = O.clip_factor(float(norm), 32768.0)
+    assert (g[:-1] == torch.tensor(by).bfloat16().cuda()).all() and g[-1] == torch.tensor(by * np.float32(3)).bfloat16()

@@ -194,3 +194,15 @@ def test_large(rows, n, dim, out_dtype):
     want = (torch.mm(a.double(), w.double().t().contiguous()) * asc.double()[:, None]).mul_(wsc.double())
     off = (out.double() - want).abs_()
     assert (off <= (4 * 2.0 ** -24 + (2.0 ** -8 if out_dtype == BF16 else 0)) * want.abs_()).all()
+
+
+def test_more_than_2_to_the_32_results():
+    rows, n, dim = 30000, 151936, 128
+    g = torch.Generator(device="cuda").manual_seed(1)
+    a, w = (torch.randint(-127, 128, (k, dim), generator=g, device="cuda").to(torch.int8) for k in (rows, n))
+    asc, wsc = (torch.rand(k, generator=g, device="cuda") + 0.5 for k in (rows, n))
+    out = torch.full((rows, n), -7.0, dtype=torch.bfloat16, device="cuda")
+    tfe.tfe_integer_matmul(a, asc, w, wsc, rows, n, dim, out, BF16, n, H.cur_stream())
+    for at in (0, 14000, 28250, 29900):
+        want = torch.mm(a[at:at + 100].double(), w.double().t().contiguous()) * asc[at:at + 100, None].double() * wsc.double()
+        assert ((out[at:at + 100].double() - want).abs() <= (4 * 2.0 ** -24 + 2.0 ** -8) * want.abs()).all()
