@@ -212,6 +212,24 @@ __device__ __forceinline__ void load_numbers(const void* array, uint32_t first, 
 #endif
 }
 
+// Asks for a share of `rows` rows of `len` bytes that blocks of this XCD read soon, so that
+// they are in its L2 by then: a number of each 128 bytes, into 256 bytes of LDS that nobody
+// reads.  Thread t of THREADS of share `part` of `parts`; more than a number a thread: none.
+template <int THREADS>
+__device__ __forceinline__ void warm(const Operand& o, uint32_t most, uint32_t len, uint32_t part, uint32_t parts,
+                                     char* to) {
+#if defined(__HIP_DEVICE_COMPILE__)
+  typedef __attribute__((address_space(3))) void* Lds;
+  const uint32_t lines = (len + 127) / 128, rows = min(o.rows, most), all = rows * lines;
+  if (all > parts * THREADS) return;
+  const uint32_t line = part * THREADS + threadIdx.x, row = line / lines;
+  const int bytes = __builtin_amdgcn_readfirstlane(rows ? (int)((rows - 1) * o.pitch + len) : 0);
+  const auto d = __builtin_amdgcn_make_buffer_rsrc((void*)o.at, 0, bytes, 0x00020000);
+  const uint32_t at = line < all ? row * o.pitch + (line - row * lines) * 128 : 0x70000000u;
+  __builtin_amdgcn_raw_ptr_buffer_load_lds(d, (Lds)to, 4, (int)at, 0, 0, 0);
+#endif
+}
+
 // Steps [s0, s1) of a tile's operands.
 struct Segment {
   Operand p, q;

@@ -124,6 +124,7 @@ __global__ __launch_bounds__(WP* WQ * 64) void k_int8_tiles(TileArgs b) {
                          a.pitch / gemm::kStep};
   };
   uint32_t at = blockIdx.x, p0, q0, np0 = 0, nq0 = 0;
+  bool more = true;
   if (!find(at, &p0, &q0)) return;
   t.clear();
   // The rows' scales, then the columns'.
@@ -165,7 +166,7 @@ __global__ __launch_bounds__(WP* WQ * 64) void k_int8_tiles(TileArgs b) {
           }
         } else {
           E* out = (E*)a.out + (size_t)r * a.ldo + p0 + t.wp + n * 16 + piece_of(t.g);
-          // Passed by, these stores took 373 us of 2048 rows of 151936 x 1024 to 334.
+          // They pass by (2048 rows of 151936 x 1024 on one input over and over: 373 us, 334 so).
           __builtin_nontemporal_store(pair_of((const float*)&v[0], (const float*)&v[1]), (u32x4_a2*)out);
         }
       }
@@ -176,7 +177,7 @@ __global__ __launch_bounds__(WP* WQ * 64) void k_int8_tiles(TileArgs b) {
       segment(p0, q0),
       [&](gemm::Segment* s) {
         at += gridDim.x;
-        const bool more = find(at, &np0, &nq0);
+        more = find(at, &np0, &nq0);
         if (more) *s = segment(np0, nq0);
         return more;
       },
@@ -185,6 +186,11 @@ __global__ __launch_bounds__(WP* WQ * 64) void k_int8_tiles(TileArgs b) {
         static_assert(TP / 64 <= T::WAVES && TQ / 64 <= T::WAVES, "a wave for each 64 scales");
         if (t.wave < TQ / 64) gemm::load_numbers(a.as, q0, a.rows, t.wave, to);
         if (t.wave < TP / 64) gemm::load_numbers(a.ws, p0, a.n, t.wave, to + TQ * 4);
+        // The next tile's part of W: its row tiles' blocks share it out.  A tile's steps are few,
+        // and each waits for W's first reader: 2048 rows of 151936 x 1024 450 us without, 388 so.
+        if (T::LARGE && more && np0 != p0)
+          gemm::warm<T::THREADS>(segment(np0, nq0).p, TP, a.pitch, nq0 / TQ, b.tiles_q,
+                                 lds + T::LDS + 2 * INFO + t.wave * 256);
       },
       [&](uint32_t odd) {
         const bool stored = write(lds + T::LDS + odd * INFO);
@@ -214,7 +220,7 @@ template <int TP, int TQ, int WP, int WQ, int DT>
 hipError_t tiles(const Int8MatmulArgs& m, hipStream_t s) {
   typedef Tile<Int8, TP, TQ, WP, WQ, false, false, false> T;
   auto* k = k_int8_tiles<TP, TQ, WP, WQ, DT>;
-  constexpr int LDS = T::LDS + 2 * (TP + TQ) * 4;
+  constexpr int LDS = T::LDS + 2 * (TP + TQ) * 4 + (T::LARGE ? T::WAVES * 256 : 0);
   static std::atomic<uint64_t> told{0};
   const hipError_t e = allow(k, LDS, &told);
   if (e != hipSuccess) return e;
