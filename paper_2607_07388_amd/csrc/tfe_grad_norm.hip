@@ -18,27 +18,40 @@ constexpr uint32_t kUnit = 1024;    // elements; a tensor begins a unit of its o
 constexpr uint32_t kBlocks = 2048;  // of a launch at most
 constexpr uint32_t kParts = 1024;   // of a launch of sums: a partial sum each
 constexpr uint32_t kMostUnits = 1u << 30;  // of a launch, but for its last tensor
-constexpr int kSlots = 80;          // tensors of a launch: its arguments stay below 4 KB
+constexpr int kSlots = 160;         // tensors of a launch: its arguments stay below 4 KB
+constexpr int kPitches = 16;        // of them with rows apart
 constexpr int kDeep = 8;            // vectors of a thread under way
 
-// A tensor of a launch; cols 0: its elements lie one behind the other.
+// A tensor of a launch, in 24 bytes: its elements are kUnit for each of its units but the last,
+// and bits % 1024 + 1 there; then its dtype; then 0, or 1 + the place of its pitches.
 struct Slot {
   const char* grad;
   char* out;
-  uint64_t n;
   uint32_t first;  // its first unit
+  uint32_t bits;
+};
+struct Pitch {
   uint32_t cols, ldg, ldo;
-  int32_t dtype;
 };
 template <int SLOTS> struct Batch {
   Slot slot[SLOTS];
-  uint32_t slots, units;
+  Pitch pitch[kPitches];
+  uint32_t slots, units, pitches;
+};
+static_assert(sizeof(Batch<kSlots>) <= 4064, "a launch's arguments, with the others");
+// The same as a run is worked on; cols 0: its elements lie one behind the other.
+struct Tensor {
+  const char* grad;
+  char* out;
+  uint64_t n;
+  uint32_t cols, ldg, ldo;
+  int32_t dtype;
 };
 // A launch's arguments are copied by the host: few tensors have short ones.
 constexpr int kShort = 16;
 
-// The last slot whose first unit is not behind `unit`: all are looked at by one load, or
-// two, where a search would wait for one after another.
+// The last slot whose first unit is not behind `unit`: all are looked at by one to three
+// loads, where a search would wait for one after another.
 template <int SLOTS> __device__ __forceinline__ uint32_t find(const Batch<SLOTS>& b, uint32_t unit) {
   const uint32_t lane = threadIdx.x & 63;
   uint32_t n = 0;
@@ -52,14 +65,24 @@ template <int SLOTS> __device__ __forceinline__ uint32_t find(const Batch<SLOTS>
 }
 // Element i of a tensor in its memory.
 __device__ __forceinline__ uint64_t place(uint64_t i, uint32_t cols, uint32_t ld) {
-  return cols ? i / cols * ld + i % cols : i;
+  if (!cols) return i;
+  if (i >> 32 == 0) {  // the 64-bit quotient is a long one
+    const uint32_t row = (uint32_t)i / cols;
+    return (uint64_t)row * ld + ((uint32_t)i - row * cols);
+  }
+  const uint64_t row = i / cols;
+  return row * ld + (i - row * cols);
 }
 // The units [u0, u1) as runs of one tensor's elements [at, at + n).
 template <int SLOTS, class F> __device__ __forceinline__ void runs(const Batch<SLOTS>& b, uint32_t u0, uint32_t u1, F go) {
   for (uint32_t k = find(b, u0); u0 < u1; ++k) {
-    const Slot& t = b.slot[k];
-    const uint32_t end = k + 1 < b.slots ? min(u1, b.slot[k + 1].first) : u1;
-    const uint64_t at = (uint64_t)(u0 - t.first) * kUnit;
+    const Slot& x = b.slot[k];
+    const uint32_t behind = k + 1 < b.slots ? b.slot[k + 1].first : b.units, end = min(u1, behind);
+    const uint64_t at = (uint64_t)(u0 - x.first) * kUnit;
+    const uint32_t apart = x.bits >> 11;
+    const Pitch p = apart ? b.pitch[apart - 1] : Pitch{0, 0, 0};
+    const Tensor t{x.grad, x.out, (uint64_t)(behind - x.first - 1) * kUnit + (x.bits & (kUnit - 1)) + 1,
+                   p.cols, p.ldg, p.ldo, (int32_t)(x.bits >> 10 & 1)};
     go(t, at, min((uint64_t)(end - u0) * kUnit, t.n - at));
     u0 = end;
   }
@@ -105,7 +128,7 @@ __device__ __forceinline__ uint64_t vectors(const char* p, uint64_t n, F go) {
 
 // Squares are summed in float64: neither large nor small gradients leave its range.
 template <int DT, int THREADS, bool PASS>
-__device__ __forceinline__ double squares(const Slot& t, uint64_t at, uint64_t n) {
+__device__ __forceinline__ double squares(const Tensor& t, uint64_t at, uint64_t n) {
   constexpr uint32_t N = Elem<DT>::N;
   double sum = 0, sum2 = 0;
   uint32_t head = 0;
@@ -122,6 +145,14 @@ __device__ __forceinline__ double squares(const Slot& t, uint64_t at, uint64_t n
         sum2 += (double)f[j + 1] * f[j + 1];
       }
     });
+  } else if (t.cols % N == 0) {  // whole vectors in a row
+    from = n;
+    for (uint64_t e = threadIdx.x * N; e < n; e += THREADS * N) {
+      float f[N];
+      unpack<DT>(load_vec<DT>(t.grad + place(at + e, t.cols, t.ldg) * sizeof(typename Elem<DT>::T), 0), f);
+#pragma unroll
+      for (uint32_t j = 0; j < N; ++j) sum += (double)f[j] * f[j];
+    }
   }
   // What the vectors leave, at either end.
   for (uint64_t i = threadIdx.x; i < n - from; i += THREADS) {
@@ -132,7 +163,7 @@ __device__ __forceinline__ double squares(const Slot& t, uint64_t at, uint64_t n
   return sum + sum2;
 }
 template <int THREADS, bool PASS>
-__device__ __forceinline__ double squares(const Slot& t, uint64_t at, uint64_t n) {
+__device__ __forceinline__ double squares(const Tensor& t, uint64_t at, uint64_t n) {
   return t.dtype == TFE_F32 ? squares<TFE_F32, THREADS, PASS>(t, at, n)
                             : squares<TFE_BF16, THREADS, PASS>(t, at, n);
 }
@@ -142,7 +173,7 @@ template <int SLOTS, bool PASS>
 __global__ __launch_bounds__(kThreads) void k_squares(Batch<SLOTS> b, double* part) {
   __shared__ double red[kThreads / 64];
   double sum = 0;
-  part_of(b, blockIdx.x, [&](const Slot& t, uint64_t at, uint64_t n) { sum += squares<kThreads, PASS>(t, at, n); });
+  part_of(b, blockIdx.x, [&](const Tensor& t, uint64_t at, uint64_t n) { sum += squares<kThreads, PASS>(t, at, n); });
   sum = block_add<double, kThreads>(sum, red);
   if (threadIdx.x == 0) part[blockIdx.x] = sum;
 }
@@ -160,7 +191,7 @@ __global__ __launch_bounds__(kThreads) void k_norm(const double* part, uint32_t 
 }
 
 template <int DT, int THREADS>
-__device__ __forceinline__ void scale(const Slot& t, uint64_t at, uint64_t n, float by) {
+__device__ __forceinline__ void scale(const Tensor& t, uint64_t at, uint64_t n, float by) {
   constexpr uint32_t N = Elem<DT>::N;
   uint32_t head = 0;
   uint64_t from = 0;
@@ -175,6 +206,16 @@ __device__ __forceinline__ void scale(const Slot& t, uint64_t at, uint64_t n, fl
       for (uint32_t j = 0; j < N; ++j) f[j] *= by;
       __builtin_nontemporal_store(pack<DT>(f), (typename Elem<DT>::V*)(o + v * 16));
     });
+  } else if (t.cols % N == 0) {
+    constexpr size_t SIZE = sizeof(typename Elem<DT>::T);
+    from = n;
+    for (uint64_t e = threadIdx.x * N; e < n; e += THREADS * N) {
+      float f[N];
+      unpack<DT>(load_vec<DT>(t.grad + place(at + e, t.cols, t.ldg) * SIZE, 0), f);
+#pragma unroll
+      for (uint32_t j = 0; j < N; ++j) f[j] *= by;
+      store_vec<DT>(t.out + place(at + e, t.cols, t.ldo) * SIZE, 0, pack<DT>(f));
+    }
   }
   for (uint64_t i = threadIdx.x; i < n - from; i += THREADS) {
     const uint64_t e = i < head ? i : from + i;
@@ -190,7 +231,7 @@ __device__ __forceinline__ Factor factor_of(float norm, float max_norm) {
   return Factor{clip, clip ? max_norm / norm : 1.f};
 }
 template <int THREADS>
-__device__ __forceinline__ void scale(const Slot& t, uint64_t at, uint64_t n, Factor f) {
+__device__ __forceinline__ void scale(const Tensor& t, uint64_t at, uint64_t n, Factor f) {
   if (!f.clip && t.grad == t.out) return;
   if (t.dtype == TFE_F32)
     scale<TFE_F32, THREADS>(t, at, n, f.by);
@@ -212,25 +253,26 @@ template <int SLOTS> __global__ __launch_bounds__(kThreads) void k_clip(Batch<SL
   const Factor f = factor_of(norm, a.max_norm);
   // What was read last is read first: it is still in the cache.
   part_of(b, gridDim.x - 1 - blockIdx.x,
-          [&](const Slot& t, uint64_t at, uint64_t n) { scale<kThreads>(t, at, n, f); });
+          [&](const Tensor& t, uint64_t at, uint64_t n) { scale<kThreads>(t, at, n, f); });
 }
 
 // Runs `go` with batches of up to SLOTS tensors that have elements; `out`: theirs is used.
 template <int SLOTS, class F> hipError_t batches_of(const GradArgs& a, bool out, F go) {
   Batch<SLOTS> b;
-  b.slots = b.units = 0;
+  b.slots = b.units = b.pitches = 0;
   for (int64_t k = 0; k < a.n; ++k) {
     const tfe_grad_tensor& g = a.tensors[k];
     const uint64_t n = (uint64_t)g.rows * g.cols;
     if (n == 0) continue;
     const bool whole = g.rows == 1 || (g.ldg == g.cols && (!out || g.ldo == g.cols));
-    b.slot[b.slots++] = Slot{(const char*)g.grad, (char*)g.out, n, b.units, whole ? 0 : (uint32_t)g.cols,
-                             (uint32_t)g.ldg, (uint32_t)g.ldo, g.dtype};
+    if (!whole) b.pitch[b.pitches++] = Pitch{(uint32_t)g.cols, (uint32_t)g.ldg, (uint32_t)g.ldo};
+    b.slot[b.slots++] = Slot{(const char*)g.grad, (char*)g.out, b.units,
+                             (uint32_t)((n - 1) % kUnit) | (uint32_t)g.dtype << 10 | (whole ? 0 : b.pitches) << 11};
     b.units += (uint32_t)((n + kUnit - 1) / kUnit);
-    if (b.slots == SLOTS || b.units >= kMostUnits) {
+    if (b.slots == SLOTS || b.pitches == kPitches || b.units >= kMostUnits) {
       const hipError_t e = go(b);
       if (e != hipSuccess) return e;
-      b.slots = b.units = 0;
+      b.slots = b.units = b.pitches = 0;
     }
   }
   return b.slots ? go(b) : hipSuccess;
@@ -267,11 +309,15 @@ hipError_t clip(const GradArgs& a, const double* part, uint32_t parts, hipStream
 
 }  // namespace
 
-// A launch's sums, for each kSlots tensors and for each kMostUnits units.
+// Sums of as many launches as there can be: each but the last has kSlots tensors (kShort of
+// few), kPitches with rows apart or kMostUnits units.
 int64_t grad_space(const tfe_grad_tensor* t, int64_t n) {
-  int64_t units = 0;
-  for (int64_t k = 0; k < n; ++k) units += (int64_t)(((uint64_t)t[k].rows * t[k].cols + kUnit - 1) / kUnit);
-  return ((n + kSlots - 1) / kSlots + units / kMostUnits) * (int64_t)kParts * 8;
+  int64_t units = 0, apart = 0;
+  for (int64_t k = 0; k < n; ++k) {
+    units += (int64_t)(((uint64_t)t[k].rows * t[k].cols + kUnit - 1) / kUnit);
+    apart += t[k].rows > 1;
+  }
+  return ((n + kSlots - 1) / kSlots + apart / kPitches + units / kMostUnits) * (int64_t)kParts * 8;
 }
 
 hipError_t launch_grad_norm(const GradArgs& a, hipStream_t s) {

@@ -213,3 +213,12 @@ def test_more_than_2_to_the_32_elements():
     assert abs(float(norm) - want) <= 2.0 ** -23 * want
     by = O.clip_factor(float(norm), 32768.0)
     assert (g[:-1] == torch.tensor(by).bfloat16().cuda()).all() and g[-1] == torch.tensor(by * np.float32(3)).bfloat16()
+
+
+@pytest.mark.parametrize("place", [False, True])
+def test_more_tensors_with_rows_apart_than_a_launch_has(place):
+    shapes = [(2 + k % 3, 3 + k % 7, 1 + k % 4, k % 3, k % 2) for k in range(50)] + [(1, 1024 * k, 0, 0, F32) for k in (1, 2)]
+    g = Grads(shapes, place=place)
+    seen = g.seen()
+    g.clip(0.9)
+    g.check(seen, 0.9)
