@@ -486,13 +486,19 @@ int64_t tfe_distill_workspace(int64_t rows, int32_t vocab); /* -1: bad size */
  *               pitches ldgh and ldgw; apart from each other and every input.
  *               Sums are float32.  For TFE_BF16 results dz is rounded to
  *               bfloat16 before the products with W and H, for TFE_F32 ones to
- *               the sum of two bfloat16 numbers (17 bits), at twice the products.
+ *               the sum of two bfloat16 numbers (16 bits), at twice the products;
+ *               what that leaves of dz at a row's target is added in float32
+ *               (to grad_w where at most 32 rows have theirs among the same 128
+ *               tokens, counted from 0).
  *   accumulate  not 0: grad_w (TFE_F32 only) is added to, not written.
  * A row with a logit of +infinity or NaN has a loss and gradients that are NaN,
  * and grad_w with it.  Results do not change from call to call.
  * tfe_cross_entropy_grad takes lse as tfe_cross_entropy_loss wrote it.
  * Pointers 16-byte aligned, with pitches and dim multiples of 8 (and pitches up
- * to 2^21), are read in place; others are copied in pieces first.
+ * to 2^21), are read in place; others are copied in pieces first.  With no rows
+ * grad_w becomes 0 (accumulate: stays).  The workspace is for a piece of the
+ * vocabulary at a time: about 4 bytes for each of its numbers of dz (2^27 at most, or
+ * 2048 a row), a copy of its rows of W, and 12 to 24 bytes a number of hidden.
  * 1 <= vocab <= 2^18, 1 <= dim <= 16384, rows <= 2^20. */
 tfe_status tfe_cross_entropy_loss(const void *hidden, int64_t ldh, const void *w, int64_t ldw,
                                   const int32_t *targets, int64_t rows, int32_t vocab,

@@ -101,6 +101,13 @@ __global__ __launch_bounds__(256) void k_pack(PackArgs a) { packed<256>(a, block
 
 // ---- logits: their sums, or dz -----------------------------------------------------
 
+// Bound by the matrix cores, which the products keep 59 to 62% busy (a wave's registers hold
+// 128 x 64 sums: a larger tile does not fit, and each step reads 192 KB of LDS), and by what
+// follows a tile's products: exponentials (16 cycles a wave) beside maxima and sums, and dz's
+// stores.  4096 rows of 151936 x 1024 on one input over and over: sums 1060 us (1.2 PFLOP/s; 840
+// without what follows the products), dz of 32768 columns 265 (195).  Few rows: bound by W's
+// bytes, 64 rows 53 to 61 us for 311 MB.
+
 struct LogitsArgs {
   Matrix w, h;      // h: the rows of this launch
   uint32_t tiles_q, total;
@@ -404,6 +411,11 @@ __global__ __launch_bounds__(1024) void k_prepare(PackArgs a, ListArgs l) {
     packed<1024>(a, blockIdx.x, gridDim.x - 1);
 }
 
+// dH = dz W over a piece of the vocabulary, cut along it where the tiles are few (the parts are
+// joined by k_finish_h, in float32), and dW = dz^T H.  k runs across W, H, and for dW dz: such
+// operands are turned by the LDS reads (ds_read_b64_tr_b16: four k of 16 columns a lane row).
+// Bound by the matrix cores and the loads beside them; 4096 rows x 32768 columns x 1024: dH 235 us,
+// dW 250 (1.1 PFLOP/s; 165 and 170 where nothing was loaded).  Few rows: dW by its stores.
 struct GradHArgs {
   Matrix w;  // a piece of the vocabulary
   Dz dz;
@@ -667,7 +679,7 @@ __global__ __launch_bounds__(WP* WQ * 64) void k_grad_w(GradWArgs a) {
 
 // ---- launches ------------------------------------------------------------------------
 
-// Rows of a tile of logits.  Loss and gradients in us with tiles of 64 / 128 / 256 rows
+// Rows of a tile of logits (the first rule that holds).  Loss and gradients in us with tiles of 64 / 128 / 256 rows
 // (and 128 / 256 / 256 columns), dim 1024: 100 rows of vocabulary 3001 48 / 73 / 78, of 70000
 // 166 / 194 / 190, of 151936 429 / 394 / 421; 200 rows of 20000 97 / 103 / 108, of 151936
 // 647 / 549 / 452; 700 rows of 3000 70 / 90 / 98, of 20000 211 / 191 / 152.
@@ -709,7 +721,7 @@ Plan plan_of(int64_t n_rows, int32_t n_vocab, int32_t n_dim) {
   Plan p{};
   p.pitch = up(dim, 64);
   p.tile = tile_of(rows, vocab);
-  const int64_t most = std::max<int64_t>(2048, (1 << 27) / n_rows / 256 * 256);
+  const int64_t most = std::max<int64_t>(4096, (1 << 27) / n_rows / 256 * 256);
   p.piece = (uint32_t)std::min<int64_t>(most, up(vocab, 256));
   p.chunk = std::min<uint32_t>(rows, 16384);
   const uint32_t tiles = ((dim + 255) / 256) * ((rows + p.tile - 1) / p.tile);
