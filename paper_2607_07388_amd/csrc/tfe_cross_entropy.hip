@@ -101,8 +101,9 @@ __global__ __launch_bounds__(256) void k_pack(PackArgs a) { packed<256>(a, block
 
 // ---- logits: their sums, or dz -----------------------------------------------------
 
-// Bound by the matrix cores, which the products keep 59 to 62% busy (a wave's registers hold
-// 128 x 64 sums: a larger tile does not fit, and each step reads 192 KB of LDS), and by what
+// Bound by the matrix cores, which k_sums keeps 66% busy and the gradients' products 54 to 56%
+// (a wave's registers hold 128 x 64 sums: a larger tile does not fit, and each step reads 192 KB
+// of LDS), and by what
 // follows a tile's products: exponentials (16 cycles a wave) beside maxima and sums, and dz's
 // stores.  4096 rows of 151936 x 1024 on one input over and over: sums 1060 us (1.2 PFLOP/s; 840
 // without what follows the products), dz of 32768 columns 265 (195).  Few rows: bound by W's
@@ -351,10 +352,15 @@ __global__ __launch_bounds__(WP* WQ * 64) void k_dz(LogitsArgs a) {
 // ---- gradients -----------------------------------------------------------------------
 
 // dz at a row's target is most of its dz (p - 1 beside small p), and its rounding most
-// of the gradients' error: 0.0027 of their norm in bfloat16, 0.0018 with what it leaves
+// of the gradients' error: up to 0.0027 of their norm in bfloat16, 0.0017 with what it leaves
 // (`rest`) added in float32.  For dW the rows are listed by their target's 128 columns;
-// where more than kListed rows share those, their roundings average out, and none is added.
-constexpr uint32_t kBucket = 128, kListed = 32, kMostBuckets = (1 << 18) / kBucket;
+// where more than kListed rows share those, none is added, and dW's rows of the tokens there
+// keep that error: 0.0024 of their norm beside 0.00166 in the others, which is bfloat16's own
+// rounding, and 0.0018 over all of dW (4096 rows whose targets are drawn as text has them, 4 or 5
+// of 1187 lists too long, the commonest token the target of 209 to 222 rows).  With lists of 32
+// rows dW's was 0.00184, and the call 0.4% faster.  Longer lists took the registers of the sums:
+// 985 us a launch instead of 250.
+constexpr uint32_t kBucket = 128, kListed = 64, kMostBuckets = (1 << 18) / kBucket;
 
 struct ListArgs {
   const int32_t* targets;

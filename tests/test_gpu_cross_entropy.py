@@ -290,7 +290,7 @@ def test_target_roundings_are_not_lost(rows):
 
 
 @pytest.mark.parametrize("dtype", [F32, BF16])
-@pytest.mark.parametrize("rows,same", [(33, 1), (200, 1), (200, 3), (1000, 20), (70, 2)])
+@pytest.mark.parametrize("rows,same", [(33, 1), (64, 1), (66, 1), (80, 1), (200, 1), (200, 3), (1000, 20), (70, 2)])
 def test_common_targets(rows, same, dtype):
     """Few tokens are everybody's targets: more rows than are listed share a block of columns."""
     c = Case(rows, 700, 72)
