@@ -488,10 +488,8 @@ int64_t tfe_distill_workspace(int64_t rows, int32_t vocab); /* -1: bad size */
  *               bfloat16 before the products with W and H, for TFE_F32 ones to
  *               the sum of two bfloat16 numbers (16 bits), at twice the products;
  *               what that leaves of dz at a row's target is added in float32
- *               (to grad_w where at most 64 rows have theirs among the same 128
- *               tokens, counted from 0: for TFE_BF16, grad_w's rows of other
- *               targets are off by 0.0024 of their norm where these are by
- *               0.0017, on 4096 rows).
+ *               (to grad_w where more than 64 rows have theirs among the same 128
+ *               tokens, counted from 0: summed by token, rounded to bfloat16).
  *   accumulate  not 0: grad_w (TFE_F32 only) is added to, not written.
  * A row with a logit of +infinity or NaN has a loss and gradients that are NaN,
  * and grad_w with it.  Results do not change from call to call.

@@ -353,13 +353,9 @@ __global__ __launch_bounds__(WP* WQ * 64) void k_dz(LogitsArgs a) {
 
 // dz at a row's target is most of its dz (p - 1 beside small p), and its rounding most
 // of the gradients' error: up to 0.0027 of their norm in bfloat16, 0.0017 with what it leaves
-// (`rest`) added in float32.  For dW the rows are listed by their target's 128 columns;
-// where more than kListed rows share those, none is added, and dW's rows of the tokens there
-// keep that error: 0.0024 of their norm beside 0.00166 in the others, which is bfloat16's own
-// rounding, and 0.0018 over all of dW (4096 rows whose targets are drawn as text has them, 4 or 5
-// of 1187 lists too long, the commonest token the target of 209 to 222 rows).  With lists of 32
-// rows dW's was 0.00184, and the call 0.4% faster.  Longer lists took the registers of the sums:
-// 985 us a launch instead of 250.
+// (`rest`) added in float32.  For dW the rows are listed by their target's 128 columns, in
+// their order.  Up to kListed rows of a list are added one by one; of longer lists those of
+// each token are summed by k_rests before: a row more of the product for each token.
 constexpr uint32_t kBucket = 128, kListed = 64, kMostBuckets = (1 << 18) / kBucket;
 
 struct ListArgs {
@@ -367,54 +363,155 @@ struct ListArgs {
   const float* weight;
   uint32_t rows, vocab;
   uint32_t* start;  // [buckets + 1]
-  uint32_t* order;  // [rows]: row numbers, a bucket's in any order
+  uint32_t* order;  // [rows]: row numbers, a bucket's in their order
 };
-__device__ __forceinline__ void list_rows(const ListArgs& a) {
-  __shared__ uint32_t count[kMostBuckets], sums[1024];
-  const uint32_t buckets = (a.vocab + kBucket - 1) / kBucket, tid = threadIdx.x;
-  constexpr uint32_t EACH = kMostBuckets / 1024;
+// Each wave lists a run of the rows, with counts of its own: [waves][buckets].
+constexpr uint32_t kListers = 16;
+__device__ __forceinline__ void list_rows(const ListArgs& a, uint32_t* count) {
+  __shared__ uint32_t sums[kListers * 64];
+  const uint32_t buckets = (a.vocab + kBucket - 1) / kBucket, tid = threadIdx.x, lane = tid & 63;
+  constexpr uint32_t EACH = kMostBuckets / (kListers * 64);
+  uint32_t* const own = count + tid / 64 * buckets;
+  const uint32_t run = (a.rows + kListers * 64 - 1) / (kListers * 64) * 64;
+  const uint32_t r0 = min(tid / 64 * run, a.rows), r1 = min(r0 + run, a.rows);
   auto bucket_of = [&](uint32_t r) {
     const uint32_t t = (uint32_t)a.targets[r];
     return t < a.vocab && !(a.weight && a.weight[r] == 0.f) ? t / kBucket : kMostBuckets;
   };
-  for (uint32_t b = tid; b < kMostBuckets; b += 1024) count[b] = 0;
+  for (uint32_t k = tid; k < kListers * buckets; k += kListers * 64) count[k] = 0;
   __syncthreads();
-  for (uint32_t r = tid; r < a.rows; r += 1024) {
+  for (uint32_t r = r0 + lane; r < r1; r += 64) {
     const uint32_t b = bucket_of(r);
-    if (b < kMostBuckets) atomicAdd(&count[b], 1u);
+    if (b < kMostBuckets) atomicAdd(&own[b], 1u);
   }
   __syncthreads();
   uint32_t mine = 0;
-  for (uint32_t k = 0; k < EACH; ++k) mine += count[tid * EACH + k];
+  for (uint32_t b = tid * EACH; b < min((tid + 1) * EACH, buckets); ++b)
+    for (uint32_t w = 0; w < kListers; ++w) mine += count[w * buckets + b];
   sums[tid] = mine;
   __syncthreads();
-  for (uint32_t o = 1; o < 1024; o <<= 1) {
+  for (uint32_t o = 1; o < kListers * 64; o <<= 1) {
     const uint32_t x = tid >= o ? sums[tid - o] : 0u;
     __syncthreads();
     sums[tid] += x;
     __syncthreads();
   }
   uint32_t at = sums[tid] - mine;
-  for (uint32_t k = 0; k < EACH; ++k) {
-    const uint32_t b = tid * EACH + k, n = count[b];
-    count[b] = at;
-    if (b <= buckets) a.start[b] = at;
-    at += n;
+  for (uint32_t b = tid * EACH; b < min((tid + 1) * EACH, buckets); ++b) {
+    a.start[b] = at;
+    for (uint32_t w = 0; w < kListers; ++w) {
+      const uint32_t n = count[w * buckets + b];
+      count[w * buckets + b] = at;
+      at += n;
+    }
   }
-  if (tid == 1023 && buckets == kMostBuckets) a.start[buckets] = at;
+  if (tid == kListers * 64 - 1) a.start[buckets] = at;
   __syncthreads();
-  for (uint32_t r = tid; r < a.rows; r += 1024) {
-    const uint32_t b = bucket_of(r);
-    if (b < kMostBuckets) a.order[atomicAdd(&count[b], 1u)] = r;
+  for (uint32_t k = r0; k < r1; k += 64) {
+    const uint32_t b = k + lane < r1 ? bucket_of(k + lane) : kMostBuckets;
+    // The lanes before this one with its bucket, and whether none is behind.
+    uint32_t before = 0;
+    bool last = false;
+    uint64_t left = __builtin_amdgcn_ballot_w64(b < kMostBuckets);
+    while (left) {
+      const uint32_t one = __builtin_amdgcn_readlane(b, __builtin_ctzll(left));
+      const uint64_t same = __builtin_amdgcn_ballot_w64(b == one);
+      if (b == one) {
+        before = __builtin_popcountll(same & ((1ull << lane) - 1));
+        last = same >> lane == 1;
+      }
+      left &= ~same;
+    }
+    if (b < kMostBuckets) {
+      const uint32_t to = own[b] + before;
+      a.order[to] = k + lane;
+      if (last) own[b] = to + 1;
+    }
+    // The next rows' lanes see what these wrote.
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
   }
 }
 
 // The rows that take part packed, and listed by the last block.
 __global__ __launch_bounds__(1024) void k_prepare(PackArgs a, ListArgs l) {
+  extern __shared__ uint32_t counts[];
   if (blockIdx.x + 1 == gridDim.x)
-    list_rows(l);
+    list_rows(l, counts);
   else
     packed<1024>(a, blockIdx.x, gridDim.x - 1);
+}
+
+// The sums of rest * hidden over the rows of a token, for the tokens of lists longer than
+// kListed: a block has kRestTokens of them and 512 columns, a wave every fourth 64 rows of the
+// list.  Rounded to bfloat16: 2^-8 of what is itself 2^-8 (float32 gradients 2^-16) of dW.
+struct RestArgs {
+  const int32_t* targets;
+  const float* rest;
+  const uint32_t* start;
+  const uint32_t* order;
+  const uint16_t* h;
+  uint32_t pitch, bucket0;
+  uint16_t* sums;   // [rows][pitch]: a token's at the place in `order` of its first row
+  uint32_t* place;  // [128 a bucket]: that place, or kNoRow
+};
+constexpr uint32_t kRestTokens = 8, kRestWaves = 4, kNoRow = 0xFFFFFFFFu;
+__global__ __launch_bounds__(kRestWaves * 64) void k_rests(RestArgs a) {
+  const uint32_t b = a.bucket0 + blockIdx.x, from = a.start[b], n = a.start[b + 1] - from;
+  if (n <= kListed) return;
+  __shared__ uint32_t first[kRestTokens];
+  __shared__ float part[kRestWaves][512];
+  const uint32_t tid = threadIdx.x, lane = tid & 63, wave = tid / 64;
+  const uint32_t t0 = b * kBucket + blockIdx.z * kRestTokens, c0 = blockIdx.y * 512;
+  if (tid < kRestTokens) first[tid] = n;
+  __syncthreads();
+  for (uint32_t k = tid; k < n; k += kRestWaves * 64) {
+    const uint32_t t = (uint32_t)a.targets[a.order[from + k]] - t0;
+    if (t < kRestTokens) atomicMin(&first[t], k);
+  }
+  __syncthreads();
+  const bool in = c0 + lane * 8 < a.pitch;
+  for (uint32_t s = 0; s < kRestTokens; ++s) {
+    const uint32_t at = __builtin_amdgcn_readfirstlane(first[s]);
+    if (tid == 0 && blockIdx.y == 0) a.place[t0 + s] = at < n ? from + at : kNoRow;
+    if (at >= n) continue;
+    float sum[8] = {};
+    for (uint32_t k = wave * 64; k < n; k += kRestWaves * 64) {
+      const bool there = k + lane < n;
+      const uint32_t row = there ? a.order[from + k + lane] : 0u;
+      const bool its = there && (uint32_t)a.targets[row] == t0 + s;
+      const float rest = its ? a.rest[row] : 0.f;
+      uint64_t left = __builtin_amdgcn_ballot_w64(its);
+      while (left) {
+        u32x4 x[8];
+        float by[8];
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+          const int l = left ? __builtin_ctzll(left) : 0;
+          const uint32_t r = __builtin_amdgcn_readlane(row, l);
+          by[j] = left ? __int_as_float(__builtin_amdgcn_readlane(__float_as_int(rest), l)) : 0.f;
+          x[j] = left && in ? *(const u32x4*)(a.h + (size_t)r * a.pitch + c0 + lane * 8) : u32x4{0, 0, 0, 0};
+          left &= left - 1;
+        }
+#pragma unroll
+        for (int j = 0; j < 8; ++j)
+#pragma unroll
+          for (int e = 0; e < 8; ++e)
+            sum[e] = fmaf(by[j], __uint_as_float(e & 1 ? x[j][e / 2] & 0xFFFF0000u : x[j][e / 2] << 16), sum[e]);
+      }
+    }
+#pragma unroll
+    for (int e = 0; e < 8; ++e) part[wave][lane * 8 + e] = sum[e];
+    __syncthreads();
+    for (uint32_t c = tid; c < min(512u, a.pitch - c0); c += kRestWaves * 64) {
+      float v = 0.f;
+      for (uint32_t w = 0; w < kRestWaves; ++w) v += part[w][c];
+      // An infinite one would make NaN of the columns beside it, to which 0 of it is added.
+      constexpr float MOST = 0x1.fep127f;
+      v = v > MOST ? MOST : v < -MOST ? -MOST : v;
+      rows::store1<TFE_BF16>(a.sums + (size_t)(from + at) * a.pitch, c0 + c, v);
+    }
+    __syncthreads();
+  }
 }
 
 // dH = dz W over a piece of the vocabulary, cut along it where the tiles are few (the parts are
@@ -528,6 +625,8 @@ struct GradWArgs {
   const uint32_t* start;
   const uint32_t* order;
   uint32_t buckets;
+  const uint16_t* sums;   // of k_rests, pitch of h
+  const uint32_t* place;
   void* out;
   int64_t ldo;
   bool add;
@@ -568,36 +667,33 @@ __global__ __launch_bounds__(WP* WQ * 64) void k_grad_w(GradWArgs a) {
     return own;
   };
   auto add_rests = [&](uint32_t p0, uint32_t q0, const char* info) {
+    if (q0 + t.wq >= a.vocab) return;  // behind the last bucket there is no start
     uint32_t i, g;
     const uint32_t lane = lane_of(&i, &g);
     // Of the tile's first bucket on.
     const uint32_t* starts = (const uint32_t*)info + (t.wq / kBucket);
     const uint32_t from = __builtin_amdgcn_readfirstlane(starts[0]);
     const uint32_t n = __builtin_amdgcn_readfirstlane(starts[1]) - from;
-    if (n == 0 || n > kListed) return;
-    uint32_t row = 0, target = 0;
-    float rest = 0.f;
-    if (lane < n) {
+    if (n == 0) return;
+    const uint32_t first = a.vocab0 + q0 + t.wq;
+    const bool many = n > kListed;
+    uint32_t row = kNoRow, target = first + lane;
+    float rest = 1.f;
+    if (many) {
+      row = a.place[target];
+    } else if (lane < n) {
       row = a.order[from + lane];
       target = (uint32_t)a.targets[row];
       rest = a.rest[row];
     }
-    const uint32_t first = a.vocab0 + q0 + t.wq;
-    // In the order of their numbers, so that sums do not change from call to call.
-    uint32_t rank = lane < n ? 0 : lane;
-#pragma unroll 1
-    for (uint32_t k = 0; k < n; ++k)
-      rank += lane < n && (uint32_t)__builtin_amdgcn_readlane(row, k) < row;
-    row = __builtin_amdgcn_ds_permute(rank * 4, row);
-    target = __builtin_amdgcn_ds_permute(rank * 4, target);
-    rest = __int_as_float(__builtin_amdgcn_ds_permute(rank * 4, __float_as_int(rest)));
-    uint64_t mine = __builtin_amdgcn_ballot_w64(lane < n && target - first < 64u);
+    const uint16_t* const from_rows = many ? a.sums : a.h.at;
+    uint64_t mine = __builtin_amdgcn_ballot_w64(row != kNoRow && target - first < 64u);
     while (mine) {
       const int l = __builtin_ctzll(mine);
       mine &= mine - 1;
       const uint32_t r = __builtin_amdgcn_readlane(row, l), in = __builtin_amdgcn_readlane(target, l) - first;
       const float by = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(rest), l));
-      const uint16_t* x = a.h.at + (size_t)r * a.h.ld + p0 + t.wp + g * 4;
+      const uint16_t* x = from_rows + (size_t)r * a.h.ld + p0 + t.wp + g * 4;
       u32x2 y[T::NT];
 #pragma unroll
       for (int n = 0; n < T::NT; ++n)
@@ -712,7 +808,7 @@ struct Plan {
   uint32_t tile;         // rows of a tile
   uint32_t log;          // dz is in blocks of 2^log = tile rows
   int64_t plane;         // its bytes, of which there are two for float32 gradients
-  int64_t h, masked, w, part, picked, rest, start, order, dz, sums, bytes;
+  int64_t h, masked, w, part, picked, rest, start, order, place, dz, sums, bytes;
 };
 
 int64_t take(int64_t* at, int64_t bytes) {
@@ -741,6 +837,7 @@ Plan plan_of(int64_t n_rows, int32_t n_vocab, int32_t n_dim) {
   p.rest = take(&at, (int64_t)rows * 4);
   p.start = take(&at, (kMostBuckets + 1) * 4);
   p.order = take(&at, (int64_t)rows * 4);
+  p.place = take(&at, (int64_t)up(vocab, kBucket) * 4);
   p.log = p.tile == 256 ? 8 : p.tile == 128 ? 7 : 6;
   p.plane = (int64_t)(up(rows, p.tile) / p.tile) * (p.piece / 64) * gemm::block_bytes(p.log);
   p.dz = take(&at, p.plane * 2);
@@ -897,7 +994,10 @@ hipError_t launch_xent_grad(const XentArgs& a, bool behind_loss, hipStream_t s) 
   const PackArgs packed{a.hidden, a.ldh, a.rows, a.dim, p.pitch, a.targets, a.weight, a.vocab, masked};
   const ListArgs list{a.targets, a.weight, a.rows, a.vocab, (uint32_t*)(a.space + p.start), (uint32_t*)(a.space + p.order)};
   const uint64_t pieces = ((uint64_t)a.rows * (p.pitch / 8) + 1023) / 1024;
-  k_prepare<<<dim3((uint32_t)std::min<uint64_t>(pieces, 2048) + 1), dim3(1024), 0, s>>>(packed, list);
+  static std::atomic<uint64_t> told{0};
+  const int counts = (int)(kListers * ((a.vocab + kBucket - 1) / kBucket) * 4);
+  TRY_HIP(allow(k_prepare, (int)(kListers * kMostBuckets * 4), &told));
+  k_prepare<<<dim3((uint32_t)std::min<uint64_t>(pieces, 2048) + 1), dim3(1024), counts, s>>>(packed, list);
   TRY_HIP(hipGetLastError());
   for (uint32_t v0 = 0; v0 < a.vocab; v0 += p.piece) {
     const uint32_t n = std::min(p.piece, a.vocab - v0);
@@ -934,7 +1034,16 @@ hipError_t launch_xent_grad(const XentArgs& a, bool behind_loss, hipStream_t s) 
     TRY_HIP((p.tile == 256   ? grad_h<256, 256, 2, 4>(gh, s)
              : p.tile == 128 ? grad_h<256, 128, 2, 2>(gh, s)
                              : grad_h<256, 64, 2, 2>(gh, s)));
+    RestArgs rest{a.targets, l.rest, list.start, list.order, masked, p.pitch, v0 / kBucket,
+                  (uint16_t*)(a.space + p.h), (uint32_t*)(a.space + p.place)};  // p.h: of the loss, done with
+    if (a.rows > kListed) {
+      k_rests<<<dim3((n + kBucket - 1) / kBucket, (p.pitch + 511) / 512, kBucket / kRestTokens), dim3(kRestWaves * 64),
+                0, s>>>(rest);
+      TRY_HIP(hipGetLastError());
+    }
     GradWArgs gw{};
+    gw.sums = rest.sums;
+    gw.place = rest.place;
     gw.h = h;
     gw.dz = l.dz;
     gw.planes = gh.planes;
