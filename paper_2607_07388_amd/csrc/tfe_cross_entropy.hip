@@ -364,21 +364,25 @@ struct ListArgs {
   uint32_t rows, vocab;
   uint32_t* start;  // [buckets + 1]
   uint32_t* order;  // [rows]: row numbers, a bucket's in their order
+  uint32_t* longer; // the buckets of more than kListed rows: how many, which
 };
-// Each wave lists a run of the rows, with counts of its own: [waves][buckets].
+// Each wave lists a run of the rows, with counts of its own: [listers][buckets].
 constexpr uint32_t kListers = 16;
+constexpr uint32_t run_of(uint32_t rows) { return (rows + kListers * 64 - 1) / (kListers * 64) * 64; }
+constexpr uint32_t listers_of(uint32_t rows) { return (rows + run_of(rows) - 1) / run_of(rows); }
 __device__ __forceinline__ void list_rows(const ListArgs& a, uint32_t* count) {
-  __shared__ uint32_t sums[kListers * 64];
+  __shared__ uint32_t sums[kListers * 64], longer;
   const uint32_t buckets = (a.vocab + kBucket - 1) / kBucket, tid = threadIdx.x, lane = tid & 63;
   constexpr uint32_t EACH = kMostBuckets / (kListers * 64);
   uint32_t* const own = count + tid / 64 * buckets;
-  const uint32_t run = (a.rows + kListers * 64 - 1) / (kListers * 64) * 64;
+  const uint32_t run = run_of(a.rows), listers = listers_of(a.rows);
   const uint32_t r0 = min(tid / 64 * run, a.rows), r1 = min(r0 + run, a.rows);
   auto bucket_of = [&](uint32_t r) {
     const uint32_t t = (uint32_t)a.targets[r];
     return t < a.vocab && !(a.weight && a.weight[r] == 0.f) ? t / kBucket : kMostBuckets;
   };
-  for (uint32_t k = tid; k < kListers * buckets; k += kListers * 64) count[k] = 0;
+  for (uint32_t k = tid; k < listers * buckets; k += kListers * 64) count[k] = 0;
+  if (tid == 0) longer = 0;
   __syncthreads();
   for (uint32_t r = r0 + lane; r < r1; r += 64) {
     const uint32_t b = bucket_of(r);
@@ -387,7 +391,7 @@ __device__ __forceinline__ void list_rows(const ListArgs& a, uint32_t* count) {
   __syncthreads();
   uint32_t mine = 0;
   for (uint32_t b = tid * EACH; b < min((tid + 1) * EACH, buckets); ++b)
-    for (uint32_t w = 0; w < kListers; ++w) mine += count[w * buckets + b];
+    for (uint32_t w = 0; w < listers; ++w) mine += count[w * buckets + b];
   sums[tid] = mine;
   __syncthreads();
   for (uint32_t o = 1; o < kListers * 64; o <<= 1) {
@@ -398,34 +402,32 @@ __device__ __forceinline__ void list_rows(const ListArgs& a, uint32_t* count) {
   }
   uint32_t at = sums[tid] - mine;
   for (uint32_t b = tid * EACH; b < min((tid + 1) * EACH, buckets); ++b) {
+    const uint32_t here = at;
     a.start[b] = at;
-    for (uint32_t w = 0; w < kListers; ++w) {
+    for (uint32_t w = 0; w < listers; ++w) {
       const uint32_t n = count[w * buckets + b];
       count[w * buckets + b] = at;
       at += n;
     }
+    if (at - here > kListed) a.longer[1 + atomicAdd(&longer, 1u)] = b;
   }
   if (tid == kListers * 64 - 1) a.start[buckets] = at;
   __syncthreads();
+  if (tid == 0) a.longer[0] = longer;
   for (uint32_t k = r0; k < r1; k += 64) {
     const uint32_t b = k + lane < r1 ? bucket_of(k + lane) : kMostBuckets;
-    // The lanes before this one with its bucket, and whether none is behind.
-    uint32_t before = 0;
-    bool last = false;
-    uint64_t left = __builtin_amdgcn_ballot_w64(b < kMostBuckets);
-    while (left) {
-      const uint32_t one = __builtin_amdgcn_readlane(b, __builtin_ctzll(left));
-      const uint64_t same = __builtin_amdgcn_ballot_w64(b == one);
-      if (b == one) {
-        before = __builtin_popcountll(same & ((1ull << lane) - 1));
-        last = same >> lane == 1;
-      }
-      left &= ~same;
+    // The lanes with its bucket: those that agree in every bit.
+    uint64_t same = ~0ull;
+#pragma unroll
+    for (uint32_t bit = 1; bit <= kMostBuckets; bit <<= 1) {
+      const uint64_t set = __builtin_amdgcn_ballot_w64((b & bit) != 0);
+      same &= b & bit ? set : ~set;
     }
+    const uint32_t before = __builtin_popcountll(same & ((1ull << lane) - 1));
     if (b < kMostBuckets) {
       const uint32_t to = own[b] + before;
       a.order[to] = k + lane;
-      if (last) own[b] = to + 1;
+      if (same >> lane == 1) own[b] = to + 1;
     }
     // The next rows' lanes see what these wrote.
     __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
@@ -442,35 +444,38 @@ __global__ __launch_bounds__(1024) void k_prepare(PackArgs a, ListArgs l) {
 }
 
 // The sums of rest * hidden over the rows of a token, for the tokens of lists longer than
-// kListed: a block has kRestTokens of them and 512 columns, a wave every fourth 64 rows of the
+// kListed: a block has `tokens` of them and 512 columns, a wave every fourth 64 rows of the
 // list.  Rounded to bfloat16: 2^-8 of what is itself 2^-8 (float32 gradients 2^-16) of dW.
 struct RestArgs {
   const int32_t* targets;
   const float* rest;
   const uint32_t* start;
   const uint32_t* order;
+  const uint32_t* longer;
   const uint16_t* h;
-  uint32_t pitch, bucket0;
+  uint32_t pitch, tokens, bucket0, buckets;  // of this piece
   uint16_t* sums;   // [rows][pitch]: a token's at the place in `order` of its first row
   uint32_t* place;  // [128 a bucket]: that place, or kNoRow
 };
-constexpr uint32_t kRestTokens = 8, kRestWaves = 4, kNoRow = 0xFFFFFFFFu;
+constexpr uint32_t kRestWaves = 4, kNoRow = 0xFFFFFFFFu;
 __global__ __launch_bounds__(kRestWaves * 64) void k_rests(RestArgs a) {
-  const uint32_t b = a.bucket0 + blockIdx.x, from = a.start[b], n = a.start[b + 1] - from;
-  if (n <= kListed) return;
-  __shared__ uint32_t first[kRestTokens];
+  if (blockIdx.x >= a.longer[0]) return;
+  const uint32_t b = a.longer[1 + blockIdx.x];
+  if (b - a.bucket0 >= a.buckets) return;
+  const uint32_t from = a.start[b], n = a.start[b + 1] - from;
+  __shared__ uint32_t first[kBucket];
   __shared__ float part[kRestWaves][512];
   const uint32_t tid = threadIdx.x, lane = tid & 63, wave = tid / 64;
-  const uint32_t t0 = b * kBucket + blockIdx.z * kRestTokens, c0 = blockIdx.y * 512;
-  if (tid < kRestTokens) first[tid] = n;
+  const uint32_t t0 = b * kBucket + blockIdx.z * a.tokens, c0 = blockIdx.y * 512;
+  if (tid < a.tokens) first[tid] = n;
   __syncthreads();
   for (uint32_t k = tid; k < n; k += kRestWaves * 64) {
     const uint32_t t = (uint32_t)a.targets[a.order[from + k]] - t0;
-    if (t < kRestTokens) atomicMin(&first[t], k);
+    if (t < a.tokens) atomicMin(&first[t], k);
   }
   __syncthreads();
   const bool in = c0 + lane * 8 < a.pitch;
-  for (uint32_t s = 0; s < kRestTokens; ++s) {
+  for (uint32_t s = 0; s < a.tokens; ++s) {
     const uint32_t at = __builtin_amdgcn_readfirstlane(first[s]);
     if (tid == 0 && blockIdx.y == 0) a.place[t0 + s] = at < n ? from + at : kNoRow;
     if (at >= n) continue;
@@ -676,17 +681,41 @@ __global__ __launch_bounds__(WP* WQ * 64) void k_grad_w(GradWArgs a) {
     const uint32_t n = __builtin_amdgcn_readfirstlane(starts[1]) - from;
     if (n == 0) return;
     const uint32_t first = a.vocab0 + q0 + t.wq;
+    // Small tiles: a lane's columns have a row of k_rests each, or none.  In large ones this way
+    // beside the other takes the registers of the sums.
+    constexpr bool EACH = TQ == 128;
     const bool many = n > kListed;
+    if (EACH && many) {
+#pragma unroll
+      for (int m = 0; m < T::MT; ++m) {
+        const uint32_t r = a.place[first + m * 16 + i];
+        const uint16_t* x = a.sums + (size_t)r * a.h.ld + p0 + t.wp + g * 4;
+        u32x2 y[T::NT];
+#pragma unroll
+        for (int n = 0; n < T::NT; ++n) y[n] = u32x2{0, 0};
+        if (r != kNoRow) {
+#pragma unroll
+          for (int n = 0; n < T::NT; ++n)
+            if (p0 + t.wp + n * 16 + g * 4 < a.h.cols) y[n] = *(const u32x2*)(x + n * 16);
+        }
+#pragma unroll
+        for (int n = 0; n < T::NT; ++n)
+#pragma unroll
+          for (int j = 0; j < 4; ++j)
+            t.acc[n][m][j] += __uint_as_float(j & 1 ? y[n][j / 2] & 0xFFFF0000u : y[n][j / 2] << 16);
+      }
+      return;
+    }
     uint32_t row = kNoRow, target = first + lane;
     float rest = 1.f;
-    if (many) {
+    if (!EACH && many) {
       row = a.place[target];
     } else if (lane < n) {
       row = a.order[from + lane];
       target = (uint32_t)a.targets[row];
       rest = a.rest[row];
     }
-    const uint16_t* const from_rows = many ? a.sums : a.h.at;
+    const uint16_t* const from_rows = !EACH && many ? a.sums : a.h.at;
     uint64_t mine = __builtin_amdgcn_ballot_w64(row != kNoRow && target - first < 64u);
     while (mine) {
       const int l = __builtin_ctzll(mine);
@@ -808,7 +837,7 @@ struct Plan {
   uint32_t tile;         // rows of a tile
   uint32_t log;          // dz is in blocks of 2^log = tile rows
   int64_t plane;         // its bytes, of which there are two for float32 gradients
-  int64_t h, masked, w, part, picked, rest, start, order, place, dz, sums, bytes;
+  int64_t h, masked, w, part, picked, rest, start, order, longer, place, dz, sums, bytes;
 };
 
 int64_t take(int64_t* at, int64_t bytes) {
@@ -837,6 +866,7 @@ Plan plan_of(int64_t n_rows, int32_t n_vocab, int32_t n_dim) {
   p.rest = take(&at, (int64_t)rows * 4);
   p.start = take(&at, (kMostBuckets + 1) * 4);
   p.order = take(&at, (int64_t)rows * 4);
+  p.longer = take(&at, (int64_t)(1 + std::min(rows / (kListed + 1), kMostBuckets)) * 4);
   p.place = take(&at, (int64_t)up(vocab, kBucket) * 4);
   p.log = p.tile == 256 ? 8 : p.tile == 128 ? 7 : 6;
   p.plane = (int64_t)(up(rows, p.tile) / p.tile) * (p.piece / 64) * gemm::block_bytes(p.log);
@@ -992,10 +1022,11 @@ hipError_t launch_xent_grad(const XentArgs& a, bool behind_loss, hipStream_t s) 
   uint16_t* masked = (uint16_t*)(a.space + p.masked);
   const Matrix h{masked, p.pitch, a.rows, p.pitch};
   const PackArgs packed{a.hidden, a.ldh, a.rows, a.dim, p.pitch, a.targets, a.weight, a.vocab, masked};
-  const ListArgs list{a.targets, a.weight, a.rows, a.vocab, (uint32_t*)(a.space + p.start), (uint32_t*)(a.space + p.order)};
+  const ListArgs list{a.targets, a.weight, a.rows, a.vocab, (uint32_t*)(a.space + p.start),
+                      (uint32_t*)(a.space + p.order), (uint32_t*)(a.space + p.longer)};
   const uint64_t pieces = ((uint64_t)a.rows * (p.pitch / 8) + 1023) / 1024;
   static std::atomic<uint64_t> told{0};
-  const int counts = (int)(kListers * ((a.vocab + kBucket - 1) / kBucket) * 4);
+  const int counts = (int)(listers_of(a.rows) * ((a.vocab + kBucket - 1) / kBucket) * 4);
   TRY_HIP(allow(k_prepare, (int)(kListers * kMostBuckets * 4), &told));
   k_prepare<<<dim3((uint32_t)std::min<uint64_t>(pieces, 2048) + 1), dim3(1024), counts, s>>>(packed, list);
   TRY_HIP(hipGetLastError());
@@ -1034,11 +1065,13 @@ hipError_t launch_xent_grad(const XentArgs& a, bool behind_loss, hipStream_t s) 
     TRY_HIP((p.tile == 256   ? grad_h<256, 256, 2, 4>(gh, s)
              : p.tile == 128 ? grad_h<256, 128, 2, 2>(gh, s)
                              : grad_h<256, 64, 2, 2>(gh, s)));
-    RestArgs rest{a.targets, l.rest, list.start, list.order, masked, p.pitch, v0 / kBucket,
-                  (uint16_t*)(a.space + p.h), (uint32_t*)(a.space + p.place)};  // p.h: of the loss, done with
+    // p.h was the loss's.  Tokens of a block: a few thousand blocks at most.
+    RestArgs rest{a.targets, l.rest, list.start, list.order, list.longer, masked, p.pitch, 1, v0 / kBucket,
+                  (n + kBucket - 1) / kBucket, (uint16_t*)(a.space + p.h), (uint32_t*)(a.space + p.place)};
     if (a.rows > kListed) {
-      k_rests<<<dim3((n + kBucket - 1) / kBucket, (p.pitch + 511) / 512, kBucket / kRestTokens), dim3(kRestWaves * 64),
-                0, s>>>(rest);
+      const uint32_t lists = std::min((a.vocab + kBucket - 1) / kBucket, a.rows / (kListed + 1)), across = (p.pitch + 511) / 512;
+      while (rest.tokens < kBucket && lists * across * (kBucket / rest.tokens) > 8192) rest.tokens *= 2;
+      k_rests<<<dim3(lists, across, kBucket / rest.tokens), dim3(kRestWaves * 64), 0, s>>>(rest);
       TRY_HIP(hipGetLastError());
     }
     GradWArgs gw{};
