@@ -101,7 +101,7 @@ __global__ __launch_bounds__(256) void k_pack(PackArgs a) { packed<256>(a, block
 
 // ---- logits: their sums, or dz -----------------------------------------------------
 
-// Bound by the matrix cores, which k_sums keeps 66% busy and the gradients' products 53 to 56%
+// Bound by the matrix cores, which k_sums keeps 66% busy and the gradients' products 52 to 56%
 // (a wave's registers hold 128 x 64 sums: a larger tile does not fit, and each step reads 192 KB
 // of LDS), and by what
 // follows a tile's products: exponentials (16 cycles a wave) beside maxima and sums, and dz's
