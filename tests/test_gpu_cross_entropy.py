@@ -305,7 +305,7 @@ def test_target_roundings_of_common_tokens(rows, same, dim):
 
 
 @pytest.mark.parametrize("dtype", [F32, BF16])
-@pytest.mark.parametrize("rows,same", [(33, 1), (64, 1), (66, 1), (80, 1), (200, 1), (200, 3), (1000, 20), (70, 2), (1000, 1), (2500, 2)])
+@pytest.mark.parametrize("rows,same", [(33, 1), (64, 1), (66, 1), (80, 1), (200, 1), (200, 3), (1000, 20), (70, 2), (1000, 1), (2500, 2), (20000, 3)])
 def test_common_targets(rows, same, dtype):
     """Few tokens are everybody's targets: more rows than are listed share a block of columns."""
     c = Case(rows, 700, 72)
@@ -338,5 +338,27 @@ def test_captured_and_on_another_stream(rows, dtype):
             getattr(c, a).copy_(getattr(cases[k], a))
         g.replay()
         cases[0].both(dtype)
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip((loss, lse, gx, gw), want[k]))
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+def test_captured_while_targets_become_common(dtype):
+    """One graph replayed on targets that are few, many and few again: which lists are long is the device's to see."""
+    c = Case(300, 700, 96)
+    targets = [c.t.clone(), (c.t % 2 * 130 % 700).int(), (c.t % 5).int(), torch.full_like(c.t, -1)]
+    want = []
+    for t in targets:
+        c.t.copy_(t)
+        want.append(c.both(dtype))
+    loss, lse = torch.empty(300, device="cuda"), torch.empty(300, device="cuda")
+    gx, gw, space = empty(300, 96, dtype), empty(700, 96, dtype), c.space()
+    torch.cuda.synchronize()
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g):
+        tfe.tfe_cross_entropy_loss_grad(*c.head(), c.g, loss, lse, gx, 96, gw, 96, dtype, 0, *space, H.cur_stream())
+    for k in (1, 0, 2, 3, 1, 2, 0):
+        c.t.copy_(targets[k])
+        g.replay()
         torch.cuda.synchronize()
         assert all(torch.equal(a, b) for a, b in zip((loss, lse, gx, gw), want[k]))
