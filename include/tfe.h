@@ -484,9 +484,9 @@ int64_t tfe_distill_workspace(int64_t rows, int32_t vocab); /* -1: bad size */
  *               hidden state holds.
  *   grad_hidden, grad_w  DEVICE of grad_dtype, [rows x dim] and [vocab x dim],
  *               pitches ldgh and ldgw; apart from each other and every input.
- *               Sums are float32.  For TFE_BF16 results dz is rounded to
- *               bfloat16 before the products with W and H, for TFE_F32 ones to
- *               the sum of two bfloat16 numbers (16 bits), at twice the products;
+ *               Sums are float32.  For TFE_F32 results dz is float32 (the sum of
+ *               three bfloat16 numbers, at three times the products).  For TFE_BF16
+ *               ones it is rounded to bfloat16 before the products with W and H;
  *               what that leaves of dz at a row's target is added in float32
  *               (to grad_w where more than 64 rows have theirs among the same 128
  *               tokens, counted from 0: summed by token, rounded to bfloat16).
@@ -497,7 +497,7 @@ int64_t tfe_distill_workspace(int64_t rows, int32_t vocab); /* -1: bad size */
  * Pointers 16-byte aligned, with pitches and dim multiples of 8 (and pitches up
  * to 2^21), are read in place; others are copied in pieces first.  With no rows
  * grad_w becomes 0 (accumulate: stays).  The workspace is for a piece of the
- * vocabulary at a time: about 4 bytes for each of its numbers of dz (2^27 at most, or
+ * vocabulary at a time: about 6 bytes for each of its numbers of dz (2^27 at most, or
  * 2048 a row), a copy of its rows of W, and 12 to 24 bytes a number of hidden.
  * 1 <= vocab <= 2^18, 1 <= dim <= 16384, rows <= 2^20. */
 tfe_status tfe_cross_entropy_loss(const void *hidden, int64_t ldh, const void *w, int64_t ldw,

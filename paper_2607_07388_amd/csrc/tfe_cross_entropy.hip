@@ -43,7 +43,7 @@ __device__ __forceinline__ Operand across(const Matrix& m, uint32_t col) {
 // read them 20 us longer of 235, and writing them 30 of 285.
 struct Dz {
   uint16_t* at;
-  uint64_t plane;  // elements to the second numbers of float32 gradients
+  uint64_t plane;  // elements to the next numbers of float32 gradients
   uint32_t log, blocks, rows, cols;  // rows and columns of whole blocks
   __device__ __forceinline__ size_t block(uint32_t row, uint32_t col) const {
     return ((size_t)(row >> log) * blocks + (col >> 6)) * (gemm::block_bytes(log) / 2);
@@ -272,6 +272,12 @@ __global__ __launch_bounds__(1024) void k_join(JoinArgs a) {
   a.loss[r] = (uint32_t)a.targets[r] < a.vocab ? (top - a.picked[r]) + rest : 0.f;
 }
 
+// Numbers of bfloat16 that a number of dz is the sum of: float32 gradients take three, whose
+// 24 bits are its own.  With two, dH and dW of few rows over 1000 tokens were off by up to 1.3e-6
+// of their norm, where products of dz in float32 are by 4.6e-7; with three by up to 7e-7, the
+// logits' own error.  257 rows of 40001 x 999 take 386 us, with two 330.
+constexpr uint32_t planes_of(bool f32) { return f32 ? 3 : 1; }
+
 // Two tiles of 16 columns of a row, each lane's 4 + 4, as 16 bytes of bfloat16 at
 // column piece_of(g): lanes of neighbouring rows of 16 exchange halves.
 __device__ __forceinline__ u32x4 pair_of(const float* p, const float* q) {
@@ -314,14 +320,14 @@ __global__ __launch_bounds__(WP* WQ * 64) void k_dz(LogitsArgs a) {
         for (int n = 0; n < t.NT; ++n)
 #pragma unroll
           for (int j = 0; j < 4; ++j) t.acc[n][m][j] -= at == (uint32_t)(n * 16 + j) ? 1.f : 0.f;
-        float d = 0.f;
+        if (PLANES == 1) {
+          float d = 0.f;
 #pragma unroll
-        for (int n = 0; n < T::NT; ++n)
+          for (int n = 0; n < T::NT; ++n)
 #pragma unroll
-          for (int j = 0; j < 4; ++j) d = at == (uint32_t)(n * 16 + j) ? t.acc[n][m][j] * weight : d;
-        float e = d - (float)(__bf16)d;
-        if (PLANES == 2) e -= (float)(__bf16)e;
-        if (hit && q0 + in < a.h.rows) a.rest[q0 + in] = weight == 0.f ? 0.f : e;
+            for (int j = 0; j < 4; ++j) d = at == (uint32_t)(n * 16 + j) ? t.acc[n][m][j] * weight : d;
+          if (hit && q0 + in < a.h.rows) a.rest[q0 + in] = weight == 0.f ? 0.f : d - (float)(__bf16)d;
+        }
       }
       // Rows without a gradient are zeros, whatever their probabilities.
       if (__builtin_amdgcn_ballot_w64(weight == 0.f)) {
@@ -333,16 +339,19 @@ __global__ __launch_bounds__(WP* WQ * 64) void k_dz(LogitsArgs a) {
       uint16_t* const row = tile + in * 64;
 #pragma unroll
       for (int n = 0; n < t.NT; n += 2) {
-        float d[8], e[8];
+        float d[8];
 #pragma unroll
         for (int j = 0; j < 8; ++j) {
           d[j] = t.acc[n + j / 4][m][j & 3] * weight;
           if (ends && c0 + (n + j / 4) * 16 + (j & 3) >= a.w.rows) d[j] = 0.f;
-          if (PLANES == 2) e[j] = d[j] - (float)(__bf16)d[j];
         }
         uint16_t* const out = row + (n / 4) * (gemm::block_bytes(__builtin_ctz(TQ)) / 2) + (n & 2) * 16;
-        *(u32x4*)out = pair_of(d, d + 4);
-        if (PLANES == 2) *(u32x4*)(out + a.dz.plane) = pair_of(e, e + 4);
+#pragma unroll
+        for (int p = 0; p < PLANES; ++p) {
+          *(u32x4*)(out + p * a.dz.plane) = pair_of(d, d + 4);
+#pragma unroll
+          for (int j = 0; j < 8; ++j) d[j] -= (float)(__bf16)d[j];  // exact
+        }
       }
     }
     return true;
@@ -352,7 +361,7 @@ __global__ __launch_bounds__(WP* WQ * 64) void k_dz(LogitsArgs a) {
 // ---- gradients -----------------------------------------------------------------------
 
 // dz at a row's target is most of its dz (p - 1 beside small p), and its rounding most
-// of the gradients' error: up to 0.0027 of their norm in bfloat16, 0.0017 with what it leaves
+// of bfloat16 gradients' error: up to 0.0027 of their norm, 0.0017 with what it leaves
 // (`rest`) added in float32.  For dW the rows are listed by their target's 128 columns, in
 // their order.  Up to kListed rows of a list are added one by one; of longer lists those of
 // each token are summed by k_rests before: a row more of the product for each token.
@@ -445,9 +454,9 @@ __global__ __launch_bounds__(1024) void k_prepare(PackArgs a, ListArgs l) {
 
 // The sums of rest * hidden over the rows of a token, for the tokens of lists longer than
 // kListed: a block has `tokens` of them and 512 columns, a wave every eighth 64 rows of the
-// list.  Rounded to bfloat16: 2^-8 of what is itself 2^-8 (float32 gradients 2^-16) of dW.
-// Without them dW was off by 2.6e-6 of its norm in float32 and 0.0024 in bfloat16 where every
-// list is long (4096 rows of 3001 x 256), with them by 7e-7 and 0.0017.  Bound by the chain of
+// list.  Rounded to bfloat16: 2^-8 of what is itself 2^-8 of dW.
+// Without them dW was off by 0.0024 of its norm where every list is long (4096 rows of
+// 3001 x 256), with them by 0.0017.  Bound by the chain of
 // loads of the commonest token: 4096 rows of 1000 x 1024 16 us (22 with four waves a block).
 struct RestArgs {
   const int32_t* targets;
@@ -612,13 +621,15 @@ template <int DT> __global__ __launch_bounds__(64) void k_finish_h(FinishArgs a)
     // 0 x an infinity of W is not a gradient of a row without one.
     const uint32_t target = (uint32_t)a.targets[r];
     const bool none = target >= a.vocab || (a.weight && a.weight[r] == 0.f);
-    const float rest = none ? 0.f : a.rest[r];
+    const float rest = DT == TFE_F32 || none ? 0.f : a.rest[r];
     const uint16_t* const at_w = a.w + (size_t)(none ? 0 : target) * a.ldw;
     char* out = (char*)a.out + ((size_t)r * a.ldo) * sizeof(typename rows::Elem<DT>::T);
 #pragma unroll
     for (int j = 0; j < 4; ++j)
-      if (c + j < a.dim)
-        rows::store1<DT>(out, c + j, none ? 0.f : fmaf(rest, rows::load1<TFE_BF16>(at_w, c + j), v[j]));
+      if (c + j < a.dim) {
+        const float x = DT == TFE_F32 ? v[j] : fmaf(rest, rows::load1<TFE_BF16>(at_w, c + j), v[j]);
+        rows::store1<DT>(out, c + j, none ? 0.f : x);
+      }
   }
 }
 
@@ -794,14 +805,16 @@ __global__ __launch_bounds__(WP* WQ * 64) void k_grad_w(GradWArgs a) {
         return more;
       },
       [&](uint32_t odd) {
-        if (t.wave == 0)
+        if (DT == TFE_BF16 && t.wave == 0)
           gemm::load_numbers(a.start, (a.vocab0 + cur.q0) / kBucket, a.buckets + 1, 0, lds + T::LDS + odd * 256);
       },
       [&](uint32_t odd) {
         bool stored = false;
         if (cur.plane + 1 == a.planes) {
-          add_rests(cur.p0, cur.q0, lds + T::LDS + odd * 256);
-          __builtin_amdgcn_sched_barrier(0);
+          if constexpr (DT == TFE_BF16) {
+            add_rests(cur.p0, cur.q0, lds + T::LDS + odd * 256);
+            __builtin_amdgcn_sched_barrier(0);
+          }
           stored = write(cur.p0, cur.q0);
           t.clear();
         }
@@ -839,7 +852,7 @@ struct Plan {
   uint32_t splits;       // of dH's sums over the vocabulary
   uint32_t tile;         // rows of a tile
   uint32_t log;          // dz is in blocks of 2^log = tile rows
-  int64_t plane;         // its bytes, of which there are two for float32 gradients
+  int64_t plane;         // its bytes, of which there are three for float32 gradients
   int64_t h, masked, w, part, picked, rest, start, order, longer, place, dz, sums, bytes;
 };
 
@@ -873,7 +886,7 @@ Plan plan_of(int64_t n_rows, int32_t n_vocab, int32_t n_dim) {
   p.place = take(&at, (int64_t)up(vocab, kBucket) * 4);
   p.log = p.tile == 256 ? 8 : p.tile == 128 ? 7 : 6;
   p.plane = (int64_t)(up(rows, p.tile) / p.tile) * (p.piece / 64) * gemm::block_bytes(p.log);
-  p.dz = take(&at, p.plane * 2);
+  p.dz = take(&at, p.plane * planes_of(true));
   p.sums = take(&at, (int64_t)p.splits * rows * p.pitch * 4);
   p.bytes = at;
   return p;
@@ -884,12 +897,14 @@ bool direct(const void* p, int64_t ld, uint32_t dim) {
   return ((uintptr_t)p & 15) == 0 && ld % 8 == 0 && dim % 8 == 0 && ld <= kXentMaxPitch;
 }
 
-hipError_t pack(const uint16_t* x, int64_t ldx, uint32_t rows, uint32_t cols, uint32_t pitch,
-                uint16_t* out, hipStream_t s) {
-  const PackArgs a{x, ldx, rows, cols, pitch, nullptr, nullptr, 0, out};
-  const uint64_t n = (uint64_t)rows * (pitch / 8);
+hipError_t pack(const PackArgs& a, hipStream_t s) {
+  const uint64_t n = (uint64_t)a.rows * (a.pitch / 8);
   k_pack<<<dim3((uint32_t)std::min<uint64_t>((n + 255) / 256, 8192)), dim3(256), 0, s>>>(a);
   return hipGetLastError();
+}
+hipError_t pack(const uint16_t* x, int64_t ldx, uint32_t rows, uint32_t cols, uint32_t pitch,
+                uint16_t* out, hipStream_t s) {
+  return pack(PackArgs{x, ldx, rows, cols, pitch, nullptr, nullptr, 0, out}, s);
 }
 
 // More LDS than a kernel may have by default: told once for each device.
@@ -1027,12 +1042,16 @@ hipError_t launch_xent_grad(const XentArgs& a, bool behind_loss, hipStream_t s) 
   const PackArgs packed{a.hidden, a.ldh, a.rows, a.dim, p.pitch, a.targets, a.weight, a.vocab, masked};
   const ListArgs list{a.targets, a.weight, a.rows, a.vocab, (uint32_t*)(a.space + p.start),
                       (uint32_t*)(a.space + p.order), (uint32_t*)(a.space + p.longer)};
-  const uint64_t pieces = ((uint64_t)a.rows * (p.pitch / 8) + 1023) / 1024;
-  static std::atomic<uint64_t> told{0};
-  const int counts = (int)(listers_of(a.rows) * ((a.vocab + kBucket - 1) / kBucket) * 4);
-  TRY_HIP(allow(k_prepare, (int)(kListers * kMostBuckets * 4), &told));
-  k_prepare<<<dim3((uint32_t)std::min<uint64_t>(pieces, 2048) + 1), dim3(1024), counts, s>>>(packed, list);
-  TRY_HIP(hipGetLastError());
+  if (f32) {
+    TRY_HIP(pack(packed, s));
+  } else {
+    const uint64_t pieces = ((uint64_t)a.rows * (p.pitch / 8) + 1023) / 1024;
+    static std::atomic<uint64_t> told{0};
+    const int counts = (int)(listers_of(a.rows) * ((a.vocab + kBucket - 1) / kBucket) * 4);
+    TRY_HIP(allow(k_prepare, (int)(kListers * kMostBuckets * 4), &told));
+    k_prepare<<<dim3((uint32_t)std::min<uint64_t>(pieces, 2048) + 1), dim3(1024), counts, s>>>(packed, list);
+    TRY_HIP(hipGetLastError());
+  }
   for (uint32_t v0 = 0; v0 < a.vocab; v0 += p.piece) {
     const uint32_t n = std::min(p.piece, a.vocab - v0);
     LogitsArgs l{};
@@ -1048,18 +1067,18 @@ hipError_t launch_xent_grad(const XentArgs& a, bool behind_loss, hipStream_t s) 
     l.dz = Dz{(uint16_t*)(a.space + p.dz), (uint64_t)p.plane / 2, p.log, p.piece / 64, up(a.rows, p.tile), up(n, 64)};
     l.h.cols = l.w.cols;  // zeros from dim on
     if (f32)
-      TRY_HIP((p.tile == 256   ? dz<256, 256, 2, 4, 2>(l, s)
-               : p.tile == 128 ? dz<256, 128, 2, 2, 2>(l, s)
-                               : dz<128, 64, 1, 4, 2>(l, s)));
+      TRY_HIP((p.tile == 256   ? dz<256, 256, 2, 4, planes_of(true)>(l, s)
+               : p.tile == 128 ? dz<256, 128, 2, 2, planes_of(true)>(l, s)
+                               : dz<128, 64, 1, 4, planes_of(true)>(l, s)));
     else
-      TRY_HIP((p.tile == 256   ? dz<256, 256, 2, 4, 1>(l, s)
-               : p.tile == 128 ? dz<256, 128, 2, 2, 1>(l, s)
-                               : dz<128, 64, 1, 4, 1>(l, s)));
+      TRY_HIP((p.tile == 256   ? dz<256, 256, 2, 4, planes_of(false)>(l, s)
+               : p.tile == 128 ? dz<256, 128, 2, 2, planes_of(false)>(l, s)
+                               : dz<128, 64, 1, 4, planes_of(false)>(l, s)));
     GradHArgs gh{};
     gh.w = l.w;
     gh.dz = l.dz;
     gh.rows = a.rows;
-    gh.planes = f32 ? 2 : 1;
+    gh.planes = planes_of(f32);
     gh.splits = p.splits;
     gh.dim = a.dim;
     gh.sums = (float*)(a.space + p.sums);
@@ -1071,7 +1090,7 @@ hipError_t launch_xent_grad(const XentArgs& a, bool behind_loss, hipStream_t s) 
     // p.h was the loss's.  Tokens of a block: a few thousand blocks at most.
     RestArgs rest{a.targets, l.rest, list.start, list.order, list.longer, masked, p.pitch, 1, v0 / kBucket,
                   (n + kBucket - 1) / kBucket, (uint16_t*)(a.space + p.h), (uint32_t*)(a.space + p.place)};
-    if (a.rows > kListed) {
+    if (!f32 && a.rows > kListed) {
       const uint32_t lists = std::min((a.vocab + kBucket - 1) / kBucket, a.rows / (kListed + 1)), across = (p.pitch + 511) / 512;
       while (rest.tokens < kBucket && lists * across * (kBucket / rest.tokens) > 8192) rest.tokens *= 2;
       k_rests<<<dim3(lists, across, kBucket / rest.tokens), dim3(kRestWaves * 64), 0, s>>>(rest);
