@@ -521,7 +521,11 @@ int64_t tfe_cross_entropy_workspace(int64_t rows, int32_t vocab, int32_t dim); /
 
 /* One gradient: `rows` rows of `cols` elements, ldg apart (ldo in `out`).  `out`
  * is where its clipped form goes: `grad` itself, at the same pitch, or memory
- * apart from every gradient; tfe_grad_norm does not look at it. */
+ * apart from every gradient, and from every other's `out`: a gradient that is
+ * listed twice may not be clipped in place.  Lists that break this are refused
+ * (of rows apart the first ones are compared); of more than 512 tensors it is
+ * seen in host memory that is freed within the call.  tfe_grad_norm does not
+ * look at `out`. */
 typedef struct {
   const void *grad; /* DEVICE, dtype */
   void *out;        /* DEVICE, dtype */

@@ -1,9 +1,13 @@
 // C ABI of the calls that learn the head from tokens and serve it in integers:
 // cross entropy, gradient norm and clipping, the integer product.  Host checks
-// only; nothing is allocated and no state kept.
+// only; no device memory is allocated and no state kept.
 #include <hip/hip_runtime_api.h>
 #include <math.h>
 #include <stdint.h>
+
+#include <algorithm>
+#include <memory>
+#include <new>
 
 #include "../../include/tfe.h"
 #include "tfe_checks.h"
@@ -85,6 +89,52 @@ tfe_status grad_tensors(const tfe_grad_tensor* t, int64_t n, bool out) {
     TRY(matrix(g.out, g.dtype, g.rows == 1 ? 0 : g.ldo, rows, g.rows == 1 ? 0 : g.cols, "clipped gradient"));
     NEED(none || g.rows == 1 || g.grad != g.out || g.ldg == g.ldo, "tensor %lld: in place at another pitch",
          (long long)k);
+  }
+  return TFE_OK;
+}
+
+// The bytes of a clipped gradient or a gradient that surely are its own: of rows apart, between
+// which other tensors may lie (columns of one matrix), the first.
+struct Range {
+  uintptr_t from, to;
+  int64_t tensor;
+};
+Range range_of(const tfe_grad_tensor& g, const void* p, int64_t ld, int64_t k) {
+  const bool whole = g.rows == 1 || ld == g.cols;
+  return Range{(uintptr_t)p, (uintptr_t)p + (whole ? g.rows * g.cols : g.cols) * elem(g.dtype), k};
+}
+
+// Clipped gradients lie apart from each other and from every gradient but their own, which they
+// are as a whole or not at all: blocks read and write them in no order.
+tfe_status grad_places(const tfe_grad_tensor* t, int64_t n) {
+  constexpr int64_t kNear = 512;
+  Range near[kNear];
+  std::unique_ptr<Range[]> many;
+  if (n > kNear) {
+    many.reset(alloc_fails() ? nullptr : new (std::nothrow) Range[n]);
+    if (!many) return fail(TFE_ERR_OOM, "host memory for %lld tensors", (long long)n);
+  }
+  Range* const r = many ? many.get() : near;
+  int64_t m = 0;
+  bool sorted = true;
+  for (int64_t k = 0; k < n; ++k) {
+    if (t[k].rows == 0 || t[k].cols == 0) continue;
+    r[m] = range_of(t[k], t[k].out, t[k].ldo, k);
+    sorted = sorted && (m == 0 || r[m - 1].from <= r[m].from);
+    ++m;
+  }
+  if (!sorted) std::sort(r, r + m, [](const Range& a, const Range& b) { return a.from < b.from; });
+  for (int64_t k = 1; k < m; ++k)
+    NEED(r[k - 1].to <= r[k].from, "tensors %lld and %lld: clipped into the same memory",
+         (long long)r[k - 1].tensor, (long long)r[k].tensor);
+  for (int64_t k = 0; k < n; ++k) {
+    const tfe_grad_tensor& g = t[k];
+    if (g.rows == 0 || g.cols == 0 || g.grad == g.out) continue;
+    const Range x = range_of(g, g.grad, g.ldg, k);
+    // The first that ends behind where this one begins.
+    const Range* o = std::partition_point(r, r + m, [&](const Range& a) { return a.to <= x.from; });
+    NEED(o == r + m || o->from >= x.to, "tensors %lld and %lld: a gradient under a clipped one",
+         (long long)k, (long long)o->tensor);
   }
   return TFE_OK;
 }
@@ -200,6 +250,7 @@ tfe_status tfe_grad_clip(const tfe_grad_tensor* tensors, int64_t n, float max_no
   using namespace tfe;
   begin_call();
   TRY(grad_tensors(tensors, n, true));
+  TRY(grad_places(tensors, n));
   TRY(max_norm_ok(max_norm));
   NEED(norm && aligned(norm, 4), "norm: null or not aligned");
   return launched(launch_grad_clip(GradArgs{tensors, n, max_norm, const_cast<float*>(norm), nullptr},
@@ -212,6 +263,7 @@ tfe_status tfe_grad_norm_clip(const tfe_grad_tensor* tensors, int64_t n, float m
   using namespace tfe;
   begin_call();
   TRY(grad_tensors(tensors, n, true));
+  TRY(grad_places(tensors, n));
   TRY(max_norm_ok(max_norm));
   NEED(norm && aligned(norm, 4), "norm: null or not aligned");
   TRY(space(workspace, workspace_bytes, grad_space(tensors, n)));
