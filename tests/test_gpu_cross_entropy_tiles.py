@@ -100,6 +100,15 @@ def test_numbers(rows, vocab, dim, pad, dtype):
     c.check(c.run(dtype, out_pad=pad), dtype)
 
 
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("rows,vocab,dim", [(30000, 20000, 24), (30000, 9000, 5000), (20000, 16384, 600), (300, 25000, 16384),
+                                            (1 << 20, 300, 16), (5, 1 << 18, 16), (1, 1, 16384)])
+def test_many_rows_and_wide_ones(rows, vocab, dim, dtype):
+    """Every list of targets long, several tokens a block; pieces of a few thousand tokens; the longest rows."""
+    c = Case(rows, vocab, dim)
+    c.check(c.run(dtype), dtype)
+
+
 def test_training_batch():
     """4096 rows of 151936 x 1024: five pieces."""
     c = Case(4096, 151936, 1024)
