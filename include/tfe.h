@@ -37,9 +37,10 @@
  *   - A table handle is not thread-safe: calls on one handle must be issued
  *     from one host thread at a time.
  *   - HIP graph capture: lookups on resident tables (tfe_lookup_inject,
- *     tfe_lookup_inject_multi), tfe_head_topk and the calls on logits
- *     (tfe_quantize, tfe_quantized_..., tfe_sample, tfe_distill_...) enqueue
- *     kernels only and may be captured.  Lookups on tiered tables,
+ *     tfe_lookup_inject_multi), tfe_head_topk, the calls on logits
+ *     (tfe_quantize, tfe_quantized_..., tfe_sample, tfe_distill_...) and those that
+ *     learn and serve the head (tfe_cross_entropy_..., tfe_grad_..., tfe_integer_...)
+ *     enqueue kernels only and may be captured.  Lookups on tiered tables,
  *     tfe_prefetch, tfe_prefetch_scored and tfe_ngram_top keep per-call host
  *     state or synchronise; on a capturing stream they return
  *     TFE_ERR_UNSUPPORTED without enqueuing anything.
@@ -496,9 +497,12 @@ int64_t tfe_distill_workspace(int64_t rows, int32_t vocab); /* -1: bad size */
  * tfe_cross_entropy_grad takes lse as tfe_cross_entropy_loss wrote it.
  * Pointers 16-byte aligned, with pitches and dim multiples of 8 (and pitches up
  * to 2^21), are read in place; others are copied in pieces first.  With no rows
- * grad_w becomes 0 (accumulate: stays).  The workspace is for a piece of the
- * vocabulary at a time: about 6 bytes for each of its numbers of dz (2^27 at most, or
- * 2048 a row), a copy of its rows of W, and 12 to 24 bytes a number of hidden.
+ * grad_w becomes 0 (accumulate: stays).  One size of workspace serves the three calls and
+ * both types (the loss alone needs none of dz's, TFE_BF16 a third): up to 7 bytes for
+ * each number of dz of a piece of the vocabulary, of at most max(4096, 2^27 / rows)
+ * tokens, with rows in whole tiles of 64, 128 (more than 64 rows) or 256 (more than
+ * 128); a copy of the piece's rows of W; 4 bytes for each number of hidden, and 4 more
+ * or 64 MiB; 8 bytes for each row, up to 16384 of them, and 128 tokens.
  * 1 <= vocab <= 2^18, 1 <= dim <= 16384, rows <= 2^20. */
 tfe_status tfe_cross_entropy_loss(const void *hidden, int64_t ldh, const void *w, int64_t ldw,
                                   const int32_t *targets, int64_t rows, int32_t vocab,
@@ -557,8 +561,9 @@ int64_t tfe_grad_workspace(const tfe_grad_tensor *tensors, int64_t n); /* -1: ba
  * value = code * scale: one scale for each token (hidden states) or output
  * channel (rows of W).  With m the largest finite |x| of the row,
  *   scale = m / 127,  code = x * (127 * (1 / m)) rounded to nearest even,
- * the quotients and products each rounded to float32.  Rows with m <= 2^-100 have scale and
- * codes 0; infinities become +-127; a row with a NaN has scale NaN.
+ * the quotients and products each rounded to float32.  Rows with m <= 2^-100, also those
+ * whose other numbers are infinite, have scale and codes 0; infinities of others become
+ * +-127; a row with a NaN has scale NaN.
  * dim <= 65536, rows <= 2^20. */
 tfe_status tfe_integer_quantize(const void *x, int32_t dtype, int64_t ldx, int64_t rows, int32_t dim,
                              int8_t *codes, float *scales, void *stream);
